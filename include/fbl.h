@@ -600,6 +600,32 @@ fbl_status fbl_proj_auto_tile(uint32_t op, int64_t M, int64_t K, int64_t N, int3
  */
 fbl_status fbl_proj_float_tile(uint32_t op, int64_t M, int64_t K, int64_t N, int32_t* info);
 
+/*
+ * Layer norm over M rows of N values, row strides in elements (any, at least N):
+ *   mu = mean(x), rstd = 1 / sqrt(mean((x - mu)^2) + eps)
+ *   y  = (x - mu) rstd * weight + bias
+ * weight and bias [N] may be NULL (ones, zeros).  mean and rstd [M] float32, as the
+ * backward needs them, may both be NULL.  The storage type is `dtype` for x, weight,
+ * bias and y; statistics and sums are fp32 (the variance about the mean).
+ * The backward gives
+ *   dx = rstd (g - mean(g) - xh mean(g xh)),  g = dy * weight,  xh = (x - mu) rstd
+ *   dweight = sum over rows of dy xh,  dbias = sum over rows of dy   (each NULL: not wanted)
+ * from the forward's mean and rstd, with a workspace of
+ * fbl_layer_norm_bwd_workspace bytes where dweight or dbias is wanted (4-byte
+ * aligned; its contents before and after mean nothing).  Sums run in a fixed order:
+ * the same call gives the same bits.
+ * Checks: N at most 16384 (FBL_ERR_UNSUPPORTED), finite eps >= 0 (FBL_ERR_ARG),
+ * pointers aligned to their element, outputs and workspace overlapping nothing
+ * (FBL_ERR_ARG; views of other columns of the same rows are fine).
+ */
+fbl_status fbl_layer_norm_fwd(int32_t dtype, int64_t M, int64_t N, const void* x, int64_t ldx, const void* weight,
+                              const void* bias, float eps, void* y, int64_t ldy, float* mean, float* rstd,
+                              void* stream);
+fbl_status fbl_layer_norm_bwd_workspace(int32_t dtype, int64_t M, int64_t N, size_t* bytes);
+fbl_status fbl_layer_norm_bwd(int32_t dtype, int64_t M, int64_t N, const void* dy, int64_t lddy, const void* x,
+                              int64_t ldx, const void* weight, const float* mean, const float* rstd, void* dx,
+                              int64_t lddx, void* dweight, void* dbias, void* ws, size_t ws_bytes, void* stream);
+
 /* Static, human-readable name of a status code. */
 const char* fbl_status_str(fbl_status s);
 

@@ -13,6 +13,8 @@ autograd graph.
   linear(x, w) -> x @ w
       x [..., K] (rows contiguous), w [K, N]; gradients x and w by the data-
       and weight-gradient products, no transposed copy of either.
+  layer_norm(x, weight=None, bias=None, eps=1e-5) -> y
+      x [..., N] (rows one strided matrix), weight and bias [N]; gradients to all three.
 
 The incoming gradient is read in place, never copied: it must have unit
 inner stride (any row stride), like every tensor the kernels read.  Autograd
@@ -108,3 +110,34 @@ class _Linear(torch.autograd.Function):
 
 def linear(x, w):
     return _Linear.apply(x, w)
+
+
+def _matrix_of(t, what: str):
+    """[..., N] as a matrix of rows, a view."""
+    try:
+        return t.view(-1, t.shape[-1])
+    except RuntimeError as e:
+        raise _f.FblError(_f.FBL_ERR_LAYOUT, f"{what}: the rows are not one strided matrix ({e}); pass it "
+                                             f"contiguous") from None
+
+
+class _LayerNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, eps):
+        x2 = _matrix_of(x, "layer_norm")
+        y, mean, rstd = _f.layer_norm_fwd(x2, weight, bias, eps)
+        ctx.save_for_backward(x2, mean, rstd, weight)
+        ctx.xshape = x.shape
+        return y.view(x.shape)
+
+    @staticmethod
+    def backward(ctx, dy):
+        x2, mean, rstd, weight = ctx.saved_tensors
+        dy2 = _matrix_of(_unit(dy, "layer_norm"), "layer_norm: the incoming gradient")
+        dx, dw, db = _f.layer_norm_bwd(dy2, x2, mean, rstd, weight, need_weight=ctx.needs_input_grad[1],
+                                       need_bias=ctx.needs_input_grad[2])
+        return dx.view(ctx.xshape), dw, db, None
+
+
+def layer_norm(x, weight=None, bias=None, eps: float = 1e-5):
+    return _LayerNorm.apply(x, weight, bias, float(eps))

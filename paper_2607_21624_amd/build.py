@@ -16,7 +16,7 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libfbl.so")
 SOURCES = ["attn_streams.hip", "attn_rows_f32.hip", "attn_fwd_bf16.hip", "attn_bwd.hip", "attn_bwd_kv.hip", "attn_bwd_q.hip", "attn_bwd_dq.hip", "proj_gemm.hip",
-           "proj_gemm_f32.hip", "layout_map.hip", "noalloc.hip", "api.cpp"]
+           "proj_gemm_f32.hip", "layout_map.hip", "noalloc.hip", "layer_norm.hip", "column_sums.hip", "api.cpp", "api_norm.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

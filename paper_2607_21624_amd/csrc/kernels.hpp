@@ -94,6 +94,18 @@ hipError_t launch_proj_gemm_f32(int a_kmajor, int b_nmajor, const GemmArgs& p, h
 // That tile (bm, bn, bk, wavefronts, wk) and the workgroups it takes, for an M x N output.
 void proj_gemm_f32_info(const GemmArgs& p, int32_t* info);
 
+// Layer norm (layer_norm.hip); f32: fp32 storage, else bf16.  N up to kNormMaxWidth.  The
+// backward ends with launch_column_sums where a.part is given.
+constexpr int kNormMaxWidth = 16384;
+hipError_t launch_layer_norm_fwd(int f32, const NormArgs& a, hipStream_t stream);
+hipError_t launch_layer_norm_bwd(int f32, const NormArgs& a, hipStream_t stream);
+// Rows of N values that one workgroup holds at a time.
+int layer_norm_slots(int f32, int N);
+
+// out0[n], out1[n] (K = 1 or 2 of them, each may be nullptr) = sums over `groups` of part [groups][K][N].
+hipError_t launch_column_sums(int f32, const float* part, int groups, int K, int N, void* out0, void* out1,
+                              hipStream_t stream);
+
 // Diagnostic: offsets of a token-major tensor computed by the device index map.
 hipError_t launch_layout_map(const TokMap& m, int B, int H, int S, int D, int64_t* out, hipStream_t stream);
 

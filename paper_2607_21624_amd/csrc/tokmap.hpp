@@ -87,4 +87,25 @@ struct GemmArgs {
     uint32_t a_bytes, b_bytes, c_bytes;  // spans of the operands and the result (< 2 GiB)
 };
 
+// Layer norm over M rows of N values (strides in elements).  w, b, mean, rstd
+// (forward), dx, dw and db may be nullptr.
+struct NormArgs {
+    const void* x;
+    const void* dy;
+    const void* w;
+    const void* b;
+    void* y;
+    void* dx;
+    void* dw;
+    void* db;
+    float* mean;
+    float* rstd;
+    float* part;  // backward: [groups][2][N] partial sums of dw and db, or nullptr
+    int64_t ldx, lddy, ldy, lddx;
+    int64_t M;
+    int N;
+    int groups;  // backward: workgroups
+    float eps;
+};
+
 }  // namespace fbl

@@ -58,7 +58,8 @@ EXPORTED = ("fbl_layout_desc", "fbl_layout_packed_qkv", "fbl_layout_offset", "fb
             "fbl_attn_tile_info", "fbl_attn_candidates", "fbl_attn_auto_tiles", "fbl_attn_tune", "fbl_attn_tuned_tile",
             "fbl_attn_tune_reset", "fbl_proj", "fbl_proj_dt",
             "fbl_gemm_tile_count", "fbl_gemm_tile_info", "fbl_proj_candidates", "fbl_proj_tune", "fbl_proj_tuned_tile", "fbl_proj_auto_tile",
-            "fbl_proj_float_tile", "fbl_proj_tune_reset", "fbl_status_str")
+            "fbl_proj_float_tile", "fbl_proj_tune_reset", "fbl_layer_norm_fwd", "fbl_layer_norm_bwd_workspace",
+            "fbl_layer_norm_bwd", "fbl_status_str")
 
 
 class Layout(ctypes.Structure):
@@ -171,6 +172,14 @@ def _load() -> ctypes.CDLL:
     lib.fbl_proj_float_tile.restype = ctypes.c_int
     lib.fbl_proj_tune_reset.argtypes = []
     lib.fbl_proj_tune_reset.restype = None
+    i32, i64, f32 = ctypes.c_int32, ctypes.c_int64, ctypes.c_float
+    size, sizep = ctypes.c_size_t, P(ctypes.c_size_t)
+    lib.fbl_layer_norm_fwd.argtypes = [i32, i64, i64, vp, i64, vp, vp, f32, vp, i64, vp, vp, vp]
+    lib.fbl_layer_norm_fwd.restype = ctypes.c_int
+    lib.fbl_layer_norm_bwd_workspace.argtypes = [i32, i64, i64, sizep]
+    lib.fbl_layer_norm_bwd_workspace.restype = ctypes.c_int
+    lib.fbl_layer_norm_bwd.argtypes = [i32, i64, i64, vp, i64, vp, i64, vp, vp, vp, vp, i64, vp, vp, vp, size, vp]
+    lib.fbl_layer_norm_bwd.restype = ctypes.c_int
     lib.fbl_status_str.argtypes = [ctypes.c_int]
     lib.fbl_status_str.restype = ctypes.c_char_p
     return lib
@@ -786,3 +795,114 @@ def proj_float_tile(op: int, M: int, K: int, N: int):
 
 def proj_tune_reset() -> None:
     LIB.fbl_proj_tune_reset()
+
+
+# ---------------------------------------------------------------- layer norm
+def _matrix(t, where: str, name: str, shape=None, like=None):
+    """Row stride of a 2-D tensor with unit inner stride, of `shape` and of `like`'s dtype
+    where given.  (The strides of a single row or column mean nothing: the width is taken.)"""
+    if t.dim() != 2:
+        raise FblError(FBL_ERR_SHAPE, f"{where}: {name} must be 2-D, got shape {tuple(t.shape)}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise FblError(FBL_ERR_SHAPE, f"{where}: {name} has shape {tuple(t.shape)}, needs {tuple(shape)}")
+    if like is not None and t.dtype != like.dtype:
+        raise FblError(FBL_ERR_DTYPE, f"{where}: {name} is {t.dtype}, needs {like.dtype}")
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise FblError(FBL_ERR_LAYOUT, f"{where}: {name} needs inner stride 1, got strides {t.stride()}")
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def _vector(t, where: str, name: str, n: int, dtype):
+    """A contiguous 1-D tensor of n entries of `dtype`, or None."""
+    if t is None:
+        return
+    if t.dtype != dtype:
+        raise FblError(FBL_ERR_DTYPE, f"{where}: {name} is {t.dtype}, needs {dtype}")
+    if tuple(t.shape) != (n,):
+        raise FblError(FBL_ERR_SHAPE, f"{where}: {name} has shape {tuple(t.shape)}, needs {(n,)}")
+    if n > 1 and t.stride(0) != 1:
+        raise FblError(FBL_ERR_LAYOUT, f"{where}: {name} must be contiguous")
+
+
+def _scratch(workspace, need: int, where: str, like, stream):
+    """(workspace, its bytes): the caller's, or one allocated for this call.  The
+    allocator may hand that one out again when the call has returned, so it learns of the
+    stream that still works on it."""
+    import torch
+    _check_workspace(workspace, where)
+    if workspace is None:
+        workspace = torch.empty(need, dtype=torch.uint8, device=like.device)
+        if stream is not None:
+            used = torch.cuda.ExternalStream(stream, device=like.device) if isinstance(stream, int) else stream
+            workspace.record_stream(used)
+    return workspace, workspace.numel() * workspace.element_size()
+
+
+def _launch_stream(stream):
+    return _stream(stream) if stream != 0 else None
+
+
+def layer_norm_fwd(x, weight=None, bias=None, eps: float = 1e-5, out=None, mean=None, rstd=None, stream=None):
+    """Layer norm of the rows of x [M, N] (any row stride): returns (y, mean, rstd), mean
+    and rstd float32 [M].  weight and bias [N], in x's dtype, may be None."""
+    import torch
+    where = "layer_norm_fwd"
+    _check_device(where, stream, x=x, weight=weight, bias=bias, out=out, mean=mean, rstd=rstd)
+    ldx = _matrix(x, where, "x")
+    M, N = x.shape
+    dt = _dtype_code(x)
+    _vector(weight, where, "weight", N, x.dtype)
+    _vector(bias, where, "bias", N, x.dtype)
+    if out is None:
+        out = torch.empty((M, N), dtype=x.dtype, device=x.device)
+    ldy = _matrix(out, where, "out", (M, N), x)
+    if mean is None:
+        mean = torch.empty(M, dtype=torch.float32, device=x.device)
+    if rstd is None:
+        rstd = torch.empty(M, dtype=torch.float32, device=x.device)
+    _vector(mean, where, "mean", M, torch.float32)
+    _vector(rstd, where, "rstd", M, torch.float32)
+    _check(LIB.fbl_layer_norm_fwd(dt, M, N, _ptr(x), ldx, _ptr(weight), _ptr(bias), float(eps), _ptr(out), ldy, _ptr(mean),
+                                  _ptr(rstd), _launch_stream(stream)), "fbl_layer_norm_fwd")
+    return out, mean, rstd
+
+
+def layer_norm_bwd_workspace(x) -> int:
+    """Bytes of layer_norm_bwd's workspace for rows like x's."""
+    n = ctypes.c_size_t(0)
+    _check(LIB.fbl_layer_norm_bwd_workspace(_dtype_code(x), *x.shape, ctypes.byref(n)), "fbl_layer_norm_bwd_workspace")
+    return int(n.value)
+
+
+def layer_norm_bwd(dy, x, mean, rstd, weight=None, dx=None, dweight=None, dbias=None, workspace=None, stream=None,
+                   need_weight: bool = True, need_bias: bool = True):
+    """Gradients of layer_norm_fwd's rows: returns (dx, dweight, dbias), the last two
+    None where not needed.  mean and rstd are the forward's."""
+    import torch
+    where = "layer_norm_bwd"
+    _check_device(where, stream, dy=dy, x=x, mean=mean, rstd=rstd, weight=weight, dx=dx, dweight=dweight, dbias=dbias,
+                  workspace=workspace)
+    ldx = _matrix(x, where, "x")
+    M, N = x.shape
+    dt = _dtype_code(x)
+    lddy = _matrix(dy, where, "dy", (M, N), x)
+    _vector(mean, where, "mean", M, torch.float32)
+    _vector(rstd, where, "rstd", M, torch.float32)
+    _vector(weight, where, "weight", N, x.dtype)
+    if dx is None:
+        dx = torch.empty((M, N), dtype=x.dtype, device=x.device)
+    lddx = _matrix(dx, where, "dx", (M, N), x)
+    if dweight is None and need_weight:
+        dweight = torch.empty(N, dtype=x.dtype, device=x.device)
+    if dbias is None and need_bias:
+        dbias = torch.empty(N, dtype=x.dtype, device=x.device)
+    _vector(dweight, where, "dweight", N, x.dtype)
+    _vector(dbias, where, "dbias", N, x.dtype)
+    ws, ws_bytes = None, 0
+    if dweight is not None or dbias is not None:
+        need = 0 if workspace is not None else layer_norm_bwd_workspace(x)
+        ws, ws_bytes = _scratch(workspace, need, where, x, stream)
+    _check(LIB.fbl_layer_norm_bwd(dt, M, N, _ptr(dy), lddy, _ptr(x), ldx, _ptr(weight), _ptr(mean), _ptr(rstd), _ptr(dx),
+                                  lddx, _ptr(dweight), _ptr(dbias), _ptr(ws), ws_bytes, _launch_stream(stream)),
+           "fbl_layer_norm_bwd")
+    return dx, dweight, dbias

@@ -1,0 +1,81 @@
+"""The entry points of layer norm, linear layers and the losses refuse what they cannot
+compute, before any launch (CPU).  Every call here has exactly one defect."""
+import ctypes
+
+import pytest
+import torch
+
+import paper_2607_21624_amd as fbl
+from paper_2607_21624_amd import fbl as F
+
+LIB = F.LIB
+FAKE = 1 << 20  # made-up device addresses, 1 MiB apart, never dereferenced
+BF16, F32 = F.FBL_BF16, F.FBL_F32
+
+
+def at(i, off=0):
+    return ctypes.c_void_p(FAKE * (i + 1) + off)
+
+
+def _merge(base, kw):
+    assert set(kw) <= set(base), kw
+    return list({**base, **kw}.values())
+
+
+def norm_fwd(**kw):
+    return LIB.fbl_layer_norm_fwd(*_merge(dict(dt=BF16, M=4, N=64, x=at(1), ldx=64, w=at(2), b=at(3), eps=1e-5, y=at(4),
+                                               ldy=64, mean=at(5), rstd=at(6), stream=None), kw))
+
+
+def norm_bwd(**kw):
+    return LIB.fbl_layer_norm_bwd(*_merge(dict(dt=BF16, M=4, N=64, dy=at(1), lddy=64, x=at(2), ldx=64, w=at(3),
+                                               mean=at(4), rstd=at(5), dx=at(6), lddx=64, dw=at(7), db=at(8), ws=at(9),
+                                               ws_bytes=1 << 20, stream=None), kw))
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(dt=2), F.FBL_ERR_DTYPE), (dict(M=0), F.FBL_ERR_SHAPE), (dict(N=-1), F.FBL_ERR_SHAPE),
+    (dict(M=1 << 31), F.FBL_ERR_SHAPE), (dict(N=16385, ldx=16385, ldy=16385), F.FBL_ERR_UNSUPPORTED),
+    (dict(x=None), F.FBL_ERR_NULL), (dict(y=None), F.FBL_ERR_NULL), (dict(mean=None), F.FBL_ERR_NULL),
+    (dict(rstd=None), F.FBL_ERR_NULL), (dict(ldx=63), F.FBL_ERR_LAYOUT), (dict(ldy=63), F.FBL_ERR_LAYOUT),
+    (dict(ldx=1 << 31), F.FBL_ERR_LAYOUT), (dict(eps=-1e-5), F.FBL_ERR_ARG), (dict(eps=float("nan")), F.FBL_ERR_ARG),
+    (dict(x=at(1, 1)), F.FBL_ERR_ALIGN), (dict(y=at(4, 1)), F.FBL_ERR_ALIGN), (dict(mean=at(5, 2)), F.FBL_ERR_ALIGN),
+    (dict(y=at(1)), F.FBL_ERR_ARG), (dict(y=at(1, 64 * 2)), F.FBL_ERR_ARG), (dict(mean=at(2)), F.FBL_ERR_ARG),
+    (dict(rstd=at(5)), F.FBL_ERR_ARG), (dict(M=(1 << 31) - 1, ldx=(1 << 31) - 1), F.FBL_ERR_SHAPE),
+    # columns 32 .. 95 of rows of 96 against columns 0 .. 63
+    (dict(ldx=96, ldy=96, y=at(1, 32 * 2)), F.FBL_ERR_ARG),
+])
+def test_layer_norm_fwd_refusals(kw, status):
+    assert norm_fwd(**kw) == status
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(dt=-1), F.FBL_ERR_DTYPE), (dict(M=-4), F.FBL_ERR_SHAPE), (dict(N=1 << 20, lddy=1 << 20, ldx=1 << 20, lddx=1 << 20),
+                                                                   F.FBL_ERR_UNSUPPORTED),
+    (dict(dy=None), F.FBL_ERR_NULL), (dict(x=None), F.FBL_ERR_NULL), (dict(mean=None), F.FBL_ERR_NULL),
+    (dict(rstd=None), F.FBL_ERR_NULL), (dict(dx=None), F.FBL_ERR_NULL), (dict(lddy=0), F.FBL_ERR_LAYOUT),
+    (dict(lddx=60), F.FBL_ERR_LAYOUT), (dict(ws=None), F.FBL_ERR_WORKSPACE), (dict(ws_bytes=511), F.FBL_ERR_WORKSPACE),
+    (dict(ws=at(9, 2)), F.FBL_ERR_ALIGN), (dict(rstd=at(5, 1)), F.FBL_ERR_ALIGN), (dict(dx=at(1)), F.FBL_ERR_ARG),
+    (dict(dw=at(3)), F.FBL_ERR_ARG), (dict(db=at(7)), F.FBL_ERR_ARG), (dict(ws=at(6)), F.FBL_ERR_ARG),
+])
+def test_layer_norm_bwd_refusals(kw, status):
+    assert norm_bwd(**kw) == status
+
+
+def test_layer_norm_workspace():
+    n = ctypes.c_size_t(7)
+    f = LIB.fbl_layer_norm_bwd_workspace
+    assert f(BF16, 4, 64, ctypes.byref(n)) == F.FBL_OK and n.value == 1 * 2 * 64 * 4  # 4 rows: one workgroup's sums
+    assert f(BF16, 4, 64, None) == F.FBL_ERR_NULL
+    assert f(9, 4, 64, ctypes.byref(n)) == F.FBL_ERR_DTYPE
+    assert f(F32, 0, 64, ctypes.byref(n)) == F.FBL_ERR_SHAPE
+    assert f(F32, 4, 16385, ctypes.byref(n)) == F.FBL_ERR_UNSUPPORTED
+    assert f(BF16, 1 << 30, 16384, ctypes.byref(n)) == F.FBL_OK and n.value == 512 * 2 * 16384 * 4
+
+
+def test_layer_norm_binding_refuses_host_tensors():
+    x = torch.zeros(4, 64)
+    for f in (lambda: fbl.layer_norm_fwd(x), lambda: fbl.layer_norm_bwd(x, x, x[:, 0], x[:, 0])):
+        with pytest.raises(fbl.FblError) as e:
+            f()
+        assert e.value.status == F.FBL_ERR_ARG
