@@ -626,6 +626,47 @@ fbl_status fbl_layer_norm_bwd(int32_t dtype, int64_t M, int64_t N, const void* d
                               int64_t ldx, const void* weight, const float* mean, const float* rstd, void* dx,
                               int64_t lddx, void* dweight, void* dbias, void* ws, size_t ws_bytes, void* stream);
 
+/*
+ * A linear layer with its bias, activation and residual in the product's epilogue:
+ *   z = x [M, K] . w [K, N] + bias [N],   y = act(z) + res [M, N]
+ * bias and res may be NULL; z, where not NULL, receives the pre-activation that the
+ * backward needs (rounded to the storage type; an act of NONE needs none).
+ *   FBL_ACT_RELU       max(z, 0)
+ *   FBL_ACT_GELU       z Phi(z), Phi the normal distribution function
+ *   FBL_ACT_GELU_TANH  z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2
+ *   FBL_ACT_SILU       z / (1 + exp(-z))
+ * tile: as fbl_proj's for the product (FBL_PROJ_FWD, M, K, N); AUTO for fp32.
+ *
+ * fbl_linear_bwd gives, from dy [M, N], any of (NULL: not wanted)
+ *   dx = (dz . w^T) * xact'(xz),   dw = x^T . dz,   dbias = sum over rows of dz,
+ *   dz = dy * act'(z)
+ * xact and xz [M, K] are the activation and pre-activation that made x, where the
+ * caller wants the gradient of that pre-activation at once (FBL_ACT_NONE: x's own).
+ * The residual's gradient is dy.  dz is rounded to the storage type before the
+ * products; the bias' gradient sums it in fp32 unrounded.  x may be NULL without dw, w without dx,
+ * z with act NONE.  The workspace (16-byte aligned, fbl_linear_bwd_workspace
+ * bytes) is needed where act is not NONE or dbias is wanted.
+ *
+ * Row strides in elements, at least the width.  fp32: any extents, natural
+ * alignment.  bf16: 16-byte aligned pointers (bias too) and rows; forward K a
+ * multiple of 8 and N of 4; backward N a multiple of 8 and K of 4 for dx, N
+ * of 4 for dw; any number of tokens M.  Operands below 2 GiB each (FBL_ERR_UNSUPPORTED), outputs and
+ * workspace overlapping nothing (FBL_ERR_ARG).  All sums run in a fixed order.
+ */
+#define FBL_ACT_NONE 0u
+#define FBL_ACT_RELU 1u
+#define FBL_ACT_GELU 2u
+#define FBL_ACT_GELU_TANH 3u
+#define FBL_ACT_SILU 4u
+fbl_status fbl_linear_fwd(int32_t dtype, uint32_t act, int64_t M, int64_t K, int64_t N, const void* x, int64_t ldx,
+                          const void* w, int64_t ldw, const void* bias, const void* res, int64_t ldr, void* y,
+                          int64_t ldy, void* z, int64_t ldz, int32_t tile, void* stream);
+fbl_status fbl_linear_bwd_workspace(int32_t dtype, int64_t M, int64_t K, int64_t N, size_t* bytes);
+fbl_status fbl_linear_bwd(int32_t dtype, uint32_t act, int64_t M, int64_t K, int64_t N, const void* dy, int64_t lddy,
+                          const void* x, int64_t ldx, const void* w, int64_t ldw, const void* z, int64_t ldz,
+                          uint32_t xact, const void* xz, int64_t ldxz, void* dx, int64_t lddx, void* dw, int64_t lddw,
+                          void* dbias, void* ws, size_t ws_bytes, void* stream);
+
 /* Static, human-readable name of a status code. */
 const char* fbl_status_str(fbl_status s);
 

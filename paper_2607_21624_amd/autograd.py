@@ -10,9 +10,13 @@ autograd graph.
   attention_packed(qkv, Hq, Hkv, scale=None, causal=False) -> O
       qkv [B, S, (Hq + 2 Hkv) d], the packed output of a fused QKV
       projection; its gradient is one packed tensor of the same shape.
-  linear(x, w) -> x @ w
+  linear(x, w, bias=None, act="none", residual=None) -> act(x @ w + bias) + residual
       x [..., K] (rows contiguous), w [K, N]; gradients x and w by the data-
-      and weight-gradient products, no transposed copy of either.
+      and weight-gradient products, no transposed copy of either.  bias [N],
+      act "none", "relu", "gelu", "gelu_tanh" or "silu", residual [..., N].
+  mlp(x, w1, b1, w2, b2, act="gelu", residual=None) -> act(x @ w1 + b1) @ w2 + b2 + residual
+      a block's feed-forward part; its backward takes the activation's
+      derivative in the epilogue of the data gradient.  b1, b2 may be None.
   layer_norm(x, weight=None, bias=None, eps=1e-5) -> y
       x [..., N] (rows one strided matrix), weight and bias [N]; gradients to all three.
 
@@ -35,6 +39,15 @@ def _unit(t, what: str):
         raise _f.FblError(_f.FBL_ERR_LAYOUT, f"{what}: the incoming gradient needs unit inner stride, got strides "
                                              f"{tuple(t.stride())}; pass a contiguous gradient")
     return t
+
+
+def _matrix_of(t, what: str):
+    """[..., N] as a matrix of rows, a view."""
+    try:
+        return t.view(-1, t.shape[-1])
+    except RuntimeError as e:
+        raise _f.FblError(_f.FBL_ERR_LAYOUT, f"{what}: the rows are not one strided matrix ({e}); pass it "
+                                             f"contiguous") from None
 
 
 class _Attention(torch.autograd.Function):
@@ -108,17 +121,81 @@ class _Linear(torch.autograd.Function):
         return dx, dw
 
 
-def linear(x, w):
-    return _Linear.apply(x, w)
+class _LinearAct(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, w, bias, residual, act):
+        x2 = _matrix_of(x, "linear")
+        N = w.shape[1]
+        res2 = None
+        if residual is not None:
+            if residual.shape != (*x.shape[:-1], N):
+                raise _f.FblError(_f.FBL_ERR_SHAPE, f"linear: residual has shape {tuple(residual.shape)}, needs "
+                                                    f"{(*x.shape[:-1], N)}")
+            res2 = _matrix_of(residual, "linear: residual")
+        z = None
+        if act != "none" and any(ctx.needs_input_grad[:3]):
+            z = torch.empty((x2.shape[0], N), dtype=x.dtype, device=x.device)
+        y = _f.linear_fwd(x2, w, bias, act, res2, z=z)
+        ctx.save_for_backward(x2, w, z)
+        ctx.cfg = (x.shape, act)
+        return y.view(*x.shape[:-1], N)
+
+    @staticmethod
+    def backward(ctx, dy):
+        x2, w, z = ctx.saved_tensors
+        xshape, act = ctx.cfg
+        need = ctx.needs_input_grad
+        dx = dw = db = None
+        if any(need[:3]):
+            dy2 = _matrix_of(_unit(dy, "linear"), "linear: the incoming gradient")
+            dx, dw, db = _f.linear_bwd(dy2, x2, w, z, act, need_dx=need[0], need_dw=need[1], need_bias=need[2])
+        return dx.view(xshape) if need[0] else None, dw, db, dy if need[3] else None, None
 
 
-def _matrix_of(t, what: str):
-    """[..., N] as a matrix of rows, a view."""
-    try:
-        return t.view(-1, t.shape[-1])
-    except RuntimeError as e:
-        raise _f.FblError(_f.FBL_ERR_LAYOUT, f"{what}: the rows are not one strided matrix ({e}); pass it "
-                                             f"contiguous") from None
+def linear(x, w, bias=None, act: str = "none", residual=None):
+    if bias is None and act == "none" and residual is None:
+        return _Linear.apply(x, w)
+    return _LinearAct.apply(x, w, bias, residual, act)
+
+
+class _Mlp(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, w1, b1, w2, b2, residual, act):
+        x2 = _matrix_of(x, "mlp")
+        res2 = None
+        if residual is not None:
+            if residual.shape != (*x.shape[:-1], w2.shape[1]):
+                raise _f.FblError(_f.FBL_ERR_SHAPE, f"mlp: residual has shape {tuple(residual.shape)}, needs "
+                                                    f"{(*x.shape[:-1], w2.shape[1])}")
+            res2 = _matrix_of(residual, "mlp: residual")
+        z = None
+        if act != "none" and any(ctx.needs_input_grad[:3]):
+            z = torch.empty((x2.shape[0], w1.shape[1]), dtype=x.dtype, device=x.device)
+        h = _f.linear_fwd(x2, w1, b1, act, z=z)
+        y = _f.linear_fwd(h, w2, b2, residual=res2)
+        ctx.save_for_backward(x2, w1, w2, z, h)
+        ctx.cfg = (x.shape, act)
+        return y.view(*x.shape[:-1], w2.shape[1])
+
+    @staticmethod
+    def backward(ctx, dy):
+        x2, w1, w2, z, h = ctx.saved_tensors
+        xshape, act = ctx.cfg
+        need = ctx.needs_input_grad
+        first, second = any(need[:3]), need[3] or need[4]
+        dx = dw1 = db1 = dw2 = db2 = None
+        if first or second:
+            dy2 = _matrix_of(_unit(dy, "mlp"), "mlp: the incoming gradient")
+            # the hidden layer's gradient arrives as that of its pre-activation
+            dz, dw2, db2 = _f.linear_bwd(dy2, h, w2, need_dx=first, need_dw=need[3], need_bias=need[4],
+                                         x_act=act if first else "none", x_z=z if first else None)
+            if first:
+                dx, dw1, db1 = _f.linear_bwd(dz, x2, w1, need_dx=need[0], need_dw=need[1], need_bias=need[2])
+        return dx.view(xshape) if need[0] else None, dw1, db1, dw2, db2, dy if need[5] else None, None
+
+
+def mlp(x, w1, b1, w2, b2, act: str = "gelu", residual=None):
+    return _Mlp.apply(x, w1, b1, w2, b2, residual, act)
 
 
 class _LayerNorm(torch.autograd.Function):

@@ -1257,6 +1257,14 @@ int32_t default_tile(const ProjPlan& pl) {
 
 }  // namespace
 
+int fbl::proj_auto_tile(uint32_t op, int64_t M, int64_t K, int64_t N) {
+    const int32_t t = tuned_tile(op, M, K, N);
+    if (t >= 0) return t;
+    ProjPlan pl;
+    proj_shape(op, M, K, N, pl);
+    return default_tile(pl);
+}
+
 extern "C" {
 
 int32_t fbl_gemm_tile_count(void) { return fbl::kGemmTileCount; }
@@ -1382,10 +1390,7 @@ fbl_status fbl_proj_auto_tile(uint32_t op, int64_t M, int64_t K, int64_t N, int3
     if (!tile) return FBL_ERR_NULL;
     if (op > FBL_PROJ_BWD_WEIGHT) return FBL_ERR_ARG;
     if (M <= 0 || K <= 0 || N <= 0 || M > INT32_MAX || K > INT32_MAX || N > INT32_MAX) return FBL_ERR_SHAPE;
-    ProjPlan pl;
-    proj_shape(op, M, K, N, pl);
-    const int32_t t = tuned_tile(op, M, K, N);
-    *tile = t >= 0 ? t : default_tile(pl);
+    *tile = fbl::proj_auto_tile(op, M, K, N);
     return FBL_OK;
 }
 

@@ -1,0 +1,168 @@
+// api_linear.cpp -- the C ABI of linear layers with bias, activation and residual:
+// validation and dispatch.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "act.hpp"
+#include "kernels.hpp"
+#include "products.hpp"
+
+using fbl::overlap;
+using fbl::RowsView;
+
+namespace {
+
+size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
+
+hipError_t run_linear_gemm(int f32, int act, int grad, int tile, const fbl::LinearArgs& p, hipStream_t s) {
+    switch (act) {
+        case FBL_ACT_NONE: return f32 ? fbl::launch_linear_gemm_f32<fbl::kActNone>(grad, p, s) : fbl::launch_linear_gemm<fbl::kActNone>(grad, tile, p, s);
+        case FBL_ACT_RELU: return f32 ? fbl::launch_linear_gemm_f32<fbl::kActRelu>(grad, p, s) : fbl::launch_linear_gemm<fbl::kActRelu>(grad, tile, p, s);
+        case FBL_ACT_GELU: return f32 ? fbl::launch_linear_gemm_f32<fbl::kActGelu>(grad, p, s) : fbl::launch_linear_gemm<fbl::kActGelu>(grad, tile, p, s);
+        case FBL_ACT_GELU_TANH:
+            return f32 ? fbl::launch_linear_gemm_f32<fbl::kActGeluTanh>(grad, p, s) : fbl::launch_linear_gemm<fbl::kActGeluTanh>(grad, tile, p, s);
+        default: return f32 ? fbl::launch_linear_gemm_f32<fbl::kActSilu>(grad, p, s) : fbl::launch_linear_gemm<fbl::kActSilu>(grad, tile, p, s);
+    }
+}
+
+// Blocks of rows of the elementwise pass: enough workgroups for eight a CU, no more partial
+// sums than 512 rows.
+struct ActGrid {
+    int64_t rows;
+    int groups;
+};
+ActGrid act_grid(int f32, int64_t M, int64_t N) {
+    const int64_t cols = f32 ? 256 : 512, ct = (N + cols - 1) / cols;
+    const int64_t want = std::min<int64_t>(512, std::max<int64_t>(1, 2048 / ct));
+    const int64_t rows = ((M + want - 1) / want + 3) / 4 * 4;
+    return {rows, (int)((M + rows - 1) / rows)};
+}
+
+struct LinearWs {
+    size_t part, dz, total;
+};
+LinearWs linear_ws(int f32, int64_t M, int64_t N) {
+    LinearWs w;
+    w.part = align256((size_t)act_grid(f32, M, N).groups * (size_t)N * 4);
+    w.dz = (size_t)M * (size_t)N * (f32 ? 4 : 2);
+    w.total = w.part + w.dz;
+    return w;
+}
+
+fbl_status linear_shape(int32_t dtype, uint32_t act, int64_t M, int64_t K, int64_t N) {
+    if (!fbl::dtype_size(dtype)) return FBL_ERR_DTYPE;
+    if (act > FBL_ACT_SILU) return FBL_ERR_ARG;
+    if (!fbl::extent(M) || !fbl::extent(K) || !fbl::extent(N)) return FBL_ERR_SHAPE;
+    if (M * N >= ((int64_t)1 << 31) / fbl::dtype_size(dtype)) return FBL_ERR_UNSUPPORTED;  // y, dy, dz
+    return FBL_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+fbl_status fbl_linear_fwd(int32_t dtype, uint32_t act, int64_t M, int64_t K, int64_t N, const void* x, int64_t ldx,
+                          const void* w, int64_t ldw, const void* bias, const void* res, int64_t ldr, void* y,
+                          int64_t ldy, void* z, int64_t ldz, int32_t tile, void* stream) {
+    fbl_status st = linear_shape(dtype, act, M, K, N);
+    if (st != FBL_OK) return st;
+    if (!x || !w || !y) return FBL_ERR_NULL;
+    const int es = (int)fbl::dtype_size(dtype);
+    const RowsView vx{x, M, K, ldx, es}, vw{w, K, N, ldw, es}, vb{bias, 1, N, (N + 7) / 8 * 8, es},
+        vr{res, M, N, ldr, es}, vy{y, M, N, ldy, es}, vz{z, M, N, ldz, es};
+    for (const RowsView* v : {&vx, &vw, &vb, &vr, &vy, &vz})
+        if ((st = fbl::check_operand(*v)) != FBL_OK) return st;
+    if (es == 2 && (K % 8 || N % 4)) return FBL_ERR_UNSUPPORTED;
+    if (tile < FBL_GEMM_TILE_AUTO || tile >= fbl::kGemmTileCount || (es == 4 && tile != FBL_GEMM_TILE_AUTO))
+        return FBL_ERR_ARG;
+    for (const RowsView* out : {&vy, &vz})
+        for (const RowsView* in : {&vx, &vw, &vb, &vr})
+            if (overlap(*out, *in)) return FBL_ERR_ARG;
+    if (overlap(vy, vz)) return FBL_ERR_ARG;
+    fbl::LinearArgs p{};
+    fbl::product(p, FBL_PROJ_FWD, vx, vw, vy, M, K, N);
+    p.bias = bias, p.res = res, p.z = z, p.ldr = ldr, p.ldz = ldz;
+    p.res_bytes = res ? fbl::load_span(vr) : 0;
+    p.z_bytes = z ? (uint32_t)vz.bytes() : 0;
+    if (es == 2 && tile == FBL_GEMM_TILE_AUTO) tile = fbl::proj_auto_tile(FBL_PROJ_FWD, M, K, N);
+    const hipError_t e = run_linear_gemm(es == 4, (int)act, 0, tile, p, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? FBL_OK : FBL_ERR_HIP;
+}
+
+fbl_status fbl_linear_bwd_workspace(int32_t dtype, int64_t M, int64_t K, int64_t N, size_t* bytes) {
+    if (!bytes) return FBL_ERR_NULL;
+    const fbl_status st = linear_shape(dtype, FBL_ACT_NONE, M, K, N);
+    if (st == FBL_OK) *bytes = linear_ws(dtype == FBL_F32, M, N).total;
+    return st;
+}
+
+fbl_status fbl_linear_bwd(int32_t dtype, uint32_t act, int64_t M, int64_t K, int64_t N, const void* dy, int64_t lddy,
+                          const void* x, int64_t ldx, const void* w, int64_t ldw, const void* z, int64_t ldz,
+                          uint32_t xact, const void* xz, int64_t ldxz, void* dx, int64_t lddx, void* dw, int64_t lddw,
+                          void* dbias, void* ws, size_t ws_bytes, void* stream) {
+    fbl_status st = linear_shape(dtype, act, M, K, N);
+    if (st != FBL_OK) return st;
+    if (xact > FBL_ACT_SILU) return FBL_ERR_ARG;
+    if (!dy || (dw && !x) || (dx && !w)) return FBL_ERR_NULL;
+    const bool has_act = act != FBL_ACT_NONE, has_xact = dx && xact != FBL_ACT_NONE;
+    if ((has_act && !z) || (has_xact && !xz)) return FBL_ERR_NULL;
+    const int es = (int)fbl::dtype_size(dtype), f32 = es == 4;
+    const RowsView vdy{dy, M, N, lddy, es}, vx{dw ? x : nullptr, M, K, ldx, es}, vw{dx ? w : nullptr, K, N, ldw, es},
+        vz{has_act ? z : nullptr, M, N, ldz, es}, vxz{has_xact ? xz : nullptr, M, K, ldxz, es}, vdx{dx, M, K, lddx, es},
+        vdw{dw, K, N, lddw, es};
+    const RowsView vdb{dbias, 1, N, N, es};
+    for (const RowsView* v : {&vdy, &vx, &vw, &vz, &vxz, &vdx, &vdw})
+        if ((st = fbl::check_operand(*v)) != FBL_OK) return st;
+    if (!vdb.natural()) return FBL_ERR_ALIGN;
+    if (es == 2 && ((dx && (N % 8 || K % 4)) || (dw && N % 4))) return FBL_ERR_UNSUPPORTED;
+    // what is needed of the workspace: partial sums for the bias, dz where an activation makes it
+    const LinearWs lw = linear_ws(f32, M, N);
+    const bool pass = has_act ? (dx || dw || dbias) : dbias != nullptr;
+    const size_t need = pass ? lw.total : 0;
+    if (pass && (!ws || ws_bytes < need)) return FBL_ERR_WORKSPACE;
+    const RowsView vws{pass ? ws : nullptr, 1, (int64_t)need, (int64_t)need + 1, 1};
+    if (vws.begin() % 16) return FBL_ERR_ALIGN;
+    const RowsView* outs[] = {&vdx, &vdw, &vdb, &vws};
+    for (int i = 0; i < 4; ++i) {
+        for (const RowsView* in : {&vdy, &vx, &vw, &vz, &vxz})
+            if (overlap(*outs[i], *in)) return FBL_ERR_ARG;
+        for (int j = 0; j < i; ++j)
+            if (overlap(*outs[i], *outs[j])) return FBL_ERR_ARG;
+    }
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    hipError_t e = hipSuccess;
+    RowsView g = vdy;  // the gradient of the pre-activation
+    if (pass) {
+        const ActGrid ag = act_grid(f32, M, N);
+        fbl::LinearActArgs a{};
+        a.dy = dy, a.z = z, a.lddy = lddy, a.ldz = ldz, a.M = M, a.N = (int)N, a.rows = ag.rows, a.groups = ag.groups;
+        a.part = dbias ? static_cast<float*>(ws) : nullptr;
+        if (has_act) {
+            g = RowsView{static_cast<char*>(ws) + lw.part, M, N, N, es};
+            a.dz = const_cast<void*>(g.p), a.lddz = N;
+        }
+        e = fbl::launch_linear_act_bwd(f32, (int)act, a, s);
+        if (e == hipSuccess && dbias) e = fbl::launch_column_sums(f32, a.part, a.groups, 1, (int)N, dbias, nullptr, s);
+    }
+    if (e == hipSuccess && dx) {
+        fbl::LinearArgs p{};
+        fbl::product(p, FBL_PROJ_BWD_DATA, g, vw, vdx, M, K, N);
+        const int tile = f32 ? 0 : fbl::proj_auto_tile(FBL_PROJ_BWD_DATA, M, K, N);
+        if (has_xact) {
+            p.z = const_cast<void*>(xz), p.ldz = ldxz, p.z_bytes = fbl::load_span(vxz);
+            e = run_linear_gemm(f32, (int)xact, 1, tile, p, s);
+        } else {
+            e = f32 ? fbl::launch_proj_gemm_f32(0, 1, p, s) : fbl::launch_proj_gemm(0, 1, tile, p, s);
+        }
+    }
+    if (e == hipSuccess && dw) {
+        fbl::GemmArgs p{};
+        fbl::product(p, FBL_PROJ_BWD_WEIGHT, vx, g, vdw, M, K, N);
+        e = f32 ? fbl::launch_proj_gemm_f32(1, 0, p, s)
+                : fbl::launch_proj_gemm(1, 0, fbl::proj_auto_tile(FBL_PROJ_BWD_WEIGHT, M, K, N), p, s);
+    }
+    return e == hipSuccess ? FBL_OK : FBL_ERR_HIP;
+}
+
+}  // extern "C"

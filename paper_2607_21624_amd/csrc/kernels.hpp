@@ -106,6 +106,17 @@ int layer_norm_slots(int f32, int N);
 hipError_t launch_column_sums(int f32, const float* part, int groups, int K, int N, void* out0, void* out1,
                               hipStream_t stream);
 
+// Products with a linear layer's epilogue (linear_gemm.hpp), ACT of act.hpp: the forward, or with
+// `grad` the data gradient times act'.  bf16 with `tile` of kGemmTiles; fp32 with its own choice.
+template <int ACT>
+hipError_t launch_linear_gemm(int grad, int tile, const LinearArgs& p, hipStream_t stream);
+template <int ACT>
+hipError_t launch_linear_gemm_f32(int grad, const LinearArgs& p, hipStream_t stream);
+hipError_t launch_linear_act_bwd(int f32, int act, const LinearActArgs& a, hipStream_t stream);
+
+// The tile of kGemmTiles that FBL_GEMM_TILE_AUTO names for a projection product (api.cpp).
+int proj_auto_tile(uint32_t op, int64_t M, int64_t K, int64_t N);
+
 // Diagnostic: offsets of a token-major tensor computed by the device index map.
 hipError_t launch_layout_map(const TokMap& m, int B, int H, int S, int D, int64_t* out, hipStream_t stream);
 

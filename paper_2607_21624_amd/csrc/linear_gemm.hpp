@@ -1,0 +1,141 @@
+// linear_gemm.hpp -- the matrix products of a linear layer with its bias, activation
+// and residual in their epilogue, and the data gradient times the previous layer's
+// activation derivative, gfx950.  One translation unit per activation
+// (linear_gemm_*.hip) defines FBL_ACT and includes this.
+//
+//   forward        z = X W + bias;  y = act(z) + residual   (z stored too where the backward needs it)
+//   data gradient  dX = (dZ W^T) act'(zp)                   (zp: the layer before's z)
+//
+// The tile loops are those of the projection products; the epilogue works on the
+// accumulators where they are, so the layer writes y once and reads nothing back: a
+// separate pass over y would cost 2 to 3 times its bytes again.  bf16: the sums stay in
+// fp32 up to the one rounding of y and of z each.
+#include "act.hpp"
+#include "gemm_bf16.hpp"
+#include "gemm_f32.hpp"
+
+namespace fbl {
+
+namespace {
+
+using i32x2 = int __attribute__((ext_vector_type(2)));
+
+FBL_DEV __amdgpu_buffer_rsrc_t span(const void* p, uint32_t bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, p ? (int)bytes : 0, 0x00020000);
+}
+constexpr uint32_t kNowhere = 0x80000000u;  // past every span: loads give 0, stores are dropped
+
+FBL_DEV bf16x4 load4(__amdgpu_buffer_rsrc_t r, uint32_t off) {
+    return __builtin_bit_cast(bf16x4, __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, 0));
+}
+
+// Values of rows m and columns n .. n+3 (a multiple of 4), or of element (m, n) in fp32.
+template <int ACT, bool GRAD>
+struct LinearEp {
+    using Args = LinearArgs;
+
+    // bf16: C^T accumulators, four consecutive columns of a row in four registers
+    template <typename C>
+    static FBL_DEV void done(const Args& p, uint32_t, f32x16 (&acc)[C::TN][C::TM], int m0, int n0, int wm, int wn) {
+        const int lane = threadIdx.x & 63, g = lane >> 5;
+        const __amdgpu_buffer_rsrc_t rc = span(p.c, p.c_bytes), rz = span(p.z, p.z_bytes), rr_ = span(p.res, p.res_bytes),
+                                     rb = span(p.bias, (uint32_t)p.N * 2);
+        const bool has_res = p.res != nullptr, has_z = p.z != nullptr;
+#pragma unroll
+        for (int tn = 0; tn < C::TN; ++tn) {
+            const int nb = n0 + (wn * C::TN + tn) * 32 + 4 * g;
+            bf16x4 b[4];
+            if constexpr (!GRAD) {
+#pragma unroll
+                for (int rr = 0; rr < 4; ++rr) b[rr] = load4(rb, (uint32_t)(nb + 8 * rr) * 2);  // past N: 0
+            }
+#pragma unroll
+            for (int tm = 0; tm < C::TM; ++tm) {
+                const int m = m0 + (wm * C::TM + tm) * 32 + (lane & 31);
+#pragma unroll
+                for (int rr = 0; rr < 4; ++rr) {
+                    const int n = nb + 8 * rr;
+                    const bool in = m < p.M && n < p.N;
+                    const uint32_t off = in ? (uint32_t)(((int64_t)m * p.ldc + n) * 2) : kNowhere;
+                    const uint32_t zoff = in ? (uint32_t)(((int64_t)m * p.ldz + n) * 2) : kNowhere;
+                    float v[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] = acc[tn][tm][4 * rr + e];
+                    if constexpr (GRAD) {
+                        const bf16x4 z = load4(rz, zoff);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) v[e] *= act_grad<ACT, true>((float)z[e]);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) v[e] += (float)b[rr][e];
+                        if (has_z) {
+                            const bf16x4 z = bf16x4{(bf16)v[0], (bf16)v[1], (bf16)v[2], (bf16)v[3]};
+                            __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(i32x2, z), rz, zoff, 0, 0);
+                        }
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) v[e] = act<ACT, true>(v[e]);
+                        if (has_res) {
+                            const bf16x4 x = load4(rr_, in ? (uint32_t)(((int64_t)m * p.ldr + n) * 2) : kNowhere);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) v[e] += (float)x[e];
+                        }
+                    }
+                    const bf16x4 y = bf16x4{(bf16)v[0], (bf16)v[1], (bf16)v[2], (bf16)v[3]};
+                    __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(i32x2, y), rc, off, 0, 0);
+                }
+            }
+        }
+    }
+
+    // fp32: 32 consecutive columns of a row across the lanes of a half
+    template <typename C>
+    static FBL_DEV void done(const Args& p, float*, f32x16 (&acc)[C::TM][C::TN], int m0, int n0, int wm, int wn) {
+        const int lane = threadIdx.x & 63, g = lane >> 5;
+        const __amdgpu_buffer_rsrc_t rc = span(p.c, p.c_bytes), rz = span(p.z, p.z_bytes), rr = span(p.res, p.res_bytes),
+                                     rb = span(p.bias, (uint32_t)p.N * 4);
+        const auto load = [](__amdgpu_buffer_rsrc_t r, uint32_t off) __attribute__((always_inline)) {
+            return __int_as_float(__builtin_amdgcn_raw_buffer_load_b32(r, off, 0, 0));
+        };
+        const bool has_res = p.res != nullptr, has_z = p.z != nullptr;
+#pragma unroll
+        for (int tn = 0; tn < C::TN; ++tn) {
+            const int n = n0 + (wn * C::TN + tn) * 32 + (lane & 31);
+            const float b = GRAD ? 0.f : load(rb, n < p.N ? (uint32_t)n * 4 : kNowhere);
+#pragma unroll
+            for (int tm = 0; tm < C::TM; ++tm)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int m = m0 + (wm * C::TM + tm) * 32 + acc_row(r, g);
+                    const bool in = m < p.M && n < p.N;
+                    const uint32_t off = in ? (uint32_t)(((int64_t)m * p.ldc + n) * 4) : kNowhere;
+                    const uint32_t zoff = in ? (uint32_t)(((int64_t)m * p.ldz + n) * 4) : kNowhere;
+                    float v = acc[tm][tn][r];
+                    if constexpr (GRAD) {
+                        v *= act_grad<ACT, false>(load(rz, zoff));
+                    } else {
+                        v += b;
+                        if (has_z) __builtin_amdgcn_raw_buffer_store_b32(__float_as_int(v), rz, zoff, 0, 0);
+                        v = act<ACT, false>(v);
+                        if (has_res) v += load(rr, in ? (uint32_t)(((int64_t)m * p.ldr + n) * 4) : kNowhere);
+                    }
+                    __builtin_amdgcn_raw_buffer_store_b32(__float_as_int(v), rc, off, 0, 0);
+                }
+        }
+    }
+};
+
+}  // namespace
+
+template <>
+hipError_t launch_linear_gemm<FBL_ACT>(int grad, int tile, const LinearArgs& p, hipStream_t stream) {
+    if (grad) return launch_gemm_tile<false, true, LinearEp<FBL_ACT, true>>(tile, p, stream);
+    return launch_gemm_tile<false, false, LinearEp<FBL_ACT, false>>(tile, p, stream);
+}
+
+template <>
+hipError_t launch_linear_gemm_f32<FBL_ACT>(int grad, const LinearArgs& p, hipStream_t stream) {
+    if (grad) return launch_f32_tile<false, true, LinearEp<FBL_ACT, true>>(f32_tile(p), p, stream);
+    return launch_f32_tile<false, false, LinearEp<FBL_ACT, false>>(f32_tile(p), p, stream);
+}
+
+}  // namespace fbl

@@ -108,4 +108,26 @@ struct NormArgs {
     float eps;
 };
 
+// A product with a linear layer's epilogue.  Forward: C = act(A B + bias) + res, and the
+// pre-activation to z where given; data gradient: C = (A B) act'(z).  bias, res and the
+// forward's z may be nullptr; z and res have C's extents.
+struct LinearArgs : GemmArgs {
+    const void* bias;
+    const void* res;
+    void* z;
+    int64_t ldr, ldz;
+    uint32_t res_bytes, z_bytes;
+};
+
+// dz = dy act'(z) over M x N; part, where not nullptr, gets [groups][N] sums down blocks of `rows` rows.
+struct LinearActArgs {
+    const void* dy;
+    const void* z;
+    void* dz;
+    float* part;
+    int64_t lddy, ldz, lddz;
+    int64_t M, rows;
+    int N, groups;
+};
+
 }  // namespace fbl

@@ -47,6 +47,14 @@ FBL_GEMM_TILE_64x64 = 3
 FBL_TUNE_TIME = 0
 FBL_TUNE_GFLOPS_X_MEMEFF = 1
 
+FBL_ACT_NONE = 0
+FBL_ACT_RELU = 1
+FBL_ACT_GELU = 2
+FBL_ACT_GELU_TANH = 3
+FBL_ACT_SILU = 4
+ACTIVATIONS = {"none": FBL_ACT_NONE, "relu": FBL_ACT_RELU, "gelu": FBL_ACT_GELU, "gelu_tanh": FBL_ACT_GELU_TANH,
+               "silu": FBL_ACT_SILU}
+
 FBL_ATTN_FWD = 0
 FBL_ATTN_BWD_KV = 1
 FBL_ATTN_BWD_DQ = 2
@@ -59,7 +67,7 @@ EXPORTED = ("fbl_layout_desc", "fbl_layout_packed_qkv", "fbl_layout_offset", "fb
             "fbl_attn_tune_reset", "fbl_proj", "fbl_proj_dt",
             "fbl_gemm_tile_count", "fbl_gemm_tile_info", "fbl_proj_candidates", "fbl_proj_tune", "fbl_proj_tuned_tile", "fbl_proj_auto_tile",
             "fbl_proj_float_tile", "fbl_proj_tune_reset", "fbl_layer_norm_fwd", "fbl_layer_norm_bwd_workspace",
-            "fbl_layer_norm_bwd", "fbl_status_str")
+            "fbl_layer_norm_bwd", "fbl_linear_fwd", "fbl_linear_bwd_workspace", "fbl_linear_bwd", "fbl_status_str")
 
 
 class Layout(ctypes.Structure):
@@ -180,6 +188,14 @@ def _load() -> ctypes.CDLL:
     lib.fbl_layer_norm_bwd_workspace.restype = ctypes.c_int
     lib.fbl_layer_norm_bwd.argtypes = [i32, i64, i64, vp, i64, vp, i64, vp, vp, vp, vp, i64, vp, vp, vp, size, vp]
     lib.fbl_layer_norm_bwd.restype = ctypes.c_int
+    u32 = ctypes.c_uint32
+    lib.fbl_linear_fwd.argtypes = [i32, u32, i64, i64, i64, vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, i64, i32, vp]
+    lib.fbl_linear_fwd.restype = ctypes.c_int
+    lib.fbl_linear_bwd_workspace.argtypes = [i32, i64, i64, i64, sizep]
+    lib.fbl_linear_bwd_workspace.restype = ctypes.c_int
+    lib.fbl_linear_bwd.argtypes = [i32, u32, i64, i64, i64, vp, i64, vp, i64, vp, i64, vp, i64, u32, vp, i64, vp, i64, vp,
+                                   i64, vp, vp, size, vp]
+    lib.fbl_linear_bwd.restype = ctypes.c_int
     lib.fbl_status_str.argtypes = [ctypes.c_int]
     lib.fbl_status_str.restype = ctypes.c_char_p
     return lib
@@ -906,3 +922,81 @@ def layer_norm_bwd(dy, x, mean, rstd, weight=None, dx=None, dweight=None, dbias=
                                   lddx, _ptr(dweight), _ptr(dbias), _ptr(ws), ws_bytes, _launch_stream(stream)),
            "fbl_layer_norm_bwd")
     return dx, dweight, dbias
+
+
+# ------------------------------------- linear layers: bias, activation, residual
+def _act_code(act, where: str) -> int:
+    code = ACTIVATIONS.get(act)
+    if code is None:
+        raise FblError(FBL_ERR_ARG, f"{where}: no activation {act!r}, there are {', '.join(ACTIVATIONS)}")
+    return code
+
+
+def linear_fwd(x, w, bias=None, act: str = "none", residual=None, out=None, z=None, tile: int = FBL_GEMM_TILE_AUTO,
+               stream=None):
+    """y = act(x w + bias) + residual for x [M, K], w [K, N], bias [N], residual [M, N] (any row
+    strides, one storage type), act one of ACTIVATIONS.  z [M, N], where given, receives the
+    pre-activation, which linear_bwd needs for every act but "none".  Returns y."""
+    import torch
+    where = "linear_fwd"
+    _check_device(where, stream, x=x, w=w, bias=bias, residual=residual, out=out, z=z)
+    ldx = _matrix(x, where, "x")
+    M, K = x.shape
+    dt, code = _dtype_code(x), _act_code(act, where)
+    ldw = _matrix(w, where, "w", None, x)
+    N = w.shape[1]
+    if w.shape[0] != K:
+        raise FblError(FBL_ERR_SHAPE, f"{where}: x {tuple(x.shape)} and w {tuple(w.shape)} do not agree")
+    _vector(bias, where, "bias", N, x.dtype)
+    ldr = 0 if residual is None else _matrix(residual, where, "residual", (M, N), x)
+    ldz = 0 if z is None else _matrix(z, where, "z", (M, N), x)
+    if out is None:
+        out = torch.empty((M, N), dtype=x.dtype, device=x.device)
+    ldy = _matrix(out, where, "out", (M, N), x)
+    _check(LIB.fbl_linear_fwd(dt, code, M, K, N, _ptr(x), ldx, _ptr(w), ldw, _ptr(bias), _ptr(residual), ldr, _ptr(out), ldy,
+                              _ptr(z), ldz, tile, _launch_stream(stream)), "fbl_linear_fwd")
+    return out
+
+
+def linear_bwd_workspace(x, w) -> int:
+    """Bytes of linear_bwd's workspace for x [M, K] and w [K, N]."""
+    n = ctypes.c_size_t(0)
+    _check(LIB.fbl_linear_bwd_workspace(_dtype_code(x), *x.shape, w.shape[1], ctypes.byref(n)), "fbl_linear_bwd_workspace")
+    return int(n.value)
+
+
+def linear_bwd(dy, x, w, z=None, act: str = "none", dx=None, dw=None, dbias=None, workspace=None, stream=None,
+               need_dx: bool = True, need_dw: bool = True, need_bias: bool = True, x_act: str = "none", x_z=None):
+    """Gradients of linear_fwd: returns (dx, dw, dbias), each None where not needed.  z is the
+    forward's pre-activation (None for act "none"); the residual's gradient is dy.  Where x
+    itself is x_act(x_z), dx can be the gradient of x_z."""
+    import torch
+    where = "linear_bwd"
+    _check_device(where, stream, dy=dy, x=x, w=w, z=z, dx=dx, dw=dw, dbias=dbias, workspace=workspace, x_z=x_z)
+    ldx = _matrix(x, where, "x")
+    M, K = x.shape
+    dt, code, xcode = _dtype_code(x), _act_code(act, where), _act_code(x_act, where)
+    ldw = _matrix(w, where, "w", None, x)
+    N = w.shape[1]
+    if w.shape[0] != K:
+        raise FblError(FBL_ERR_SHAPE, f"{where}: x {tuple(x.shape)} and w {tuple(w.shape)} do not agree")
+    lddy = _matrix(dy, where, "dy", (M, N), x)
+    ldz = 0 if z is None else _matrix(z, where, "z", (M, N), x)
+    ldxz = 0 if x_z is None else _matrix(x_z, where, "x_z", (M, K), x)
+    if dx is None and need_dx:
+        dx = torch.empty((M, K), dtype=x.dtype, device=x.device)
+    if dw is None and need_dw:
+        dw = torch.empty((K, N), dtype=x.dtype, device=x.device)
+    if dbias is None and need_bias:
+        dbias = torch.empty(N, dtype=x.dtype, device=x.device)
+    lddx = 0 if dx is None else _matrix(dx, where, "dx", (M, K), x)
+    lddw = 0 if dw is None else _matrix(dw, where, "dw", (K, N), x)
+    _vector(dbias, where, "dbias", N, x.dtype)
+    ws, ws_bytes = None, 0
+    if code != FBL_ACT_NONE or dbias is not None:
+        need = 0 if workspace is not None else linear_bwd_workspace(x, w)
+        ws, ws_bytes = _scratch(workspace, need, where, x, stream)
+    _check(LIB.fbl_linear_bwd(dt, code, M, K, N, _ptr(dy), lddy, _ptr(x), ldx, _ptr(w), ldw, _ptr(z), ldz, xcode, _ptr(x_z),
+                              ldxz, _ptr(dx), lddx, _ptr(dw), lddw, _ptr(dbias), _ptr(ws), ws_bytes,
+                              _launch_stream(stream)), "fbl_linear_bwd")
+    return dx, dw, dbias

@@ -79,3 +79,58 @@ def test_layer_norm_binding_refuses_host_tensors():
         with pytest.raises(fbl.FblError) as e:
             f()
         assert e.value.status == F.FBL_ERR_ARG
+
+
+# ----------------------------------------------------------------- linear layers
+def lin_fwd(**kw):
+    return LIB.fbl_linear_fwd(*_merge(dict(dt=BF16, act=2, M=8, K=64, N=64, x=at(1), ldx=64, w=at(2), ldw=64, bias=at(3),
+                                           res=at(4), ldr=64, y=at(5), ldy=64, z=at(6), ldz=64, tile=-1, stream=None), kw))
+
+
+def lin_bwd(**kw):
+    return LIB.fbl_linear_bwd(*_merge(dict(dt=BF16, act=2, M=8, K=64, N=64, dy=at(1), lddy=64, x=at(2), ldx=64, w=at(3),
+                                           ldw=64, z=at(4), ldz=64, xact=3, xz=at(5), ldxz=64, dx=at(6), lddx=64, dw=at(7),
+                                           lddw=64, dbias=at(8), ws=at(9), ws_bytes=1 << 19, stream=None), kw))
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(dt=5), F.FBL_ERR_DTYPE), (dict(act=5), F.FBL_ERR_ARG), (dict(M=0), F.FBL_ERR_SHAPE), (dict(K=0), F.FBL_ERR_SHAPE),
+    (dict(N=1 << 31), F.FBL_ERR_SHAPE), (dict(x=None), F.FBL_ERR_NULL), (dict(w=None), F.FBL_ERR_NULL),
+    (dict(y=None), F.FBL_ERR_NULL), (dict(ldx=56), F.FBL_ERR_LAYOUT), (dict(ldr=0), F.FBL_ERR_LAYOUT),
+    (dict(ldz=63), F.FBL_ERR_LAYOUT), (dict(ldw=68), F.FBL_ERR_ALIGN), (dict(x=at(1, 8)), F.FBL_ERR_ALIGN),
+    (dict(bias=at(3, 2)), F.FBL_ERR_ALIGN), (dict(z=at(6, 4)), F.FBL_ERR_ALIGN), (dict(K=60), F.FBL_ERR_UNSUPPORTED),
+    (dict(N=62), F.FBL_ERR_UNSUPPORTED), (dict(tile=21), F.FBL_ERR_ARG), (dict(tile=-2), F.FBL_ERR_ARG),
+    (dict(dt=F32, tile=0), F.FBL_ERR_ARG), (dict(dt=F32, x=at(1, 2)), F.FBL_ERR_ALIGN),
+    (dict(y=at(1)), F.FBL_ERR_ARG), (dict(y=at(4)), F.FBL_ERR_ARG), (dict(z=at(5)), F.FBL_ERR_ARG),
+    (dict(z=at(3)), F.FBL_ERR_ARG), (dict(M=1 << 25), F.FBL_ERR_UNSUPPORTED), (dict(ldx=1 << 28), F.FBL_ERR_UNSUPPORTED),
+])
+def test_linear_fwd_refusals(kw, status):
+    assert lin_fwd(**kw) == status
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(dt=5), F.FBL_ERR_DTYPE), (dict(act=5), F.FBL_ERR_ARG), (dict(xact=9), F.FBL_ERR_ARG), (dict(M=-1), F.FBL_ERR_SHAPE),
+    (dict(dy=None), F.FBL_ERR_NULL), (dict(x=None), F.FBL_ERR_NULL), (dict(w=None), F.FBL_ERR_NULL),
+    (dict(z=None), F.FBL_ERR_NULL), (dict(xz=None), F.FBL_ERR_NULL), (dict(ws=None), F.FBL_ERR_WORKSPACE),
+    (dict(ws_bytes=1000), F.FBL_ERR_WORKSPACE), (dict(ws=at(9, 8)), F.FBL_ERR_ALIGN), (dict(lddx=32), F.FBL_ERR_LAYOUT),
+    (dict(dbias=at(8, 1)), F.FBL_ERR_ALIGN), (dict(N=68, lddy=72, ldw=72, ldz=72, lddw=72), F.FBL_ERR_UNSUPPORTED),
+    (dict(dx=at(1)), F.FBL_ERR_ARG), (dict(dw=at(6)), F.FBL_ERR_ARG), (dict(dbias=at(7)), F.FBL_ERR_ARG),
+    (dict(ws=at(5)), F.FBL_ERR_ARG), (dict(dx=at(5)), F.FBL_ERR_ARG),
+])
+def test_linear_bwd_refusals(kw, status):
+    assert lin_bwd(**kw) == status
+
+
+def test_linear_workspace_and_binding():
+    n = ctypes.c_size_t()
+    f = LIB.fbl_linear_bwd_workspace
+    assert f(BF16, 8, 64, 64, ctypes.byref(n)) == F.FBL_OK and n.value >= 8 * 64 * 2 + 64 * 4
+    assert f(BF16, 8, 64, 64, None) == F.FBL_ERR_NULL
+    assert f(7, 8, 64, 64, ctypes.byref(n)) == F.FBL_ERR_DTYPE
+    assert f(F32, 8, 0, 64, ctypes.byref(n)) == F.FBL_ERR_SHAPE
+    assert f(F32, (1 << 31) - 1, 64, (1 << 31) - 1, ctypes.byref(n)) == F.FBL_ERR_UNSUPPORTED
+    x = torch.zeros(4, 64)
+    for call in (lambda: fbl.linear_fwd(x, x.t()), lambda: fbl.linear_bwd(x, x, x)):
+        with pytest.raises(fbl.FblError) as e:
+            call()
+        assert e.value.status == F.FBL_ERR_ARG
