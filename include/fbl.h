@@ -667,6 +667,67 @@ fbl_status fbl_linear_bwd(int32_t dtype, uint32_t act, int64_t M, int64_t K, int
                           uint32_t xact, const void* xz, int64_t ldxz, void* dx, int64_t lddx, void* dw, int64_t lddw,
                           void* dbias, void* ws, size_t ws_bytes, void* stream);
 
+/*
+ * Softmax losses of a linear head, logits z = x [M, K] . W over a vocabulary of V, without
+ * keeping the logits: forward and backward go through the vocabulary in tiles and
+ * pieces.  `order` says how W is stored, read in place either way:
+ *   FBL_HEAD_KV   [K, V] rows, as fbl_linear_fwd's w (ldw at least V)
+ *   FBL_HEAD_VK   [V, K] rows, an embedding table shared with the head (ldw at least K)
+ *
+ * Cross entropy (fbl_linear_ce_*), labels int64 [M]:
+ *   loss[m] = lse[m] - z[m, labels[m]],   lse[m] = log sum_v exp(z[m, v])
+ * A row whose label is `ignore` does not count: loss 0, no gradient.
+ *
+ * Distillation from a teacher's top logits (fbl_linear_kd_*), index int64 [M, top] (row
+ * stride ldi) and logits [M, top] (row stride ldl, of logits_dtype), temperature T > 0, top up to 1024:
+ *   p = softmax(logits / T) over the row's entries, q = softmax(z / T) over the vocabulary
+ *   loss[m] = T^2 sum_j p_j (log p_j - log q_{index_j}),   lse = log sum exp(z / T)
+ * A negative index is an absent entry, a logit of -inf one of weight 0; a row without
+ * any other does not count.  An index that stands in a row twice counts with
+ * both weights.  prob [M, top] float32 receives p, for the backward.
+ *
+ * A label or index of V and more (or a label below 0 that is not `ignore`) gives
+ * its row a loss and gradients of nan.
+ *
+ * loss, lse [M] float32.  total [2] float32, where not NULL: the sum of the losses and the number
+ * of rows that count; mean (needs total): their quotient, 0 where no row counts.
+ *
+ * The backward takes the gradient dloss[m * dloss_stride] (float32; stride 0: one for all
+ * rows), of each row's loss where total is NULL, else of the mean (it is divided by
+ * total[1], at least 1), and the forward's lse and prob, and gives, where not NULL,
+ *   dx = dz . W^T,  dW = x^T . dz,   dz = dloss T (exp(z / T - lse) - p at the targets)
+ * dW stored as W is (row stride lddw).  dz is rounded to the storage type before the
+ * products; dx is summed over the pieces in fp32.
+ *
+ * Workspace: fbl_linear_loss_workspace bytes for W's row stride, 16-byte aligned, the
+ * same for all four calls (top 1 for cross entropy); nothing is kept in it between calls.  Its
+ * size stays about 128 MiB of dz plus small lists and M K fp32 sums.
+ * fp32: any extents, natural alignment.  bf16: 16-byte aligned pointers and rows, K a multiple
+ * of 8, for FBL_HEAD_KV V too; any number of tokens.  x, dx and a FBL_HEAD_KV W below 2 GiB
+ * (fp32 sums of dx included: M K below 2^29); a table may be larger.  Outputs and workspace overlap
+ * nothing (FBL_ERR_ARG).  All sums run in a fixed order.
+ */
+#define FBL_HEAD_KV 0u
+#define FBL_HEAD_VK 1u
+fbl_status fbl_linear_loss_workspace(int32_t dtype, uint32_t order, int64_t M, int64_t K, int64_t V, int64_t top,
+                                     int64_t ldw, size_t* bytes);
+fbl_status fbl_linear_ce_fwd(int32_t dtype, uint32_t order, int64_t M, int64_t K, int64_t V, const void* x, int64_t ldx,
+                             const void* w, int64_t ldw, const int64_t* labels, int64_t ignore, float* loss, float* lse,
+                             float* total, float* mean, void* ws, size_t ws_bytes, void* stream);
+fbl_status fbl_linear_ce_bwd(int32_t dtype, uint32_t order, int64_t M, int64_t K, int64_t V, const float* dloss,
+                             int64_t dloss_stride, const float* total, const void* x, int64_t ldx, const void* w,
+                             int64_t ldw, const int64_t* labels, int64_t ignore, const float* lse, void* dx, int64_t lddx,
+                             void* dw, int64_t lddw, void* ws, size_t ws_bytes, void* stream);
+fbl_status fbl_linear_kd_fwd(int32_t dtype, uint32_t order, int64_t M, int64_t K, int64_t V, int64_t top, const void* x,
+                             int64_t ldx, const void* w, int64_t ldw, const int64_t* index, int64_t ldi,
+                             int32_t logits_dtype, const void* logits, int64_t ldl, float temperature, float* prob,
+                             float* loss, float* lse, float* total, float* mean, void* ws, size_t ws_bytes, void* stream);
+fbl_status fbl_linear_kd_bwd(int32_t dtype, uint32_t order, int64_t M, int64_t K, int64_t V, int64_t top, const float* dloss,
+                             int64_t dloss_stride, const float* total, const void* x, int64_t ldx, const void* w,
+                             int64_t ldw, const int64_t* index, int64_t ldi, float temperature, const float* prob,
+                             const float* lse, void* dx, int64_t lddx, void* dw, int64_t lddw, void* ws, size_t ws_bytes,
+                             void* stream);
+
 /* Static, human-readable name of a status code. */
 const char* fbl_status_str(fbl_status s);
 

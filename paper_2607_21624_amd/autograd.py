@@ -19,6 +19,13 @@ autograd graph.
       derivative in the epilogue of the data gradient.  b1, b2 may be None.
   layer_norm(x, weight=None, bias=None, eps=1e-5) -> y
       x [..., N] (rows one strided matrix), weight and bias [N]; gradients to all three.
+  linear_cross_entropy(x, w, labels, ignore_index=-100, reduction="mean") -> loss
+      softmax cross entropy of the logits x @ w over a vocabulary, which are never kept:
+      x [..., K], w [K, V] (or table.t() of a [V, K] table), labels [...]
+      int64; gradients to x and w.  loss float32: the mean over the rows not
+      labelled ignore_index, their "sum", or every row's ("none", [...]).
+  linear_distillation(x, w, index, logits, temperature=1.0, reduction="mean") -> loss
+      the same from a teacher's top logits: index int64 and logits [..., top].
 
 The incoming gradient is read in place, never copied: it must have unit
 inner stride (any row stride), like every tensor the kernels read.  Autograd
@@ -218,3 +225,82 @@ class _LayerNorm(torch.autograd.Function):
 
 def layer_norm(x, weight=None, bias=None, eps: float = 1e-5):
     return _LayerNorm.apply(x, weight, bias, float(eps))
+
+
+def _reduction(reduction, where: str):
+    if reduction not in ("mean", "sum", "none"):
+        raise _f.FblError(_f.FBL_ERR_ARG, f"{where}: reduction {reduction!r}, there are mean, sum and none")
+
+
+def _reduced(loss, total, mean, reduction, shape):
+    if reduction == "mean":
+        return mean
+    return total[0] if reduction == "sum" else loss.view(shape)
+
+
+def _loss_grad(dloss, reduction, M: int):
+    """The incoming gradient as the library takes it: one number, or one for each row (a broadcast
+    one included)."""
+    if reduction != "none":
+        return dloss
+    return dloss.reshape(M)
+
+
+class _LinearCrossEntropy(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, w, labels, ignore_index, reduction):
+        where = "linear_cross_entropy"
+        _reduction(reduction, where)
+        x2 = _matrix_of(x, where)
+        if labels.shape != x.shape[:-1]:
+            raise _f.FblError(_f.FBL_ERR_SHAPE, f"{where}: labels have shape {tuple(labels.shape)}, need "
+                                                f"{tuple(x.shape[:-1])}")
+        labels2 = labels.reshape(-1)
+        mean = torch.empty((), dtype=torch.float32, device=x.device)
+        loss, lse, total = _f.linear_ce_fwd(x2, w, labels2, ignore_index, mean=mean)
+        ctx.save_for_backward(x2, w, labels2, lse, total)
+        ctx.cfg = (x.shape, ignore_index, reduction)
+        return _reduced(loss, total, mean, reduction, x.shape[:-1])
+
+    @staticmethod
+    def backward(ctx, dloss):
+        x2, w, labels, lse, total = ctx.saved_tensors
+        xshape, ignore_index, reduction = ctx.cfg
+        need = ctx.needs_input_grad
+        dx, dw = _f.linear_ce_bwd(_loss_grad(dloss, reduction, x2.shape[0]), x2, w, labels, lse,
+                                  total if reduction == "mean" else None, ignore_index, need_dx=need[0], need_dw=need[1])
+        return dx.view(xshape) if need[0] else None, dw, None, None, None
+
+
+def linear_cross_entropy(x, w, labels, ignore_index: int = -100, reduction: str = "mean"):
+    return _LinearCrossEntropy.apply(x, w, labels, int(ignore_index), reduction)
+
+
+class _LinearDistillation(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, w, index, logits, temperature, reduction):
+        where = "linear_distillation"
+        _reduction(reduction, where)
+        x2 = _matrix_of(x, where)
+        if index.shape[:-1] != x.shape[:-1] or logits.shape != index.shape:
+            raise _f.FblError(_f.FBL_ERR_SHAPE, f"{where}: index {tuple(index.shape)} and logits {tuple(logits.shape)} need "
+                                                f"the shape {tuple(x.shape[:-1])} + (top,)")
+        index2, logits2 = _matrix_of(index, where), _matrix_of(logits, where)
+        mean = torch.empty((), dtype=torch.float32, device=x.device)
+        loss, lse, prob, total = _f.linear_kd_fwd(x2, w, index2, logits2, temperature, mean=mean)
+        ctx.save_for_backward(x2, w, index2, prob, lse, total)
+        ctx.cfg = (x.shape, temperature, reduction)
+        return _reduced(loss, total, mean, reduction, x.shape[:-1])
+
+    @staticmethod
+    def backward(ctx, dloss):
+        x2, w, index, prob, lse, total = ctx.saved_tensors
+        xshape, temperature, reduction = ctx.cfg
+        need = ctx.needs_input_grad
+        dx, dw = _f.linear_kd_bwd(_loss_grad(dloss, reduction, x2.shape[0]), x2, w, index, prob, lse, temperature,
+                                  total if reduction == "mean" else None, need_dx=need[0], need_dw=need[1])
+        return dx.view(xshape) if need[0] else None, dw, None, None, None, None
+
+
+def linear_distillation(x, w, index, logits, temperature: float = 1.0, reduction: str = "mean"):
+    return _LinearDistillation.apply(x, w, index, logits, float(temperature), reduction)

@@ -41,8 +41,9 @@ struct GTile {
 };
 
 // AT: A stored k-major ([K, M] rows); BT: B stored n-major ([N, K] rows).
-template <int BM, int BN, int BK, int NS, int WM, int WN, int WK, bool AT, bool BT>
+template <int BM_, int BN_, int BK, int NS, int WM_, int WN_, int WK, bool AT, bool BT>
 struct GemmCfg {
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
     static constexpr int NW = WM * WN * WK;
     using TA = GTile<AT ? BK : BM, AT ? BM : BK, NW>;
     using TB = GTile<BT ? BN : BK, BT ? BK : BN, NW>;

@@ -1,0 +1,260 @@
+// head_gemm.hip -- softmax losses of a linear head over a large vocabulary without
+// keeping the logits, gfx950: the products.
+//
+//   z = X W,  lse = log sum_v exp(z_v / T)                        forward
+//   dz = g (exp(z / T - lse) - targets),  dX = dz W^T,  dW = X^T dz   backward
+//
+// The logits exist only as accumulators.  The forward reduces each tile to its
+// rows' maximum and sum of exponentials (8 bytes for 256 columns instead of 512) and picks the
+// targets' logits out of it; the backward computes a piece of the vocabulary again, turns it into dz
+// where it stands and writes that, for the two gradient products to read.  With
+// tokens along the lanes and the vocabulary along the registers (C^T accumulators)
+// a row's reduction is in-lane but for one exchange between the halves of a wavefront and
+// one between the wavefronts that share its columns.
+//
+// Bound by the matrix products: 2 M K V forward and 6 M K V backward (one third of it z again).
+#include "gemm_bf16.hpp"
+#include "gemm_f32.hpp"
+
+namespace fbl {
+
+namespace {
+
+using i32x2 = int __attribute__((ext_vector_type(2)));
+using i32x4 = int __attribute__((ext_vector_type(4)));
+
+// A wavefront's share of a tile: NV x NM blocks of 32 x 32, vocabulary entries v0 + 32 i + acc_row(r, g)
+// (within the piece) and tokens m0 + 32 j + lane % 32.
+//
+// Entries of the list `index` that fall on this lane's registers: hit(r, i, j, t) for target t.
+// Few tiles hold any: the registers are searched only where a lane of the wavefront has one.
+template <int NV, int NM, typename F>
+FBL_DEV void for_targets(const HeadArgs& p, int v0, int m0, F&& hit) {
+    const int lane = threadIdx.x & 63, g = lane >> 5;
+#pragma unroll
+    for (int j = 0; j < NM; ++j) {
+        const int m = m0 + 32 * j + (lane & 31);
+        for (int t = 0; t < p.top; ++t) {
+            const int at = (m < p.tokens ? p.index[(int64_t)t * p.tokens + m] : -1) - p.first - v0;
+            const bool here = (unsigned)at < 32u * NV && ((at >> 2) & 1) == g;
+            if (__builtin_amdgcn_ballot_w64(here) == 0) continue;
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (here && at == 32 * i + acc_row(r, g)) hit(i, j, r, m, t);
+        }
+    }
+}
+
+// Forward: part[tile][m] and target[t][m].  WV wavefronts share a token's columns; wv is this
+// one's place among them and mw its first token within the tile.
+template <int NV, int NM, int WV, int TOKENS, int NT>
+FBL_DEV void head_stats(const HeadArgs& p, f32x16 (&acc)[NV][NM], float2* shared, int v0, int m0, int wv, int mw, int tile,
+                        int tile_m0) {
+    const int lane = threadIdx.x & 63, g = lane >> 5;
+    for_targets<NV, NM>(p, v0, m0, [&](int i, int j, int r, int m, int t) __attribute__((always_inline)) {
+        p.target[(int64_t)t * p.tokens + m] = acc[i][j][r];
+    });
+    if (v0 + 32 * NV > p.width) {  // columns past the piece count for nothing
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if (v0 + 32 * i + acc_row(r, g) >= p.width) {
+#pragma unroll
+                    for (int j = 0; j < NM; ++j) acc[i][j][r] = -INFINITY;
+                }
+    }
+    __syncthreads();  // the last step's operands have been read
+#pragma unroll
+    for (int j = 0; j < NM; ++j) {
+        float top = acc[0][j][0];
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) top = fmaxf(top, acc[i][j][r]);
+        top = fmaxf(top, other_half(top)) * p.unit;
+        const float ref = top == -INFINITY ? 0.f : top;
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sum += fast_exp2(__builtin_fmaf(acc[i][j][r], p.unit, -ref));
+        sum += other_half(sum);
+        if (g == 0) shared[wv * TOKENS + mw + 32 * j + lane] = make_float2(top, sum);
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < TOKENS; i += NT) {
+        if (tile_m0 + i >= p.tokens) break;
+        float2 s = shared[i];
+#pragma unroll
+        for (int w = 1; w < WV; ++w) {
+            const float2 o = shared[w * TOKENS + i];
+            const float top = fmaxf(s.x, o.x), ref = top == -INFINITY ? 0.f : top;
+            s = make_float2(top, s.y * fast_exp2(s.x - ref) + o.y * fast_exp2(o.x - ref));
+        }
+        p.part[(int64_t)(p.tile0 + tile) * p.tokens + tile_m0 + i] = s;
+    }
+}
+
+FBL_DEV void put4(__amdgpu_buffer_rsrc_t rs, uint32_t off, const float (&v)[4], bf16) {
+    const bf16x4 x = bf16x4{(bf16)v[0], (bf16)v[1], (bf16)v[2], (bf16)v[3]};
+    __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(i32x2, x), rs, off, 0, 0);
+}
+FBL_DEV void put4(__amdgpu_buffer_rsrc_t rs, uint32_t off, const float (&v)[4], float) {
+    const f32x4 x = f32x4{v[0], v[1], v[2], v[3]};
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(i32x4, x), rs, off, 0, 0);
+}
+
+// Backward: dz, rounded to the storage type once, after the targets' part.
+template <typename T, int NV, int NM>
+FBL_DEV void head_dz(const HeadArgs& p, f32x16 (&acc)[NV][NM], int v0, int m0) {
+    const int lane = threadIdx.x & 63, g = lane >> 5;
+    float scale[NM];
+#pragma unroll
+    for (int j = 0; j < NM; ++j) {
+        const int m = m0 + 32 * j + (lane & 31);
+        const float2 row = m < p.tokens ? p.row[m] : make_float2(0.f, 0.f);
+        scale[j] = row.x;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[i][j][r] = fast_exp2(__builtin_fmaf(acc[i][j][r], p.unit, -row.y));
+    }
+    for_targets<NV, NM>(p, v0, m0, [&](int i, int j, int r, int m, int t) __attribute__((always_inline)) {
+        acc[i][j][r] -= p.weight ? p.weight[(int64_t)t * p.tokens + m] : 1.f;
+    });
+    const __amdgpu_buffer_rsrc_t rz = __builtin_amdgcn_make_buffer_rsrc(p.dz, 0, (int)p.dz_bytes, 0x00020000);
+#pragma unroll
+    for (int j = 0; j < NM; ++j) {
+        const int m = m0 + 32 * j + (lane & 31);
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int v = v0 + 32 * i + 8 * q + 4 * g;
+                float x[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = v + e < p.width && scale[j] != 0.f ? acc[i][j][4 * q + e] * scale[j] : 0.f;
+                const uint32_t off = m < p.tokens && v < p.ldz ? (uint32_t)(((int64_t)m * p.ldz + v) * sizeof(T)) : 0x80000000u;
+                put4(rz, off, x, T{});
+            }
+    }
+}
+
+struct HeadFwd {
+    using Args = HeadArgs;
+    template <typename C>
+    static FBL_DEV void done(const Args& p, uint32_t, f32x16 (&acc)[C::TN][C::TM], int m0, int n0, int wm, int wn) {
+        extern __shared__ __attribute__((aligned(1024))) unsigned char gemm_smem[];
+        constexpr int BM = C::BM, BN = C::BN;
+        head_stats<C::TN, C::TM, C::WN, BM, 64 * C::NW>(p, acc, (float2*)gemm_smem, n0 + wn * C::TN * 32,
+                                                        m0 + wm * C::TM * 32, wn, wm * C::TM * 32, n0 / BN, m0);
+    }
+    template <typename C>
+    static FBL_DEV void done(const Args& p, float* smem, f32x16 (&acc)[C::TM][C::TN], int m0, int n0, int wm, int wn) {
+        head_stats<C::TM, C::TN, C::t.wm, C::t.bn, C::NT>(p, acc, (float2*)smem, m0 + wm * C::TM * 32, n0 + wn * C::TN * 32,
+                                                          wm, wn * C::TN * 32, m0 / C::t.bm, n0);
+    }
+};
+
+struct HeadGrad {
+    using Args = HeadArgs;
+    template <typename C>
+    static FBL_DEV void done(const Args& p, uint32_t, f32x16 (&acc)[C::TN][C::TM], int m0, int n0, int wm, int wn) {
+        head_dz<bf16>(p, acc, n0 + wn * C::TN * 32, m0 + wm * C::TM * 32);
+    }
+    template <typename C>
+    static FBL_DEV void done(const Args& p, float*, f32x16 (&acc)[C::TM][C::TN], int m0, int n0, int wm, int wn) {
+        head_dz<float>(p, acc, m0 + wm * C::TM * 32, n0 + wn * C::TN * 32);
+    }
+};
+
+// dX over the pieces of the vocabulary: sums in fp32, rounded once with the last piece.
+struct SumPieces {
+    using Args = SumArgs;
+    template <typename C>
+    static FBL_DEV void done(const Args& p, uint32_t, f32x16 (&acc)[C::TN][C::TM], int m0, int n0, int wm, int wn) {
+        const int lane = threadIdx.x & 63, g = lane >> 5;
+        const __amdgpu_buffer_rsrc_t rc = __builtin_amdgcn_make_buffer_rsrc(p.c, 0, (int)p.c_bytes, 0x00020000),
+                                     rs = __builtin_amdgcn_make_buffer_rsrc(p.sum, 0, (int)p.sum_bytes, 0x00020000);
+#pragma unroll
+        for (int tm = 0; tm < C::TM; ++tm) {
+            const int m = m0 + (wm * C::TM + tm) * 32 + (lane & 31);
+#pragma unroll
+            for (int tn = 0; tn < C::TN; ++tn)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int n = n0 + (wn * C::TN + tn) * 32 + 8 * q + 4 * g;
+                    const bool in = m < p.M && n < p.N;
+                    const uint32_t soff = in ? (uint32_t)(((int64_t)m * p.lds + n) * 4) : 0x80000000u;
+                    float v[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] = acc[tn][tm][4 * q + e];
+                    if (!p.first) {
+                        const f32x4 s = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, soff, 0, 0));
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) v[e] += s[e];
+                    }
+                    if (p.last) put4(rc, in ? (uint32_t)(((int64_t)m * p.ldc + n) * 2) : 0x80000000u, v, bf16{});
+                    else put4(rs, soff, v, 0.f);
+                }
+        }
+    }
+    template <typename C>
+    static FBL_DEV void done(const Args& p, float*, f32x16 (&acc)[C::TM][C::TN], int m0, int n0, int wm, int wn) {
+        const int lane = threadIdx.x & 63, g = lane >> 5;
+        const __amdgpu_buffer_rsrc_t rc = __builtin_amdgcn_make_buffer_rsrc(p.c, 0, (int)p.c_bytes, 0x00020000);
+#pragma unroll
+        for (int tm = 0; tm < C::TM; ++tm)
+#pragma unroll
+            for (int tn = 0; tn < C::TN; ++tn)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int m = m0 + (wm * C::TM + tm) * 32 + acc_row(r, g), n = n0 + (wn * C::TN + tn) * 32 + (lane & 31);
+                    const uint32_t off = m < p.M && n < p.N ? (uint32_t)(((int64_t)m * p.ldc + n) * 4) : 0x80000000u;
+                    float v = acc[tm][tn][r];
+                    if (!p.first) v += __int_as_float(__builtin_amdgcn_raw_buffer_load_b32(rc, off, 0, 0));
+                    __builtin_amdgcn_raw_buffer_store_b32(__float_as_int(v), rc, off, 0, 0);
+                }
+    }
+};
+
+// Tiles whose wavefronts each have the whole contraction, by the number of tokens: 32, 64, 128 or 256
+// rows (a vocabulary has enough columns to fill the card with any of them).
+int head_tile(int64_t M) { return M <= 32 ? 15 : M <= 64 ? 6 : M <= 128 ? 4 : 19; }
+// fp32: vocabulary x tokens
+int head_tile_f32(int64_t M) { return M <= 64 ? 2 : 0; }
+
+template <typename EP>
+hipError_t launch_head(int f32, int table, HeadArgs& p, hipStream_t s) {
+    if (!f32) {  // C = X W: tokens are the rows
+        switch (head_tile(p.tokens)) {
+            case 15: return table ? launch_gemm_bf16<15, false, true, EP>(p, s) : launch_gemm_bf16<15, false, false, EP>(p, s);
+            case 6: return table ? launch_gemm_bf16<6, false, true, EP>(p, s) : launch_gemm_bf16<6, false, false, EP>(p, s);
+            case 4: return table ? launch_gemm_bf16<4, false, true, EP>(p, s) : launch_gemm_bf16<4, false, false, EP>(p, s);
+            default: return table ? launch_gemm_bf16<19, false, true, EP>(p, s) : launch_gemm_bf16<19, false, false, EP>(p, s);
+        }
+    }
+    // C = W^T X^T: the vocabulary is the rows, so that tokens lie along the lanes here too
+    std::swap(p.a, p.b), std::swap(p.lda, p.ldb), std::swap(p.a_bytes, p.b_bytes), std::swap(p.M, p.N);
+    if (head_tile_f32(p.tokens) == 2) return table ? launch_gemm_f32<2, false, true, EP>(p, s) : launch_gemm_f32<2, true, true, EP>(p, s);
+    return table ? launch_gemm_f32<0, false, true, EP>(p, s) : launch_gemm_f32<0, true, true, EP>(p, s);
+}
+
+}  // namespace
+
+int head_tile_width(int f32, int64_t M) { return f32 ? kF32Tiles[head_tile_f32(M)].bm : kGemmTiles[head_tile(M)].bn; }
+
+hipError_t launch_head_fwd(int f32, int table, HeadArgs p, hipStream_t s) { return launch_head<HeadFwd>(f32, table, p, s); }
+hipError_t launch_head_grad(int f32, int table, HeadArgs p, hipStream_t s) { return launch_head<HeadGrad>(f32, table, p, s); }
+
+hipError_t launch_sum_gemm(int b_nmajor, int tile, const SumArgs& p, hipStream_t s) {
+    return b_nmajor ? launch_gemm_tile<false, true, SumPieces>(tile, p, s) : launch_gemm_tile<false, false, SumPieces>(tile, p, s);
+}
+hipError_t launch_sum_gemm_f32(int b_nmajor, const SumArgs& p, hipStream_t s) {
+    return b_nmajor ? launch_f32_tile<false, true, SumPieces>(f32_tile(p), p, s) : launch_f32_tile<false, false, SumPieces>(f32_tile(p), p, s);
+}
+
+}  // namespace fbl

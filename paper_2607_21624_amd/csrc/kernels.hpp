@@ -114,6 +114,18 @@ template <int ACT>
 hipError_t launch_linear_gemm_f32(int grad, const LinearArgs& p, hipStream_t stream);
 hipError_t launch_linear_act_bwd(int f32, int act, const LinearActArgs& a, hipStream_t stream);
 
+// Softmax losses of a linear head (head_gemm.hip, head_rows.hip); table: the weight is stored
+// [V, K], else [K, V].
+constexpr int kHeadMaxTop = 1024;
+int head_tile_width(int f32, int64_t M);  // vocabulary entries of a forward tile
+hipError_t launch_head_fwd(int f32, int table, HeadArgs p, hipStream_t stream);
+hipError_t launch_head_grad(int f32, int table, HeadArgs p, hipStream_t stream);
+hipError_t launch_sum_gemm(int b_nmajor, int tile, const SumArgs& p, hipStream_t stream);
+hipError_t launch_sum_gemm_f32(int b_nmajor, const SumArgs& p, hipStream_t stream);
+hipError_t launch_head_targets(const HeadRowArgs& a, hipStream_t stream);       // forward: targets, probabilities
+hipError_t launch_head_join(const HeadRowArgs& a, hipStream_t stream);          // parts -> loss, lse, sums
+hipError_t launch_head_grad_rows(const HeadRowArgs& a, hipStream_t stream);     // backward: targets, factors
+
 // The tile of kGemmTiles that FBL_GEMM_TILE_AUTO names for a projection product (api.cpp).
 int proj_auto_tile(uint32_t op, int64_t M, int64_t K, int64_t N);
 

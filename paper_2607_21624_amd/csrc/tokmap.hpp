@@ -130,4 +130,68 @@ struct LinearActArgs {
     int N, groups;
 };
 
+// Softmax of a linear head over one piece of the vocabulary: the product is X W for the piece's
+// columns (bf16: tokens are the rows; fp32: the vocabulary is).  Targets are [top][tokens].
+struct HeadArgs : GemmArgs {
+    int tokens;
+    int first, width;   // the piece: vocabulary entries first .. first + width - 1
+    int top;
+    float unit;         // log2(e) / temperature
+    const int* index;   // vocabulary entries of the targets, -1: none
+    // forward: (maximum, sum of exp2 relative to it) of each tile's columns, both in units of unit times the
+    // logit: [tile0 + tile][tokens]; logits of the targets
+    float2* part;
+    int tile0;
+    float* target;
+    // backward: dz = row.x (exp2(unit z - row.y) - sum of the targets' weights there), 0 where row.x is
+    const float2* row;
+    const float* weight;  // of the targets, nullptr: 1
+    void* dz;             // [tokens][ldz]; columns width .. ldz - 1 become 0
+    int64_t ldz;
+    uint32_t dz_bytes;
+};
+
+// A product added up over the pieces of its contraction: sum (fp32, [M][ldc] in C's place for
+// fp32 storage) is overwritten (first), added to, or, for bf16, rounded to C (last).
+struct SumArgs : GemmArgs {
+    float* sum;
+    int64_t lds;
+    uint32_t sum_bytes;
+    int first, last;
+};
+
+// The small steps around a head's loss, one row (token) of M each.
+struct HeadRowArgs {
+    int64_t M;
+    int V, top;
+    const int64_t* labels;  // cross entropy: one target a row
+    int64_t ignore;
+    const int64_t* given;  // distillation: targets [M][ldi], negative: absent
+    int64_t ldi;
+    const void* logits;  // the teacher's [M][ldl]
+    int64_t ldl;
+    int logits_f32;
+    float T;
+    // rows -> targets
+    int* index;     // [top][M]
+    float* prob;    // [M][top], weights of the targets (forward: written, backward: read)
+    float* weight;  // [top][M], the same for the backward's tiles
+    float* entropy; // [M] sum of p log p; nan: a target outside the vocabulary
+    float* counted; // [M] 1 or 0
+    // backward: factors of the rows
+    const float* dloss;
+    int64_t dloss_stride;
+    const float* total;
+    const float* lse_in;
+    float2* row;
+    // the tiles' parts -> loss
+    const float2* part;
+    int parts;
+    const float* target;  // [top][M]
+    float* loss;
+    float* lse;
+    float* sums;  // [2]: losses, rows counted
+    float* mean;  // their quotient (0 where no row counts)
+};
+
 }  // namespace fbl

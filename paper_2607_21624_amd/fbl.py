@@ -55,6 +55,9 @@ FBL_ACT_SILU = 4
 ACTIVATIONS = {"none": FBL_ACT_NONE, "relu": FBL_ACT_RELU, "gelu": FBL_ACT_GELU, "gelu_tanh": FBL_ACT_GELU_TANH,
                "silu": FBL_ACT_SILU}
 
+FBL_HEAD_KV = 0
+FBL_HEAD_VK = 1
+
 FBL_ATTN_FWD = 0
 FBL_ATTN_BWD_KV = 1
 FBL_ATTN_BWD_DQ = 2
@@ -67,7 +70,9 @@ EXPORTED = ("fbl_layout_desc", "fbl_layout_packed_qkv", "fbl_layout_offset", "fb
             "fbl_attn_tune_reset", "fbl_proj", "fbl_proj_dt",
             "fbl_gemm_tile_count", "fbl_gemm_tile_info", "fbl_proj_candidates", "fbl_proj_tune", "fbl_proj_tuned_tile", "fbl_proj_auto_tile",
             "fbl_proj_float_tile", "fbl_proj_tune_reset", "fbl_layer_norm_fwd", "fbl_layer_norm_bwd_workspace",
-            "fbl_layer_norm_bwd", "fbl_linear_fwd", "fbl_linear_bwd_workspace", "fbl_linear_bwd", "fbl_status_str")
+            "fbl_layer_norm_bwd", "fbl_linear_fwd", "fbl_linear_bwd_workspace", "fbl_linear_bwd",
+            "fbl_linear_loss_workspace", "fbl_linear_ce_fwd", "fbl_linear_ce_bwd", "fbl_linear_kd_fwd", "fbl_linear_kd_bwd",
+            "fbl_status_str")
 
 
 class Layout(ctypes.Structure):
@@ -196,6 +201,19 @@ def _load() -> ctypes.CDLL:
     lib.fbl_linear_bwd.argtypes = [i32, u32, i64, i64, i64, vp, i64, vp, i64, vp, i64, vp, i64, u32, vp, i64, vp, i64, vp,
                                    i64, vp, vp, size, vp]
     lib.fbl_linear_bwd.restype = ctypes.c_int
+    lib.fbl_linear_loss_workspace.argtypes = [i32, u32] + [i64] * 5 + [sizep]
+    lib.fbl_linear_loss_workspace.restype = ctypes.c_int
+    lib.fbl_linear_ce_fwd.argtypes = [i32, u32, i64, i64, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, vp, size, vp]
+    lib.fbl_linear_ce_fwd.restype = ctypes.c_int
+    lib.fbl_linear_ce_bwd.argtypes = [i32, u32, i64, i64, i64, vp, i64, vp, vp, i64, vp, i64, vp, i64, vp, vp, i64, vp, i64,
+                                      vp, size, vp]
+    lib.fbl_linear_ce_bwd.restype = ctypes.c_int
+    lib.fbl_linear_kd_fwd.argtypes = [i32, u32, i64, i64, i64, i64, vp, i64, vp, i64, vp, i64, i32, vp, i64, f32, vp, vp, vp,
+                                      vp, vp, vp, size, vp]
+    lib.fbl_linear_kd_fwd.restype = ctypes.c_int
+    lib.fbl_linear_kd_bwd.argtypes = [i32, u32, i64, i64, i64, i64, vp, i64, vp, vp, i64, vp, i64, vp, i64, f32, vp, vp, vp,
+                                      i64, vp, i64, vp, size, vp]
+    lib.fbl_linear_kd_bwd.restype = ctypes.c_int
     lib.fbl_status_str.argtypes = [ctypes.c_int]
     lib.fbl_status_str.restype = ctypes.c_char_p
     return lib
@@ -1000,3 +1018,209 @@ def linear_bwd(dy, x, w, z=None, act: str = "none", dx=None, dw=None, dbias=None
                               ldxz, _ptr(dx), lddx, _ptr(dw), lddw, _ptr(dbias), _ptr(ws), ws_bytes,
                               _launch_stream(stream)), "fbl_linear_bwd")
     return dx, dw, dbias
+
+
+# ------------------------------------- losses of a linear head over a vocabulary
+def _head(w, x, where: str, name: str = "w"):
+    """(order, row stride) of a head's weight [K, V]: stored by rows of V, or, as the
+    transposed view of a table, by rows of K."""
+    if w.dim() != 2:
+        raise FblError(FBL_ERR_SHAPE, f"{where}: {name} must be 2-D, got shape {tuple(w.shape)}")
+    if w.dtype != x.dtype:
+        raise FblError(FBL_ERR_DTYPE, f"{where}: {name} is {w.dtype}, needs {x.dtype}")
+    K, V = w.shape
+    if K != x.shape[1]:
+        raise FblError(FBL_ERR_SHAPE, f"{where}: x {tuple(x.shape)} and {name} {tuple(w.shape)} do not agree")
+    if w.stride(1) == 1 and (K == 1 or w.stride(0) >= V):
+        return FBL_HEAD_KV, (w.stride(0) if K > 1 else max(w.stride(0), V))
+    if w.stride(0) == 1 or K == 1:
+        return FBL_HEAD_VK, (w.stride(1) if V > 1 else max(w.stride(1), K))
+    raise FblError(FBL_ERR_LAYOUT, f"{where}: {name} [K, V] needs rows of V or, as a table's transposed view, of K, got "
+                                   f"strides {w.stride()}")
+
+
+def linear_loss_workspace(x, w, top: int = 1) -> int:
+    """Bytes of the workspace of linear_ce_fwd and _bwd (top 1) or linear_kd_fwd and _bwd."""
+    order, ldw = _head(w, x, "linear_loss_workspace")
+    n = ctypes.c_size_t(0)
+    _check(LIB.fbl_linear_loss_workspace(_dtype_code(x), order, *x.shape, w.shape[1], top, ldw, ctypes.byref(n)),
+           "fbl_linear_loss_workspace")
+    return int(n.value)
+
+
+def _new_f32(t, n: int, like, where: str, name: str):
+    import torch
+    if t is None:
+        t = torch.empty(n, dtype=torch.float32, device=like.device)
+    _vector(t, where, name, n, torch.float32)
+    return t
+
+
+def _loss_scratch(workspace, x, w, top: int, where: str, stream):
+    need = 0 if workspace is not None else linear_loss_workspace(x, w, top)
+    return _scratch(workspace, need, where, x, stream)
+
+
+def _mean_ptr(mean, where: str):
+    import torch
+    if mean is None:
+        return None
+    if mean.dtype != torch.float32 or mean.numel() != 1:
+        raise FblError(FBL_ERR_SHAPE, f"{where}: mean must be one float32")
+    return _ptr(mean)
+
+
+def _dloss(dloss, M: int, where: str) -> int:
+    """Stride of the loss' gradient: one number, or one a row."""
+    import torch
+    if dloss.dtype != torch.float32:
+        raise FblError(FBL_ERR_DTYPE, f"{where}: dloss is {dloss.dtype}, needs torch.float32")
+    if dloss.dim() == 0 or tuple(dloss.shape) == (1,) and M != 1:
+        return 0
+    if tuple(dloss.shape) != (M,):
+        raise FblError(FBL_ERR_SHAPE, f"{where}: dloss has shape {tuple(dloss.shape)}, needs () or {(M,)}")
+    return dloss.stride(0)
+
+
+def _head_grads(x, w, dx, dw, need_dx: bool, need_dw: bool, order: int, where: str):
+    """(dx, its row stride, dw, its row stride): the given ones, or new ones where needed."""
+    import torch
+    if dx is None and need_dx:
+        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    lddx = 0 if dx is None else _matrix(dx, where, "dx", x.shape, x)
+    if dw is None and need_dw:
+        K, V = w.shape
+        dw = (torch.empty((V, K), dtype=x.dtype, device=x.device).t() if order == FBL_HEAD_VK else
+              torch.empty((K, V), dtype=x.dtype, device=x.device))
+    lddw = 0
+    if dw is not None:
+        if tuple(dw.shape) != tuple(w.shape):
+            raise FblError(FBL_ERR_SHAPE, f"{where}: dw has shape {tuple(dw.shape)}, needs {tuple(w.shape)}")
+        dorder, lddw = _head(dw, x, where, "dw")
+        if dorder != order:
+            raise FblError(FBL_ERR_LAYOUT, f"{where}: dw must be stored by the same rows as w")
+    return dx, lddx, dw, lddw
+
+
+def linear_ce_fwd(x, w, labels, ignore_index: int = -100, loss=None, lse=None, total=None, mean=None, workspace=None,
+                  stream=None):
+    """Softmax cross entropy of the logits x w, which are never kept: x [M, K], w [K, V] (rows of V,
+    or the transposed view of a [V, K] table), labels int64 [M].  Returns (loss, lse, total): each row's loss and
+    log-sum-exp, float32 [M], and [their sum, the number of rows that count].  Rows labelled
+    ignore_index do not count; a label outside the vocabulary makes its row's loss nan.  mean: one float32 that
+    receives total[0] / total[1]."""
+    import torch
+    where = "linear_ce_fwd"
+    _check_device(where, stream, x=x, w=w, labels=labels, loss=loss, lse=lse, total=total, mean=mean, workspace=workspace)
+    ldx = _matrix(x, where, "x")
+    M, K = x.shape
+    dt = _dtype_code(x)
+    order, ldw = _head(w, x, where)
+    _vector(labels, where, "labels", M, torch.int64)
+    loss, lse = _new_f32(loss, M, x, where, "loss"), _new_f32(lse, M, x, where, "lse")
+    total = _new_f32(total, 2, x, where, "total")
+    ws, ws_bytes = _loss_scratch(workspace, x, w, 1, where, stream)
+    _check(LIB.fbl_linear_ce_fwd(dt, order, M, K, w.shape[1], _ptr(x), ldx, _ptr(w), ldw, _ptr(labels), ignore_index, _ptr(loss),
+                                 _ptr(lse), _ptr(total), _mean_ptr(mean, where), _ptr(ws), ws_bytes,
+                                 _launch_stream(stream)), "fbl_linear_ce_fwd")
+    return loss, lse, total
+
+
+def linear_ce_bwd(dloss, x, w, labels, lse, total=None, ignore_index: int = -100, dx=None, dw=None, workspace=None,
+                  stream=None, need_dx: bool = True, need_dw: bool = True):
+    """Gradients (dx, dw) of linear_ce_fwd, each None where not needed; dw is stored as w is.  dloss,
+    float32, is the gradient of each row's loss ([M], or one number for all), or with the
+    forward's total that of the mean over the rows that count."""
+    import torch
+    where = "linear_ce_bwd"
+    _check_device(where, stream, dloss=dloss, x=x, w=w, labels=labels, lse=lse, total=total, dx=dx, dw=dw,
+                  workspace=workspace)
+    ldx = _matrix(x, where, "x")
+    M, K = x.shape
+    dt = _dtype_code(x)
+    order, ldw = _head(w, x, where)
+    _vector(labels, where, "labels", M, torch.int64)
+    _vector(lse, where, "lse", M, torch.float32)
+    _vector(total, where, "total", 2, torch.float32)
+    gstride = _dloss(dloss, M, where)
+    dx, lddx, dw, lddw = _head_grads(x, w, dx, dw, need_dx, need_dw, order, where)
+    ws, ws_bytes = _loss_scratch(workspace, x, w, 1, where, stream)
+    _check(LIB.fbl_linear_ce_bwd(dt, order, M, K, w.shape[1], _ptr(dloss), gstride, _ptr(total), _ptr(x), ldx, _ptr(w), ldw,
+                                 _ptr(labels), ignore_index, _ptr(lse), _ptr(dx), lddx, _ptr(dw), lddw, _ptr(ws), ws_bytes,
+                                 _launch_stream(stream)), "fbl_linear_ce_bwd")
+    return dx, dw
+
+
+def _teacher(index, logits, x, where: str):
+    """(top, row strides of index and logits, logits' dtype code)."""
+    import torch
+    if index.dim() != 2 or index.shape[0] != x.shape[0]:
+        raise FblError(FBL_ERR_SHAPE, f"{where}: index has shape {tuple(index.shape)}, needs ({x.shape[0]}, top)")
+    if index.dtype != torch.int64:
+        raise FblError(FBL_ERR_DTYPE, f"{where}: index is {index.dtype}, needs torch.int64")
+    ldi = _matrix(index, where, "index")
+    if logits is None:
+        return index.shape[1], ldi, 0, 0
+    ldl = _matrix(logits, where, "logits", index.shape)
+    return index.shape[1], ldi, ldl, _dtype_code(logits)
+
+
+def linear_kd_fwd(x, w, index, logits, temperature: float = 1.0, loss=None, lse=None, prob=None, total=None, mean=None,
+                  workspace=None, stream=None):
+    """Distillation from a teacher's top logits on the student's logits x w, which are never kept: index int64 and
+    logits (float32 or bfloat16) [M, top] are the teacher's, loss[m] = T^2 sum p (log p - log q) with p = softmax(logits /
+    T) over the row's entries and q = softmax(x w / T) over the vocabulary.  A negative index is an absent entry; a
+    row without entries does not count.  Returns (loss, lse, prob, total); prob float32 [M, top]."""
+    import torch
+    where = "linear_kd_fwd"
+    _check_device(where, stream, x=x, w=w, index=index, logits=logits, loss=loss, lse=lse, prob=prob, total=total, mean=mean,
+                  workspace=workspace)
+    ldx = _matrix(x, where, "x")
+    M, K = x.shape
+    dt = _dtype_code(x)
+    order, ldw = _head(w, x, where)
+    top, ldi, ldl, ldt = _teacher(index, logits, x, where)
+    loss, lse = _new_f32(loss, M, x, where, "loss"), _new_f32(lse, M, x, where, "lse")
+    total = _new_f32(total, 2, x, where, "total")
+    if prob is None:
+        prob = torch.empty((M, top), dtype=torch.float32, device=x.device)
+    _contiguous(prob, where, "prob", (M, top))
+    ws, ws_bytes = _loss_scratch(workspace, x, w, top, where, stream)
+    _check(LIB.fbl_linear_kd_fwd(dt, order, M, K, w.shape[1], top, _ptr(x), ldx, _ptr(w), ldw, _ptr(index), ldi, ldt,
+                                 _ptr(logits), ldl, float(temperature), _ptr(prob), _ptr(loss), _ptr(lse), _ptr(total),
+                                 _mean_ptr(mean, where), _ptr(ws), ws_bytes, _launch_stream(stream)), "fbl_linear_kd_fwd")
+    return loss, lse, prob, total
+
+
+def _contiguous(t, where: str, name: str, shape):
+    import torch
+    if t.dtype != torch.float32:
+        raise FblError(FBL_ERR_DTYPE, f"{where}: {name} is {t.dtype}, needs torch.float32")
+    if tuple(t.shape) != tuple(shape):
+        raise FblError(FBL_ERR_SHAPE, f"{where}: {name} has shape {tuple(t.shape)}, needs {tuple(shape)}")
+    if not t.is_contiguous():
+        raise FblError(FBL_ERR_LAYOUT, f"{where}: {name} must be contiguous")
+
+
+def linear_kd_bwd(dloss, x, w, index, prob, lse, temperature: float = 1.0, total=None, dx=None, dw=None, workspace=None,
+                  stream=None, need_dx: bool = True, need_dw: bool = True):
+    """Gradients (dx, dw) of linear_kd_fwd from its prob and lse; the rest as linear_ce_bwd."""
+    import torch
+    where = "linear_kd_bwd"
+    _check_device(where, stream, dloss=dloss, x=x, w=w, index=index, prob=prob, lse=lse, total=total, dx=dx, dw=dw,
+                  workspace=workspace)
+    ldx = _matrix(x, where, "x")
+    M, K = x.shape
+    dt = _dtype_code(x)
+    order, ldw = _head(w, x, where)
+    top, ldi, _, _ = _teacher(index, None, x, where)
+    _contiguous(prob, where, "prob", (M, top))
+    _vector(lse, where, "lse", M, torch.float32)
+    _vector(total, where, "total", 2, torch.float32)
+    gstride = _dloss(dloss, M, where)
+    dx, lddx, dw, lddw = _head_grads(x, w, dx, dw, need_dx, need_dw, order, where)
+    ws, ws_bytes = _loss_scratch(workspace, x, w, top, where, stream)
+    _check(LIB.fbl_linear_kd_bwd(dt, order, M, K, w.shape[1], top, _ptr(dloss), gstride, _ptr(total), _ptr(x), ldx, _ptr(w), ldw,
+                                 _ptr(index), ldi, float(temperature), _ptr(prob), _ptr(lse), _ptr(dx), lddx, _ptr(dw), lddw,
+                                 _ptr(ws), ws_bytes, _launch_stream(stream)), "fbl_linear_kd_bwd")
+    return dx, dw

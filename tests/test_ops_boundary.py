@@ -134,3 +134,117 @@ def test_linear_workspace_and_binding():
         with pytest.raises(fbl.FblError) as e:
             call()
         assert e.value.status == F.FBL_ERR_ARG
+
+
+# ------------------------------------------------------- losses of a linear head
+def ce_fwd(**kw):
+    return LIB.fbl_linear_ce_fwd(*_merge(dict(dt=BF16, order=1, M=8, K=64, V=100, x=at(1), ldx=64, w=at(2), ldw=64, labels=at(3),
+                                              ignore=-100, loss=at(4), lse=at(5), total=at(6), mean=at(7), ws=at(8),
+                                              ws_bytes=1 << 19, stream=None), kw))
+
+
+def ce_bwd(**kw):
+    return LIB.fbl_linear_ce_bwd(*_merge(dict(dt=BF16, order=1, M=8, K=64, V=100, dloss=at(1), stride=0, total=at(2), x=at(3),
+                                              ldx=64, w=at(4), ldw=64, labels=at(5), ignore=-100, lse=at(6), dx=at(7), lddx=64,
+                                              dw=at(8), lddw=64, ws=at(9), ws_bytes=1 << 19, stream=None), kw))
+
+
+def kd_fwd(**kw):
+    return LIB.fbl_linear_kd_fwd(*_merge(dict(dt=BF16, order=0, M=8, K=64, V=104, top=4, x=at(1), ldx=64, w=at(2), ldw=104,
+                                              index=at(3), ldi=4, ldt=F32, logits=at(4), ldl=4, T=2.0, prob=at(5), loss=at(6),
+                                              lse=at(7), total=at(8), mean=at(9), ws=at(10), ws_bytes=1 << 19, stream=None), kw))
+
+
+def kd_bwd(**kw):
+    return LIB.fbl_linear_kd_bwd(*_merge(dict(dt=BF16, order=0, M=8, K=64, V=104, top=4, dloss=at(1), stride=1, total=None,
+                                              x=at(2), ldx=64, w=at(3), ldw=104, index=at(4), ldi=4, T=2.0, prob=at(5), lse=at(6),
+                                              dx=at(7), lddx=64, dw=at(8), lddw=104, ws=at(9), ws_bytes=1 << 19, stream=None),
+                                         kw))
+
+
+COMMON = [
+    (dict(dt=3), F.FBL_ERR_DTYPE), (dict(order=2), F.FBL_ERR_ARG), (dict(M=0), F.FBL_ERR_SHAPE), (dict(K=-8), F.FBL_ERR_SHAPE),
+    (dict(V=1 << 31), F.FBL_ERR_SHAPE), (dict(K=60), F.FBL_ERR_UNSUPPORTED), (dict(M=1 << 24), F.FBL_ERR_UNSUPPORTED),
+    (dict(x=None), F.FBL_ERR_NULL), (dict(w=None), F.FBL_ERR_NULL), (dict(lse=None), F.FBL_ERR_NULL),
+    (dict(ldx=56), F.FBL_ERR_LAYOUT), (dict(ldw=56), F.FBL_ERR_LAYOUT), (dict(ldx=68), F.FBL_ERR_ALIGN),
+    (dict(w=at(2, 4)), F.FBL_ERR_ALIGN), (dict(lse=at(5, 2)), F.FBL_ERR_ALIGN), (dict(ws=None), F.FBL_ERR_WORKSPACE),
+    (dict(ws_bytes=64), F.FBL_ERR_WORKSPACE), (dict(ws=at(8, 8)), F.FBL_ERR_ALIGN),
+    (dict(dt=F32, x=at(1, 2), ldx=64), F.FBL_ERR_ALIGN),
+]
+
+
+@pytest.mark.parametrize("kw,status", COMMON + [
+    (dict(labels=None), F.FBL_ERR_NULL), (dict(loss=None), F.FBL_ERR_NULL), (dict(total=None), F.FBL_ERR_NULL),  # mean needs total
+    (dict(labels=at(3, 4)), F.FBL_ERR_ALIGN), (dict(order=0, V=100, ldw=104), F.FBL_ERR_UNSUPPORTED),
+    (dict(loss=at(1)), F.FBL_ERR_ARG), (dict(lse=at(4)), F.FBL_ERR_ARG), (dict(ws=at(2)), F.FBL_ERR_ARG),
+    (dict(mean=at(6, 4)), F.FBL_ERR_ARG), (dict(total=at(8)), F.FBL_ERR_ARG), (dict(loss=at(3)), F.FBL_ERR_ARG),
+])
+def test_linear_ce_fwd_refusals(kw, status):
+    assert ce_fwd(**kw) == status
+
+
+@pytest.mark.parametrize("kw,status", COMMON + [
+    (dict(dloss=None), F.FBL_ERR_NULL), (dict(labels=None), F.FBL_ERR_NULL), (dict(stride=-1), F.FBL_ERR_LAYOUT),
+    (dict(lddx=0), F.FBL_ERR_LAYOUT), (dict(lddw=63), F.FBL_ERR_LAYOUT), (dict(dx=at(7, 8)), F.FBL_ERR_ALIGN),
+    (dict(dw=at(8, 2)), F.FBL_ERR_ALIGN), (dict(dloss=at(1, 1)), F.FBL_ERR_ALIGN), (dict(dx=at(3)), F.FBL_ERR_ARG),
+    (dict(dw=at(4)), F.FBL_ERR_ARG), (dict(dw=at(7)), F.FBL_ERR_ARG), (dict(ws=at(6)), F.FBL_ERR_ARG),
+])
+def test_linear_ce_bwd_refusals(kw, status):
+    assert ce_bwd(**kw) == status
+
+
+@pytest.mark.parametrize("kw,status", [(k, s) for k, s in COMMON if "ldw" not in k and "lse" not in k and "ws" not in k] + [
+    (dict(top=0), F.FBL_ERR_SHAPE), (dict(top=1025, ldi=1025, ldl=1025), F.FBL_ERR_UNSUPPORTED), (dict(T=0.0), F.FBL_ERR_ARG),
+    (dict(T=-1.0), F.FBL_ERR_ARG), (dict(T=float("inf")), F.FBL_ERR_ARG), (dict(T=float("nan")), F.FBL_ERR_ARG),
+    (dict(index=None), F.FBL_ERR_NULL), (dict(logits=None), F.FBL_ERR_NULL), (dict(prob=None), F.FBL_ERR_NULL),
+    (dict(ldt=4), F.FBL_ERR_DTYPE), (dict(ldi=3), F.FBL_ERR_LAYOUT), (dict(ldl=3), F.FBL_ERR_LAYOUT), (dict(ldw=103), F.FBL_ERR_LAYOUT),
+    (dict(ldw=108), F.FBL_ERR_ALIGN), (dict(V=100), F.FBL_ERR_UNSUPPORTED), (dict(prob=at(3)), F.FBL_ERR_ARG),
+    (dict(prob=at(6)), F.FBL_ERR_ARG), (dict(index=at(3, 4)), F.FBL_ERR_ALIGN), (dict(ws=at(4)), F.FBL_ERR_ARG),
+])
+def test_linear_kd_fwd_refusals(kw, status):
+    assert kd_fwd(**kw) == status
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(top=-1), F.FBL_ERR_SHAPE), (dict(T=0.0), F.FBL_ERR_ARG), (dict(index=None), F.FBL_ERR_NULL), (dict(prob=None), F.FBL_ERR_NULL),
+    (dict(lse=None), F.FBL_ERR_NULL), (dict(ldi=2), F.FBL_ERR_LAYOUT), (dict(prob=at(5, 2)), F.FBL_ERR_ALIGN),
+    (dict(dx=at(5)), F.FBL_ERR_ARG), (dict(dw=at(3)), F.FBL_ERR_ARG), (dict(ws=at(2)), F.FBL_ERR_ARG),
+    (dict(ws_bytes=100), F.FBL_ERR_WORKSPACE), (dict(lddw=96), F.FBL_ERR_LAYOUT),
+])
+def test_linear_kd_bwd_refusals(kw, status):
+    assert kd_bwd(**kw) == status
+
+
+def test_linear_loss_workspace():
+    n = ctypes.c_size_t()
+    f = lambda dt=BF16, order=1, M=4096, K=1024, V=50257, top=1, ldw=1024: LIB.fbl_linear_loss_workspace(
+        dt, order, M, K, V, top, ldw, ctypes.byref(n))
+    assert f() == F.FBL_OK
+    # never the logits of 50257 entries, let alone in fp32: pieces of 128 MiB, 16 MiB of sums and lists
+    assert n.value < 4096 * 50257 * 2 / 2
+    assert f(V=16) == F.FBL_OK and n.value < 1 << 20
+    assert LIB.fbl_linear_loss_workspace(BF16, 1, 8, 64, 64, 1, 64, None) == F.FBL_ERR_NULL
+    assert f(dt=9) == F.FBL_ERR_DTYPE and f(order=3) == F.FBL_ERR_ARG and f(V=0) == F.FBL_ERR_SHAPE
+    assert f(ldw=1000) == F.FBL_ERR_LAYOUT and f(ldw=1028) == F.FBL_ERR_ALIGN and f(top=1025) == F.FBL_ERR_UNSUPPORTED
+    # [K, V] rows beyond a span are refused, a table of any size is not
+    assert f(order=0, K=8192, V=262144, ldw=262144) == F.FBL_ERR_UNSUPPORTED
+    assert f(order=1, K=8192, V=262144, ldw=8192) == F.FBL_OK
+
+
+def test_losses_binding_refuses_host_tensors_and_layouts():
+    x, w, lab = torch.zeros(4, 64), torch.zeros(64, 100), torch.zeros(4, dtype=torch.int64)
+    for call in (lambda: fbl.linear_ce_fwd(x, w, lab), lambda: fbl.linear_kd_fwd(x, w, lab[:, None], x[:, :1]),
+                 lambda: fbl.linear_ce_bwd(x[0, 0], x, w, lab, x[:, 0]),
+                 lambda: fbl.linear_kd_bwd(x[0, 0], x, w, lab[:, None], x[:, :1], x[:, 0])):
+        with pytest.raises(fbl.FblError) as e:
+            call()
+        assert e.value.status == F.FBL_ERR_ARG
+    head = F._head
+    assert head(w, x, "") == (0, 100) and head(torch.zeros(100, 64).t(), x, "") == (1, 64)
+    assert head(torch.zeros(64, 120)[:, :100], x, "") == (0, 120) and head(torch.zeros(100, 80)[:, :64].t(), x, "") == (1, 80)
+    with pytest.raises(fbl.FblError) as e:
+        head(torch.zeros(64, 200)[:, ::2], x, "")
+    assert e.value.status == F.FBL_ERR_LAYOUT
+    with pytest.raises(fbl.FblError) as e:
+        head(torch.zeros(1, 100).expand(64, 100), x, "")  # one row for all
+    assert e.value.status == F.FBL_ERR_LAYOUT
