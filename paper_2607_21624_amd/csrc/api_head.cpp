@@ -74,7 +74,7 @@ int64_t padded64(int64_t n) { return (n + 63) / 64 * 64; }
 
 struct HeadWs {
     size_t index, target, part, entropy, counted, fwd;  // forward
-    size_t weight, row, dz, sum, bwd;                   // backward
+    size_t weight, row, scale, dz, sum, bwd;            // backward
 };
 HeadWs head_ws(const Shape& s, int64_t ldw) {
     HeadWs w{};
@@ -86,7 +86,8 @@ HeadWs head_ws(const Shape& s, int64_t ldw) {
     w.counted = w.entropy + row, w.fwd = w.counted + row;
     const int64_t bp = backward_piece(s, ldw);
     w.weight = list, w.row = w.weight + list;
-    w.dz = w.row + align256((size_t)s.M * 8);
+    w.scale = w.row + align256((size_t)s.M * 8);
+    w.dz = w.scale + 256;
     w.sum = w.dz + align256((size_t)s.M * (size_t)padded64(bp) * (size_t)s.es());
     w.bwd = w.sum + (bp < s.V && !s.f32() ? align256((size_t)s.M * (size_t)s.K * 4) : 0);
     return w;
@@ -233,6 +234,9 @@ fbl_status head_bwd(const Shape& s, const float* dloss, int64_t dloss_stride, co
     fbl::HeadRowArgs a = row_args(s, t);
     a.index = reinterpret_cast<int*>(base + lay.index), a.weight = reinterpret_cast<float*>(base + lay.weight);
     a.row = reinterpret_cast<float2*>(base + lay.row);
+    // bf16: one factor for all rows stays out of dz, rows' own are in it
+    float* const scale = s.f32() ? nullptr : reinterpret_cast<float*>(base + lay.scale);
+    a.scale = scale;
     a.dloss = dloss, a.dloss_stride = dloss_stride, a.total = total, a.lse_in = lse;
     hipError_t e = fbl::launch_head_grad_rows(a, hs);
     const int64_t piece = backward_piece(s, ldw);
@@ -257,23 +261,25 @@ fbl_status head_bwd(const Shape& s, const float* dloss, int64_t dloss_stride, co
             else fbl::product(q, op, az, wp, vdx, s.M, s.K, kc);
             q.first = first, q.last = last;
             const int tile = s.f32() ? 0 : s.table() ? fbl::proj_auto_tile(op, s.M, kc, s.K) : fbl::proj_auto_tile(op, s.M, s.K, kc);
-            if (first && last) {
-                e = s.f32() ? fbl::launch_proj_gemm_f32(0, !s.table(), q, hs) : fbl::launch_proj_gemm(0, !s.table(), tile, q, hs);
-            } else if (s.f32()) {
+            if (s.f32()) {
                 e = fbl::launch_sum_gemm_f32(!s.table(), q, hs);
             } else {
-                q.sum = reinterpret_cast<float*>(base + lay.sum), q.lds = s.K;
-                q.sum_bytes = (uint32_t)(s.M * s.K * 4);
-                e = fbl::launch_sum_gemm(!s.table(), tile, q, hs);
+                q.scale = scale;
+                if (!first || !last) {
+                    q.sum = reinterpret_cast<float*>(base + lay.sum), q.lds = s.K;
+                    q.sum_bytes = (uint32_t)(s.M * s.K * 4);
+                }
+                e = fbl::launch_sum_gemm(0, !s.table(), tile, q, hs);
             }
         }
         if (e == hipSuccess && dw) {
             const RowsView dz{vz.p, s.M, width, ldz, s.es()}, dwp = weight_view(s, dw, lddw, v0, width);
-            fbl::GemmArgs q{};
+            fbl::SumArgs q{};
             const int64_t rows = s.table() ? width : s.K, cols = s.table() ? s.K : width;
             fbl::product(q, FBL_PROJ_BWD_WEIGHT, s.table() ? dz : vx, s.table() ? vx : dz, dwp, s.M, rows, cols);
+            q.scale = scale, q.first = q.last = 1;
             e = s.f32() ? fbl::launch_proj_gemm_f32(1, 0, q, hs)
-                        : fbl::launch_proj_gemm(1, 0, fbl::proj_auto_tile(FBL_PROJ_BWD_WEIGHT, s.M, rows, cols), q, hs);
+                        : fbl::launch_sum_gemm(1, 0, fbl::proj_auto_tile(FBL_PROJ_BWD_WEIGHT, s.M, rows, cols), q, hs);
         }
     }
     return e == hipSuccess ? FBL_OK : FBL_ERR_HIP;

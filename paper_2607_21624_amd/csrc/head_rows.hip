@@ -147,6 +147,11 @@ __global__ __launch_bounds__(1024) void head_sums(HeadRowArgs a) {
 FBL_DEV float2 row_factor(const HeadRowArgs& a, int64_t m, bool counted, bool bad) {
     float g = a.dloss[m * a.dloss_stride] * a.T;
     if (a.total) g /= fmaxf(a.total[1], 1.f);
+    if (a.scale) {
+        const bool one = a.dloss_stride == 0;  // one factor for all rows
+        if (m == 0) *a.scale = one ? g : 1.f;
+        if (one) g = 1.f;
+    }
     return make_float2(!counted ? 0.f : bad ? quiet_nan() : g, a.lse_in[m] * kLog2e);
 }
 

@@ -120,7 +120,7 @@ constexpr int kHeadMaxTop = 1024;
 int head_tile_width(int f32, int64_t M);  // vocabulary entries of a forward tile
 hipError_t launch_head_fwd(int f32, int table, HeadArgs p, hipStream_t stream);
 hipError_t launch_head_grad(int f32, int table, HeadArgs p, hipStream_t stream);
-hipError_t launch_sum_gemm(int b_nmajor, int tile, const SumArgs& p, hipStream_t stream);
+hipError_t launch_sum_gemm(int a_kmajor, int b_nmajor, int tile, const SumArgs& p, hipStream_t stream);
 hipError_t launch_sum_gemm_f32(int b_nmajor, const SumArgs& p, hipStream_t stream);
 hipError_t launch_head_targets(const HeadRowArgs& a, hipStream_t stream);       // forward: targets, probabilities
 hipError_t launch_head_join(const HeadRowArgs& a, hipStream_t stream);          // parts -> loss, lse, sums

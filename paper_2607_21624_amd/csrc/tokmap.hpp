@@ -151,10 +151,12 @@ struct HeadArgs : GemmArgs {
     uint32_t dz_bytes;
 };
 
-// A product added up over the pieces of its contraction: sum (fp32, [M][ldc] in C's place for
-// fp32 storage) is overwritten (first), added to, or, for bf16, rounded to C (last).
+// A product added up over the pieces of its contraction.  bf16: sum (fp32) is overwritten
+// (first) or added to, and with the last piece scaled by *scale and rounded to C; a piece that is both is C
+// at once.  fp32: C itself is overwritten (first) or added to.
 struct SumArgs : GemmArgs {
     float* sum;
+    const float* scale;
     int64_t lds;
     uint32_t sum_bytes;
     int first, last;
@@ -184,6 +186,7 @@ struct HeadRowArgs {
     const float* total;
     const float* lse_in;
     float2* row;
+    float* scale;  // bf16: what dx and dw are multiplied by -- the factor, where it is the same for all rows, and row.x 1 or 0
     // the tiles' parts -> loss
     const float2* part;
     int parts;
