@@ -62,6 +62,8 @@ struct GemmCfg {
     static_assert((TM - 1) * 32 * BK * 2 < 65536 && (TN - 1) * 32 * BK * 2 < 65536 &&
                       (KCW - 1) * 16 * (BM > BN ? BM : BN) * 2 + 128 < 65536,
                   "LDS read immediates fit 16 bits");
+    static constexpr int ROWS_BYTES = WM * WN * 32 * (32 * TN + 4) * 4;  // of by_rows below
+    static_assert(ROWS_BYTES <= 160 * 1024, "LDS");
     static_assert(BYTES <= 160 * 1024 && NS * STAGE <= BYTES && (WK - 1) * WM * WN * PART <= BYTES, "LDS");
     static_assert((NS - 1) * LOADS < 64, "vmcnt range");
     // wavefronts per SIMD the registers must allow: two workgroups per CU where LDS does
@@ -77,6 +79,7 @@ struct GemmCfg {
 // The loads have all landed; LDS is free once the wavefronts have met at a barrier.
 struct PlainStore {
     using Args = GemmArgs;
+    static constexpr bool kByRows = false;  // done uses by_rows
 };
 
 template <int BM, int BN, int BK, int NS, int WM, int WN, int WK, bool AT, bool BT, typename EP>
@@ -362,16 +365,79 @@ proj_gemm_bf16(typename EP::Args p) {
     }
 }
 
+// A wavefront's accumulators by rows: f(m, n, v) gets 8 consecutive columns n .. n+7 of row m,
+// neighbouring lanes the next 8, so that whole 128-byte lines are loaded and stored beside them.  (As they
+// stand a lane has 4 columns of a row and the lanes 32 rows: a layer that writes y and z that
+// way and reads a residual spends as long on it as on a contraction of 1500.  4096 x 8192 from 2048,
+// GELU: 208 us, 140 through here.)  Each 32 rows go through LDS, 32 x (32 TN + 4) floats of
+// the wavefront's own; the pitch puts 16 rows' writes on different banks.
+template <typename C, typename F>
+FBL_DEV void by_rows(uint32_t lds, const f32x16 (&acc)[C::TN][C::TM], int m0, int n0, int wm, int wn, F&& f) {
+    constexpr int PITCH = 32 * C::TN + 4, LANES = 4 * C::TN, ROWS = 64 / LANES;  // lanes a row, rows a turn
+    const int lane = threadIdx.x & 63, g = lane >> 5;
+    const uint32_t mine = lds + (uint32_t)((wn * C::WM + wm) * 32 * PITCH * 4);
+    const uint32_t put = mine + (uint32_t)(((lane & 31) * PITCH + 4 * g) * 4);
+    const uint32_t get = mine + (uint32_t)((lane / LANES * PITCH + lane % LANES * 8) * 4);
+    __syncthreads();  // the stages have been read
+#pragma unroll
+    for (int tm = 0; tm < C::TM; ++tm) {
+#pragma unroll
+        for (int tn = 0; tn < C::TN; ++tn)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                *(FBL_LDS f32x4*)(uintptr_t)(put + (tn * 32 + 8 * q) * 4) =
+                    f32x4{acc[tn][tm][4 * q], acc[tn][tm][4 * q + 1], acc[tn][tm][4 * q + 2], acc[tn][tm][4 * q + 3]};
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll
+        for (int i = 0; i < 32 / ROWS; ++i) {
+            const f32x4 a = *(const FBL_LDS f32x4*)(uintptr_t)(get + i * ROWS * PITCH * 4);
+            const f32x4 b = *(const FBL_LDS f32x4*)(uintptr_t)(get + i * ROWS * PITCH * 4 + 16);
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = a[e], v[4 + e] = b[e];
+            f(m0 + (wm * C::TM + tm) * 32 + i * ROWS + lane / LANES, n0 + wn * C::TN * 32 + lane % LANES * 8, v);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    }
+}
+
+using i32x2 = int __attribute__((ext_vector_type(2)));
+using i32x4 = int __attribute__((ext_vector_type(4)));
+
+FBL_DEV __amdgpu_buffer_rsrc_t span(const void* p, uint32_t bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, p ? (int)bytes : 0, 0x00020000);
+}
+constexpr uint32_t kNowhere = 0x80000000u;  // past every span: loads give 0, stores are dropped
+
+// 8 elements of a row, from a column that is a multiple of 8 on
+FBL_DEV bf16x8 load8(__amdgpu_buffer_rsrc_t r, uint32_t off) {
+    return __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0));
+}
+// ... stored where columns n .. of a row of N (a multiple of 4) have room for them
+FBL_DEV void store8(__amdgpu_buffer_rsrc_t r, uint32_t off, const float (&v)[8], int n, int N) {
+    bf16x8 x;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = (bf16)v[e];
+    const i32x4 w = __builtin_bit_cast(i32x4, x);
+    __builtin_amdgcn_raw_buffer_store_b128(w, r, n + 8 <= N ? off : kNowhere, 0, 0);
+    if (N & 4) __builtin_amdgcn_raw_buffer_store_b64(i32x2{w[0], w[1]}, r, n + 4 == N ? off : kNowhere, 0, 0);
+}
+
 // Launch of tile I of kGemmTiles.
 template <int I, bool AT, bool BT, typename EP>
 hipError_t launch_gemm_bf16(const typename EP::Args& p, hipStream_t stream) {
     constexpr GemmTile t = kGemmTiles[I];
     using C = GemmCfg<t.bm, t.bn, t.bk, t.ns, t.wm, t.wn, t.wk, AT, BT>;
     constexpr auto kernel = &proj_gemm_bf16<t.bm, t.bn, t.bk, t.ns, t.wm, t.wn, t.wk, AT, BT, EP>;
-    const hipError_t once = ensure_dynamic_lds<kernel>(C::BYTES);
+    constexpr int bytes = EP::kByRows && C::ROWS_BYTES > C::BYTES ? C::ROWS_BYTES : C::BYTES;
+    const hipError_t once = ensure_dynamic_lds<kernel>(bytes);
     if (once != hipSuccess) return once;
     const int tiles = ((p.M + t.bm - 1) / t.bm) * ((p.N + t.bn - 1) / t.bn);
-    hipLaunchKernelGGL(kernel, dim3((tiles + 7) / 8 * 8), dim3(64 * C::NW), C::BYTES, stream, p);
+    hipLaunchKernelGGL(kernel, dim3((tiles + 7) / 8 * 8), dim3(64 * C::NW), bytes, stream, p);
     return hipGetLastError();
 }
 

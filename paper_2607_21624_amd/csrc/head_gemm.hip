@@ -20,30 +20,45 @@ namespace fbl {
 
 namespace {
 
-using i32x2 = int __attribute__((ext_vector_type(2)));
-using i32x4 = int __attribute__((ext_vector_type(4)));
-
 // A wavefront's share of a tile: NV x NM blocks of 32 x 32, vocabulary entries v0 + 32 i + acc_row(r, g)
 // (within the piece) and tokens m0 + 32 j + lane % 32.
 //
-// Entries of the list `index` that fall on this lane's registers: hit(r, i, j, t) for target t.
-// Few tiles hold any: the registers are searched only where a lane of the wavefront has one.
+// Entries of the list `index` that fall on this lane's registers: hit(j, a, here, m, t) for target t of token m,
+// the lane's j-th: entry v0 + a where `here`.  Few tiles hold any: called only where some
+// lane of the wavefront has one.
 template <int NV, int NM, typename F>
 FBL_DEV void for_targets(const HeadArgs& p, int v0, int m0, F&& hit) {
     const int lane = threadIdx.x & 63, g = lane >> 5;
+    // 16 reads at a time, for all the wavefront's tokens: one by one each waits out its latency
+    constexpr int U = 16 / NM;
+    for (int t0 = 0; t0 < p.top; t0 += U) {
+        int at[NM][U];
 #pragma unroll
-    for (int j = 0; j < NM; ++j) {
-        const int m = m0 + 32 * j + (lane & 31);
-        for (int t = 0; t < p.top; ++t) {
-            const int at = (m < p.tokens ? p.index[(int64_t)t * p.tokens + m] : -1) - p.first - v0;
-            const bool here = (unsigned)at < 32u * NV && ((at >> 2) & 1) == g;
-            if (__builtin_amdgcn_ballot_w64(here) == 0) continue;
+        for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
+            for (int j = 0; j < NM; ++j) {
+                const int m = m0 + 32 * j + (lane & 31);
+                at[j][u] = t0 + u < p.top && m < p.tokens ? p.index[(int64_t)(t0 + u) * p.tokens + m] : -1;
+            }
+        unroll_steps(std::make_integer_sequence<int, NM>{}, [&](auto j_c) __attribute__((always_inline)) {
+            constexpr int J = decltype(j_c)::value;
+            bool any = false;
 #pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (here && at == 32 * i + acc_row(r, g)) hit(i, j, r, m, t);
-        }
+            for (int u = 0; u < U; ++u) {
+                at[J][u] -= p.first + v0;
+                if (((at[J][u] >> 2) & 1) != g) at[J][u] = -1;
+                any |= (unsigned)at[J][u] < 32u * NV;
+            }
+            if (__builtin_amdgcn_ballot_w64(any) == 0) return;
+            const int here = p.top - t0 < U ? p.top - t0 : U;
+            for (int u = 0; u < here; ++u) {
+                int a = at[J][0];
+#pragma unroll
+                for (int k = 1; k < U; ++k) a = u == k ? at[J][k] : a;
+                if (__builtin_amdgcn_ballot_w64((unsigned)a < 32u * NV) == 0) continue;
+                hit(j_c, a, (unsigned)a < 32u * NV, m0 + 32 * J + (lane & 31), t0 + u);
+            }
+        });
     }
 }
 
@@ -53,8 +68,13 @@ template <int NV, int NM, int WV, int TOKENS, int NT>
 FBL_DEV void head_stats(const HeadArgs& p, f32x16 (&acc)[NV][NM], float2* shared, int v0, int m0, int wv, int mw, int tile,
                         int tile_m0) {
     const int lane = threadIdx.x & 63, g = lane >> 5;
-    for_targets<NV, NM>(p, v0, m0, [&](int i, int j, int r, int m, int t) __attribute__((always_inline)) {
-        p.target[(int64_t)t * p.tokens + m] = acc[i][j][r];
+    for_targets<NV, NM>(p, v0, m0, [&](auto j_c, int a, bool here, int m, int t) __attribute__((always_inline)) {
+        float z = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) z = a == 32 * i + acc_row(r, g) ? acc[i][decltype(j_c)::value][r] : z;
+        if (here) p.target[(int64_t)t * p.tokens + m] = z;
     });
     if (v0 + 32 * NV > p.width) {  // columns past the piece count for nothing
 #pragma unroll
@@ -98,17 +118,8 @@ FBL_DEV void head_stats(const HeadArgs& p, f32x16 (&acc)[NV][NM], float2* shared
     }
 }
 
-FBL_DEV void put4(__amdgpu_buffer_rsrc_t rs, uint32_t off, const float (&v)[4], bf16) {
-    const bf16x4 x = bf16x4{(bf16)v[0], (bf16)v[1], (bf16)v[2], (bf16)v[3]};
-    __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(i32x2, x), rs, off, 0, 0);
-}
-FBL_DEV void put4(__amdgpu_buffer_rsrc_t rs, uint32_t off, const float (&v)[4], float) {
-    const f32x4 x = f32x4{v[0], v[1], v[2], v[3]};
-    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(i32x4, x), rs, off, 0, 0);
-}
-
-// Backward: dz, rounded to the storage type once, after the targets' part.
-template <typename T, int NV, int NM>
+// Backward: the accumulators become dz, columns past the piece 0.
+template <int NV, int NM>
 FBL_DEV void head_dz(const HeadArgs& p, f32x16 (&acc)[NV][NM], int v0, int m0) {
     const int lane = threadIdx.x & 63, g = lane >> 5;
     float scale[NM];
@@ -122,29 +133,25 @@ FBL_DEV void head_dz(const HeadArgs& p, f32x16 (&acc)[NV][NM], int v0, int m0) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][j][r] = fast_exp2(__builtin_fmaf(acc[i][j][r], p.unit, -row.y));
     }
-    for_targets<NV, NM>(p, v0, m0, [&](int i, int j, int r, int m, int t) __attribute__((always_inline)) {
-        acc[i][j][r] -= p.weight ? p.weight[(int64_t)t * p.tokens + m] : 1.f;
-    });
-    const __amdgpu_buffer_rsrc_t rz = __builtin_amdgcn_make_buffer_rsrc(p.dz, 0, (int)p.dz_bytes, 0x00020000);
-#pragma unroll
-    for (int j = 0; j < NM; ++j) {
-        const int m = m0 + 32 * j + (lane & 31);
+    for_targets<NV, NM>(p, v0, m0, [&](auto j_c, int a, bool here, int m, int t) __attribute__((always_inline)) {
+        const float w = here && p.weight ? p.weight[(int64_t)t * p.tokens + m] : 1.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int v = v0 + 32 * i + 8 * q + 4 * g;
-                float x[4];
+            for (int r = 0; r < 16; ++r) acc[i][decltype(j_c)::value][r] -= a == 32 * i + acc_row(r, g) ? w : 0.f;
+    });
 #pragma unroll
-                for (int e = 0; e < 4; ++e) x[e] = v + e < p.width && scale[j] != 0.f ? acc[i][j][4 * q + e] * scale[j] : 0.f;
-                const uint32_t off = m < p.tokens && v < p.ldz ? (uint32_t)(((int64_t)m * p.ldz + v) * sizeof(T)) : 0x80000000u;
-                put4(rz, off, x, T{});
-            }
-    }
+    for (int j = 0; j < NM; ++j)
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                acc[i][j][r] = v0 + 32 * i + acc_row(r, g) < p.width && scale[j] != 0.f ? acc[i][j][r] * scale[j] : 0.f;
 }
 
 struct HeadFwd {
     using Args = HeadArgs;
+    static constexpr bool kByRows = false;
     template <typename C>
     static FBL_DEV void done(const Args& p, uint32_t, f32x16 (&acc)[C::TN][C::TM], int m0, int n0, int wm, int wn) {
         extern __shared__ __attribute__((aligned(1024))) unsigned char gemm_smem[];
@@ -161,13 +168,34 @@ struct HeadFwd {
 
 struct HeadGrad {
     using Args = HeadArgs;
+    static constexpr bool kByRows = true;
     template <typename C>
-    static FBL_DEV void done(const Args& p, uint32_t, f32x16 (&acc)[C::TN][C::TM], int m0, int n0, int wm, int wn) {
-        head_dz<bf16>(p, acc, n0 + wn * C::TN * 32, m0 + wm * C::TM * 32);
+    static FBL_DEV void done(const Args& p, uint32_t lds, f32x16 (&acc)[C::TN][C::TM], int m0, int n0, int wm, int wn) {
+        head_dz(p, acc, n0 + wn * C::TN * 32, m0 + wm * C::TM * 32);
+        const __amdgpu_buffer_rsrc_t rz = span(p.dz, p.dz_bytes);
+        by_rows<C>(lds, acc, m0, n0, wm, wn, [&](int m, int n, float (&v)[8]) __attribute__((always_inline)) {
+            const bool in = m < p.tokens && n < p.ldz;
+            store8(rz, in ? (uint32_t)(((int64_t)m * p.ldz + n) * 2) : kNowhere, v, n, (int)p.ldz);
+        });
     }
     template <typename C>
     static FBL_DEV void done(const Args& p, float*, f32x16 (&acc)[C::TM][C::TN], int m0, int n0, int wm, int wn) {
-        head_dz<float>(p, acc, m0 + wm * C::TM * 32, n0 + wn * C::TN * 32);
+        const int lane = threadIdx.x & 63, g = lane >> 5, v0 = m0 + wm * C::TM * 32;
+        head_dz(p, acc, v0, n0 + wn * C::TN * 32);
+        const __amdgpu_buffer_rsrc_t rz = span(p.dz, p.dz_bytes);
+#pragma unroll
+        for (int j = 0; j < C::TN; ++j) {
+            const int m = n0 + (wn * C::TN + j) * 32 + (lane & 31);
+#pragma unroll
+            for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int v = v0 + 32 * i + 8 * q + 4 * g;
+                    const uint32_t off = m < p.tokens && v < p.ldz ? (uint32_t)(((int64_t)m * p.ldz + v) * 4) : kNowhere;
+                    const f32x4 x = f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+                    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(i32x4, x), rz, off, 0, 0);
+                }
+        }
     }
 };
 
@@ -180,36 +208,34 @@ struct HeadGrad {
 // which are the result's own rounding).
 struct SumPieces {
     using Args = SumArgs;
+    static constexpr bool kByRows = true;
     template <typename C>
-    static FBL_DEV void done(const Args& p, uint32_t, f32x16 (&acc)[C::TN][C::TM], int m0, int n0, int wm, int wn) {
-        const int lane = threadIdx.x & 63, g = lane >> 5;
+    static FBL_DEV void done(const Args& p, uint32_t lds, f32x16 (&acc)[C::TN][C::TM], int m0, int n0, int wm, int wn) {
         const float scale = p.last ? *p.scale : 1.f;
-        const __amdgpu_buffer_rsrc_t rc = __builtin_amdgcn_make_buffer_rsrc(p.c, 0, (int)p.c_bytes, 0x00020000),
-                                     rs = __builtin_amdgcn_make_buffer_rsrc(p.sum, 0, (int)p.sum_bytes, 0x00020000);
+        const __amdgpu_buffer_rsrc_t rc = span(p.c, p.c_bytes), rs = span(p.sum, p.sum_bytes);
+        by_rows<C>(lds, acc, m0, n0, wm, wn, [&](int m, int n, float (&v)[8]) __attribute__((always_inline)) {
+            const bool in = m < p.M && n < p.N;
+            const uint32_t soff = in ? (uint32_t)(((int64_t)m * p.lds + n) * 4) : kNowhere;
+            if (!p.first) {
 #pragma unroll
-        for (int tm = 0; tm < C::TM; ++tm) {
-            const int m = m0 + (wm * C::TM + tm) * 32 + (lane & 31);
+                for (int h = 0; h < 2; ++h) {
+                    const f32x4 s = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, soff, 16 * h, 0));
 #pragma unroll
-            for (int tn = 0; tn < C::TN; ++tn)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int n = n0 + (wn * C::TN + tn) * 32 + 8 * q + 4 * g;
-                    const bool in = m < p.M && n < p.N;
-                    const uint32_t soff = in ? (uint32_t)(((int64_t)m * p.lds + n) * 4) : 0x80000000u;
-                    float v[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = acc[tn][tm][4 * q + e];
-                    if (!p.first) {
-                        const f32x4 s = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, soff, 0, 0));
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) v[e] += s[e];
-                    }
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] *= scale;
-                    if (p.last) put4(rc, in ? (uint32_t)(((int64_t)m * p.ldc + n) * 2) : 0x80000000u, v, bf16{});
-                    else put4(rs, soff, v, 0.f);
+                    for (int e = 0; e < 4; ++e) v[4 * h + e] += s[e];
                 }
-        }
+            }
+            if (p.last) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] *= scale;
+                store8(rc, in ? (uint32_t)(((int64_t)m * p.ldc + n) * 2) : kNowhere, v, n, p.N);
+            } else {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const f32x4 s = f32x4{v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]};
+                    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(i32x4, s), rs, soff, 16 * h, 0);
+                }
+            }
+        });
     }
     template <typename C>
     static FBL_DEV void done(const Args& p, float*, f32x16 (&acc)[C::TM][C::TN], int m0, int n0, int wm, int wn) {

@@ -18,73 +18,47 @@ namespace fbl {
 
 namespace {
 
-using i32x2 = int __attribute__((ext_vector_type(2)));
-
-FBL_DEV __amdgpu_buffer_rsrc_t span(const void* p, uint32_t bytes) {
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, p ? (int)bytes : 0, 0x00020000);
-}
-constexpr uint32_t kNowhere = 0x80000000u;  // past every span: loads give 0, stores are dropped
-
-FBL_DEV bf16x4 load4(__amdgpu_buffer_rsrc_t r, uint32_t off) {
-    return __builtin_bit_cast(bf16x4, __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, 0));
-}
-
-// Values of rows m and columns n .. n+3 (a multiple of 4), or of element (m, n) in fp32.
 template <int ACT, bool GRAD>
 struct LinearEp {
     using Args = LinearArgs;
+    static constexpr bool kByRows = true;
 
-    // bf16: C^T accumulators, four consecutive columns of a row in four registers
+    // bf16: 8 columns of a row in a lane
     template <typename C>
-    static FBL_DEV void done(const Args& p, uint32_t, f32x16 (&acc)[C::TN][C::TM], int m0, int n0, int wm, int wn) {
-        const int lane = threadIdx.x & 63, g = lane >> 5;
-        const __amdgpu_buffer_rsrc_t rc = span(p.c, p.c_bytes), rz = span(p.z, p.z_bytes), rr_ = span(p.res, p.res_bytes),
-                                     rb = span(p.bias, (uint32_t)p.N * 2);
+    static FBL_DEV void done(const Args& p, uint32_t lds, f32x16 (&acc)[C::TN][C::TM], int m0, int n0, int wm, int wn) {
+        const __amdgpu_buffer_rsrc_t rc = span(p.c, p.c_bytes), rz = span(p.z, p.z_bytes), rr = span(p.res, p.res_bytes);
         const bool has_res = p.res != nullptr, has_z = p.z != nullptr;
+        // every turn is at the same columns
+        const int nb = n0 + wn * C::TN * 32 + (threadIdx.x & 63) % (4 * C::TN) * 8;
+        float b[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (!GRAD && p.bias) {
+            const bf16x8 x = load8(span(p.bias, (uint32_t)p.N * 2), (uint32_t)nb * 2);  // past N: 0
 #pragma unroll
-        for (int tn = 0; tn < C::TN; ++tn) {
-            const int nb = n0 + (wn * C::TN + tn) * 32 + 4 * g;
-            bf16x4 b[4];
-            if constexpr (!GRAD) {
+            for (int e = 0; e < 8; ++e) b[e] = (float)x[e];
+        }
+        by_rows<C>(lds, acc, m0, n0, wm, wn, [&](int m, int n, float (&v)[8]) __attribute__((always_inline)) {
+            const bool in = m < p.M && n < p.N;
+            const uint32_t off = in ? (uint32_t)(((int64_t)m * p.ldc + n) * 2) : kNowhere;
+            const uint32_t zoff = in ? (uint32_t)(((int64_t)m * p.ldz + n) * 2) : kNowhere;
+            if constexpr (GRAD) {
+                const bf16x8 z = load8(rz, zoff);
 #pragma unroll
-                for (int rr = 0; rr < 4; ++rr) b[rr] = load4(rb, (uint32_t)(nb + 8 * rr) * 2);  // past N: 0
-            }
+                for (int e = 0; e < 8; ++e) v[e] *= act_grad<ACT, true>((float)z[e]);
+            } else {
+                bf16x8 x;
+                if (has_res) x = load8(rr, in ? (uint32_t)(((int64_t)m * p.ldr + n) * 2) : kNowhere);
 #pragma unroll
-            for (int tm = 0; tm < C::TM; ++tm) {
-                const int m = m0 + (wm * C::TM + tm) * 32 + (lane & 31);
+                for (int e = 0; e < 8; ++e) v[e] += b[e];
+                if (has_z) store8(rz, zoff, v, n, p.N);
 #pragma unroll
-                for (int rr = 0; rr < 4; ++rr) {
-                    const int n = nb + 8 * rr;
-                    const bool in = m < p.M && n < p.N;
-                    const uint32_t off = in ? (uint32_t)(((int64_t)m * p.ldc + n) * 2) : kNowhere;
-                    const uint32_t zoff = in ? (uint32_t)(((int64_t)m * p.ldz + n) * 2) : kNowhere;
-                    float v[4];
+                for (int e = 0; e < 8; ++e) v[e] = act<ACT, true>(v[e]);
+                if (has_res) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = acc[tn][tm][4 * rr + e];
-                    if constexpr (GRAD) {
-                        const bf16x4 z = load4(rz, zoff);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) v[e] *= act_grad<ACT, true>((float)z[e]);
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) v[e] += (float)b[rr][e];
-                        if (has_z) {
-                            const bf16x4 z = bf16x4{(bf16)v[0], (bf16)v[1], (bf16)v[2], (bf16)v[3]};
-                            __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(i32x2, z), rz, zoff, 0, 0);
-                        }
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) v[e] = act<ACT, true>(v[e]);
-                        if (has_res) {
-                            const bf16x4 x = load4(rr_, in ? (uint32_t)(((int64_t)m * p.ldr + n) * 2) : kNowhere);
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) v[e] += (float)x[e];
-                        }
-                    }
-                    const bf16x4 y = bf16x4{(bf16)v[0], (bf16)v[1], (bf16)v[2], (bf16)v[3]};
-                    __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(i32x2, y), rc, off, 0, 0);
+                    for (int e = 0; e < 8; ++e) v[e] += (float)x[e];
                 }
             }
-        }
+            store8(rc, off, v, n, p.N);
+        });
     }
 
     // fp32: 32 consecutive columns of a row across the lanes of a half
