@@ -60,26 +60,44 @@ int64_t forward_piece(const Shape& s, int64_t ldw) {
 }
 
 // Vocabulary entries of a piece of the backward.  dz [M][piece] goes through memory twice and dX's fp32
-// sums once a piece, so pieces are as large as 128 MiB of dz allow, 4096 entries at
-// least, and equal.
+// sums once a piece, so pieces are large, up to 128 MiB of dz; of those, the width whose tiles
+// fill the CUs' rounds best.  (4096 tokens, K 1024, V 50257: 3 pieces of 16384 and one of 1105 make 13 rounds of dz
+// and 4 of dW, 4 pieces of 12800 make 16 and 4.)
 int64_t backward_piece(const Shape& s, int64_t ldw) {
-    int64_t piece = std::max<int64_t>(4096, ((int64_t)128 << 20) / (s.M * s.es()));
-    piece = std::min(piece, std::max<int64_t>(64, (kSpan - 1) / (s.M * s.es()) - 64));
-    if (s.table()) piece = std::min(piece, ((kSpan - 1) / s.es() - s.K) / ldw + 1);
-    if (piece >= s.V) return s.V;
-    const int64_t n = (s.V + piece - 1) / piece, even = ((s.V + n - 1) / n + 255) / 256 * 256;
-    return std::max<int64_t>(64, std::min(even, piece / 64 * 64));
+    int64_t most = std::max<int64_t>(4096, ((int64_t)128 << 20) / (s.M * s.es()));
+    most = std::min(most, std::max<int64_t>(64, (kSpan - 1) / (s.M * s.es()) - 64));
+    if (s.table()) most = std::min(most, ((kSpan - 1) / s.es() - s.K) / ldw + 1);
+    if (most >= s.V) return s.V;
+    if (most < 512) return most / 64 * 64;
+    // cost in products of a CU: its rounds of dz tiles (256 x 256: fp32's smaller ones waste less) and of dW tiles,
+    // dX's sums read and written (8 bytes at 16 a CU and cycle, 1000 products meanwhile), and the launches
+    const auto tiles = [](int64_t n) { return (double)((n + 255) / 256); };
+    const auto cost = [&](int64_t width) {
+        const double dz = std::ceil(tiles(s.M) * tiles(width) / 256) * 65536.0 * (double)s.K;
+        const double dw = std::ceil(tiles(s.K) * tiles(width) / 256) * 65536.0 * (double)s.M;
+        return dz + dw + (double)s.M * (double)s.K * 4 + 2e7;
+    };
+    const int64_t step = std::max<int64_t>(1, most / 256 / 64) * 256;
+    int64_t best = 0;
+    double best_cost = 0;
+    for (int64_t width = most / 256 * 256; width >= std::max<int64_t>(256, most / 4); width -= step) {
+        const int64_t whole = s.V / width, rest = s.V % width;
+        const double c = (double)whole * cost(width) + (rest ? cost(rest) : 0);
+        if (!best || c < best_cost) best = width, best_cost = c;
+    }
+    return best;
 }
 int64_t padded64(int64_t n) { return (n + 63) / 64 * 64; }
 
 struct HeadWs {
     size_t index, target, part, entropy, counted, fwd;  // forward
     size_t weight, row, scale, dz, sum, bwd;            // backward
+    int splits;                                         // of dX's contraction
 };
 HeadWs head_ws(const Shape& s, int64_t ldw) {
     HeadWs w{};
     const size_t list = align256((size_t)s.M * (size_t)s.top * 4), row = align256((size_t)s.M * 4);
-    const int64_t tw = fbl::head_tile_width(s.f32(), s.M), fp = forward_piece(s, ldw);
+    const int64_t tw = fbl::head_tile_width(s.f32(), fbl::head_tile(s.f32(), s.table(), s.M, s.V, s.K)), fp = forward_piece(s, ldw);
     const int64_t parts = (s.V + tw - 1) / tw + (s.V + fp - 1) / fp;
     w.index = 0, w.target = list, w.part = w.target + list;
     w.entropy = w.part + align256((size_t)parts * (size_t)s.M * 8);
@@ -89,7 +107,9 @@ HeadWs head_ws(const Shape& s, int64_t ldw) {
     w.scale = w.row + align256((size_t)s.M * 8);
     w.dz = w.scale + 256;
     w.sum = w.dz + align256((size_t)s.M * (size_t)padded64(bp) * (size_t)s.es());
-    w.bwd = w.sum + (bp < s.V && !s.f32() ? align256((size_t)s.M * (size_t)s.K * 4) : 0);
+    const size_t plane = (size_t)s.M * (size_t)s.K * 4;
+    w.splits = fbl::sum_splits(s.f32(), s.M, s.K, bp);
+    w.bwd = w.sum + (w.splits > 1 ? align256((size_t)w.splits * plane) : bp < s.V && !s.f32() ? align256(plane) : 0);
     return w;
 }
 
@@ -183,7 +203,9 @@ fbl_status head_fwd(const Shape& s, const void* x, int64_t ldx, const void* w, i
     a.index = reinterpret_cast<int*>(base + lay.index);
     a.entropy = reinterpret_cast<float*>(base + lay.entropy), a.counted = reinterpret_cast<float*>(base + lay.counted);
     hipError_t e = fbl::launch_head_targets(a, hs);
-    const int64_t piece = forward_piece(s, ldw), tw = fbl::head_tile_width(s.f32(), s.M);
+    const int64_t piece = forward_piece(s, ldw);
+    const int shape = fbl::head_tile(s.f32(), s.table(), s.M, s.V, s.K);
+    const int64_t tw = fbl::head_tile_width(s.f32(), shape);
     int tiles = 0;
     for (int64_t v0 = 0; v0 < s.V && e == hipSuccess; v0 += piece) {
         const int64_t width = std::min(piece, s.V - v0);
@@ -192,6 +214,7 @@ fbl_status head_fwd(const Shape& s, const void* x, int64_t ldx, const void* w, i
         p.index = a.index;
         p.part = reinterpret_cast<float2*>(base + lay.part), p.target = reinterpret_cast<float*>(base + lay.target);
         p.tile0 = tiles;
+        p.shape = shape;
         tiles += (int)((width + tw - 1) / tw);
         e = fbl::launch_head_fwd(s.f32(), s.table(), p, hs);
     }
@@ -248,6 +271,7 @@ fbl_status head_bwd(const Shape& s, const float* dloss, int64_t dloss_stride, co
         p.N = (int)ldz;  // dz's padding is written too (zeros)
         p.unit = fbl::kLog2e / t.T;
         p.index = a.index, p.weight = t.labels ? nullptr : a.weight, p.row = a.row;
+        p.shape = fbl::head_tile(s.f32(), s.table(), s.M, ldz, s.K);
         p.dz = base + lay.dz, p.ldz = ldz, p.dz_bytes = (uint32_t)vz.bytes();
         e = fbl::launch_head_grad(s.f32(), s.table(), p, hs);
         const RowsView wp = weight_view(s, w, ldw, v0, width);
@@ -259,25 +283,23 @@ fbl_status head_bwd(const Shape& s, const float* dloss, int64_t dloss_stride, co
             fbl::SumArgs q{};
             if (s.table()) fbl::product(q, op, az, wp, vdx, s.M, kc, s.K);
             else fbl::product(q, op, az, wp, vdx, s.M, s.K, kc);
-            q.first = first, q.last = last;
-            const int tile = s.f32() ? 0 : s.table() ? fbl::proj_auto_tile(op, s.M, kc, s.K) : fbl::proj_auto_tile(op, s.M, s.K, kc);
-            if (s.f32()) {
-                e = fbl::launch_sum_gemm_f32(!s.table(), q, hs);
-            } else {
-                q.scale = scale;
-                if (!first || !last) {
-                    q.sum = reinterpret_cast<float*>(base + lay.sum), q.lds = s.K;
-                    q.sum_bytes = (uint32_t)(s.M * s.K * 4);
-                }
-                e = fbl::launch_sum_gemm(0, !s.table(), tile, q, hs);
+            q.first = first, q.last = last, q.scale = scale, q.splits = lay.splits;
+            q.share = (int)(((kc + lay.splits - 1) / lay.splits + 63) / 64 * 64);
+            if (lay.splits > 1 || (!s.f32() && !(first && last))) {
+                q.sum = reinterpret_cast<float*>(base + lay.sum), q.lds = s.K;
+                q.sum_bytes = (uint32_t)(s.M * s.K * 4);
             }
+            const int tile = s.f32() ? 0 : s.table() ? fbl::proj_auto_tile(op, s.M, kc, s.K) : fbl::proj_auto_tile(op, s.M, s.K, kc);
+            e = s.f32() ? fbl::launch_sum_gemm_f32(!s.table(), q, hs) : fbl::launch_sum_gemm(0, !s.table(), tile, q, hs);
+            if (e == hipSuccess && last && lay.splits > 1)
+                e = fbl::launch_sum_planes(s.f32(), q.sum, lay.splits, s.M, s.K, scale, dx, lddx, hs);
         }
         if (e == hipSuccess && dw) {
             const RowsView dz{vz.p, s.M, width, ldz, s.es()}, dwp = weight_view(s, dw, lddw, v0, width);
             fbl::SumArgs q{};
             const int64_t rows = s.table() ? width : s.K, cols = s.table() ? s.K : width;
             fbl::product(q, FBL_PROJ_BWD_WEIGHT, s.table() ? dz : vx, s.table() ? vx : dz, dwp, s.M, rows, cols);
-            q.scale = scale, q.first = q.last = 1;
+            q.scale = scale, q.first = q.last = q.splits = 1;
             e = s.f32() ? fbl::launch_proj_gemm_f32(1, 0, q, hs)
                         : fbl::launch_sum_gemm(1, 0, fbl::proj_auto_tile(FBL_PROJ_BWD_WEIGHT, s.M, rows, cols), q, hs);
         }

@@ -80,6 +80,7 @@ struct GemmCfg {
 struct PlainStore {
     using Args = GemmArgs;
     static constexpr bool kByRows = false;  // done uses by_rows
+    static constexpr bool kSplits = false;  // gridDim.y workgroups share a tile's contraction (take_share)
 };
 
 template <int BM, int BN, int BK, int NS, int WM, int WN, int WK, bool AT, bool BT, typename EP>
@@ -91,6 +92,7 @@ proj_gemm_bf16(typename EP::Args p) {
     constexpr int TM = C::TM, TN = C::TN, KCW = C::KCW;
     extern __shared__ __attribute__((aligned(1024))) unsigned char gemm_smem[];
     const uint32_t lds = lds_addr(gemm_smem);
+    if constexpr (EP::kSplits) take_share<2, AT, BT>(p);
 
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -429,7 +431,7 @@ FBL_DEV void store8(__amdgpu_buffer_rsrc_t r, uint32_t off, const float (&v)[8],
 
 // Launch of tile I of kGemmTiles.
 template <int I, bool AT, bool BT, typename EP>
-hipError_t launch_gemm_bf16(const typename EP::Args& p, hipStream_t stream) {
+hipError_t launch_gemm_bf16(const typename EP::Args& p, hipStream_t stream, int splits = 1) {
     constexpr GemmTile t = kGemmTiles[I];
     using C = GemmCfg<t.bm, t.bn, t.bk, t.ns, t.wm, t.wn, t.wk, AT, BT>;
     constexpr auto kernel = &proj_gemm_bf16<t.bm, t.bn, t.bk, t.ns, t.wm, t.wn, t.wk, AT, BT, EP>;
@@ -437,12 +439,12 @@ hipError_t launch_gemm_bf16(const typename EP::Args& p, hipStream_t stream) {
     const hipError_t once = ensure_dynamic_lds<kernel>(bytes);
     if (once != hipSuccess) return once;
     const int tiles = ((p.M + t.bm - 1) / t.bm) * ((p.N + t.bn - 1) / t.bn);
-    hipLaunchKernelGGL(kernel, dim3((tiles + 7) / 8 * 8), dim3(64 * C::NW), bytes, stream, p);
+    hipLaunchKernelGGL(kernel, dim3((tiles + 7) / 8 * 8, splits), dim3(64 * C::NW), bytes, stream, p);
     return hipGetLastError();
 }
 
 template <typename EP>
-using GemmLauncher = hipError_t (*)(const typename EP::Args&, hipStream_t);
+using GemmLauncher = hipError_t (*)(const typename EP::Args&, hipStream_t, int);
 
 template <bool AT, bool BT, typename EP, int... I>
 constexpr std::array<GemmLauncher<EP>, sizeof...(I)> gemm_launchers(std::integer_sequence<int, I...>) {
@@ -450,9 +452,9 @@ constexpr std::array<GemmLauncher<EP>, sizeof...(I)> gemm_launchers(std::integer
 }
 
 template <bool AT, bool BT, typename EP>
-hipError_t launch_gemm_tile(int tile, const typename EP::Args& p, hipStream_t stream) {
+hipError_t launch_gemm_tile(int tile, const typename EP::Args& p, hipStream_t stream, int splits = 1) {
     static constexpr auto table = gemm_launchers<AT, BT, EP>(std::make_integer_sequence<int, kGemmTileCount>{});
-    return table[tile](p, stream);
+    return table[tile](p, stream, splits);
 }
 
 }  // namespace

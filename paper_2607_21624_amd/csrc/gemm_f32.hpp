@@ -122,6 +122,7 @@ struct F32Cfg {
 // free once the wavefronts have met at a barrier.
 struct PlainStoreF32 {
     using Args = GemmArgs;
+    static constexpr bool kSplits = false;  // gridDim.y workgroups share a tile's contraction (take_share)
 };
 
 template <int I, bool AT, bool BT, typename EP>
@@ -132,6 +133,7 @@ __global__ __launch_bounds__((F32Cfg<I, AT, BT>::NT), 2) void proj_gemm_f32(type
     constexpr F32Tile t = C::t;
     constexpr int TM = C::TM, TN = C::TN;
     extern __shared__ __attribute__((aligned(16))) float f32_smem[];
+    if constexpr (EP::kSplits) take_share<4, AT, BT>(p);
 
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -250,17 +252,17 @@ __global__ __launch_bounds__((F32Cfg<I, AT, BT>::NT), 2) void proj_gemm_f32(type
 }
 
 template <int I, bool AT, bool BT, typename EP>
-hipError_t launch_gemm_f32(const typename EP::Args& p, hipStream_t stream) {
+hipError_t launch_gemm_f32(const typename EP::Args& p, hipStream_t stream, int splits = 1) {
     using C = F32Cfg<I, AT, BT>;
     constexpr auto kernel = &proj_gemm_f32<I, AT, BT, EP>;
     const hipError_t once = ensure_dynamic_lds<kernel>(C::BYTES);
     if (once != hipSuccess) return once;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)f32_workgroups(C::t, p)), dim3(C::NT), C::BYTES, stream, p);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)f32_workgroups(C::t, p), splits), dim3(C::NT), C::BYTES, stream, p);
     return hipGetLastError();
 }
 
 template <typename EP>
-using F32Launcher = hipError_t (*)(const typename EP::Args&, hipStream_t);
+using F32Launcher = hipError_t (*)(const typename EP::Args&, hipStream_t, int);
 
 template <bool AT, bool BT, typename EP, int... I>
 constexpr std::array<F32Launcher<EP>, sizeof...(I)> f32_launchers(std::integer_sequence<int, I...>) {
@@ -268,9 +270,9 @@ constexpr std::array<F32Launcher<EP>, sizeof...(I)> f32_launchers(std::integer_s
 }
 
 template <bool AT, bool BT, typename EP>
-hipError_t launch_f32_tile(int tile, const typename EP::Args& p, hipStream_t stream) {
+hipError_t launch_f32_tile(int tile, const typename EP::Args& p, hipStream_t stream, int splits = 1) {
     static constexpr auto table = f32_launchers<AT, BT, EP>(std::make_integer_sequence<int, kF32TileCount>{});
-    return table[tile](p, stream);
+    return table[tile](p, stream, splits);
 }
 
 // The tile of a product: least rounds x area x cost, where rounds is the number

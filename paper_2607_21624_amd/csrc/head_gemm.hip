@@ -14,6 +14,7 @@
 //
 // Bound by the matrix products: 2 M K V forward and 6 M K V backward (one third of it z again).
 #include "gemm_bf16.hpp"
+#include "gemm_cost.hpp"
 #include "gemm_f32.hpp"
 
 namespace fbl {
@@ -151,7 +152,7 @@ FBL_DEV void head_dz(const HeadArgs& p, f32x16 (&acc)[NV][NM], int v0, int m0) {
 
 struct HeadFwd {
     using Args = HeadArgs;
-    static constexpr bool kByRows = false;
+    static constexpr bool kByRows = false, kSplits = false;
     template <typename C>
     static FBL_DEV void done(const Args& p, uint32_t, f32x16 (&acc)[C::TN][C::TM], int m0, int n0, int wm, int wn) {
         extern __shared__ __attribute__((aligned(1024))) unsigned char gemm_smem[];
@@ -168,7 +169,7 @@ struct HeadFwd {
 
 struct HeadGrad {
     using Args = HeadArgs;
-    static constexpr bool kByRows = true;
+    static constexpr bool kByRows = true, kSplits = false;
     template <typename C>
     static FBL_DEV void done(const Args& p, uint32_t lds, f32x16 (&acc)[C::TN][C::TM], int m0, int n0, int wm, int wn) {
         head_dz(p, acc, n0 + wn * C::TN * 32, m0 + wm * C::TM * 32);
@@ -206,13 +207,16 @@ struct HeadGrad {
 // largest entries, -1 at the labels, are then exact, where g, a constant, rounded would be off by the same
 // 2^-9 in every row (4096 x 1024 x 50257: error of dx 0.28% of its norm, 0.17% of
 // which are the result's own rounding).
+template <bool SPLIT>
 struct SumPieces {
     using Args = SumArgs;
-    static constexpr bool kByRows = true;
+    static constexpr bool kByRows = true, kSplits = SPLIT;
     template <typename C>
     static FBL_DEV void done(const Args& p, uint32_t lds, f32x16 (&acc)[C::TN][C::TM], int m0, int n0, int wm, int wn) {
-        const float scale = p.last ? *p.scale : 1.f;
-        const __amdgpu_buffer_rsrc_t rc = span(p.c, p.c_bytes), rs = span(p.sum, p.sum_bytes);
+        const bool last = !SPLIT && p.last;
+        const float scale = last ? *p.scale : 1.f;
+        const __amdgpu_buffer_rsrc_t rc = span(p.c, p.c_bytes),
+                                     rs = span(SPLIT ? p.sum + (int64_t)blockIdx.y * p.M * p.lds : p.sum, p.sum_bytes);
         by_rows<C>(lds, acc, m0, n0, wm, wn, [&](int m, int n, float (&v)[8]) __attribute__((always_inline)) {
             const bool in = m < p.M && n < p.N;
             const uint32_t soff = in ? (uint32_t)(((int64_t)m * p.lds + n) * 4) : kNowhere;
@@ -224,7 +228,7 @@ struct SumPieces {
                     for (int e = 0; e < 4; ++e) v[4 * h + e] += s[e];
                 }
             }
-            if (p.last) {
+            if (last) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] *= scale;
                 store8(rc, in ? (uint32_t)(((int64_t)m * p.ldc + n) * 2) : kNowhere, v, n, p.N);
@@ -240,7 +244,9 @@ struct SumPieces {
     template <typename C>
     static FBL_DEV void done(const Args& p, float*, f32x16 (&acc)[C::TM][C::TN], int m0, int n0, int wm, int wn) {
         const int lane = threadIdx.x & 63, g = lane >> 5;
-        const __amdgpu_buffer_rsrc_t rc = __builtin_amdgcn_make_buffer_rsrc(p.c, 0, (int)p.c_bytes, 0x00020000);
+        const __amdgpu_buffer_rsrc_t rc =
+            SPLIT ? span(p.sum + (int64_t)blockIdx.y * p.M * p.lds, p.sum_bytes) : span(p.c, p.c_bytes);
+        const int64_t ld = SPLIT ? p.lds : p.ldc;
 #pragma unroll
         for (int tm = 0; tm < C::TM; ++tm)
 #pragma unroll
@@ -248,7 +254,7 @@ struct SumPieces {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const int m = m0 + (wm * C::TM + tm) * 32 + acc_row(r, g), n = n0 + (wn * C::TN + tn) * 32 + (lane & 31);
-                    const uint32_t off = m < p.M && n < p.N ? (uint32_t)(((int64_t)m * p.ldc + n) * 4) : 0x80000000u;
+                    const uint32_t off = m < p.M && n < p.N ? (uint32_t)(((int64_t)m * ld + n) * 4) : kNowhere;
                     float v = acc[tm][tn][r];
                     if (!p.first) v += __int_as_float(__builtin_amdgcn_raw_buffer_load_b32(rc, off, 0, 0));
                     __builtin_amdgcn_raw_buffer_store_b32(__float_as_int(v), rc, off, 0, 0);
@@ -256,16 +262,23 @@ struct SumPieces {
     }
 };
 
-// Tiles whose wavefronts each have the whole contraction, by the number of tokens: 32, 64, 128 or 256
-// rows (a vocabulary has enough columns to fill the card with any of them).
-int head_tile(int64_t M) { return M <= 32 ? 15 : M <= 64 ? 6 : M <= 128 ? 4 : 19; }
-// fp32: vocabulary x tokens
-int head_tile_f32(int64_t M) { return M <= 64 ? 2 : 0; }
+template <typename T>
+__global__ __launch_bounds__(256) void sum_planes(const float* planes, int splits, int64_t M, int64_t N, const float* scale,
+                                                  T* c, int64_t ldc) {
+    const int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const float f = scale ? *scale : 1.f;
+    if (n >= N) return;
+    for (int64_t m = blockIdx.y; m < M; m += gridDim.y) {
+        float s = 0.f;
+        for (int i = 0; i < splits; ++i) s += planes[((int64_t)i * M + m) * N + n];
+        c[m * ldc + n] = (T)(s * f);
+    }
+}
 
 template <typename EP>
 hipError_t launch_head(int f32, int table, HeadArgs& p, hipStream_t s) {
     if (!f32) {  // C = X W: tokens are the rows
-        switch (head_tile(p.tokens)) {
+        switch (p.shape) {
             case 15: return table ? launch_gemm_bf16<15, false, true, EP>(p, s) : launch_gemm_bf16<15, false, false, EP>(p, s);
             case 6: return table ? launch_gemm_bf16<6, false, true, EP>(p, s) : launch_gemm_bf16<6, false, false, EP>(p, s);
             case 4: return table ? launch_gemm_bf16<4, false, true, EP>(p, s) : launch_gemm_bf16<4, false, false, EP>(p, s);
@@ -274,23 +287,72 @@ hipError_t launch_head(int f32, int table, HeadArgs& p, hipStream_t s) {
     }
     // C = W^T X^T: the vocabulary is the rows, so that tokens lie along the lanes here too
     std::swap(p.a, p.b), std::swap(p.lda, p.ldb), std::swap(p.a_bytes, p.b_bytes), std::swap(p.M, p.N);
-    if (head_tile_f32(p.tokens) == 2) return table ? launch_gemm_f32<2, false, true, EP>(p, s) : launch_gemm_f32<2, true, true, EP>(p, s);
+    if (p.shape == 2) return table ? launch_gemm_f32<2, false, true, EP>(p, s) : launch_gemm_f32<2, true, true, EP>(p, s);
     return table ? launch_gemm_f32<0, false, true, EP>(p, s) : launch_gemm_f32<0, true, true, EP>(p, s);
 }
 
+// The tile of a split product: as narrow as the few rows that split one.
+int split_tile(int64_t M) { return M <= 32 ? 15 : M <= 64 ? 6 : 4; }
+constexpr int kSplitTileF32 = 2;
+
 }  // namespace
 
-int head_tile_width(int f32, int64_t M) { return f32 ? kF32Tiles[head_tile_f32(M)].bm : kGemmTiles[head_tile(M)].bn; }
+// Tiles whose wavefronts each have the whole contraction, of 32, 64, 128 and 256 tokens: the one of least modelled
+// time (gemm_cost.hpp); fp32: 128 x 128 where that makes two workgroups for each CU, else 64 x 64.
+int head_tile(int f32, int table, int64_t M, int64_t V, int64_t K) {
+    if (f32) return ((M + 127) / 128) * ((V + 127) / 128) >= 512 ? 0 : 2;
+    int best = 19;
+    for (int t : {4, 6, 15})
+        if (gemm_cost(t, table, M, V, K) < gemm_cost(best, table, M, V, K)) best = t;
+    return best;
+}
+int head_tile_width(int f32, int tile) { return f32 ? kF32Tiles[tile].bm : kGemmTiles[tile].bn; }
 
 hipError_t launch_head_fwd(int f32, int table, HeadArgs p, hipStream_t s) { return launch_head<HeadFwd>(f32, table, p, s); }
 hipError_t launch_head_grad(int f32, int table, HeadArgs p, hipStream_t s) { return launch_head<HeadGrad>(f32, table, p, s); }
 
+// dX of few tokens has few tiles and a vocabulary for its contraction: where its tiles leave a quarter of the CUs idle
+// and more, two workgroups a CU share them, each with a contraction of 512 at least.
+int sum_splits(int f32, int64_t M, int64_t N, int64_t kc) {
+    const int t = split_tile(M), bm = f32 ? kF32Tiles[kSplitTileF32].bm : kGemmTiles[t].bm,
+              bn = f32 ? kF32Tiles[kSplitTileF32].bn : kGemmTiles[t].bn;
+    const int64_t tiles = ((M + bm - 1) / bm) * ((N + bn - 1) / bn);
+    if (tiles >= 192) return 1;
+    return (int)std::max<int64_t>(1, std::min<int64_t>((512 + tiles / 2) / tiles, kc / 512));
+}
+
 hipError_t launch_sum_gemm(int a_kmajor, int b_nmajor, int tile, const SumArgs& p, hipStream_t s) {
-    if (a_kmajor) return launch_gemm_tile<true, false, SumPieces>(tile, p, s);
-    return b_nmajor ? launch_gemm_tile<false, true, SumPieces>(tile, p, s) : launch_gemm_tile<false, false, SumPieces>(tile, p, s);
+    if (p.splits > 1) {
+        const auto run = [&](auto bt_c) {
+            constexpr bool BT = decltype(bt_c)::value;
+            switch (split_tile(p.M)) {
+                case 15: return launch_gemm_bf16<15, false, BT, SumPieces<true>>(p, s, p.splits);
+                case 6: return launch_gemm_bf16<6, false, BT, SumPieces<true>>(p, s, p.splits);
+                default: return launch_gemm_bf16<4, false, BT, SumPieces<true>>(p, s, p.splits);
+            }
+        };
+        return b_nmajor ? run(std::true_type{}) : run(std::false_type{});
+    }
+    using EP = SumPieces<false>;
+    if (a_kmajor) return launch_gemm_tile<true, false, EP>(tile, p, s);
+    return b_nmajor ? launch_gemm_tile<false, true, EP>(tile, p, s) : launch_gemm_tile<false, false, EP>(tile, p, s);
 }
 hipError_t launch_sum_gemm_f32(int b_nmajor, const SumArgs& p, hipStream_t s) {
-    return b_nmajor ? launch_f32_tile<false, true, SumPieces>(f32_tile(p), p, s) : launch_f32_tile<false, false, SumPieces>(f32_tile(p), p, s);
+    if (p.splits > 1) {
+        using EP = SumPieces<true>;
+        return b_nmajor ? launch_gemm_f32<kSplitTileF32, false, true, EP>(p, s, p.splits)
+                        : launch_gemm_f32<kSplitTileF32, false, false, EP>(p, s, p.splits);
+    }
+    using EP = SumPieces<false>;
+    return b_nmajor ? launch_f32_tile<false, true, EP>(f32_tile(p), p, s) : launch_f32_tile<false, false, EP>(f32_tile(p), p, s);
+}
+
+hipError_t launch_sum_planes(int f32, const float* planes, int splits, int64_t M, int64_t N, const float* scale, void* c,
+                             int64_t ldc, hipStream_t s) {
+    const dim3 grid((unsigned)((N + 255) / 256), (unsigned)std::min<int64_t>(M, 4096));
+    if (f32) hipLaunchKernelGGL(sum_planes<float>, grid, dim3(256), 0, s, planes, splits, M, N, scale, (float*)c, ldc);
+    else hipLaunchKernelGGL(sum_planes<bf16>, grid, dim3(256), 0, s, planes, splits, M, N, scale, (bf16*)c, ldc);
+    return hipGetLastError();
 }
 
 }  // namespace fbl

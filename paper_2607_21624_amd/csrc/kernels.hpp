@@ -117,11 +117,19 @@ hipError_t launch_linear_act_bwd(int f32, int act, const LinearActArgs& a, hipSt
 // Softmax losses of a linear head (head_gemm.hip, head_rows.hip); table: the weight is stored
 // [V, K], else [K, V].
 constexpr int kHeadMaxTop = 1024;
-int head_tile_width(int f32, int64_t M);  // vocabulary entries of a forward tile
+// The tile (HeadArgs::shape) for M tokens and V entries, and the entries it spans.
+int head_tile(int f32, int table, int64_t M, int64_t V, int64_t K);
+int head_tile_width(int f32, int tile);
 hipError_t launch_head_fwd(int f32, int table, HeadArgs p, hipStream_t stream);
 hipError_t launch_head_grad(int f32, int table, HeadArgs p, hipStream_t stream);
+// bf16 with `tile` of kGemmTiles where it is not split.
 hipError_t launch_sum_gemm(int a_kmajor, int b_nmajor, int tile, const SumArgs& p, hipStream_t stream);
 hipError_t launch_sum_gemm_f32(int b_nmajor, const SumArgs& p, hipStream_t stream);
+// Workgroups that should share the contraction of an M x N product's tiles.
+int sum_splits(int f32, int64_t M, int64_t N, int64_t kc);
+// C [M][ldc] = scale * the sum of the planes [splits][M][N] (scale nullptr: 1).
+hipError_t launch_sum_planes(int f32, const float* planes, int splits, int64_t M, int64_t N, const float* scale, void* c,
+                             int64_t ldc, hipStream_t stream);
 hipError_t launch_head_targets(const HeadRowArgs& a, hipStream_t stream);       // forward: targets, probabilities
 hipError_t launch_head_join(const HeadRowArgs& a, hipStream_t stream);          // parts -> loss, lse, sums
 hipError_t launch_head_grad_rows(const HeadRowArgs& a, hipStream_t stream);     // backward: targets, factors

@@ -21,7 +21,7 @@ namespace {
 template <int ACT, bool GRAD>
 struct LinearEp {
     using Args = LinearArgs;
-    static constexpr bool kByRows = true;
+    static constexpr bool kByRows = true, kSplits = false;
 
     // bf16: 8 columns of a row in a lane
     template <typename C>

@@ -257,6 +257,20 @@ FBL_DEV int xcd_logical_id(int id, int total, int padded_total) {
     return logical < total ? logical : -1;
 }
 
+// The share of a product's contraction that workgroup blockIdx.y computes: p.share elements (a multiple of
+// 64) from the blockIdx.y-th on, perhaps none.  Operands begin there and end where they did.
+template <int ES, bool AT, bool BT, typename Args>
+FBL_DEV void take_share(Args& p) {
+    const int64_t k0 = (int64_t)blockIdx.y * p.share;
+    const int64_t a0 = (AT ? k0 * p.lda : k0) * ES, b0 = (BT ? k0 : k0 * p.ldb) * ES;
+    p.a = static_cast<const char*>(p.a) + a0;
+    p.b = static_cast<const char*>(p.b) + b0;
+    p.a_bytes = a0 < p.a_bytes ? p.a_bytes - (uint32_t)a0 : 0;
+    p.b_bytes = b0 < p.b_bytes ? p.b_bytes - (uint32_t)b0 : 0;
+    const int64_t left = p.K - k0;
+    p.K = (int)(left < 0 ? 0 : left < p.share ? left : p.share);
+}
+
 // f(integral_constant<int, I>) for I = 0, 1, ..., in order: a loop over LDS
 // buffers whose index stays a compile-time constant (buffer offsets become
 // instruction immediates).

@@ -134,6 +134,7 @@ struct LinearActArgs {
 // columns (bf16: tokens are the rows; fp32: the vocabulary is).  Targets are [top][tokens].
 struct HeadArgs : GemmArgs {
     int tokens;
+    int shape;          // tile: id of kGemmTiles, or of the fp32 tiles
     int first, width;   // the piece: vocabulary entries first .. first + width - 1
     int top;
     float unit;         // log2(e) / temperature
@@ -151,15 +152,16 @@ struct HeadArgs : GemmArgs {
     uint32_t dz_bytes;
 };
 
-// A product added up over the pieces of its contraction.  bf16: sum (fp32) is overwritten
-// (first) or added to, and with the last piece scaled by *scale and rounded to C; a piece that is both is C
-// at once.  fp32: C itself is overwritten (first) or added to.
+// A product added up over the pieces of its contraction, each perhaps shared by `splits` workgroups a tile:
+// sum (fp32, one plane [M][N] a share) is overwritten (first) or added to.  A bf16 product that
+// is not split is scaled by *scale and rounded to C with the last piece, and an fp32 one is summed in C.
 struct SumArgs : GemmArgs {
     float* sum;
     const float* scale;
     int64_t lds;
-    uint32_t sum_bytes;
+    uint32_t sum_bytes;  // of a plane
     int first, last;
+    int share, splits;
 };
 
 // The small steps around a head's loss, one row (token) of M each.
