@@ -636,6 +636,8 @@ fbl_status fbl_layer_norm_bwd(int32_t dtype, int64_t M, int64_t N, const void* d
  *   FBL_ACT_GELU_TANH  z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2
  *   FBL_ACT_SILU       z / (1 + exp(-z))
  * tile: as fbl_proj's for the product (FBL_PROJ_FWD, M, K, N); AUTO for fp32.
+ * ws: NULL, or fbl_linear_fwd_workspace bytes (16-byte aligned), with which tile AUTO lets several
+ * workgroups share the contraction of a few tokens' tiles (serving: 0 bytes where it does not).
  *
  * fbl_linear_bwd gives, from dy [M, N], any of (NULL: not wanted)
  *   dx = (dz . w^T) * xact'(xz),   dw = x^T . dz,   dbias = sum over rows of dz,
@@ -660,7 +662,8 @@ fbl_status fbl_layer_norm_bwd(int32_t dtype, int64_t M, int64_t N, const void* d
 #define FBL_ACT_SILU 4u
 fbl_status fbl_linear_fwd(int32_t dtype, uint32_t act, int64_t M, int64_t K, int64_t N, const void* x, int64_t ldx,
                           const void* w, int64_t ldw, const void* bias, const void* res, int64_t ldr, void* y,
-                          int64_t ldy, void* z, int64_t ldz, int32_t tile, void* stream);
+                          int64_t ldy, void* z, int64_t ldz, int32_t tile, void* ws, size_t ws_bytes, void* stream);
+fbl_status fbl_linear_fwd_workspace(int32_t dtype, int64_t M, int64_t K, int64_t N, size_t* bytes);
 fbl_status fbl_linear_bwd_workspace(int32_t dtype, int64_t M, int64_t K, int64_t N, size_t* bytes);
 fbl_status fbl_linear_bwd(int32_t dtype, uint32_t act, int64_t M, int64_t K, int64_t N, const void* dy, int64_t lddy,
                           const void* x, int64_t ldx, const void* w, int64_t ldw, const void* z, int64_t ldz,

@@ -15,7 +15,7 @@ from .fbl import (  # noqa: F401
     NOALLOC_SCRATCH_BYTES, attn_bwd_noalloc, fbl_attn_bwd_noalloc_raw,
     FBL_ATTN_FWD, FBL_ATTN_BWD_KV, FBL_ATTN_BWD_DQ, FBL_ATTN_TILE_AUTO, attn_tiles, attn_candidates, attn_auto_tiles, attn_bwd_launches,
     attn_tune, attn_tuned_tile, attn_tune_reset,
-    FBL_ACT_NONE, FBL_ACT_RELU, FBL_ACT_GELU, FBL_ACT_GELU_TANH, FBL_ACT_SILU, ACTIVATIONS, linear_fwd, linear_bwd, linear_bwd_workspace,
+    FBL_ACT_NONE, FBL_ACT_RELU, FBL_ACT_GELU, FBL_ACT_GELU_TANH, FBL_ACT_SILU, ACTIVATIONS, linear_fwd, linear_fwd_workspace, linear_bwd, linear_bwd_workspace,
     FBL_HEAD_KV, FBL_HEAD_VK, linear_loss_workspace, linear_ce_fwd, linear_ce_bwd, linear_kd_fwd, linear_kd_bwd,
     layer_norm_fwd, layer_norm_bwd, layer_norm_bwd_workspace,
 )

@@ -17,7 +17,7 @@ OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libfbl.so")
 ACTS = ["none", "relu", "gelu", "gelu_tanh", "silu"]
 SOURCES = ["head_gemm.hip", *(f"linear_gemm_{a}.hip" for a in ACTS), "attn_streams.hip", "attn_rows_f32.hip", "attn_fwd_bf16.hip", "attn_bwd.hip", "attn_bwd_kv.hip", "attn_bwd_q.hip", "attn_bwd_dq.hip", "proj_gemm.hip",
-           "proj_gemm_f32.hip", "layout_map.hip", "noalloc.hip", "layer_norm.hip", "column_sums.hip", "linear_act.hip", "head_rows.hip",
+           "proj_gemm_f32.hip", "layout_map.hip", "noalloc.hip", "layer_norm.hip", "column_sums.hip", "linear_act.hip", "linear_finish.hip", "head_rows.hip",
            "api.cpp", "api_norm.cpp", "api_linear.cpp", "api_head.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

@@ -50,6 +50,23 @@ LinearWs linear_ws(int f32, int64_t M, int64_t N) {
     return w;
 }
 
+// Workgroups that share the contraction of a few tokens' tiles.  A tile alone has too few of w's bytes on the
+// way, and the longer its contraction the more that costs; sharing it costs a second launch and the planes
+// (cold weights, us, alone and shared: bf16, 1 token 4096 x 4096 18.3 and 12.3, 8192 x 2048 31.4 and 12.1, 2048 x
+// 8192 11.3 and 12.1, 1024 x 4096 6.8 and 8.9; 64 tokens 4096 x 4096 20.1 and 15.1, 128 tokens 22.7 and 25.0, but
+// 8192 x 2048 33.6 and 25.4; fp32, 12 tokens 4096 x 4096 38 and 23, 1024 x 1024 11.6 and 7.7, 96 tokens 60 and 52).
+int few_splits(int f32, int64_t M, int64_t K, int64_t N) {
+    return (f32 ? M <= 128 && K >= 1024 : M <= 64 ? K > 2048 : M <= 128 && K >= 8192) ? fbl::sum_splits(f32, M, N, K) : 1;
+}
+// The tile of a bf16 forward that is not shared.  Up to 32 tokens and 8192 columns that is 32 x 32 on four
+// wavefronts, whose many workgroups have the most loads on the way (1 token, 2048 x 8192: 11.3 us, 16.9 with the
+// products' own choice below 32 rows; 4096 x 12288: 37.7 and 34.5).
+int forward_tile(int64_t M, int64_t K, int64_t N) {
+    if (M <= 32 && N <= 8192 && fbl_proj_tuned_tile(FBL_PROJ_FWD, M, K, N) < 0) return 16;
+    return fbl::proj_auto_tile(FBL_PROJ_FWD, M, K, N);
+}
+size_t few_ws(int splits, int64_t M, int64_t N) { return splits > 1 ? (size_t)splits * (size_t)M * (size_t)N * 4 : 0; }
+
 fbl_status linear_shape(int32_t dtype, uint32_t act, int64_t M, int64_t K, int64_t N) {
     if (!fbl::dtype_size(dtype)) return FBL_ERR_DTYPE;
     if (act > FBL_ACT_SILU) return FBL_ERR_ARG;
@@ -62,9 +79,16 @@ fbl_status linear_shape(int32_t dtype, uint32_t act, int64_t M, int64_t K, int64
 
 extern "C" {
 
+fbl_status fbl_linear_fwd_workspace(int32_t dtype, int64_t M, int64_t K, int64_t N, size_t* bytes) {
+    if (!bytes) return FBL_ERR_NULL;
+    const fbl_status st = linear_shape(dtype, FBL_ACT_NONE, M, K, N);
+    if (st == FBL_OK) *bytes = few_ws(few_splits(dtype == FBL_F32, M, K, N), M, N);
+    return st;
+}
+
 fbl_status fbl_linear_fwd(int32_t dtype, uint32_t act, int64_t M, int64_t K, int64_t N, const void* x, int64_t ldx,
                           const void* w, int64_t ldw, const void* bias, const void* res, int64_t ldr, void* y,
-                          int64_t ldy, void* z, int64_t ldz, int32_t tile, void* stream) {
+                          int64_t ldy, void* z, int64_t ldz, int32_t tile, void* ws, size_t ws_bytes, void* stream) {
     fbl_status st = linear_shape(dtype, act, M, K, N);
     if (st != FBL_OK) return st;
     if (!x || !w || !y) return FBL_ERR_NULL;
@@ -80,13 +104,33 @@ fbl_status fbl_linear_fwd(int32_t dtype, uint32_t act, int64_t M, int64_t K, int
         for (const RowsView* in : {&vx, &vw, &vb, &vr})
             if (overlap(*out, *in)) return FBL_ERR_ARG;
     if (overlap(vy, vz)) return FBL_ERR_ARG;
+    // with a workspace for the shares of it
+    int splits = tile == FBL_GEMM_TILE_AUTO && ws ? few_splits(es == 4, M, K, N) : 1;
+    if (splits > 1) {
+        const size_t need = few_ws(splits, M, N);
+        if (ws_bytes < need) return FBL_ERR_WORKSPACE;
+        const RowsView vws{ws, 1, (int64_t)need, (int64_t)need, 1};
+        if (vws.begin() % 16) return FBL_ERR_ALIGN;
+        for (const RowsView* v : {&vx, &vw, &vb, &vr, &vy, &vz})
+            if (overlap(vws, *v)) return FBL_ERR_ARG;
+    }
     fbl::LinearArgs p{};
     fbl::product(p, FBL_PROJ_FWD, vx, vw, vy, M, K, N);
     p.bias = bias, p.res = res, p.z = z, p.ldr = ldr, p.ldz = ldz;
     p.res_bytes = res ? fbl::load_span(vr) : 0;
     p.z_bytes = z ? (uint32_t)vz.bytes() : 0;
-    if (es == 2 && tile == FBL_GEMM_TILE_AUTO) tile = fbl::proj_auto_tile(FBL_PROJ_FWD, M, K, N);
-    const hipError_t e = run_linear_gemm(es == 4, (int)act, 0, tile, p, static_cast<hipStream_t>(stream));
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    if (splits > 1) {
+        fbl::SumArgs q{};
+        static_cast<fbl::GemmArgs&>(q) = p;
+        q.sum = static_cast<float*>(ws), q.lds = N, q.sum_bytes = (uint32_t)(M * N * 4);
+        q.first = 1, q.splits = splits, q.share = (int)(((K + splits - 1) / splits + 63) / 64 * 64);
+        hipError_t e = es == 4 ? fbl::launch_sum_gemm_f32(0, q, s) : fbl::launch_sum_gemm(0, 0, 0, q, s);
+        if (e == hipSuccess) e = fbl::launch_linear_finish(es == 4, (int)act, p, q.sum, splits, s);
+        return e == hipSuccess ? FBL_OK : FBL_ERR_HIP;
+    }
+    if (es == 2 && tile == FBL_GEMM_TILE_AUTO) tile = forward_tile(M, K, N);
+    const hipError_t e = run_linear_gemm(es == 4, (int)act, 0, tile, p, s);
     return e == hipSuccess ? FBL_OK : FBL_ERR_HIP;
 }
 

@@ -293,7 +293,7 @@ hipError_t launch_head(int f32, int table, HeadArgs& p, hipStream_t s) {
 
 // The tile of a split product: as narrow as the few rows that split one.
 int split_tile(int64_t M) { return M <= 32 ? 15 : M <= 64 ? 6 : 4; }
-constexpr int kSplitTileF32 = 2;
+constexpr int kSplitTileF32 = 4;
 
 }  // namespace
 
@@ -311,14 +311,16 @@ int head_tile_width(int f32, int tile) { return f32 ? kF32Tiles[tile].bm : kGemm
 hipError_t launch_head_fwd(int f32, int table, HeadArgs p, hipStream_t s) { return launch_head<HeadFwd>(f32, table, p, s); }
 hipError_t launch_head_grad(int f32, int table, HeadArgs p, hipStream_t s) { return launch_head<HeadGrad>(f32, table, p, s); }
 
-// dX of few tokens has few tiles and a vocabulary for its contraction: where its tiles leave a quarter of the CUs idle
-// and more, two workgroups a CU share them, each with a contraction of 512 at least.
+// Products of few rows have few tiles for a long contraction (dX over a vocabulary, a layer's forward for a few
+// tokens): where they do not fill the card, workgroups share them, two a CU in all with a contraction
+// of 512 at least (fp32: four a CU of its small tiles, 256).
 int sum_splits(int f32, int64_t M, int64_t N, int64_t kc) {
     const int t = split_tile(M), bm = f32 ? kF32Tiles[kSplitTileF32].bm : kGemmTiles[t].bm,
               bn = f32 ? kF32Tiles[kSplitTileF32].bn : kGemmTiles[t].bn;
     const int64_t tiles = ((M + bm - 1) / bm) * ((N + bn - 1) / bn);
-    if (tiles >= 192) return 1;
-    return (int)std::max<int64_t>(1, std::min<int64_t>((512 + tiles / 2) / tiles, kc / 512));
+    const int64_t want = f32 ? 1024 : 512;
+    if (tiles > want / 2) return 1;
+    return (int)std::max<int64_t>(1, std::min<int64_t>((want + tiles / 2) / tiles, kc / (f32 ? 256 : 512)));
 }
 
 hipError_t launch_sum_gemm(int a_kmajor, int b_nmajor, int tile, const SumArgs& p, hipStream_t s) {

@@ -70,7 +70,7 @@ EXPORTED = ("fbl_layout_desc", "fbl_layout_packed_qkv", "fbl_layout_offset", "fb
             "fbl_attn_tune_reset", "fbl_proj", "fbl_proj_dt",
             "fbl_gemm_tile_count", "fbl_gemm_tile_info", "fbl_proj_candidates", "fbl_proj_tune", "fbl_proj_tuned_tile", "fbl_proj_auto_tile",
             "fbl_proj_float_tile", "fbl_proj_tune_reset", "fbl_layer_norm_fwd", "fbl_layer_norm_bwd_workspace",
-            "fbl_layer_norm_bwd", "fbl_linear_fwd", "fbl_linear_bwd_workspace", "fbl_linear_bwd",
+            "fbl_layer_norm_bwd", "fbl_linear_fwd", "fbl_linear_fwd_workspace", "fbl_linear_bwd_workspace", "fbl_linear_bwd",
             "fbl_linear_loss_workspace", "fbl_linear_ce_fwd", "fbl_linear_ce_bwd", "fbl_linear_kd_fwd", "fbl_linear_kd_bwd",
             "fbl_status_str")
 
@@ -194,7 +194,9 @@ def _load() -> ctypes.CDLL:
     lib.fbl_layer_norm_bwd.argtypes = [i32, i64, i64, vp, i64, vp, i64, vp, vp, vp, vp, i64, vp, vp, vp, size, vp]
     lib.fbl_layer_norm_bwd.restype = ctypes.c_int
     u32 = ctypes.c_uint32
-    lib.fbl_linear_fwd.argtypes = [i32, u32, i64, i64, i64, vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, i64, i32, vp]
+    lib.fbl_linear_fwd.argtypes = [i32, u32, i64, i64, i64, vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, i64, i32, vp, size, vp]
+    lib.fbl_linear_fwd_workspace.argtypes = [i32, i64, i64, i64, sizep]
+    lib.fbl_linear_fwd_workspace.restype = ctypes.c_int
     lib.fbl_linear_fwd.restype = ctypes.c_int
     lib.fbl_linear_bwd_workspace.argtypes = [i32, i64, i64, i64, sizep]
     lib.fbl_linear_bwd_workspace.restype = ctypes.c_int
@@ -834,7 +836,7 @@ def proj_tune_reset() -> None:
 # ---------------------------------------------------------------- layer norm
 def _matrix(t, where: str, name: str, shape=None, like=None):
     """Row stride of a 2-D tensor with unit inner stride, of `shape` and of `like`'s dtype
-    where given.  (The strides of a single row or column mean nothing: the width is taken.)"""
+    where given.  (The stride of a single row means nothing: its width, in whole 16-byte chunks.)"""
     if t.dim() != 2:
         raise FblError(FBL_ERR_SHAPE, f"{where}: {name} must be 2-D, got shape {tuple(t.shape)}")
     if shape is not None and tuple(t.shape) != tuple(shape):
@@ -843,7 +845,7 @@ def _matrix(t, where: str, name: str, shape=None, like=None):
         raise FblError(FBL_ERR_DTYPE, f"{where}: {name} is {t.dtype}, needs {like.dtype}")
     if t.shape[1] > 1 and t.stride(1) != 1:
         raise FblError(FBL_ERR_LAYOUT, f"{where}: {name} needs inner stride 1, got strides {t.stride()}")
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+    return t.stride(0) if t.shape[0] > 1 else -(-t.shape[1] // 8) * 8
 
 
 def _vector(t, where: str, name: str, n: int, dtype):
@@ -950,14 +952,22 @@ def _act_code(act, where: str) -> int:
     return code
 
 
+def linear_fwd_workspace(x, w) -> int:
+    """Bytes of linear_fwd's workspace for x [M, K] and w [K, N]: 0 but for a few tokens."""
+    n = ctypes.c_size_t(0)
+    _check(LIB.fbl_linear_fwd_workspace(_dtype_code(x), *x.shape, w.shape[1], ctypes.byref(n)), "fbl_linear_fwd_workspace")
+    return int(n.value)
+
+
 def linear_fwd(x, w, bias=None, act: str = "none", residual=None, out=None, z=None, tile: int = FBL_GEMM_TILE_AUTO,
-               stream=None):
+               workspace=None, stream=None):
     """y = act(x w + bias) + residual for x [M, K], w [K, N], bias [N], residual [M, N] (any row
     strides, one storage type), act one of ACTIVATIONS.  z [M, N], where given, receives the
-    pre-activation, which linear_bwd needs for every act but "none".  Returns y."""
+    pre-activation, which linear_bwd needs for every act but "none".  workspace: linear_fwd_workspace bytes, allocated
+    where they are needed and it is None.  Returns y."""
     import torch
     where = "linear_fwd"
-    _check_device(where, stream, x=x, w=w, bias=bias, residual=residual, out=out, z=z)
+    _check_device(where, stream, x=x, w=w, bias=bias, residual=residual, out=out, z=z, workspace=workspace)
     ldx = _matrix(x, where, "x")
     M, K = x.shape
     dt, code = _dtype_code(x), _act_code(act, where)
@@ -971,8 +981,12 @@ def linear_fwd(x, w, bias=None, act: str = "none", residual=None, out=None, z=No
     if out is None:
         out = torch.empty((M, N), dtype=x.dtype, device=x.device)
     ldy = _matrix(out, where, "out", (M, N), x)
+    ws, ws_bytes = None, 0
+    need = linear_fwd_workspace(x, w) if workspace is None and M <= 128 and tile == FBL_GEMM_TILE_AUTO else 0
+    if workspace is not None or need:
+        ws, ws_bytes = _scratch(workspace, need, where, x, stream)
     _check(LIB.fbl_linear_fwd(dt, code, M, K, N, _ptr(x), ldx, _ptr(w), ldw, _ptr(bias), _ptr(residual), ldr, _ptr(out), ldy,
-                              _ptr(z), ldz, tile, _launch_stream(stream)), "fbl_linear_fwd")
+                              _ptr(z), ldz, tile, _ptr(ws), ws_bytes, _launch_stream(stream)), "fbl_linear_fwd")
     return out
 
 

@@ -106,6 +106,35 @@ def test_few_tokens(M, dt):
         _check_fwd(fbl.linear_fwd(x, w, None, act, None, z=z), z, (ref[0], ref[1], None, None, None), act, dt)
 
 
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_few_tokens_shared_contraction(dt):
+    """A contraction that several workgroups share: strided operands, a share that ends inside a step, and the same
+    bits with the caller's workspace, an allocated one and on another stream."""
+    dt = DTYPES[dt]
+    for M, K, N in ((1, 4104, 260), (13, 5000, 132), (32, 8200, 64)):
+        if dt == torch.float32:
+            K, N = K + 1, N + 1
+        (x, w, b, r, _), ref = _case(M, K, N, dt, "gelu", True, True)
+        x, w, r = (padded(t, 4 if N % 8 == 4 and dt == torch.bfloat16 and t is not x else 8)[0] for t in (x, w, r))
+        need = fbl.linear_fwd_workspace(x, w)
+        assert need > 0 and need % (M * N * 4) == 0
+        z, zbuf = padded(torch.zeros(M, N, dtype=dt, device="cuda"), 4 if N % 8 == 4 else 8, 7.0)
+        new = lambda: padded(torch.zeros(M, N, dtype=dt, device="cuda"), 4 if N % 8 == 4 else 8, 7.0)[0]
+        y = fbl.linear_fwd(x, w, b, "gelu", r, z=z, out=new())
+        _check_fwd(y, z, ref, "gelu", dt)
+        assert torch.all(zbuf[:, N:] == 7.0) and torch.all(zbuf[-1] == 7.0)
+        ws = torch.full((need + 64,), 0xff, dtype=torch.uint8, device="cuda")  # nan, if it were read before it is written
+        assert torch.equal(y, fbl.linear_fwd(x, w, b, "gelu", r, out=new(), workspace=ws[:need]))
+        assert torch.all(ws[need:] == 0xff)
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        got = fbl.linear_fwd(x, w, b, "gelu", r, out=new(), stream=side)
+        torch.cuda.synchronize()
+        assert torch.equal(y, got)
+        with pytest.raises(fbl.FblError):
+            fbl.linear_fwd(x, w, b, "gelu", r, out=new(), workspace=ws[:need - 16])
+
+
 @pytest.mark.parametrize("tile", range(21))
 def test_every_tile(tile):
     """Ragged against every tile: a partial last step, partial rows and columns, into NaN."""

@@ -84,7 +84,7 @@ def test_layer_norm_binding_refuses_host_tensors():
 # ----------------------------------------------------------------- linear layers
 def lin_fwd(**kw):
     return LIB.fbl_linear_fwd(*_merge(dict(dt=BF16, act=2, M=8, K=64, N=64, x=at(1), ldx=64, w=at(2), ldw=64, bias=at(3),
-                                           res=at(4), ldr=64, y=at(5), ldy=64, z=at(6), ldz=64, tile=-1, stream=None), kw))
+                                           res=at(4), ldr=64, y=at(5), ldy=64, z=at(6), ldz=64, tile=-1, ws=None, ws_bytes=0, stream=None), kw))
 
 
 def lin_bwd(**kw):
