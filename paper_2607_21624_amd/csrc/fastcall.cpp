@@ -7,7 +7,7 @@
 // takes under 1 us beside the launches.  Host time of a pass, before and after:
 // forward + backward in two launches 29 -> 6.2 us, in four 34 -> 10.4, three
 // projection products 31 -> 8.5, a LoRA adapter's six 62 -> 17 (its step 64 ->
-// 26 us: now the kernels').
+// 26 us: now the kernels'); a layer norm's two calls 30 -> 10, one linear layer 20 -> 8.5.
 //
 // Every function takes all arguments of its namesake by position and either
 // does the whole call and returns its result, or does nothing and returns None:
@@ -24,6 +24,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/version.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "../../include/fbl.h"
@@ -76,6 +77,18 @@ struct Args {
     bool flag(int i) {
         if (a[i] != Py_True && a[i] != Py_False) ok = false;
         return a[i] == Py_True;
+    }
+    float real(int i) {
+        if (!PyFloat_CheckExact(a[i])) return ok = false, 0.f;
+        return (float)PyFloat_AS_DOUBLE(a[i]);
+    }
+    // name of an activation
+    uint32_t act(int i) {
+        static const char* const names[] = {"none", "relu", "gelu", "gelu_tanh", "silu"};
+        if (PyUnicode_CheckExact(a[i]))
+            for (uint32_t k = 0; k <= FBL_ACT_SILU; ++k)
+                if (PyUnicode_CompareWithASCIIString(a[i], names[k]) == 0) return k;
+        return ok = false, 0;
     }
     // softmax scale: None is 1 / sqrt(D)
     float scale(int i, int64_t D) {
@@ -349,12 +362,374 @@ PyObject* proj(PyObject*, PyObject* const* a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// ------------------------------------------------- layer norm, linear layers, losses
+// (the binding's _matrix, _vector, _head and _scratch)
+bool matrix(const Tensor* t, int64_t rows, int64_t width, at::ScalarType type) {
+    return !t || (t->dim() == 2 && t->size(0) == rows && t->size(1) == width && t->scalar_type() == type &&
+                  (width <= 1 || t->stride(1) == 1));
+}
+int64_t row_stride(const Tensor* t) {
+    return !t ? 0 : t->size(0) > 1 ? t->stride(0) : (t->size(1) + 7) / 8 * 8;
+}
+bool vector(const Tensor* t, int64_t n, at::ScalarType type) {
+    return !t || (t->dim() == 1 && t->size(0) == n && t->scalar_type() == type && (n <= 1 || t->stride(0) == 1));
+}
+template <typename T = void>
+T* data(const Tensor* t) {
+    return t ? static_cast<T*>(t->data_ptr()) : nullptr;
+}
+struct Scratch {
+    Tensor made;
+    void* p = nullptr;
+    size_t bytes = 0;
+    // false: not a plain workspace
+    bool set(const Tensor* given, size_t need, const Tensor& like) {
+        if (given && !given->is_contiguous()) return false;
+        if (!given && need) made = empty({(int64_t)need}, at::kByte, like), given = &made;
+        if (given) p = given->data_ptr(), bytes = (size_t)(given->numel() * given->element_size());
+        return true;
+    }
+};
+PyObject* object_or_none(PyObject* given, const Tensor& made) {
+    return given == Py_None && !made.defined() ? Py_NewRef(Py_None) : object_of(given, made);
+}
+
+// layer_norm_fwd(x, weight, bias, eps, out, mean, rstd, stream)
+PyObject* layer_norm_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (n != 8) Py_RETURN_NONE;
+    Args g{a};
+    const Tensor *x = g.tensor(0), *w = g.tensor_or_none(1), *b = g.tensor_or_none(2);
+    const float eps = g.real(3);
+    const Tensor *out = g.tensor_or_none(4), *mean = g.tensor_or_none(5), *rstd = g.tensor_or_none(6);
+    g.no_stream(7);
+    if (!g.ready() || x->dim() != 2 || dtype_code(*x) < 0) Py_RETURN_NONE;
+    const int64_t M = x->size(0), N = x->size(1);
+    const at::ScalarType dt = x->scalar_type();
+    if (!matrix(x, M, N, dt) || !matrix(out, M, N, dt) || !vector(w, N, dt) || !vector(b, N, dt) || !vector(mean, M, at::kFloat) ||
+        !vector(rstd, M, at::kFloat))
+        Py_RETURN_NONE;
+    Tensor mo, mm, mr;
+    if (!out) mo = empty({M, N}, dt, *x), out = &mo;
+    if (!mean) mm = empty({M}, at::kFloat, *x), mean = &mm;
+    if (!rstd) mr = empty({M}, at::kFloat, *x), rstd = &mr;
+    void *s = g.stream(), *px = data(x), *pw = data(w), *pb = data(b), *po = data(out);
+    float *pm = data<float>(mean), *pr = data<float>(rstd);
+    const int64_t ldx = row_stride(x), ldo = row_stride(out);
+    const int code = dtype_code(*x);
+    const fbl_status st =
+        unlocked([&] { return fbl_layer_norm_fwd(code, M, N, px, ldx, pw, pb, eps, po, ldo, pm, pr, s); });
+    if (st != FBL_OK) Py_RETURN_NONE;
+    return tuple_of<3>({object_of(a[4], mo), object_of(a[5], mm), object_of(a[6], mr)});
+    END_HANDLE_TH_ERRORS
+}
+
+// layer_norm_bwd(dy, x, mean, rstd, weight, dx, dweight, dbias, workspace, stream, need_weight, need_bias)
+PyObject* layer_norm_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (n != 12) Py_RETURN_NONE;
+    Args g{a};
+    const Tensor *dy = g.tensor(0), *x = g.tensor(1), *mean = g.tensor(2), *rstd = g.tensor(3), *w = g.tensor_or_none(4);
+    const Tensor *dx = g.tensor_or_none(5), *dw = g.tensor_or_none(6), *db = g.tensor_or_none(7), *ws = g.tensor_or_none(8);
+    g.no_stream(9);
+    const bool need_w = g.flag(10), need_b = g.flag(11);
+    if (!g.ready() || x->dim() != 2 || dtype_code(*x) < 0) Py_RETURN_NONE;
+    const int64_t M = x->size(0), N = x->size(1);
+    const at::ScalarType dt = x->scalar_type();
+    const int code = dtype_code(*x);
+    if (!matrix(x, M, N, dt) || !matrix(dy, M, N, dt) || !matrix(dx, M, N, dt) || !vector(mean, M, at::kFloat) ||
+        !vector(rstd, M, at::kFloat) || !vector(w, N, dt) || !vector(dw, N, dt) || !vector(db, N, dt))
+        Py_RETURN_NONE;
+    Tensor mx, mw, mb;
+    if (!dx) mx = empty({M, N}, dt, *x), dx = &mx;
+    if (!dw && need_w) mw = empty({N}, dt, *x), dw = &mw;
+    if (!db && need_b) mb = empty({N}, dt, *x), db = &mb;
+    Scratch sc;
+    size_t need = 0;
+    if (dw || db) {
+        if (!ws && fbl_layer_norm_bwd_workspace(code, M, N, &need) != FBL_OK) Py_RETURN_NONE;
+        if (!sc.set(ws, need, *x)) Py_RETURN_NONE;
+    }
+    void *s = g.stream(), *py = data(dy), *px = data(x), *pw = data(w), *pdx = data(dx), *pdw = data(dw), *pdb = data(db);
+    float *pm = data<float>(mean), *pr = data<float>(rstd);
+    const int64_t ldy = row_stride(dy), ldx = row_stride(x), lddx = row_stride(dx);
+    const fbl_status st = unlocked([&] {
+        return fbl_layer_norm_bwd(code, M, N, py, ldy, px, ldx, pw, pm, pr, pdx, lddx, pdw, pdb, sc.p, sc.bytes, s);
+    });
+    if (st != FBL_OK) Py_RETURN_NONE;
+    return tuple_of<3>({object_of(a[5], mx), object_or_none(a[6], mw), object_or_none(a[7], mb)});
+    END_HANDLE_TH_ERRORS
+}
+
+// linear_fwd(x, w, bias, act, residual, out, z, tile, workspace, stream)
+PyObject* linear_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (n != 10) Py_RETURN_NONE;
+    Args g{a};
+    const Tensor *x = g.tensor(0), *w = g.tensor(1), *b = g.tensor_or_none(2);
+    const uint32_t act = g.act(3);
+    const Tensor *res = g.tensor_or_none(4), *out = g.tensor_or_none(5), *z = g.tensor_or_none(6);
+    const int64_t tile = g.integer(7);
+    const Tensor* ws = g.tensor_or_none(8);
+    g.no_stream(9);
+    if (!g.ready() || x->dim() != 2 || w->dim() != 2 || dtype_code(*x) < 0) Py_RETURN_NONE;
+    const int64_t M = x->size(0), K = x->size(1), N = w->size(1);
+    const at::ScalarType dt = x->scalar_type();
+    const int code = dtype_code(*x);
+    if (!matrix(x, M, K, dt) || !matrix(w, K, N, dt) || !vector(b, N, dt) || !matrix(res, M, N, dt) || !matrix(out, M, N, dt) ||
+        !matrix(z, M, N, dt))
+        Py_RETURN_NONE;
+    Tensor mo;
+    if (!out) mo = empty({M, N}, dt, *x), out = &mo;
+    Scratch sc;
+    size_t need = 0;
+    if (!ws && tile == FBL_GEMM_TILE_AUTO && M <= 128 && fbl_linear_fwd_workspace(code, M, K, N, &need) != FBL_OK) Py_RETURN_NONE;
+    if (!sc.set(ws, need, *x)) Py_RETURN_NONE;
+    void *s = g.stream(), *px = data(x), *pw = data(w), *pb = data(b), *pr = data(res), *po = data(out), *pz = data(z);
+    const int64_t ldx = row_stride(x), ldw = row_stride(w), ldr = row_stride(res), ldo = row_stride(out), ldz = row_stride(z);
+    const fbl_status st = unlocked([&] {
+        return fbl_linear_fwd(code, act, M, K, N, px, ldx, pw, ldw, pb, pr, ldr, po, ldo, pz, ldz, (int32_t)tile, sc.p, sc.bytes, s);
+    });
+    if (st != FBL_OK) Py_RETURN_NONE;
+    return object_of(a[5], mo);
+    END_HANDLE_TH_ERRORS
+}
+
+// linear_bwd(dy, x, w, z, act, dx, dw, dbias, workspace, stream, need_dx, need_dw, need_bias, x_act, x_z)
+PyObject* linear_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (n != 15) Py_RETURN_NONE;
+    Args g{a};
+    const Tensor *dy = g.tensor(0), *x = g.tensor(1), *w = g.tensor(2), *z = g.tensor_or_none(3);
+    const uint32_t act = g.act(4), xact = g.act(13);
+    const Tensor *dx = g.tensor_or_none(5), *dw = g.tensor_or_none(6), *db = g.tensor_or_none(7), *ws = g.tensor_or_none(8);
+    g.no_stream(9);
+    const bool need_x = g.flag(10), need_w = g.flag(11), need_b = g.flag(12);
+    const Tensor* xz = g.tensor_or_none(14);
+    if (!g.ready() || x->dim() != 2 || w->dim() != 2 || dtype_code(*x) < 0) Py_RETURN_NONE;
+    const int64_t M = x->size(0), K = x->size(1), N = w->size(1);
+    const at::ScalarType dt = x->scalar_type();
+    const int code = dtype_code(*x);
+    if (!matrix(x, M, K, dt) || !matrix(w, K, N, dt) || !matrix(dy, M, N, dt) || !matrix(z, M, N, dt) || !matrix(xz, M, K, dt) ||
+        !matrix(dx, M, K, dt) || !matrix(dw, K, N, dt) || !vector(db, N, dt))
+        Py_RETURN_NONE;
+    Tensor mx, mw, mb;
+    if (!dx && need_x) mx = empty({M, K}, dt, *x), dx = &mx;
+    if (!dw && need_w) mw = empty({K, N}, dt, *x), dw = &mw;
+    if (!db && need_b) mb = empty({N}, dt, *x), db = &mb;
+    Scratch sc;
+    size_t need = 0;
+    if (act != FBL_ACT_NONE || db) {
+        if (!ws && fbl_linear_bwd_workspace(code, M, K, N, &need) != FBL_OK) Py_RETURN_NONE;
+        if (!sc.set(ws, need, *x)) Py_RETURN_NONE;
+    }
+    void *s = g.stream(), *py = data(dy), *px = data(x), *pw = data(w), *pz = data(z), *pxz = data(xz), *pdx = data(dx),
+         *pdw = data(dw), *pdb = data(db);
+    const int64_t ldy = row_stride(dy), ldx = row_stride(x), ldw = row_stride(w), ldz = row_stride(z), ldxz = row_stride(xz),
+                  lddx = row_stride(dx), lddw = row_stride(dw);
+    const fbl_status st = unlocked([&] {
+        return fbl_linear_bwd(code, act, M, K, N, py, ldy, px, ldx, pw, ldw, pz, ldz, xact, pxz, ldxz, pdx, lddx, pdw, lddw, pdb,
+                              sc.p, sc.bytes, s);
+    });
+    if (st != FBL_OK) Py_RETURN_NONE;
+    return tuple_of<3>({object_or_none(a[5], mx), object_or_none(a[6], mw), object_or_none(a[7], mb)});
+    END_HANDLE_TH_ERRORS
+}
+
+// A head's weight [K, V]: the way it is stored and its row stride.
+bool head(const Tensor* w, const Tensor* x, uint32_t* order, int64_t* ld) {
+    if (w->dim() != 2 || w->scalar_type() != x->scalar_type() || w->size(0) != x->size(1)) return false;
+    const int64_t K = w->size(0), V = w->size(1);
+    if (w->stride(1) == 1 && (K == 1 || w->stride(0) >= V)) {
+        *order = FBL_HEAD_KV, *ld = K > 1 ? w->stride(0) : std::max(w->stride(0), V);
+        return true;
+    }
+    if (w->stride(0) != 1 && K != 1) return false;
+    *order = FBL_HEAD_VK, *ld = V > 1 ? w->stride(1) : std::max(w->stride(1), K);
+    return true;
+}
+// x [M, K] and w of a loss, their arguments and workspace
+struct HeadCall {
+    int64_t M, K, V, ldx, ldw;
+    uint32_t order;
+    int code;
+    Scratch sc;
+    bool set(const Tensor* x, const Tensor* w, const Tensor* ws, int64_t top) {
+        if (x->dim() != 2 || dtype_code(*x) < 0 || !matrix(x, x->size(0), x->size(1), x->scalar_type())) return false;
+        if (!head(w, x, &order, &ldw)) return false;
+        M = x->size(0), K = x->size(1), V = w->size(1), ldx = row_stride(x), code = dtype_code(*x);
+        size_t need = 0;
+        if (!ws && fbl_linear_loss_workspace(code, order, M, K, V, top, ldw, &need) != FBL_OK) return false;
+        return sc.set(ws, need, *x);
+    }
+};
+// The gradients' tensors: the given ones or new ones
+struct HeadGrads {
+    Tensor mx, mw;
+    const Tensor *dx, *dw;
+    int64_t lddx = 0, lddw = 0;
+    bool set(const HeadCall& h, const Tensor* x, const Tensor* gx, const Tensor* gw, bool need_x, bool need_w) {
+        dx = gx, dw = gw;
+        const at::ScalarType dt = x->scalar_type();
+        if (!matrix(dx, h.M, h.K, dt)) return false;
+        if (!dx && need_x) mx = empty({h.M, h.K}, dt, *x), dx = &mx;
+        if (!dw && need_w) mw = h.order == FBL_HEAD_VK ? empty({h.V, h.K}, dt, *x).t() : empty({h.K, h.V}, dt, *x), dw = &mw;
+        uint32_t order = h.order;
+        if (dw && (!head(dw, x, &order, &lddw) || order != h.order || dw->size(1) != h.V)) return false;
+        lddx = row_stride(dx);
+        return true;
+    }
+};
+// the loss' gradient: one number, or one a row
+bool loss_grad(const Tensor* t, int64_t M, int64_t* stride) {
+    if (t->scalar_type() != at::kFloat) return false;
+    if (t->dim() == 0) return *stride = 0, true;
+    if (t->dim() != 1 || t->size(0) != M) return false;
+    return *stride = t->stride(0), true;
+}
+float* mean_of(const Tensor* t) { return data<float>(t); }
+bool mean_fits(const Tensor* t) { return !t || (t->scalar_type() == at::kFloat && t->numel() == 1); }
+
+// linear_ce_fwd(x, w, labels, ignore_index, loss, lse, total, mean, workspace, stream)
+PyObject* linear_ce_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (n != 10) Py_RETURN_NONE;
+    Args g{a};
+    const Tensor *x = g.tensor(0), *w = g.tensor(1), *labels = g.tensor(2);
+    const int64_t ignore = g.integer(3);
+    const Tensor *loss = g.tensor_or_none(4), *lse = g.tensor_or_none(5), *total = g.tensor_or_none(6), *mean = g.tensor_or_none(7),
+                 *ws = g.tensor_or_none(8);
+    g.no_stream(9);
+    HeadCall h;
+    if (!g.ready() || !h.set(x, w, ws, 1) || !vector(labels, h.M, at::kLong) || !vector(loss, h.M, at::kFloat) ||
+        !vector(lse, h.M, at::kFloat) || !vector(total, 2, at::kFloat) || !mean_fits(mean))
+        Py_RETURN_NONE;
+    Tensor ml, me, mt;
+    if (!loss) ml = empty({h.M}, at::kFloat, *x), loss = &ml;
+    if (!lse) me = empty({h.M}, at::kFloat, *x), lse = &me;
+    if (!total) mt = empty({2}, at::kFloat, *x), total = &mt;
+    void *s = g.stream(), *px = data(x), *pw = data(w);
+    const int64_t* pl = data<int64_t>(labels);
+    float *po = data<float>(loss), *pe = data<float>(lse), *pt = data<float>(total), *pm = mean_of(mean);
+    const fbl_status st = unlocked([&] {
+        return fbl_linear_ce_fwd(h.code, h.order, h.M, h.K, h.V, px, h.ldx, pw, h.ldw, pl, ignore, po, pe, pt, pm, h.sc.p, h.sc.bytes, s);
+    });
+    if (st != FBL_OK) Py_RETURN_NONE;
+    return tuple_of<3>({object_of(a[4], ml), object_of(a[5], me), object_of(a[6], mt)});
+    END_HANDLE_TH_ERRORS
+}
+
+// linear_ce_bwd(dloss, x, w, labels, lse, total, ignore_index, dx, dw, workspace, stream, need_dx, need_dw)
+PyObject* linear_ce_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (n != 13) Py_RETURN_NONE;
+    Args g{a};
+    const Tensor *dl = g.tensor(0), *x = g.tensor(1), *w = g.tensor(2), *labels = g.tensor(3), *lse = g.tensor(4),
+                 *total = g.tensor_or_none(5);
+    const int64_t ignore = g.integer(6);
+    const Tensor *dx = g.tensor_or_none(7), *dw = g.tensor_or_none(8), *ws = g.tensor_or_none(9);
+    g.no_stream(10);
+    const bool need_x = g.flag(11), need_w = g.flag(12);
+    HeadCall h;
+    HeadGrads d;
+    int64_t ldl = 0;
+    if (!g.ready() || !h.set(x, w, ws, 1) || !vector(labels, h.M, at::kLong) || !vector(lse, h.M, at::kFloat) ||
+        !vector(total, 2, at::kFloat) || !loss_grad(dl, h.M, &ldl) || !d.set(h, x, dx, dw, need_x, need_w))
+        Py_RETURN_NONE;
+    void *s = g.stream(), *px = data(x), *pw = data(w), *pdx = data(d.dx), *pdw = data(d.dw);
+    const int64_t* pl = data<int64_t>(labels);
+    const float *pg = data<float>(dl), *pe = data<float>(lse), *pt = data<float>(total);
+    const fbl_status st = unlocked([&] {
+        return fbl_linear_ce_bwd(h.code, h.order, h.M, h.K, h.V, pg, ldl, pt, px, h.ldx, pw, h.ldw, pl, ignore, pe, pdx, d.lddx, pdw,
+                                 d.lddw, h.sc.p, h.sc.bytes, s);
+    });
+    if (st != FBL_OK) Py_RETURN_NONE;
+    return tuple_of<2>({object_or_none(a[7], d.mx), object_or_none(a[8], d.mw)});
+    END_HANDLE_TH_ERRORS
+}
+
+// linear_kd_fwd(x, w, index, logits, temperature, loss, lse, prob, total, mean, workspace, stream)
+PyObject* linear_kd_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (n != 12) Py_RETURN_NONE;
+    Args g{a};
+    const Tensor *x = g.tensor(0), *w = g.tensor(1), *index = g.tensor(2), *logits = g.tensor(3);
+    const float T = g.real(4);
+    const Tensor *loss = g.tensor_or_none(5), *lse = g.tensor_or_none(6), *prob = g.tensor_or_none(7), *total = g.tensor_or_none(8),
+                 *mean = g.tensor_or_none(9), *ws = g.tensor_or_none(10);
+    g.no_stream(11);
+    if (!g.ready() || index->dim() != 2 || dtype_code(*logits) < 0) Py_RETURN_NONE;
+    const int64_t top = index->size(1);
+    HeadCall h;
+    if (!h.set(x, w, ws, top) || !matrix(index, h.M, top, at::kLong) || !matrix(logits, h.M, top, logits->scalar_type()) ||
+        !vector(loss, h.M, at::kFloat) || !vector(lse, h.M, at::kFloat) || !vector(total, 2, at::kFloat) || !mean_fits(mean) ||
+        !matrix(prob, h.M, top, at::kFloat) || (prob && !prob->is_contiguous()))
+        Py_RETURN_NONE;
+    Tensor ml, me, mp, mt;
+    if (!loss) ml = empty({h.M}, at::kFloat, *x), loss = &ml;
+    if (!lse) me = empty({h.M}, at::kFloat, *x), lse = &me;
+    if (!prob) mp = empty({h.M, top}, at::kFloat, *x), prob = &mp;
+    if (!total) mt = empty({2}, at::kFloat, *x), total = &mt;
+    void *s = g.stream(), *px = data(x), *pw = data(w), *pz = data(logits);
+    const int64_t* pi = data<int64_t>(index);
+    float *pp = data<float>(prob), *po = data<float>(loss), *pe = data<float>(lse), *pt = data<float>(total), *pm = mean_of(mean);
+    const int64_t ldi = row_stride(index), ldz = row_stride(logits);
+    const int zcode = dtype_code(*logits);
+    const fbl_status st = unlocked([&] {
+        return fbl_linear_kd_fwd(h.code, h.order, h.M, h.K, h.V, top, px, h.ldx, pw, h.ldw, pi, ldi, zcode, pz, ldz, T, pp, po, pe, pt,
+                                 pm, h.sc.p, h.sc.bytes, s);
+    });
+    if (st != FBL_OK) Py_RETURN_NONE;
+    return tuple_of<4>({object_of(a[5], ml), object_of(a[6], me), object_of(a[7], mp), object_of(a[8], mt)});
+    END_HANDLE_TH_ERRORS
+}
+
+// linear_kd_bwd(dloss, x, w, index, prob, lse, temperature, total, dx, dw, workspace, stream, need_dx, need_dw)
+PyObject* linear_kd_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (n != 14) Py_RETURN_NONE;
+    Args g{a};
+    const Tensor *dl = g.tensor(0), *x = g.tensor(1), *w = g.tensor(2), *index = g.tensor(3), *prob = g.tensor(4), *lse = g.tensor(5);
+    const float T = g.real(6);
+    const Tensor *total = g.tensor_or_none(7), *dx = g.tensor_or_none(8), *dw = g.tensor_or_none(9), *ws = g.tensor_or_none(10);
+    g.no_stream(11);
+    const bool need_x = g.flag(12), need_w = g.flag(13);
+    if (!g.ready() || index->dim() != 2) Py_RETURN_NONE;
+    const int64_t top = index->size(1);
+    HeadCall h;
+    HeadGrads d;
+    int64_t ldl = 0;
+    if (!h.set(x, w, ws, top) || !matrix(index, h.M, top, at::kLong) || !matrix(prob, h.M, top, at::kFloat) || !prob->is_contiguous() ||
+        !vector(lse, h.M, at::kFloat) || !vector(total, 2, at::kFloat) || !loss_grad(dl, h.M, &ldl) ||
+        !d.set(h, x, dx, dw, need_x, need_w))
+        Py_RETURN_NONE;
+    void *s = g.stream(), *px = data(x), *pw = data(w), *pdx = data(d.dx), *pdw = data(d.dw);
+    const int64_t* pi = data<int64_t>(index);
+    const float *pg = data<float>(dl), *pp = data<float>(prob), *pe = data<float>(lse), *pt = data<float>(total);
+    const int64_t ldi = row_stride(index);
+    const fbl_status st = unlocked([&] {
+        return fbl_linear_kd_bwd(h.code, h.order, h.M, h.K, h.V, top, pg, ldl, pt, px, h.ldx, pw, h.ldw, pi, ldi, T, pp, pe, pdx, d.lddx,
+                                 pdw, d.lddw, h.sc.p, h.sc.bytes, s);
+    });
+    if (st != FBL_OK) Py_RETURN_NONE;
+    return tuple_of<2>({object_or_none(a[8], d.mx), object_or_none(a[9], d.mw)});
+    END_HANDLE_TH_ERRORS
+}
+
 PyMethodDef kMethods[] = {
     {"attn_fwd", (PyCFunction)(void (*)())attn_fwd, METH_FASTCALL, nullptr},
     {"attn_bwd", (PyCFunction)(void (*)())attn_bwd, METH_FASTCALL, nullptr},
     {"attn_fwd_packed", (PyCFunction)(void (*)())attn_fwd_packed, METH_FASTCALL, nullptr},
     {"attn_bwd_packed", (PyCFunction)(void (*)())attn_bwd_packed, METH_FASTCALL, nullptr},
     {"proj", (PyCFunction)(void (*)())proj, METH_FASTCALL, nullptr},
+    {"layer_norm_fwd", (PyCFunction)(void (*)())layer_norm_fwd, METH_FASTCALL, nullptr},
+    {"layer_norm_bwd", (PyCFunction)(void (*)())layer_norm_bwd, METH_FASTCALL, nullptr},
+    {"linear_fwd", (PyCFunction)(void (*)())linear_fwd, METH_FASTCALL, nullptr},
+    {"linear_bwd", (PyCFunction)(void (*)())linear_bwd, METH_FASTCALL, nullptr},
+    {"linear_ce_fwd", (PyCFunction)(void (*)())linear_ce_fwd, METH_FASTCALL, nullptr},
+    {"linear_ce_bwd", (PyCFunction)(void (*)())linear_ce_bwd, METH_FASTCALL, nullptr},
+    {"linear_kd_fwd", (PyCFunction)(void (*)())linear_kd_fwd, METH_FASTCALL, nullptr},
+    {"linear_kd_bwd", (PyCFunction)(void (*)())linear_kd_bwd, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};

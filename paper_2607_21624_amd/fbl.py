@@ -223,10 +223,14 @@ def _load() -> ctypes.CDLL:
 
 LIB = _load()
 
-# The plain calls of attn_fwd, attn_bwd, their packed forms and proj run natively
+# The plain calls of these functions run natively
 # (csrc/fastcall.cpp): each does the whole call, or nothing and returns None --
 # any argument that is not a plain one, any error -- and the Python below then
 # makes the call with every check.
+_NATIVE = ("attn_fwd", "attn_bwd", "attn_fwd_packed", "attn_bwd_packed", "proj", "layer_norm_fwd", "layer_norm_bwd",
+           "linear_fwd", "linear_bwd", "linear_ce_fwd", "linear_ce_bwd", "linear_kd_fwd", "linear_kd_bwd")
+
+
 def _load_native():
     """The _fastcall module, or a stand-in that handles no call.  It is compiled
     against one torch and one Python: without it, or with one of another build, the
@@ -244,7 +248,7 @@ def _load_native():
         import warnings
         warnings.warn(f"native call path unavailable, calls take the Python path: {e}", RuntimeWarning)
         no = staticmethod(lambda *args: None)
-        return type("NoNative", (), dict.fromkeys(("attn_fwd", "attn_bwd", "attn_fwd_packed", "attn_bwd_packed", "proj"), no))
+        return type("NoNative", (), dict.fromkeys(_NATIVE, no))
 
 
 _FAST = _load_native()
@@ -860,17 +864,29 @@ def _vector(t, where: str, name: str, n: int, dtype):
         raise FblError(FBL_ERR_LAYOUT, f"{where}: {name} must be contiguous")
 
 
+def _empty(shape, dtype, like, stream, result: bool = True):
+    """New memory for work on `stream` (None: the current one).  Another stream's comes from that stream's own pool:
+    a block of the current stream's may still be in use by work that is queued there.  A
+    result is known to the current stream too, whose program reads it."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=like.device)
+    here = torch.cuda.current_stream(like.device)
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream, device=like.device) if stream else torch.cuda.default_stream(like.device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=like.device)
+    if result:
+        t.record_stream(here)
+    return t
+
+
 def _scratch(workspace, need: int, where: str, like, stream):
-    """(workspace, its bytes): the caller's, or one allocated for this call.  The
-    allocator may hand that one out again when the call has returned, so it learns of the
-    stream that still works on it."""
+    """(workspace, its bytes): the caller's, or one allocated for this call."""
     import torch
     _check_workspace(workspace, where)
     if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=like.device)
-        if stream is not None:
-            used = torch.cuda.ExternalStream(stream, device=like.device) if isinstance(stream, int) else stream
-            workspace.record_stream(used)
+        workspace = _empty(need, torch.uint8, like, stream, result=False)
     return workspace, workspace.numel() * workspace.element_size()
 
 
@@ -881,6 +897,9 @@ def _launch_stream(stream):
 def layer_norm_fwd(x, weight=None, bias=None, eps: float = 1e-5, out=None, mean=None, rstd=None, stream=None):
     """Layer norm of the rows of x [M, N] (any row stride): returns (y, mean, rstd), mean
     and rstd float32 [M].  weight and bias [N], in x's dtype, may be None."""
+    done = _FAST.layer_norm_fwd(x, weight, bias, eps, out, mean, rstd, stream)
+    if done is not None:
+        return done
     import torch
     where = "layer_norm_fwd"
     _check_device(where, stream, x=x, weight=weight, bias=bias, out=out, mean=mean, rstd=rstd)
@@ -890,12 +909,12 @@ def layer_norm_fwd(x, weight=None, bias=None, eps: float = 1e-5, out=None, mean=
     _vector(weight, where, "weight", N, x.dtype)
     _vector(bias, where, "bias", N, x.dtype)
     if out is None:
-        out = torch.empty((M, N), dtype=x.dtype, device=x.device)
+        out = _empty((M, N), x.dtype, x, stream)
     ldy = _matrix(out, where, "out", (M, N), x)
     if mean is None:
-        mean = torch.empty(M, dtype=torch.float32, device=x.device)
+        mean = _empty(M, torch.float32, x, stream)
     if rstd is None:
-        rstd = torch.empty(M, dtype=torch.float32, device=x.device)
+        rstd = _empty(M, torch.float32, x, stream)
     _vector(mean, where, "mean", M, torch.float32)
     _vector(rstd, where, "rstd", M, torch.float32)
     _check(LIB.fbl_layer_norm_fwd(dt, M, N, _ptr(x), ldx, _ptr(weight), _ptr(bias), float(eps), _ptr(out), ldy, _ptr(mean),
@@ -914,6 +933,10 @@ def layer_norm_bwd(dy, x, mean, rstd, weight=None, dx=None, dweight=None, dbias=
                    need_weight: bool = True, need_bias: bool = True):
     """Gradients of layer_norm_fwd's rows: returns (dx, dweight, dbias), the last two
     None where not needed.  mean and rstd are the forward's."""
+    done = _FAST.layer_norm_bwd(dy, x, mean, rstd, weight, dx, dweight,
+                                   dbias, workspace, stream, need_weight, need_bias)
+    if done is not None:
+        return done
     import torch
     where = "layer_norm_bwd"
     _check_device(where, stream, dy=dy, x=x, mean=mean, rstd=rstd, weight=weight, dx=dx, dweight=dweight, dbias=dbias,
@@ -926,12 +949,12 @@ def layer_norm_bwd(dy, x, mean, rstd, weight=None, dx=None, dweight=None, dbias=
     _vector(rstd, where, "rstd", M, torch.float32)
     _vector(weight, where, "weight", N, x.dtype)
     if dx is None:
-        dx = torch.empty((M, N), dtype=x.dtype, device=x.device)
+        dx = _empty((M, N), x.dtype, x, stream)
     lddx = _matrix(dx, where, "dx", (M, N), x)
     if dweight is None and need_weight:
-        dweight = torch.empty(N, dtype=x.dtype, device=x.device)
+        dweight = _empty(N, x.dtype, x, stream)
     if dbias is None and need_bias:
-        dbias = torch.empty(N, dtype=x.dtype, device=x.device)
+        dbias = _empty(N, x.dtype, x, stream)
     _vector(dweight, where, "dweight", N, x.dtype)
     _vector(dbias, where, "dbias", N, x.dtype)
     ws, ws_bytes = None, 0
@@ -965,6 +988,9 @@ def linear_fwd(x, w, bias=None, act: str = "none", residual=None, out=None, z=No
     strides, one storage type), act one of ACTIVATIONS.  z [M, N], where given, receives the
     pre-activation, which linear_bwd needs for every act but "none".  workspace: linear_fwd_workspace bytes, allocated
     where they are needed and it is None.  Returns y."""
+    done = _FAST.linear_fwd(x, w, bias, act, residual, out, z, tile, workspace, stream)
+    if done is not None:
+        return done
     import torch
     where = "linear_fwd"
     _check_device(where, stream, x=x, w=w, bias=bias, residual=residual, out=out, z=z, workspace=workspace)
@@ -979,7 +1005,7 @@ def linear_fwd(x, w, bias=None, act: str = "none", residual=None, out=None, z=No
     ldr = 0 if residual is None else _matrix(residual, where, "residual", (M, N), x)
     ldz = 0 if z is None else _matrix(z, where, "z", (M, N), x)
     if out is None:
-        out = torch.empty((M, N), dtype=x.dtype, device=x.device)
+        out = _empty((M, N), x.dtype, x, stream)
     ldy = _matrix(out, where, "out", (M, N), x)
     ws, ws_bytes = None, 0
     need = linear_fwd_workspace(x, w) if workspace is None and M <= 128 and tile == FBL_GEMM_TILE_AUTO else 0
@@ -1002,6 +1028,9 @@ def linear_bwd(dy, x, w, z=None, act: str = "none", dx=None, dw=None, dbias=None
     """Gradients of linear_fwd: returns (dx, dw, dbias), each None where not needed.  z is the
     forward's pre-activation (None for act "none"); the residual's gradient is dy.  Where x
     itself is x_act(x_z), dx can be the gradient of x_z."""
+    done = _FAST.linear_bwd(dy, x, w, z, act, dx, dw, dbias, workspace, stream, need_dx, need_dw, need_bias, x_act, x_z)
+    if done is not None:
+        return done
     import torch
     where = "linear_bwd"
     _check_device(where, stream, dy=dy, x=x, w=w, z=z, dx=dx, dw=dw, dbias=dbias, workspace=workspace, x_z=x_z)
@@ -1016,11 +1045,11 @@ def linear_bwd(dy, x, w, z=None, act: str = "none", dx=None, dw=None, dbias=None
     ldz = 0 if z is None else _matrix(z, where, "z", (M, N), x)
     ldxz = 0 if x_z is None else _matrix(x_z, where, "x_z", (M, K), x)
     if dx is None and need_dx:
-        dx = torch.empty((M, K), dtype=x.dtype, device=x.device)
+        dx = _empty((M, K), x.dtype, x, stream)
     if dw is None and need_dw:
-        dw = torch.empty((K, N), dtype=x.dtype, device=x.device)
+        dw = _empty((K, N), x.dtype, x, stream)
     if dbias is None and need_bias:
-        dbias = torch.empty(N, dtype=x.dtype, device=x.device)
+        dbias = _empty(N, x.dtype, x, stream)
     lddx = 0 if dx is None else _matrix(dx, where, "dx", (M, K), x)
     lddw = 0 if dw is None else _matrix(dw, where, "dw", (K, N), x)
     _vector(dbias, where, "dbias", N, x.dtype)
@@ -1062,10 +1091,10 @@ def linear_loss_workspace(x, w, top: int = 1) -> int:
     return int(n.value)
 
 
-def _new_f32(t, n: int, like, where: str, name: str):
+def _new_f32(t, n: int, like, where: str, name: str, stream):
     import torch
     if t is None:
-        t = torch.empty(n, dtype=torch.float32, device=like.device)
+        t = _empty(n, torch.float32, like, stream)
     _vector(t, where, name, n, torch.float32)
     return t
 
@@ -1096,16 +1125,16 @@ def _dloss(dloss, M: int, where: str) -> int:
     return dloss.stride(0)
 
 
-def _head_grads(x, w, dx, dw, need_dx: bool, need_dw: bool, order: int, where: str):
+def _head_grads(x, w, dx, dw, need_dx: bool, need_dw: bool, order: int, where: str, stream):
     """(dx, its row stride, dw, its row stride): the given ones, or new ones where needed."""
     import torch
     if dx is None and need_dx:
-        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        dx = _empty(x.shape, x.dtype, x, stream)
     lddx = 0 if dx is None else _matrix(dx, where, "dx", x.shape, x)
     if dw is None and need_dw:
         K, V = w.shape
-        dw = (torch.empty((V, K), dtype=x.dtype, device=x.device).t() if order == FBL_HEAD_VK else
-              torch.empty((K, V), dtype=x.dtype, device=x.device))
+        dw = (_empty((V, K), x.dtype, x, stream).t() if order == FBL_HEAD_VK else
+              _empty((K, V), x.dtype, x, stream))
     lddw = 0
     if dw is not None:
         if tuple(dw.shape) != tuple(w.shape):
@@ -1123,6 +1152,9 @@ def linear_ce_fwd(x, w, labels, ignore_index: int = -100, loss=None, lse=None, t
     log-sum-exp, float32 [M], and [their sum, the number of rows that count].  Rows labelled
     ignore_index do not count; a label outside the vocabulary makes its row's loss nan.  mean: one float32 that
     receives total[0] / total[1]."""
+    done = _FAST.linear_ce_fwd(x, w, labels, ignore_index, loss, lse, total, mean, workspace, stream)
+    if done is not None:
+        return done
     import torch
     where = "linear_ce_fwd"
     _check_device(where, stream, x=x, w=w, labels=labels, loss=loss, lse=lse, total=total, mean=mean, workspace=workspace)
@@ -1131,8 +1163,8 @@ def linear_ce_fwd(x, w, labels, ignore_index: int = -100, loss=None, lse=None, t
     dt = _dtype_code(x)
     order, ldw = _head(w, x, where)
     _vector(labels, where, "labels", M, torch.int64)
-    loss, lse = _new_f32(loss, M, x, where, "loss"), _new_f32(lse, M, x, where, "lse")
-    total = _new_f32(total, 2, x, where, "total")
+    loss, lse = _new_f32(loss, M, x, where, "loss", stream), _new_f32(lse, M, x, where, "lse", stream)
+    total = _new_f32(total, 2, x, where, "total", stream)
     ws, ws_bytes = _loss_scratch(workspace, x, w, 1, where, stream)
     _check(LIB.fbl_linear_ce_fwd(dt, order, M, K, w.shape[1], _ptr(x), ldx, _ptr(w), ldw, _ptr(labels), ignore_index, _ptr(loss),
                                  _ptr(lse), _ptr(total), _mean_ptr(mean, where), _ptr(ws), ws_bytes,
@@ -1145,6 +1177,10 @@ def linear_ce_bwd(dloss, x, w, labels, lse, total=None, ignore_index: int = -100
     """Gradients (dx, dw) of linear_ce_fwd, each None where not needed; dw is stored as w is.  dloss,
     float32, is the gradient of each row's loss ([M], or one number for all), or with the
     forward's total that of the mean over the rows that count."""
+    done = _FAST.linear_ce_bwd(dloss, x, w, labels, lse, total, ignore_index,
+                                  dx, dw, workspace, stream, need_dx, need_dw)
+    if done is not None:
+        return done
     import torch
     where = "linear_ce_bwd"
     _check_device(where, stream, dloss=dloss, x=x, w=w, labels=labels, lse=lse, total=total, dx=dx, dw=dw,
@@ -1157,7 +1193,7 @@ def linear_ce_bwd(dloss, x, w, labels, lse, total=None, ignore_index: int = -100
     _vector(lse, where, "lse", M, torch.float32)
     _vector(total, where, "total", 2, torch.float32)
     gstride = _dloss(dloss, M, where)
-    dx, lddx, dw, lddw = _head_grads(x, w, dx, dw, need_dx, need_dw, order, where)
+    dx, lddx, dw, lddw = _head_grads(x, w, dx, dw, need_dx, need_dw, order, where, stream)
     ws, ws_bytes = _loss_scratch(workspace, x, w, 1, where, stream)
     _check(LIB.fbl_linear_ce_bwd(dt, order, M, K, w.shape[1], _ptr(dloss), gstride, _ptr(total), _ptr(x), ldx, _ptr(w), ldw,
                                  _ptr(labels), ignore_index, _ptr(lse), _ptr(dx), lddx, _ptr(dw), lddw, _ptr(ws), ws_bytes,
@@ -1185,6 +1221,9 @@ def linear_kd_fwd(x, w, index, logits, temperature: float = 1.0, loss=None, lse=
     logits (float32 or bfloat16) [M, top] are the teacher's, loss[m] = T^2 sum p (log p - log q) with p = softmax(logits /
     T) over the row's entries and q = softmax(x w / T) over the vocabulary.  A negative index is an absent entry; a
     row without entries does not count.  Returns (loss, lse, prob, total); prob float32 [M, top]."""
+    done = _FAST.linear_kd_fwd(x, w, index, logits, temperature, loss, lse, prob, total, mean, workspace, stream)
+    if done is not None:
+        return done
     import torch
     where = "linear_kd_fwd"
     _check_device(where, stream, x=x, w=w, index=index, logits=logits, loss=loss, lse=lse, prob=prob, total=total, mean=mean,
@@ -1194,10 +1233,10 @@ def linear_kd_fwd(x, w, index, logits, temperature: float = 1.0, loss=None, lse=
     dt = _dtype_code(x)
     order, ldw = _head(w, x, where)
     top, ldi, ldl, ldt = _teacher(index, logits, x, where)
-    loss, lse = _new_f32(loss, M, x, where, "loss"), _new_f32(lse, M, x, where, "lse")
-    total = _new_f32(total, 2, x, where, "total")
+    loss, lse = _new_f32(loss, M, x, where, "loss", stream), _new_f32(lse, M, x, where, "lse", stream)
+    total = _new_f32(total, 2, x, where, "total", stream)
     if prob is None:
-        prob = torch.empty((M, top), dtype=torch.float32, device=x.device)
+        prob = _empty((M, top), torch.float32, x, stream)
     _contiguous(prob, where, "prob", (M, top))
     ws, ws_bytes = _loss_scratch(workspace, x, w, top, where, stream)
     _check(LIB.fbl_linear_kd_fwd(dt, order, M, K, w.shape[1], top, _ptr(x), ldx, _ptr(w), ldw, _ptr(index), ldi, ldt,
@@ -1219,6 +1258,10 @@ def _contiguous(t, where: str, name: str, shape):
 def linear_kd_bwd(dloss, x, w, index, prob, lse, temperature: float = 1.0, total=None, dx=None, dw=None, workspace=None,
                   stream=None, need_dx: bool = True, need_dw: bool = True):
     """Gradients (dx, dw) of linear_kd_fwd from its prob and lse; the rest as linear_ce_bwd."""
+    done = _FAST.linear_kd_bwd(dloss, x, w, index, prob, lse, temperature, total,
+                                  dx, dw, workspace, stream, need_dx, need_dw)
+    if done is not None:
+        return done
     import torch
     where = "linear_kd_bwd"
     _check_device(where, stream, dloss=dloss, x=x, w=w, index=index, prob=prob, lse=lse, total=total, dx=dx, dw=dw,
@@ -1232,7 +1275,7 @@ def linear_kd_bwd(dloss, x, w, index, prob, lse, temperature: float = 1.0, total
     _vector(lse, where, "lse", M, torch.float32)
     _vector(total, where, "total", 2, torch.float32)
     gstride = _dloss(dloss, M, where)
-    dx, lddx, dw, lddw = _head_grads(x, w, dx, dw, need_dx, need_dw, order, where)
+    dx, lddx, dw, lddw = _head_grads(x, w, dx, dw, need_dx, need_dw, order, where, stream)
     ws, ws_bytes = _loss_scratch(workspace, x, w, top, where, stream)
     _check(LIB.fbl_linear_kd_bwd(dt, order, M, K, w.shape[1], top, _ptr(dloss), gstride, _ptr(total), _ptr(x), ldx, _ptr(w), ldw,
                                  _ptr(index), ldi, float(temperature), _ptr(prob), _ptr(lse), _ptr(dx), lddx, _ptr(dw), lddw,

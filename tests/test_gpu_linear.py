@@ -126,9 +126,9 @@ def test_few_tokens_shared_contraction(dt):
         ws = torch.full((need + 64,), 0xff, dtype=torch.uint8, device="cuda")  # nan, if it were read before it is written
         assert torch.equal(y, fbl.linear_fwd(x, w, b, "gelu", r, out=new(), workspace=ws[:need]))
         assert torch.all(ws[need:] == 0xff)
-        side = torch.cuda.Stream()
+        side, got = torch.cuda.Stream(), new()
         side.wait_stream(torch.cuda.current_stream())
-        got = fbl.linear_fwd(x, w, b, "gelu", r, out=new(), stream=side)
+        fbl.linear_fwd(x, w, b, "gelu", r, out=got, stream=side)
         torch.cuda.synchronize()
         assert torch.equal(y, got)
         with pytest.raises(fbl.FblError):
@@ -286,3 +286,21 @@ def test_stream_graph_and_repeats():
         torch.cuda.synchronize()
         assert all(torch.equal(a, c) for a, c in zip(want, out))
         assert torch.isfinite(torch.randn(1 << 16, device="cuda").sum())
+
+
+def test_another_stream_shares_no_memory_with_queued_work():
+    """Results and workspaces of a call on another stream do not come out of blocks that the current stream's queue
+    still writes: temporaries of a long queue are freed, then a call goes to a stream that does not wait for it."""
+    (x, w, b, r, dy), _ = _case(16, 4096, 512, torch.bfloat16, "gelu", True, True)
+    want = fbl.linear_fwd(x, w, b, "gelu", r)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for stream in (side, side.cuda_stream):
+        a = torch.randn(2048, 2048, device="cuda")
+        for _ in range(20):  # some milliseconds
+            a = a @ a * 1e-3
+        for size in (want.numel() * 2, fbl.linear_fwd_workspace(x, w)):
+            torch.full((size,), 0xff, dtype=torch.uint8, device="cuda")  # queued behind, freed at once
+        got = fbl.linear_fwd(x, w, b, "gelu", r, stream=stream)
+        torch.cuda.synchronize()
+        assert torch.equal(got, want)
