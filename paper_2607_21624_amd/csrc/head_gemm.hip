@@ -236,7 +236,9 @@ struct SumPieces {
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const f32x4 s = f32x4{v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]};
-                    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(i32x4, s), rs, soff, 16 * h, 0);
+                    // the second four may be past the row (N a multiple of 4), where the next one begins
+                    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(i32x4, s), rs,
+                                                           n + 4 * h < p.N ? soff + 16 * h : kNowhere, 0, 0);
                 }
             }
         });
