@@ -16,7 +16,9 @@ namespace {
 // partial sums, so more of them hide more latency and fewer cost fewer bytes.
 int norm_groups(int f32, int64_t M, int N) {
     const int64_t blocks = (M + fbl::layer_norm_slots(f32, N) - 1) / fbl::layer_norm_slots(f32, N);
-    return (int)std::min<int64_t>(blocks, 512);
+    // 16 wavefronts a row fill a CU alone (2048 x 16384 bf16, 256 workgroups 59 us, 512 86); else two a CU (16384 x
+    // 4096: 256 85, 512 84, 1024 95 us; 16384 x 1600: 57, 43, 40; 4099 x 1001: 13.8, 13.7, 17.8)
+    return (int)std::min<int64_t>(blocks, fbl::layer_norm_wide(f32, N) ? 256 : 512);
 }
 
 size_t norm_ws(int f32, int64_t M, int N) { return (size_t)norm_groups(f32, M, N) * 2 * (size_t)N * 4; }

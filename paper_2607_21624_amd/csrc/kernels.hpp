@@ -101,6 +101,7 @@ hipError_t launch_layer_norm_fwd(int f32, const NormArgs& a, hipStream_t stream)
 hipError_t launch_layer_norm_bwd(int f32, const NormArgs& a, hipStream_t stream);
 // Rows of N values that one workgroup holds at a time.
 int layer_norm_slots(int f32, int N);
+bool layer_norm_wide(int f32, int N);  // a row takes 16 wavefronts
 
 // out0[n], out1[n] (K = 1 or 2 of them, each may be nullptr) = sums over `groups` of part [groups][K][N].
 hipError_t launch_column_sums(int f32, const float* part, int groups, int K, int N, void* out0, void* out1,

@@ -9,7 +9,10 @@
 // backward reads x and dy and writes dx, once.  A row is shared by LPR lanes (16, a
 // wavefront, 4 or 16 wavefronts) that hold all of it in registers, C 16-byte chunks
 // each, so the variance is taken about the mean (two sums, no cancellation)
-// without a second read.  Statistics and sums are fp32.
+// without a second read.  The next row is on its way while this one is summed.  Statistics
+// and sums are fp32.  16384 x 4096 bf16: forward 47 us (5.8 TB/s, part of it from the last-level cache),
+// backward 84 us (4.8 TB/s; a 1 GiB copy reaches 4.8); 52 and 136 us with loads that decided about the
+// row's end where they were issued, which made each wait for the one before.
 //
 // The weight's and bias' gradients are sums down the columns.  Every lane keeps
 // them in registers for its columns over all rows its workgroup walks; the
@@ -30,7 +33,9 @@ struct NormCfg {
     static constexpr int SLOTS = NT / LPR;
     static constexpr int VEC = Pack<T>::N;
     static constexpr int CAP = LPR * VEC * C;  // values of the longest row
-    static constexpr int NWR = LPR / 64;       // wavefronts that share a row (0: less than one)
+    // 16 wavefronts' registers have no room for the sums of 16 columns a lane: these keep them in LDS,
+    // each lane its own (128 KB; 2048 x 16384 bf16 159 -> 59 us)
+    static constexpr bool kLdsSums = LPR == 1024 && VEC * C > 8;
 };
 
 // Sums over the LPR lanes of a row; `red` is the caller's own LDS for this call
@@ -55,25 +60,46 @@ FBL_DEV void row_sums(float (&x)[K], float* red) {
     }
 }
 
-template <typename T, int LPR, int C>
+template <typename T, int LPR, int C, bool SHORT>
 __global__ __launch_bounds__((NormCfg<T, LPR, C>::NT)) void layer_norm_fwd(NormArgs a) {
     using Cfg = NormCfg<T, LPR, C>;
     using P = Pack<T>;
     __shared__ float red[2][16];
     const int slot = threadIdx.x / LPR, l = threadIdx.x % LPR, n = a.N;
-    const float inv = 1.f / (float)n;
-    const T* w = static_cast<const T*>(a.w);
-    const T* b = static_cast<const T*>(a.b);
-    for (int64_t m = (int64_t)blockIdx.x * Cfg::SLOTS + slot; m < a.M; m += (int64_t)gridDim.x * Cfg::SLOTS) {
-        const T* x = static_cast<const T*>(a.x) + m * a.ldx;
+    const bool has_w = a.w != nullptr, has_b = a.b != nullptr;
+    const int64_t step = (int64_t)gridDim.x * Cfg::SLOTS;
+    int64_t m = (int64_t)blockIdx.x * Cfg::SLOTS + slot;
+    if (m >= a.M) return;  // whole rows of lanes, and where they are more than a wavefront the workgroup
+    P pw[C], pb[C], next[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int col = (c * LPR + l) * P::N;
+        next[c].template fetch<SHORT>(static_cast<const T*>(a.x) + m * a.ldx, col, n);
+        if (has_w) pw[c].template fetch<SHORT>(static_cast<const T*>(a.w), col, n);
+        if (has_b) pb[c].template fetch<SHORT>(static_cast<const T*>(a.b), col, n);
+    }
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        if (has_w) pw[c].template settle<SHORT>((c * LPR + l) * P::N, n);
+        if (has_b) pb[c].template settle<SHORT>((c * LPR + l) * P::N, n);
+    }
+    for (; m < a.M; m += step) {
         P px[C];
-        float s[1] = {0.f};
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            px[c].load(x, (c * LPR + l) * P::N, n);
+            px[c] = next[c];
+            px[c].template settle<SHORT>((c * LPR + l) * P::N, n);
+        }
+        if (m + step < a.M) {  // the next row is on its way during this one's sums
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+                next[c].template fetch<SHORT>(static_cast<const T*>(a.x) + (m + step) * a.ldx, (c * LPR + l) * P::N, n);
+        }
+        float s[1] = {0.f};
+#pragma unroll
+        for (int c = 0; c < C; ++c)
 #pragma unroll
             for (int e = 0; e < P::N; ++e) s[0] += px[c][e];
-        }
         row_sums<LPR>(s, red[0]);
         const float mean = s[0] / (float)n;  // a row of equal values has them for its mean, where their sum is exact
         float q[1] = {0.f};
@@ -81,11 +107,11 @@ __global__ __launch_bounds__((NormCfg<T, LPR, C>::NT)) void layer_norm_fwd(NormA
         for (int c = 0; c < C; ++c)
 #pragma unroll
             for (int e = 0; e < P::N; ++e) {
-                const float d = px[c][e] - mean;
-                if ((c * LPR + l) * P::N + e < n) q[0] = __builtin_fmaf(d, d, q[0]);
+                const float d = (c * LPR + l) * P::N + e < n ? px[c][e] - mean : 0.f;
+                q[0] = __builtin_fmaf(d, d, q[0]);
             }
         row_sums<LPR>(q, red[1]);
-        const float rstd = 1.f / sqrtf(q[0] * inv + a.eps);
+        const float rstd = 1.f / sqrtf(q[0] / (float)n + a.eps);
         if (l == 0 && a.mean) {
             a.mean[m] = mean;
             a.rstd[m] = rstd;
@@ -93,76 +119,97 @@ __global__ __launch_bounds__((NormCfg<T, LPR, C>::NT)) void layer_norm_fwd(NormA
         T* y = static_cast<T*>(a.y) + m * a.ldy;
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            const int col = (c * LPR + l) * P::N;
-            if (col >= n) break;
-            P pw, pb, py;
-            if (w) pw.load(w, col, n);
-            if (b) pb.load(b, col, n);
+            P py;
 #pragma unroll
             for (int e = 0; e < P::N; ++e) {
                 const float xh = (px[c][e] - mean) * rstd;
-                py.set(e, __builtin_fmaf(xh, w ? pw[e] : 1.f, b ? pb[e] : 0.f));
+                py.set(e, __builtin_fmaf(xh, has_w ? pw[c][e] : 1.f, has_b ? pb[c][e] : 0.f));
             }
-            py.store(y, col, n);
+            py.store(y, (c * LPR + l) * P::N, n);
         }
     }
 }
 
-template <typename T, int LPR, int C>
+template <typename T, int LPR, int C, bool SHORT>
 __global__ __launch_bounds__((NormCfg<T, LPR, C>::NT)) void layer_norm_bwd(NormArgs a) {
     using Cfg = NormCfg<T, LPR, C>;
     using P = Pack<T>;
     constexpr int V = P::N;
+    extern __shared__ __attribute__((aligned(16))) float wide[];  // kLdsSums: [2][CAP]
     __shared__ float red[2][32];
     __shared__ float cols[Cfg::SLOTS > 1 ? Cfg::SLOTS * Cfg::CAP : 1];
     const int slot = threadIdx.x / LPR, l = threadIdx.x % LPR, n = a.N;
-    const float inv = 1.f / (float)n;
-    const T* w = static_cast<const T*>(a.w);
+    const bool has_w = a.w != nullptr;
     float sw[C][V], sb[C][V];
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
-        for (int e = 0; e < V; ++e) sw[c][e] = sb[c][e] = 0.f;
+        for (int e = 0; e < V; ++e) {
+            if constexpr (Cfg::kLdsSums) wide[(c * LPR + l) * V + e] = wide[Cfg::CAP + (c * LPR + l) * V + e] = 0.f;
+            else sw[c][e] = sb[c][e] = 0.f;
+        }
     int turn = 0;
-    for (int64_t m = (int64_t)blockIdx.x * Cfg::SLOTS + slot; m < a.M; m += (int64_t)gridDim.x * Cfg::SLOTS) {
-        const T* x = static_cast<const T*>(a.x) + m * a.ldx;
-        const T* dy = static_cast<const T*>(a.dy) + m * a.lddy;
-        const float mean = a.mean[m], rstd = a.rstd[m];
+    const int64_t step = (int64_t)gridDim.x * Cfg::SLOTS;
+    int64_t m = (int64_t)blockIdx.x * Cfg::SLOTS + slot;
+    P pw[C], nx[C], nd[C];
+    float nmean, nrstd;
+    const auto fetch = [&](int64_t row) __attribute__((always_inline)) {
+        nmean = a.mean[row], nrstd = a.rstd[row];
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            nx[c].template fetch<SHORT>(static_cast<const T*>(a.x) + row * a.ldx, (c * LPR + l) * V, n);
+            nd[c].template fetch<SHORT>(static_cast<const T*>(a.dy) + row * a.lddy, (c * LPR + l) * V, n);
+        }
+    };
+    if (m < a.M) fetch(m);
+    if (has_w) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            pw[c].template fetch<SHORT>(static_cast<const T*>(a.w), (c * LPR + l) * V, n);
+            pw[c].template settle<SHORT>((c * LPR + l) * V, n);
+        }
+    }
+    for (; m < a.M; m += step) {
+        const float mean = nmean, rstd = nrstd;
         P px[C], pd[C];
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            px[c].load(x, (c * LPR + l) * V, n);
-            pd[c].load(dy, (c * LPR + l) * V, n);
+            px[c] = nx[c], pd[c] = nd[c];
+            px[c].template settle<SHORT>((c * LPR + l) * V, n);
+            pd[c].template settle<SHORT>((c * LPR + l) * V, n);
         }
-        P pw[C];
+        if (m + step < a.M) fetch(m + step);  // the next row is on its way during this one's sums
         float s[2] = {0.f, 0.f};  // sums of g and of g xh
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            if (w) pw[c].load(w, (c * LPR + l) * V, n);
+            float* const lw = wide + (c * LPR + l) * V;
 #pragma unroll
             for (int e = 0; e < V; ++e) {  // past the row's end dy is 0, and so are both terms
-                const float xh = (px[c][e] - mean) * rstd, d = pd[c][e], g = w ? d * pw[c][e] : d;
+                const float xh = (px[c][e] - mean) * rstd, d = pd[c][e], g = has_w ? d * pw[c][e] : d;
                 s[0] += g;
                 s[1] = __builtin_fmaf(g, xh, s[1]);
-                sw[c][e] = __builtin_fmaf(d, xh, sw[c][e]);
-                sb[c][e] += d;
+                if constexpr (Cfg::kLdsSums) {
+                    lw[e] = __builtin_fmaf(d, xh, lw[e]);
+                    lw[Cfg::CAP + e] += d;
+                } else {
+                    sw[c][e] = __builtin_fmaf(d, xh, sw[c][e]);
+                    sb[c][e] += d;
+                }
             }
         }
         row_sums<LPR>(s, red[turn]);
         turn ^= 1;
-        const float c1 = s[0] * inv, c2 = s[1] * inv;
+        const float c1 = s[0] / (float)n, c2 = s[1] / (float)n;
         T* dx = static_cast<T*>(a.dx) + m * a.lddx;
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            const int col = (c * LPR + l) * V;
-            if (col >= n) break;
             P po;
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                const float xh = (px[c][e] - mean) * rstd, g = w ? pd[c][e] * pw[c][e] : pd[c][e];
+                const float xh = (px[c][e] - mean) * rstd, g = has_w ? pd[c][e] * pw[c][e] : pd[c][e];
                 po.set(e, rstd * (g - c1 - xh * c2));
             }
-            po.store(dx, col, n);
+            po.store(dx, (c * LPR + l) * V, n);
         }
     }
     if (!a.part) return;
@@ -177,7 +224,7 @@ __global__ __launch_bounds__((NormCfg<T, LPR, C>::NT)) void layer_norm_bwd(NormA
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
                     const int col = (c * LPR + l) * V + e;
-                    if (col < n) part[k * n + col] = v[c][e];
+                    if (col < n) part[k * n + col] = Cfg::kLdsSums ? wide[k * Cfg::CAP + col] : v[c][e];
                 }
         } else {
             __syncthreads();
@@ -197,39 +244,46 @@ __global__ __launch_bounds__((NormCfg<T, LPR, C>::NT)) void layer_norm_bwd(NormA
 }
 
 // lanes and chunks of a row of N values
-template <typename T, template <typename, int, int> class F>
+template <typename T, template <typename, int, int, bool> class F>
 hipError_t for_width(int N, const NormArgs& a, hipStream_t s) {
     constexpr int V = Pack<T>::N;
-    if (N <= 16 * V) return F<T, 16, 1>::run(a, s);  // (layer_norm_slots has the same limits)
-    if (N <= 64 * V) return F<T, 64, 1>::run(a, s);
-    if (N <= 128 * V) return F<T, 64, 2>::run(a, s);
-    if (N <= 256 * V) return F<T, 256, 1>::run(a, s);
-    if (N <= 512 * V) return F<T, 256, 2>::run(a, s);
+    if (N < V) return F<T, 16, 1, true>::run(a, s);
+    if (N <= 16 * V) return F<T, 16, 1, false>::run(a, s);  // (layer_norm_slots has the same limits)
+    if (N <= 64 * V) return F<T, 64, 1, false>::run(a, s);
+    if (N <= 128 * V) return F<T, 64, 2, false>::run(a, s);
+    if (N <= 256 * V) return F<T, 256, 1, false>::run(a, s);
+    if (N <= 512 * V) return F<T, 256, 2, false>::run(a, s);
     if constexpr (V == 4) {
-        if (N <= 1024 * V) return F<T, 256, 4>::run(a, s);
-        if (N <= 2048 * V) return F<T, 1024, 2>::run(a, s);
-        return F<T, 1024, 4>::run(a, s);
+        if (N <= 1024 * V) return F<T, 256, 4, false>::run(a, s);
+        if (N <= 2048 * V) return F<T, 1024, 2, false>::run(a, s);
+        return F<T, 1024, 4, false>::run(a, s);
     } else {
-        if (N <= 1024 * V) return F<T, 1024, 1>::run(a, s);
-        return F<T, 1024, 2>::run(a, s);
+        if (N <= 1024 * V) return F<T, 1024, 1, false>::run(a, s);
+        return F<T, 1024, 2, false>::run(a, s);
     }
 }
 
-template <typename T, int LPR, int C>
+template <typename T, int LPR, int C, bool SHORT>
 struct RunFwd {
     static hipError_t run(const NormArgs& a, hipStream_t s) {
         using Cfg = NormCfg<T, LPR, C>;
-        const int64_t wgs = (a.M + Cfg::SLOTS - 1) / Cfg::SLOTS;
-        hipLaunchKernelGGL((layer_norm_fwd<T, LPR, C>), dim3((unsigned)(wgs < (1 << 20) ? wgs : 1 << 20)), dim3(Cfg::NT), 0, s, a);
+        const int64_t wgs = (a.M + Cfg::SLOTS - 1) / Cfg::SLOTS, most = 256 * 2048 / Cfg::NT;
+        hipLaunchKernelGGL((layer_norm_fwd<T, LPR, C, SHORT>), dim3((unsigned)(wgs < most ? wgs : most)), dim3(Cfg::NT), 0, s, a);
         return hipGetLastError();
     }
 };
 
-template <typename T, int LPR, int C>
+template <typename T, int LPR, int C, bool SHORT>
 struct RunBwd {
     static hipError_t run(const NormArgs& a, hipStream_t s) {
         using Cfg = NormCfg<T, LPR, C>;
-        hipLaunchKernelGGL((layer_norm_bwd<T, LPR, C>), dim3((unsigned)a.groups), dim3(Cfg::NT), 0, s, a);
+        constexpr auto kernel = &layer_norm_bwd<T, LPR, C, SHORT>;
+        constexpr int lds = Cfg::kLdsSums ? 2 * Cfg::CAP * 4 : 0;
+        if constexpr (lds > 0) {
+            const hipError_t once = ensure_dynamic_lds<kernel>(lds);
+            if (once != hipSuccess) return once;
+        }
+        hipLaunchKernelGGL(kernel, dim3((unsigned)a.groups), dim3(Cfg::NT), lds, s, a);
         return hipGetLastError();
     }
 };
@@ -240,6 +294,8 @@ int layer_norm_slots(int f32, int N) {
     const int v = f32 ? Pack<float>::N : Pack<bf16>::N;
     return N <= 16 * v ? 16 : N <= 128 * v ? 4 : 1;
 }
+
+bool layer_norm_wide(int f32, int N) { return N > (f32 ? 1024 * Pack<float>::N : 512 * Pack<bf16>::N); }
 
 hipError_t launch_layer_norm_fwd(int f32, const NormArgs& a, hipStream_t s) {
     return f32 ? for_width<float, RunFwd>(a.N, a, s) : for_width<bf16, RunFwd>(a.N, a, s);

@@ -15,13 +15,35 @@ struct Pack {
         T v[N];
     };
     Raw raw;
-    // elements col .. of a row of n at `row`; those past its end read as zeros
-    FBL_DEV void load(const T* row, int col, int n) {
-        if (col + N <= n) {
-            raw = *reinterpret_cast<const Raw*>(row + col);
-        } else {
+    // Elements col .. of a row of n at `row`, those past its end zeros, in two steps: fetch has no branch
+    // and waits for nothing, so that several can be on the way, and settle puts the chunk right that would cross the
+    // row's end (fetch reads it from where it fits).  Rows shorter than a chunk: SHORT, read one by one.
+    template <bool SHORT = false>
+    FBL_DEV void fetch(const T* row, int col, int n) {
+        if constexpr (SHORT) {
 #pragma unroll
             for (int e = 0; e < N; ++e) raw.v[e] = col + e < n ? row[col + e] : (T)0.f;
+        } else {
+            raw = *reinterpret_cast<const Raw*>(row + (col < n - N ? col : n - N));
+        }
+    }
+    template <bool SHORT = false>
+    FBL_DEV void settle(int col, int n) {
+        if constexpr (!SHORT) {
+            const int past = col - (n - N);  // elements of the chunk beyond the row
+            if (past > 0) {
+                unsigned __int128 x = __builtin_bit_cast(unsigned __int128, raw);
+                x = past < N ? x >> (past * 8 * (int)sizeof(T)) : 0;
+                raw = __builtin_bit_cast(Raw, x);
+            }
+        }
+    }
+    FBL_DEV void load(const T* row, int col, int n) {
+        if (n < N) {
+            fetch<true>(row, col, n);
+        } else {
+            fetch(row, col, n);
+            settle(col, n);
         }
     }
     FBL_DEV void store(T* row, int col, int n) const {

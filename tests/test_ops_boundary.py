@@ -70,7 +70,7 @@ def test_layer_norm_workspace():
     assert f(9, 4, 64, ctypes.byref(n)) == F.FBL_ERR_DTYPE
     assert f(F32, 0, 64, ctypes.byref(n)) == F.FBL_ERR_SHAPE
     assert f(F32, 4, 16385, ctypes.byref(n)) == F.FBL_ERR_UNSUPPORTED
-    assert f(BF16, 1 << 30, 16384, ctypes.byref(n)) == F.FBL_OK and n.value == 512 * 2 * 16384 * 4
+    assert f(BF16, 1 << 30, 16384, ctypes.byref(n)) == F.FBL_OK and n.value == 256 * 2 * 16384 * 4
 
 
 def test_layer_norm_binding_refuses_host_tensors():
