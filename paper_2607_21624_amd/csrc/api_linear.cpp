@@ -56,7 +56,7 @@ LinearWs linear_ws(int f32, int64_t M, int64_t N) {
 // 8192 11.3 and 12.1, 1024 x 4096 6.8 and 8.9; 64 tokens 4096 x 4096 20.1 and 15.1, 128 tokens 22.7 and 25.0, but
 // 8192 x 2048 33.6 and 25.4; fp32, 12 tokens 4096 x 4096 38 and 23, 1024 x 1024 11.6 and 7.7, 96 tokens 60 and 52).
 int few_splits(int f32, int64_t M, int64_t K, int64_t N) {
-    return (f32 ? M <= 128 && K >= 1024 : M <= 64 ? K > 2048 : M <= 128 && K >= 8192) ? fbl::sum_splits(f32, M, N, K) : 1;
+    return (f32 ? M <= 128 && K >= 1024 : M <= 64 ? K > 2048 : M <= 128 && K >= 8192) ? fbl::sum_splits(f32, 0, M, N, K, 0) : 1;
 }
 // The tile of a bf16 forward that is not shared.  Up to 32 tokens and 8192 columns that is 32 x 32 on four
 // wavefronts, whose many workgroups have the most loads on the way (1 token, 2048 x 8192: 11.3 us, 16.9 with the

@@ -294,7 +294,8 @@ hipError_t launch_head(int f32, int table, HeadArgs& p, hipStream_t s) {
 }
 
 // The tile of a split product: as narrow as the few rows that split one.
-int split_tile(int64_t M) { return M <= 32 ? 15 : M <= 64 ? 6 : 4; }
+constexpr int kSplitTileLarge = 19;
+int split_tile(int64_t M) { return M <= 32 ? 15 : M <= 64 ? 6 : M <= 128 ? 4 : kSplitTileLarge; }
 constexpr int kSplitTileF32 = 4;
 
 }  // namespace
@@ -315,8 +316,16 @@ hipError_t launch_head_grad(int f32, int table, HeadArgs p, hipStream_t s) { ret
 
 // Products of few rows have few tiles for a long contraction (dX over a vocabulary, a layer's forward for a few
 // tokens): where they do not fill the card, workgroups share them, two a CU in all with a contraction
-// of 512 at least (fp32: four a CU of its small tiles, 256).
-int sum_splits(int f32, int64_t M, int64_t N, int64_t kc) {
+// of 512 at least (fp32: four a CU of its small tiles, 256).  From 129 rows bf16 shares a contraction only where that
+// lets 256 x 256 tiles fill the card in place of smaller ones and the model has it 5% below, the planes' 8 bytes
+// at 4.5 TB/s included (2048 x 2048 from pieces of 32768 in four shares: 270 -> 245 us; 4096 x 1024 from 16384: 160 -> 143).
+int sum_splits(int f32, int b_nmajor, int64_t M, int64_t N, int64_t kc, int tile) {
+    if (!f32 && M > 128) {
+        const int64_t tiles = ((M + 255) / 256) * ((N + 255) / 256), s = 256 / tiles;
+        if (s < 2 || s > 8 || kc / s < 2048) return 1;
+        const double shared = gemm_cost(kSplitTileLarge, b_nmajor, M * s, N, kc / s) + 8.0 * (double)(s * M * N) / 4.5e6;
+        return shared < 0.95 * gemm_cost(tile, b_nmajor, M, N, kc) ? (int)s : 1;
+    }
     const int t = split_tile(M), bm = f32 ? kF32Tiles[kSplitTileF32].bm : kGemmTiles[t].bm,
               bn = f32 ? kF32Tiles[kSplitTileF32].bn : kGemmTiles[t].bn;
     const int64_t tiles = ((M + bm - 1) / bm) * ((N + bn - 1) / bn);
@@ -332,7 +341,8 @@ hipError_t launch_sum_gemm(int a_kmajor, int b_nmajor, int tile, const SumArgs& 
             switch (split_tile(p.M)) {
                 case 15: return launch_gemm_bf16<15, false, BT, SumPieces<true>>(p, s, p.splits);
                 case 6: return launch_gemm_bf16<6, false, BT, SumPieces<true>>(p, s, p.splits);
-                default: return launch_gemm_bf16<4, false, BT, SumPieces<true>>(p, s, p.splits);
+                case 4: return launch_gemm_bf16<4, false, BT, SumPieces<true>>(p, s, p.splits);
+                default: return launch_gemm_bf16<kSplitTileLarge, false, BT, SumPieces<true>>(p, s, p.splits);
             }
         };
         return b_nmajor ? run(std::true_type{}) : run(std::false_type{});

@@ -128,8 +128,8 @@ hipError_t launch_head_grad(int f32, int table, HeadArgs p, hipStream_t stream);
 // bf16 with `tile` of kGemmTiles where it is not split.
 hipError_t launch_sum_gemm(int a_kmajor, int b_nmajor, int tile, const SumArgs& p, hipStream_t stream);
 hipError_t launch_sum_gemm_f32(int b_nmajor, const SumArgs& p, hipStream_t stream);
-// Workgroups that should share the contraction of an M x N product's tiles.
-int sum_splits(int f32, int64_t M, int64_t N, int64_t kc);
+// Workgroups that should share the contraction kc of an M x N product's tiles, which alone would run with `tile` (bf16).
+int sum_splits(int f32, int b_nmajor, int64_t M, int64_t N, int64_t kc, int tile);
 // C [M][ldc] = scale * the sum of the planes [splits][M][N] (scale nullptr: 1).
 hipError_t launch_sum_planes(int f32, const float* planes, int splits, int64_t M, int64_t N, const float* scale, void* c,
                              int64_t ldc, hipStream_t stream);
