@@ -1265,6 +1265,13 @@ int fbl::proj_auto_tile(uint32_t op, int64_t M, int64_t K, int64_t N) {
     return default_tile(pl);
 }
 
+int fbl::weight_tile(int64_t M, int64_t K, int64_t N) {
+    const int t = proj_auto_tile(FBL_PROJ_BWD_WEIGHT, M, K, N);
+    // written by rows, 8 wavefronts are ahead of the 4 that lead the plain products' order (2048 x 8192 from
+    // 4096: 120 and 127 us)
+    return t == 18 && tuned_tile(FBL_PROJ_BWD_WEIGHT, M, K, N) < 0 ? 19 : t;
+}
+
 extern "C" {
 
 int32_t fbl_gemm_tile_count(void) { return fbl::kGemmTileCount; }

@@ -306,7 +306,7 @@ fbl_status head_bwd(const Shape& s, const float* dloss, int64_t dloss_stride, co
             fbl::product(q, FBL_PROJ_BWD_WEIGHT, s.table() ? dz : vx, s.table() ? vx : dz, dwp, s.M, rows, cols);
             q.scale = scale, q.first = q.last = q.splits = 1;
             e = s.f32() ? fbl::launch_proj_gemm_f32(1, 0, q, hs)
-                        : fbl::launch_sum_gemm(1, 0, fbl::proj_auto_tile(FBL_PROJ_BWD_WEIGHT, s.M, rows, cols), q, hs);
+                        : fbl::launch_sum_gemm(1, 0, fbl::weight_tile(s.M, rows, cols), q, hs);
         }
     }
     return e == hipSuccess ? FBL_OK : FBL_ERR_HIP;

@@ -193,18 +193,13 @@ fbl_status fbl_linear_bwd(int32_t dtype, uint32_t act, int64_t M, int64_t K, int
         fbl::LinearArgs p{};
         fbl::product(p, FBL_PROJ_BWD_DATA, g, vw, vdx, M, K, N);
         const int tile = f32 ? 0 : fbl::proj_auto_tile(FBL_PROJ_BWD_DATA, M, K, N);
-        if (has_xact) {
-            p.z = const_cast<void*>(xz), p.ldz = ldxz, p.z_bytes = fbl::load_span(vxz);
-            e = run_linear_gemm(f32, (int)xact, 1, tile, p, s);
-        } else {
-            e = f32 ? fbl::launch_proj_gemm_f32(0, 1, p, s) : fbl::launch_proj_gemm(0, 1, tile, p, s);
-        }
+        if (has_xact) p.z = const_cast<void*>(xz), p.ldz = ldxz, p.z_bytes = fbl::load_span(vxz);
+        e = run_linear_gemm(f32, has_xact ? (int)xact : FBL_ACT_NONE, 1, tile, p, s);
     }
     if (e == hipSuccess && dw) {
-        fbl::GemmArgs p{};
+        fbl::LinearArgs p{};
         fbl::product(p, FBL_PROJ_BWD_WEIGHT, vx, g, vdw, M, K, N);
-        e = f32 ? fbl::launch_proj_gemm_f32(1, 0, p, s)
-                : fbl::launch_proj_gemm(1, 0, fbl::proj_auto_tile(FBL_PROJ_BWD_WEIGHT, M, K, N), p, s);
+        e = f32 ? fbl::launch_proj_gemm_f32(1, 0, p, s) : fbl::launch_weight_gemm(fbl::weight_tile(M, K, N), p, s);
     }
     return e == hipSuccess ? FBL_OK : FBL_ERR_HIP;
 }

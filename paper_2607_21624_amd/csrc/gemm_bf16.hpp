@@ -367,22 +367,28 @@ proj_gemm_bf16(typename EP::Args p) {
     }
 }
 
-// A wavefront's accumulators by rows: f(m, n, v) gets 8 consecutive columns n .. n+7 of row m,
-// neighbouring lanes the next 8, so that whole 128-byte lines are loaded and stored beside them.  (As they
+// A wavefront's accumulators by rows: f(m, n, v, d) gets 8 consecutive columns n .. n+7 of row m and what
+// d = ahead(m, n) has loaded for them, neighbouring lanes the next 8, so that whole 128-byte lines are loaded and stored beside them.  (As they
 // stand a lane has 4 columns of a row and the lanes 32 rows: a layer that writes y and z that
 // way and reads a residual spends as long on it as on a contraction of 1500.  4096 x 8192 from 2048,
 // GELU: 208 us, 140 through here.)  Each 32 rows go through LDS, 32 x (32 TN + 4) floats of
-// the wavefront's own; the pitch puts 16 rows' writes on different banks.
-template <typename C, typename F>
-FBL_DEV void by_rows(uint32_t lds, const f32x16 (&acc)[C::TN][C::TM], int m0, int n0, int wm, int wn, F&& f) {
+// the wavefront's own; the pitch puts 16 rows' writes on different banks.  The loads beside 32 rows
+// are all issued before the first store (no load is moved over a store to what might be the same memory).
+struct Nothing {};
+template <typename C, typename A, typename F>
+FBL_DEV void by_rows(uint32_t lds, const f32x16 (&acc)[C::TN][C::TM], int m0, int n0, int wm, int wn, A&& ahead, F&& f) {
     constexpr int PITCH = 32 * C::TN + 4, LANES = 4 * C::TN, ROWS = 64 / LANES;  // lanes a row, rows a turn
     const int lane = threadIdx.x & 63, g = lane >> 5;
     const uint32_t mine = lds + (uint32_t)((wn * C::WM + wm) * 32 * PITCH * 4);
     const uint32_t put = mine + (uint32_t)(((lane & 31) * PITCH + 4 * g) * 4);
     const uint32_t get = mine + (uint32_t)((lane / LANES * PITCH + lane % LANES * 8) * 4);
     __syncthreads();  // the stages have been read
+    const int nl = n0 + wn * C::TN * 32 + lane % LANES * 8, ml = m0 + wm * C::TM * 32 + lane / LANES;
 #pragma unroll
     for (int tm = 0; tm < C::TM; ++tm) {
+        decltype(ahead(0, 0)) beside[32 / ROWS];
+#pragma unroll
+        for (int i = 0; i < 32 / ROWS; ++i) beside[i] = ahead(ml + 32 * tm + i * ROWS, nl);
 #pragma unroll
         for (int tn = 0; tn < C::TN; ++tn)
 #pragma unroll
@@ -399,7 +405,7 @@ FBL_DEV void by_rows(uint32_t lds, const f32x16 (&acc)[C::TN][C::TM], int m0, in
             float v[8];
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] = a[e], v[4 + e] = b[e];
-            f(m0 + (wm * C::TM + tm) * 32 + i * ROWS + lane / LANES, n0 + wn * C::TN * 32 + lane % LANES * 8, v);
+            f(ml + 32 * tm + i * ROWS, nl, v, beside[i]);
         }
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();

@@ -174,7 +174,8 @@ struct HeadGrad {
     static FBL_DEV void done(const Args& p, uint32_t lds, f32x16 (&acc)[C::TN][C::TM], int m0, int n0, int wm, int wn) {
         head_dz(p, acc, n0 + wn * C::TN * 32, m0 + wm * C::TM * 32);
         const __amdgpu_buffer_rsrc_t rz = span(p.dz, p.dz_bytes);
-        by_rows<C>(lds, acc, m0, n0, wm, wn, [&](int m, int n, float (&v)[8]) __attribute__((always_inline)) {
+        const auto nothing = [](int, int) __attribute__((always_inline)) { return Nothing{}; };
+        by_rows<C>(lds, acc, m0, n0, wm, wn, nothing, [&](int m, int n, float (&v)[8], Nothing) __attribute__((always_inline)) {
             const bool in = m < p.tokens && n < p.ldz;
             store8(rz, in ? (uint32_t)(((int64_t)m * p.ldz + n) * 2) : kNowhere, v, n, (int)p.ldz);
         });
@@ -217,17 +218,25 @@ struct SumPieces {
         const float scale = last ? *p.scale : 1.f;
         const __amdgpu_buffer_rsrc_t rc = span(p.c, p.c_bytes),
                                      rs = span(SPLIT ? p.sum + (int64_t)blockIdx.y * p.M * p.lds : p.sum, p.sum_bytes);
-        by_rows<C>(lds, acc, m0, n0, wm, wn, [&](int m, int n, float (&v)[8]) __attribute__((always_inline)) {
+        struct Sums {
+            f32x4 h[2];
+        };
+        const auto offset = [&](int m, int n) __attribute__((always_inline)) {
+            return m < p.M && n < p.N ? (uint32_t)(((int64_t)m * p.lds + n) * 4) : kNowhere;
+        };
+        const auto ahead = [&](int m, int n) __attribute__((always_inline)) {
+            Sums s;
+            const uint32_t off = p.first ? kNowhere : offset(m, n);
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                s.h[h] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, off, 16 * h, 0));
+            return s;
+        };
+        by_rows<C>(lds, acc, m0, n0, wm, wn, ahead, [&](int m, int n, float (&v)[8], const Sums& s) __attribute__((always_inline)) {
             const bool in = m < p.M && n < p.N;
-            const uint32_t soff = in ? (uint32_t)(((int64_t)m * p.lds + n) * 4) : kNowhere;
-            if (!p.first) {
+            const uint32_t soff = offset(m, n);
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const f32x4 s = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, soff, 16 * h, 0));
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) v[4 * h + e] += s[e];
-                }
-            }
+            for (int e = 0; e < 8; ++e) v[e] += s.h[e / 4][e % 4];  // 0 with the first piece
             if (last) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] *= scale;

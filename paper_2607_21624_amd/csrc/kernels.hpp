@@ -111,6 +111,7 @@ hipError_t launch_column_sums(int f32, const float* part, int groups, int K, int
 // `grad` the data gradient times act'.  bf16 with `tile` of kGemmTiles; fp32 with its own choice.
 template <int ACT>
 hipError_t launch_linear_gemm(int grad, int tile, const LinearArgs& p, hipStream_t stream);
+hipError_t launch_weight_gemm(int tile, const LinearArgs& p, hipStream_t stream);  // A stored k-major, no epilogue
 template <int ACT>
 hipError_t launch_linear_gemm_f32(int grad, const LinearArgs& p, hipStream_t stream);
 // y and z of a forward product from its planes (launch_sum_gemm), for few rows (linear_finish.hip).
@@ -139,6 +140,8 @@ hipError_t launch_head_grad_rows(const HeadRowArgs& a, hipStream_t stream);     
 
 // The tile of kGemmTiles that FBL_GEMM_TILE_AUTO names for a projection product (api.cpp).
 int proj_auto_tile(uint32_t op, int64_t M, int64_t K, int64_t N);
+// The same for a weight gradient whose tiles are written by rows.
+int weight_tile(int64_t M, int64_t K, int64_t N);
 
 // Diagnostic: offsets of a token-major tensor computed by the device index map.
 hipError_t launch_layout_map(const TokMap& m, int B, int H, int S, int D, int64_t* out, hipStream_t stream);

@@ -36,29 +36,38 @@ struct LinearEp {
 #pragma unroll
             for (int e = 0; e < 8; ++e) b[e] = (float)x[e];
         }
-        by_rows<C>(lds, acc, m0, n0, wm, wn, [&](int m, int n, float (&v)[8]) __attribute__((always_inline)) {
-            const bool in = m < p.M && n < p.N;
-            const uint32_t off = in ? (uint32_t)(((int64_t)m * p.ldc + n) * 2) : kNowhere;
-            const uint32_t zoff = in ? (uint32_t)(((int64_t)m * p.ldz + n) * 2) : kNowhere;
-            if constexpr (GRAD) {
-                const bf16x8 z = load8(rz, zoff);
+        const auto offset = [&](int m, int n, int64_t ld) __attribute__((always_inline)) {
+            return m < p.M && n < p.N ? (uint32_t)(((int64_t)m * ld + n) * 2) : kNowhere;
+        };
+        const auto rows = [&](auto&& ahead, auto&& beside) __attribute__((always_inline)) {
+            by_rows<C>(lds, acc, m0, n0, wm, wn, ahead, [&](int m, int n, float (&v)[8], const auto& x) __attribute__((always_inline)) {
+                if constexpr (!GRAD) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] *= act_grad<ACT, true>((float)z[e]);
-            } else {
-                bf16x8 x;
-                if (has_res) x = load8(rr, in ? (uint32_t)(((int64_t)m * p.ldr + n) * 2) : kNowhere);
+                    for (int e = 0; e < 8; ++e) v[e] += b[e];
+                    if (has_z) store8(rz, offset(m, n, p.ldz), v, n, p.N);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] += b[e];
-                if (has_z) store8(rz, zoff, v, n, p.N);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = act<ACT, true>(v[e]);
-                if (has_res) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] += (float)x[e];
+                    for (int e = 0; e < 8; ++e) v[e] = act<ACT, true>(v[e]);
                 }
-            }
-            store8(rc, off, v, n, p.N);
-        });
+                beside(v, x);
+                store8(rc, offset(m, n, p.ldc), v, n, p.N);
+            });
+        };
+        if constexpr (GRAD && ACT != kActNone) {
+            rows([&](int m, int n) __attribute__((always_inline)) { return load8(rz, offset(m, n, p.ldz)); },
+                 [](float (&v)[8], const bf16x8& z) __attribute__((always_inline)) {
+#pragma unroll
+                     for (int e = 0; e < 8; ++e) v[e] *= act_grad<ACT, true>((float)z[e]);
+                 });
+        } else if (!GRAD && has_res) {
+            rows([&](int m, int n) __attribute__((always_inline)) { return load8(rr, offset(m, n, p.ldr)); },
+                 [](float (&v)[8], const bf16x8& x) __attribute__((always_inline)) {
+#pragma unroll
+                     for (int e = 0; e < 8; ++e) v[e] += (float)x[e];
+                 });
+        } else {
+            rows([](int, int) __attribute__((always_inline)) { return Nothing{}; },
+                 [](float (&)[8], Nothing) __attribute__((always_inline)) {});
+        }
     }
 
     // fp32: 32 consecutive columns of a row across the lanes of a half
@@ -76,24 +85,30 @@ struct LinearEp {
             const int n = n0 + (wn * C::TN + tn) * 32 + (lane & 31);
             const float b = GRAD ? 0.f : load(rb, n < p.N ? (uint32_t)n * 4 : kNowhere);
 #pragma unroll
-            for (int tm = 0; tm < C::TM; ++tm)
+            for (int tm = 0; tm < C::TM; ++tm) {
+                const auto offset = [&](int r, int64_t ld) __attribute__((always_inline)) {
+                    const int m = m0 + (wm * C::TM + tm) * 32 + acc_row(r, g);
+                    return m < p.M && n < p.N ? (uint32_t)(((int64_t)m * ld + n) * 4) : kNowhere;
+                };
+                float x[16];  // z of the layer before, or the residual: all on the way before the first store
+                if (GRAD ? ACT != kActNone : has_res) {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) x[r] = GRAD ? load(rz, offset(r, p.ldz)) : load(rr, offset(r, p.ldr));
+                }
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    const int m = m0 + (wm * C::TM + tm) * 32 + acc_row(r, g);
-                    const bool in = m < p.M && n < p.N;
-                    const uint32_t off = in ? (uint32_t)(((int64_t)m * p.ldc + n) * 4) : kNowhere;
-                    const uint32_t zoff = in ? (uint32_t)(((int64_t)m * p.ldz + n) * 4) : kNowhere;
                     float v = acc[tm][tn][r];
                     if constexpr (GRAD) {
-                        v *= act_grad<ACT, false>(load(rz, zoff));
+                        if constexpr (ACT != kActNone) v *= act_grad<ACT, false>(x[r]);
                     } else {
                         v += b;
-                        if (has_z) __builtin_amdgcn_raw_buffer_store_b32(__float_as_int(v), rz, zoff, 0, 0);
+                        if (has_z) __builtin_amdgcn_raw_buffer_store_b32(__float_as_int(v), rz, offset(r, p.ldz), 0, 0);
                         v = act<ACT, false>(v);
-                        if (has_res) v += load(rr, in ? (uint32_t)(((int64_t)m * p.ldr + n) * 4) : kNowhere);
+                        if (has_res) v += x[r];
                     }
-                    __builtin_amdgcn_raw_buffer_store_b32(__float_as_int(v), rc, off, 0, 0);
+                    __builtin_amdgcn_raw_buffer_store_b32(__float_as_int(v), rc, offset(r, p.ldc), 0, 0);
                 }
+            }
         }
     }
 };
@@ -105,6 +120,13 @@ hipError_t launch_linear_gemm<FBL_ACT>(int grad, int tile, const LinearArgs& p, 
     if (grad) return launch_gemm_tile<false, true, LinearEp<FBL_ACT, true>>(tile, p, stream);
     return launch_gemm_tile<false, false, LinearEp<FBL_ACT, false>>(tile, p, stream);
 }
+
+#if FBL_ACT == 0
+// A weight gradient, its tiles written by rows.
+hipError_t launch_weight_gemm(int tile, const LinearArgs& p, hipStream_t stream) {
+    return launch_gemm_tile<true, false, LinearEp<kActNone, false>>(tile, p, stream);
+}
+#endif
 
 template <>
 hipError_t launch_linear_gemm_f32<FBL_ACT>(int grad, const LinearArgs& p, hipStream_t stream) {
