@@ -39,15 +39,15 @@ ActGrid act_grid(int f32, int64_t M, int64_t N) {
     return {rows, (int)((M + rows - 1) / rows)};
 }
 
-struct LinearWs {
-    size_t part, dz, total;
-};
-LinearWs linear_ws(int f32, int64_t M, int64_t N) {
-    LinearWs w;
-    w.part = align256((size_t)act_grid(f32, M, N).groups * (size_t)N * 4);
-    w.dz = (size_t)M * (size_t)N * (f32 ? 4 : 2);
-    w.total = w.part + w.dz;
-    return w;
+
+// A product of few rows whose contraction `splits` workgroups a tile share, their planes, and what follows it.
+hipError_t run_shared(int f32, int act, int grad, int splits, const fbl::LinearArgs& p, float* planes, hipStream_t s) {
+    fbl::SumArgs q{};
+    static_cast<fbl::GemmArgs&>(q) = p;
+    q.sum = planes, q.lds = p.N, q.sum_bytes = (uint32_t)((int64_t)p.M * p.N * 4);
+    q.first = 1, q.splits = splits, q.share = (int)((((int64_t)p.K + splits - 1) / splits + 63) / 64 * 64);
+    const hipError_t e = f32 ? fbl::launch_sum_gemm_f32(grad, q, s) : fbl::launch_sum_gemm(0, grad, 0, q, s);
+    return e == hipSuccess ? fbl::launch_linear_finish(f32, act, grad, p, planes, splits, s) : e;
 }
 
 // Workgroups that share the contraction of a few tokens' tiles.  A tile alone has too few of w's bytes on the
@@ -55,6 +55,8 @@ LinearWs linear_ws(int f32, int64_t M, int64_t N) {
 // (cold weights, us, alone and shared: bf16, 1 token 4096 x 4096 18.3 and 12.3, 8192 x 2048 31.4 and 12.1, 2048 x
 // 8192 11.3 and 12.1, 1024 x 4096 6.8 and 8.9; 64 tokens 4096 x 4096 20.1 and 15.1, 128 tokens 22.7 and 25.0, but
 // 8192 x 2048 33.6 and 25.4; fp32, 12 tokens 4096 x 4096 38 and 23, 1024 x 1024 11.6 and 7.7, 96 tokens 60 and 52).
+// The data gradient, whose contraction is N, the same (dx, bf16, 1 token 2048 x 8192 25.1 and 11.9, 64 tokens 25.1 and
+// 14.9; fp32, 1 token 57 and 19, 128 tokens 59 and 52, 200 tokens 92 and 89, but 1024 x 1024 9.4 and 12.1).
 int few_splits(int f32, int64_t M, int64_t K, int64_t N) {
     return (f32 ? M <= 128 && K >= 1024 : M <= 64 ? K > 2048 : M <= 128 && K >= 8192) ? fbl::sum_splits(f32, 0, M, N, K, 0) : 1;
 }
@@ -66,6 +68,20 @@ int forward_tile(int64_t M, int64_t K, int64_t N) {
     return fbl::proj_auto_tile(FBL_PROJ_FWD, M, K, N);
 }
 size_t few_ws(int splits, int64_t M, int64_t N) { return splits > 1 ? (size_t)splits * (size_t)M * (size_t)N * 4 : 0; }
+
+// Workspace of the backward: partial sums of the bias' gradient, dz, planes of dx.
+struct LinearWs {
+    size_t dz, planes, total;
+    int splits;
+};
+LinearWs linear_ws(int f32, int64_t M, int64_t K, int64_t N) {
+    LinearWs w;
+    w.splits = few_splits(f32, M, N, K);
+    w.dz = align256((size_t)act_grid(f32, M, N).groups * (size_t)N * 4);
+    w.planes = w.dz + align256((size_t)M * (size_t)N * (f32 ? 4 : 2));
+    w.total = w.planes + few_ws(w.splits, M, K);
+    return w;
+}
 
 fbl_status linear_shape(int32_t dtype, uint32_t act, int64_t M, int64_t K, int64_t N) {
     if (!fbl::dtype_size(dtype)) return FBL_ERR_DTYPE;
@@ -121,12 +137,7 @@ fbl_status fbl_linear_fwd(int32_t dtype, uint32_t act, int64_t M, int64_t K, int
     p.z_bytes = z ? (uint32_t)vz.bytes() : 0;
     const hipStream_t s = static_cast<hipStream_t>(stream);
     if (splits > 1) {
-        fbl::SumArgs q{};
-        static_cast<fbl::GemmArgs&>(q) = p;
-        q.sum = static_cast<float*>(ws), q.lds = N, q.sum_bytes = (uint32_t)(M * N * 4);
-        q.first = 1, q.splits = splits, q.share = (int)(((K + splits - 1) / splits + 63) / 64 * 64);
-        hipError_t e = es == 4 ? fbl::launch_sum_gemm_f32(0, q, s) : fbl::launch_sum_gemm(0, 0, 0, q, s);
-        if (e == hipSuccess) e = fbl::launch_linear_finish(es == 4, (int)act, p, q.sum, splits, s);
+        const hipError_t e = run_shared(es == 4, (int)act, 0, splits, p, static_cast<float*>(ws), s);
         return e == hipSuccess ? FBL_OK : FBL_ERR_HIP;
     }
     if (es == 2 && tile == FBL_GEMM_TILE_AUTO) tile = forward_tile(M, K, N);
@@ -137,7 +148,7 @@ fbl_status fbl_linear_fwd(int32_t dtype, uint32_t act, int64_t M, int64_t K, int
 fbl_status fbl_linear_bwd_workspace(int32_t dtype, int64_t M, int64_t K, int64_t N, size_t* bytes) {
     if (!bytes) return FBL_ERR_NULL;
     const fbl_status st = linear_shape(dtype, FBL_ACT_NONE, M, K, N);
-    if (st == FBL_OK) *bytes = linear_ws(dtype == FBL_F32, M, N).total;
+    if (st == FBL_OK) *bytes = linear_ws(dtype == FBL_F32, M, K, N).total;
     return st;
 }
 
@@ -161,11 +172,11 @@ fbl_status fbl_linear_bwd(int32_t dtype, uint32_t act, int64_t M, int64_t K, int
     if (!vdb.natural()) return FBL_ERR_ALIGN;
     if (es == 2 && ((dx && (N % 8 || K % 4)) || (dw && N % 4))) return FBL_ERR_UNSUPPORTED;
     // what is needed of the workspace: partial sums for the bias, dz where an activation makes it
-    const LinearWs lw = linear_ws(f32, M, N);
-    const bool pass = has_act ? (dx || dw || dbias) : dbias != nullptr;
-    const size_t need = pass ? lw.total : 0;
-    if (pass && (!ws || ws_bytes < need)) return FBL_ERR_WORKSPACE;
-    const RowsView vws{pass ? ws : nullptr, 1, (int64_t)need, (int64_t)need + 1, 1};
+    const LinearWs lw = linear_ws(f32, M, K, N);
+    const bool pass = has_act ? (dx || dw || dbias) : dbias != nullptr, shared = dx && lw.splits > 1 && ws;
+    const size_t need = pass || shared ? lw.total : 0;
+    if (need && (!ws || ws_bytes < need)) return FBL_ERR_WORKSPACE;
+    const RowsView vws{need ? ws : nullptr, 1, (int64_t)need, (int64_t)need + 1, 1};
     if (vws.begin() % 16) return FBL_ERR_ALIGN;
     const RowsView* outs[] = {&vdx, &vdw, &vdb, &vws};
     for (int i = 0; i < 4; ++i) {
@@ -183,7 +194,7 @@ fbl_status fbl_linear_bwd(int32_t dtype, uint32_t act, int64_t M, int64_t K, int
         a.dy = dy, a.z = z, a.lddy = lddy, a.ldz = ldz, a.M = M, a.N = (int)N, a.rows = ag.rows, a.groups = ag.groups;
         a.part = dbias ? static_cast<float*>(ws) : nullptr;
         if (has_act) {
-            g = RowsView{static_cast<char*>(ws) + lw.part, M, N, N, es};
+            g = RowsView{static_cast<char*>(ws) + lw.dz, M, N, N, es};
             a.dz = const_cast<void*>(g.p), a.lddz = N;
         }
         e = fbl::launch_linear_act_bwd(f32, (int)act, a, s);
@@ -194,7 +205,10 @@ fbl_status fbl_linear_bwd(int32_t dtype, uint32_t act, int64_t M, int64_t K, int
         fbl::product(p, FBL_PROJ_BWD_DATA, g, vw, vdx, M, K, N);
         const int tile = f32 ? 0 : fbl::proj_auto_tile(FBL_PROJ_BWD_DATA, M, K, N);
         if (has_xact) p.z = const_cast<void*>(xz), p.ldz = ldxz, p.z_bytes = fbl::load_span(vxz);
-        e = run_linear_gemm(f32, has_xact ? (int)xact : FBL_ACT_NONE, 1, tile, p, s);
+        const int a = has_xact ? (int)xact : FBL_ACT_NONE;
+        e = shared ? run_shared(f32, a, 1, lw.splits, p, reinterpret_cast<float*>(static_cast<char*>(ws) + lw.planes), s)
+            : f32 && !has_xact ? fbl::launch_proj_gemm_f32(0, 1, p, s)
+                   : run_linear_gemm(f32, a, 1, tile, p, s);
     }
     if (e == hipSuccess && dw) {
         fbl::LinearArgs p{};

@@ -114,8 +114,9 @@ hipError_t launch_linear_gemm(int grad, int tile, const LinearArgs& p, hipStream
 hipError_t launch_weight_gemm(int tile, const LinearArgs& p, hipStream_t stream);  // A stored k-major, no epilogue
 template <int ACT>
 hipError_t launch_linear_gemm_f32(int grad, const LinearArgs& p, hipStream_t stream);
-// y and z of a forward product from its planes (launch_sum_gemm), for few rows (linear_finish.hip).
-hipError_t launch_linear_finish(int f32, int act, const LinearArgs& p, const float* planes, int splits, hipStream_t stream);
+// y and z of a forward product, or with `grad` dx of a data gradient, from its planes (launch_sum_gemm), for few rows
+// (linear_finish.hip).
+hipError_t launch_linear_finish(int f32, int act, int grad, const LinearArgs& p, const float* planes, int splits, hipStream_t stream);
 hipError_t launch_linear_act_bwd(int f32, int act, const LinearActArgs& a, hipStream_t stream);
 
 // Softmax losses of a linear head (head_gemm.hip, head_rows.hip); table: the weight is stored

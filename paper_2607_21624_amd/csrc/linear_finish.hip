@@ -1,6 +1,7 @@
 // linear_finish.hip -- a linear layer's forward for a few tokens (serving), gfx950: what
 // follows a product whose contraction several workgroups shared.
 //   z = sum over the shares + bias,  y = act(z) + residual
+// or, of the data gradient,  dx = (sum over the shares) act'(z)
 //
 // Such a layer is bound by reading w once, and its tiles alone have too few bytes on the way for that: the
 // shares (launch_sum_gemm) give every CU two tiles' loads.  This adds their fp32 planes in order, a thread an
@@ -12,7 +13,7 @@ namespace fbl {
 
 namespace {
 
-template <typename T, int ACT>
+template <typename T, int ACT, bool GRAD>
 __global__ __launch_bounds__(256) void linear_finish(LinearArgs p, const float* planes, int splits) {
     const int n = blockIdx.x * 256 + threadIdx.x;
     const int64_t m = blockIdx.y, at = m * p.N + n, plane = (int64_t)p.M * p.N;
@@ -25,6 +26,11 @@ __global__ __launch_bounds__(256) void linear_finish(LinearArgs p, const float* 
         z += a, z += b, z += c, z += d;
     }
     for (; i < splits; ++i) z += planes[i * plane + at];
+    if constexpr (GRAD) {
+        if constexpr (ACT != kActNone) z *= act_grad<ACT, sizeof(T) == 2>((float)static_cast<const T*>(p.z)[m * p.ldz + n]);
+        static_cast<T*>(p.c)[m * p.ldc + n] = (T)z;
+        return;
+    }
     if (p.bias) z += (float)static_cast<const T*>(p.bias)[n];
     if (p.z) static_cast<T*>(p.z)[m * p.ldz + n] = (T)z;
     float y = act<ACT, sizeof(T) == 2>(z);
@@ -32,23 +38,24 @@ __global__ __launch_bounds__(256) void linear_finish(LinearArgs p, const float* 
     static_cast<T*>(p.c)[m * p.ldc + n] = (T)y;
 }
 
-template <typename T>
+template <typename T, bool GRAD>
 hipError_t finish(int act, const LinearArgs& p, const float* planes, int splits, hipStream_t s) {
     const dim3 grid((unsigned)((p.N + 255) / 256), (unsigned)p.M);
     switch (act) {
-        case kActNone: hipLaunchKernelGGL((linear_finish<T, kActNone>), grid, dim3(256), 0, s, p, planes, splits); break;
-        case kActRelu: hipLaunchKernelGGL((linear_finish<T, kActRelu>), grid, dim3(256), 0, s, p, planes, splits); break;
-        case kActGelu: hipLaunchKernelGGL((linear_finish<T, kActGelu>), grid, dim3(256), 0, s, p, planes, splits); break;
-        case kActGeluTanh: hipLaunchKernelGGL((linear_finish<T, kActGeluTanh>), grid, dim3(256), 0, s, p, planes, splits); break;
-        default: hipLaunchKernelGGL((linear_finish<T, kActSilu>), grid, dim3(256), 0, s, p, planes, splits); break;
+        case kActNone: hipLaunchKernelGGL((linear_finish<T, kActNone, GRAD>), grid, dim3(256), 0, s, p, planes, splits); break;
+        case kActRelu: hipLaunchKernelGGL((linear_finish<T, kActRelu, GRAD>), grid, dim3(256), 0, s, p, planes, splits); break;
+        case kActGelu: hipLaunchKernelGGL((linear_finish<T, kActGelu, GRAD>), grid, dim3(256), 0, s, p, planes, splits); break;
+        case kActGeluTanh: hipLaunchKernelGGL((linear_finish<T, kActGeluTanh, GRAD>), grid, dim3(256), 0, s, p, planes, splits); break;
+        default: hipLaunchKernelGGL((linear_finish<T, kActSilu, GRAD>), grid, dim3(256), 0, s, p, planes, splits); break;
     }
     return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_linear_finish(int f32, int act, const LinearArgs& p, const float* planes, int splits, hipStream_t s) {
-    return f32 ? finish<float>(act, p, planes, splits, s) : finish<bf16>(act, p, planes, splits, s);
+hipError_t launch_linear_finish(int f32, int act, int grad, const LinearArgs& p, const float* planes, int splits, hipStream_t s) {
+    if (grad) return f32 ? finish<float, true>(act, p, planes, splits, s) : finish<bf16, true>(act, p, planes, splits, s);
+    return f32 ? finish<float, false>(act, p, planes, splits, s) : finish<bf16, false>(act, p, planes, splits, s);
 }
 
 }  // namespace fbl

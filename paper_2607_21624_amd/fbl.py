@@ -1054,7 +1054,7 @@ def linear_bwd(dy, x, w, z=None, act: str = "none", dx=None, dw=None, dbias=None
     lddw = 0 if dw is None else _matrix(dw, where, "dw", (K, N), x)
     _vector(dbias, where, "dbias", N, x.dtype)
     ws, ws_bytes = None, 0
-    if code != FBL_ACT_NONE or dbias is not None:
+    if code != FBL_ACT_NONE or dbias is not None or workspace is not None or (dx is not None and M <= 128):
         need = 0 if workspace is not None else linear_bwd_workspace(x, w)
         ws, ws_bytes = _scratch(workspace, need, where, x, stream)
     _check(LIB.fbl_linear_bwd(dt, code, M, K, N, _ptr(dy), lddy, _ptr(x), ldx, _ptr(w), ldw, _ptr(z), ldz, xcode, _ptr(x_z),

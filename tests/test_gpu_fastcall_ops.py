@@ -1,0 +1,116 @@
+"""The native call path of layer norm, linear layers and the losses against the general one:
+the same results bit for bit, and None -- the general path -- for every call that is not a
+plain one."""
+import pytest
+import torch
+
+import paper_2607_21624_amd as pkg
+from ops_util import DTYPES, note
+from paper_2607_21624_amd import fbl
+
+pytestmark = pytest.mark.gpu
+
+
+def _t(*shape, dt=torch.bfloat16, scale=1.0):
+    return (torch.randn(*shape, device="cuda") * scale).to(dt)
+
+
+def _same(a, b):
+    if a is None or b is None:
+        return a is b
+    if isinstance(a, tuple):
+        return len(a) == len(b) and all(_same(x, y) for x, y in zip(a, b))
+    return a.dtype == b.dtype and a.stride() == b.stride() and torch.equal(a, b)
+
+
+def _both(monkeypatch, call):
+    """The call natively, and through the general path."""
+    native = fbl._FAST
+    hits = []
+
+    class Spy:
+        def __getattr__(self, name):
+            def f(*args):
+                r = getattr(native, name)(*args)
+                hits.append(r is not None)
+                return r
+            return f
+    no = type("No", (), dict.fromkeys(fbl._NATIVE, staticmethod(lambda *a: None)))
+    monkeypatch.setattr(fbl, "_FAST", Spy())
+    a = call()
+    monkeypatch.setattr(fbl, "_FAST", no)
+    b = call()
+    monkeypatch.setattr(fbl, "_FAST", native)
+    torch.cuda.synchronize()
+    assert hits and all(hits), "the native path did not take a plain call"
+    assert _same(a, b)
+    return a
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_native_equals_general(monkeypatch, dt):
+    dt = DTYPES[dt]
+    g = lambda *s, **k: _t(*s, dt=dt, **k)
+    note(f"native calls {dt}")
+    x, dy, w, b = g(50, 264), g(50, 264), g(264), g(264)
+    for args in ((x,), (x, w), (x, w, b, 1e-6), (x, None, b)):
+        y, mean, rstd = _both(monkeypatch, lambda: pkg.layer_norm_fwd(*args))
+    _both(monkeypatch, lambda: pkg.layer_norm_fwd(x, w, b, out=y, mean=mean, rstd=rstd))
+    for kw in ({}, dict(need_weight=False), dict(need_weight=False, need_bias=False), dict(dx=torch.empty_like(x))):
+        _both(monkeypatch, lambda: pkg.layer_norm_bwd(dy, x, mean, rstd, w, **kw))
+    for M in (1, 50, 300):
+        x, w1, b1, r = g(M, 264), g(264, 128), g(128), g(M, 128)
+        z = torch.empty_like(r)
+        for act in pkg.ACTIVATIONS:
+            _both(monkeypatch, lambda: pkg.linear_fwd(x, w1, b1, act, r, z=z))
+            _both(monkeypatch, lambda: pkg.linear_bwd(r, x, w1, z, act))
+            _both(monkeypatch, lambda: pkg.linear_bwd(r, x, w1, x_act=act, x_z=x, need_bias=False, need_dw=False))
+    _both(monkeypatch, lambda: pkg.linear_fwd(g(4, 4096, scale=0) + 1, g(4096, 128, scale=0) + 1))  # shared contraction
+    one = torch.ones((), device="cuda")
+    for w in (g(64, 200), g(200, 64).t(), g(200, 80)[:, :64].t(), g(64, 208)[:, :200]):
+        x, lab = g(30, 64), torch.arange(30, device="cuda")
+        idx, logits = torch.randint(0, 200, (30, 3), device="cuda"), torch.randn(30, 3, device="cuda")
+        mean = torch.empty((), device="cuda")
+        loss, lse, total = _both(monkeypatch, lambda: pkg.linear_ce_fwd(x, w, lab, mean=mean))
+        for dl, tot in ((one, total), (loss, None), (one.expand(30), None)):
+            _both(monkeypatch, lambda: pkg.linear_ce_bwd(dl, x, w, lab, lse, tot))
+        _both(monkeypatch, lambda: pkg.linear_ce_bwd(one, x, w, lab, lse, total, need_dx=False))
+        loss, lse, prob, total = _both(monkeypatch, lambda: pkg.linear_kd_fwd(x, w, idx, logits, 2.0))
+        _both(monkeypatch, lambda: pkg.linear_kd_bwd(one, x, w, idx, prob, lse, 2.0, total))
+
+
+def test_what_is_not_plain_goes_the_general_way():
+    N = fbl._FAST
+    x, w, b = _t(8, 64), _t(64, 64), _t(64)
+    lab = torch.zeros(8, dtype=torch.int64, device="cuda")
+    s = torch.cuda.Stream()
+    norm = lambda **k: N.layer_norm_fwd(*{**dict(x=x, w=b, b=b, eps=1e-5, out=None, mean=None, rstd=None, stream=None), **k}.values())
+    assert norm() is not None
+    for k in (dict(x=x.cpu()), dict(x=x.float()), dict(w=b[:32]), dict(eps=1), dict(stream=s), dict(out=x[:4]), dict(x=x.half()),
+              dict(x=x.t()), dict(mean=torch.empty(8, device="cuda", dtype=torch.float64)), dict(x=x.unsqueeze(0)), dict(eps=-1.0)):
+        assert norm(**k) is None, k
+    lin = lambda **k: N.linear_fwd(*{**dict(x=x, w=w, b=b, act="gelu", res=None, out=None, z=None, tile=-1, ws=None, stream=None),
+                                     **k}.values())
+    assert lin() is not None
+    for k in (dict(act="tanh"), dict(act=None), dict(w=w[:32]), dict(w=w.t()), dict(tile=99), dict(stream=0), dict(res=x[:, :32]),
+              dict(b=b.float()), dict(x=x[:, :60], w=w[:60])):
+        assert lin(**k) is None, k
+    ce = lambda **k: N.linear_ce_fwd(*{**dict(x=x, w=w, lab=lab, ignore=-100, loss=None, lse=None, total=None, mean=None, ws=None,
+                                              stream=None), **k}.values())
+    assert ce() is not None
+    for k in (dict(lab=lab.int()), dict(lab=lab[:4]), dict(w=w[:, ::2]), dict(ignore=1.0), dict(total=torch.empty(3, device="cuda")),
+              dict(mean=torch.empty(2, device="cuda")), dict(ws=torch.empty(16, dtype=torch.uint8, device="cuda"))):
+        assert ce(**k) is None, k
+    # and the general way says why
+    for call, status in ((lambda: pkg.linear_fwd(x, w, b, "tanh"), fbl.FBL_ERR_ARG), (lambda: pkg.linear_fwd(x, w[:32]), fbl.FBL_ERR_SHAPE),
+                         (lambda: pkg.linear_fwd(x, w.float()), fbl.FBL_ERR_DTYPE), (lambda: pkg.linear_fwd(x.t(), w[:8]), fbl.FBL_ERR_LAYOUT),
+                         (lambda: pkg.layer_norm_fwd(x, b[:32]), fbl.FBL_ERR_SHAPE), (lambda: pkg.layer_norm_fwd(x, eps=-1.0), fbl.FBL_ERR_ARG),
+                         (lambda: pkg.linear_ce_fwd(x, w, lab.int()), fbl.FBL_ERR_DTYPE), (lambda: pkg.linear_ce_fwd(x, w, lab[:4]), fbl.FBL_ERR_SHAPE),
+                         (lambda: pkg.linear_ce_fwd(x, w, lab, workspace=torch.empty(16, dtype=torch.uint8, device="cuda")), fbl.FBL_ERR_WORKSPACE),
+                         (lambda: pkg.linear_kd_fwd(x, w, lab[:, None], x[:, :1].float(), 0.0), fbl.FBL_ERR_ARG),
+                         (lambda: pkg.linear_ce_bwd(torch.ones(3, device="cuda"), x, w, lab, torch.empty(8, device="cuda")), fbl.FBL_ERR_SHAPE),
+                         (lambda: pkg.linear_ce_bwd(torch.ones((), device="cuda"), x, w, lab, torch.empty(8, device="cuda"), dw=w.t()), fbl.FBL_ERR_LAYOUT),
+                         (lambda: pkg.linear_bwd(x, x, w, act="gelu"), fbl.FBL_ERR_NULL)):
+        with pytest.raises(pkg.FblError) as e:
+            call()
+        assert e.value.status == status, e.value

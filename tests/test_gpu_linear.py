@@ -135,6 +135,35 @@ def test_few_tokens_shared_contraction(dt):
             fbl.linear_fwd(x, w, b, "gelu", r, out=new(), workspace=ws[:need - 16])
 
 
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("act", ["none", "gelu"])
+def test_few_tokens_shared_data_gradient(act, dt):
+    """dx of a few tokens over a long contraction, plain and times act'(x_z), into views with gaps."""
+    dt = DTYPES[dt]
+    for M, K, N in ((1, 260, 4104), (20, 132, 5000), (64, 64, 8200)):
+        if dt == torch.float32:
+            K, N = K + 1, N + 1
+        rng = np.random.default_rng(M)
+        xz, xzr = rounded(rng, (M, K), dt)
+        w, wr = rounded(rng, (K, N), dt, N ** -0.5)
+        dy, dyr = rounded(rng, (M, N), dt)
+        note(f"shared dx {M}x{K}x{N} {dt} {act}")
+        gap = 4 if K % 8 == 4 else 8
+        dx, buf = padded(torch.zeros(M, K, dtype=dt, device="cuda"), gap, 7.0)
+        x = padded(xz, gap)[0]
+        got, _, _ = fbl.linear_bwd(dy, x, w, dx=dx, need_dw=False, need_bias=False, x_act=act, x_z=x if act != "none" else None)
+        d = oracle.act_grad(xzr, act)
+        prod = dyr @ wr.T
+        check("dx", got, prod * d, np.abs(d) * _sum_bound(dyr, wr.T) + np.abs(prod) * 2.0 ** -20 * (1 + np.abs(xzr)))
+        assert torch.all(buf[:, K:] == 7.0) and torch.all(buf[-1] == 7.0)
+        # with the bias' gradient too, and without a workspace of the caller's or with one
+        ws = torch.full((fbl.linear_bwd_workspace(xz, w),), 0xff, dtype=torch.uint8, device="cuda")
+        a = fbl.linear_bwd(dy, x, w, dx=padded(torch.zeros(M, K, dtype=dt, device="cuda"), gap)[0], need_dw=False, x_act=act,
+                           x_z=x if act != "none" else None, workspace=ws)
+        assert torch.equal(a[0], got)
+        check("db", a[2], dyr.sum(0), (M + 16) * 2.0 ** -24 * np.abs(dyr).sum(0))
+
+
 @pytest.mark.parametrize("tile", range(21))
 def test_every_tile(tile):
     """Ragged against every tile: a partial last step, partial rows and columns, into NaN."""
