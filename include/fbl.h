@@ -653,7 +653,7 @@ fbl_status fbl_layer_norm_bwd(int32_t dtype, int64_t M, int64_t N, const void* d
  * Row strides in elements, at least the width.  fp32: any extents, natural
  * alignment.  bf16: 16-byte aligned pointers (bias too) and rows; forward K a
  * multiple of 8 and N of 4; backward N a multiple of 8 and K of 4 for dx, N
- * of 4 for dw; any number of tokens M.  Operands below 2 GiB each (FBL_ERR_UNSUPPORTED), outputs and
+ * of 4 for dw; any number of tokens M.  K and N at most 2^26, operands below 2 GiB each (FBL_ERR_UNSUPPORTED), outputs and
  * workspace overlapping nothing (FBL_ERR_ARG).  All sums run in a fixed order.
  */
 #define FBL_ACT_NONE 0u

@@ -36,6 +36,7 @@ contiguous (or backpropagates a materialised tensor) instead.
 import math
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import fbl as _f
 
@@ -148,6 +149,7 @@ class _LinearAct(torch.autograd.Function):
         return y.view(*x.shape[:-1], N)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         x2, w, z = ctx.saved_tensors
         xshape, act = ctx.cfg
@@ -185,6 +187,7 @@ class _Mlp(torch.autograd.Function):
         return y.view(*x.shape[:-1], w2.shape[1])
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         x2, w1, w2, z, h = ctx.saved_tensors
         xshape, act = ctx.cfg
@@ -215,6 +218,7 @@ class _LayerNorm(torch.autograd.Function):
         return y.view(x.shape)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         x2, mean, rstd, weight = ctx.saved_tensors
         dy2 = _matrix_of(_unit(dy, "layer_norm"), "layer_norm: the incoming gradient")
@@ -263,6 +267,7 @@ class _LinearCrossEntropy(torch.autograd.Function):
         return _reduced(loss, total, mean, reduction, x.shape[:-1])
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dloss):
         x2, w, labels, lse, total = ctx.saved_tensors
         xshape, ignore_index, reduction = ctx.cfg
@@ -293,6 +298,7 @@ class _LinearDistillation(torch.autograd.Function):
         return _reduced(loss, total, mean, reduction, x.shape[:-1])
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dloss):
         x2, w, index, prob, lse, total = ctx.saved_tensors
         xshape, temperature, reduction = ctx.cfg

@@ -13,6 +13,8 @@ using fbl::RowsView;
 
 namespace {
 
+constexpr int64_t kMaxWidth = (int64_t)1 << 26;  // of a layer: a launch of 32 threads a column keeps below 2^32
+
 size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 hipError_t run_linear_gemm(int f32, int act, int grad, int tile, const fbl::LinearArgs& p, hipStream_t s) {
@@ -58,6 +60,7 @@ hipError_t run_shared(int f32, int act, int grad, int splits, const fbl::LinearA
 // The data gradient, whose contraction is N, the same (dx, bf16, 1 token 2048 x 8192 25.1 and 11.9, 64 tokens 25.1 and
 // 14.9; fp32, 1 token 57 and 19, 128 tokens 59 and 52, 200 tokens 92 and 89, but 1024 x 1024 9.4 and 12.1).
 int few_splits(int f32, int64_t M, int64_t K, int64_t N) {
+    if (M * N >= (int64_t)1 << 29) return 1;  // a plane's offsets
     return (f32 ? M <= 128 && K >= 1024 : M <= 64 ? K > 2048 : M <= 128 && K >= 8192) ? fbl::sum_splits(f32, 0, M, N, K, 0) : 1;
 }
 // The tile of a bf16 forward that is not shared.  Up to 32 tokens and 8192 columns that is 32 x 32 on four
@@ -88,6 +91,7 @@ fbl_status linear_shape(int32_t dtype, uint32_t act, int64_t M, int64_t K, int64
     if (act > FBL_ACT_SILU) return FBL_ERR_ARG;
     if (!fbl::extent(M) || !fbl::extent(K) || !fbl::extent(N)) return FBL_ERR_SHAPE;
     if (M * N >= ((int64_t)1 << 31) / fbl::dtype_size(dtype)) return FBL_ERR_UNSUPPORTED;  // y, dy, dz
+    if (K > kMaxWidth || N > kMaxWidth) return FBL_ERR_UNSUPPORTED;
     return FBL_OK;
 }
 

@@ -890,8 +890,17 @@ def _scratch(workspace, need: int, where: str, like, stream):
     return workspace, workspace.numel() * workspace.element_size()
 
 
-def _launch_stream(stream):
-    return _stream(stream) if stream != 0 else None
+def _call(name: str, like, stream, *args) -> None:
+    """One call of the library on `stream`, with like's device current (a stream given may be another's than the
+    program's current one)."""
+    import torch
+    f, args = getattr(LIB, name), args + (_stream(stream) if stream != 0 else None,)
+    if stream is not None and like.device.index != torch.cuda.current_device():
+        with torch.cuda.device(like.device):
+            status = f(*args)
+    else:
+        status = f(*args)
+    _check(status, name)
 
 
 def layer_norm_fwd(x, weight=None, bias=None, eps: float = 1e-5, out=None, mean=None, rstd=None, stream=None):
@@ -917,8 +926,8 @@ def layer_norm_fwd(x, weight=None, bias=None, eps: float = 1e-5, out=None, mean=
         rstd = _empty(M, torch.float32, x, stream)
     _vector(mean, where, "mean", M, torch.float32)
     _vector(rstd, where, "rstd", M, torch.float32)
-    _check(LIB.fbl_layer_norm_fwd(dt, M, N, _ptr(x), ldx, _ptr(weight), _ptr(bias), float(eps), _ptr(out), ldy, _ptr(mean),
-                                  _ptr(rstd), _launch_stream(stream)), "fbl_layer_norm_fwd")
+    _call("fbl_layer_norm_fwd", x, stream, dt, M, N, _ptr(x), ldx, _ptr(weight), _ptr(bias), float(eps), _ptr(out),
+          ldy, _ptr(mean), _ptr(rstd))
     return out, mean, rstd
 
 
@@ -961,9 +970,8 @@ def layer_norm_bwd(dy, x, mean, rstd, weight=None, dx=None, dweight=None, dbias=
     if dweight is not None or dbias is not None:
         need = 0 if workspace is not None else layer_norm_bwd_workspace(x)
         ws, ws_bytes = _scratch(workspace, need, where, x, stream)
-    _check(LIB.fbl_layer_norm_bwd(dt, M, N, _ptr(dy), lddy, _ptr(x), ldx, _ptr(weight), _ptr(mean), _ptr(rstd), _ptr(dx),
-                                  lddx, _ptr(dweight), _ptr(dbias), _ptr(ws), ws_bytes, _launch_stream(stream)),
-           "fbl_layer_norm_bwd")
+    _call("fbl_layer_norm_bwd", x, stream, dt, M, N, _ptr(dy), lddy, _ptr(x), ldx, _ptr(weight), _ptr(mean),
+          _ptr(rstd), _ptr(dx), lddx, _ptr(dweight), _ptr(dbias), _ptr(ws), ws_bytes)
     return dx, dweight, dbias
 
 
@@ -1011,8 +1019,8 @@ def linear_fwd(x, w, bias=None, act: str = "none", residual=None, out=None, z=No
     need = linear_fwd_workspace(x, w) if workspace is None and M <= 128 and tile == FBL_GEMM_TILE_AUTO else 0
     if workspace is not None or need:
         ws, ws_bytes = _scratch(workspace, need, where, x, stream)
-    _check(LIB.fbl_linear_fwd(dt, code, M, K, N, _ptr(x), ldx, _ptr(w), ldw, _ptr(bias), _ptr(residual), ldr, _ptr(out), ldy,
-                              _ptr(z), ldz, tile, _ptr(ws), ws_bytes, _launch_stream(stream)), "fbl_linear_fwd")
+    _call("fbl_linear_fwd", x, stream, dt, code, M, K, N, _ptr(x), ldx, _ptr(w), ldw, _ptr(bias), _ptr(residual), ldr,
+          _ptr(out), ldy, _ptr(z), ldz, tile, _ptr(ws), ws_bytes)
     return out
 
 
@@ -1057,9 +1065,8 @@ def linear_bwd(dy, x, w, z=None, act: str = "none", dx=None, dw=None, dbias=None
     if code != FBL_ACT_NONE or dbias is not None or workspace is not None or (dx is not None and M <= 128):
         need = 0 if workspace is not None else linear_bwd_workspace(x, w)
         ws, ws_bytes = _scratch(workspace, need, where, x, stream)
-    _check(LIB.fbl_linear_bwd(dt, code, M, K, N, _ptr(dy), lddy, _ptr(x), ldx, _ptr(w), ldw, _ptr(z), ldz, xcode, _ptr(x_z),
-                              ldxz, _ptr(dx), lddx, _ptr(dw), lddw, _ptr(dbias), _ptr(ws), ws_bytes,
-                              _launch_stream(stream)), "fbl_linear_bwd")
+    _call("fbl_linear_bwd", x, stream, dt, code, M, K, N, _ptr(dy), lddy, _ptr(x), ldx, _ptr(w), ldw, _ptr(z), ldz,
+          xcode, _ptr(x_z), ldxz, _ptr(dx), lddx, _ptr(dw), lddw, _ptr(dbias), _ptr(ws), ws_bytes)
     return dx, dw, dbias
 
 
@@ -1166,9 +1173,8 @@ def linear_ce_fwd(x, w, labels, ignore_index: int = -100, loss=None, lse=None, t
     loss, lse = _new_f32(loss, M, x, where, "loss", stream), _new_f32(lse, M, x, where, "lse", stream)
     total = _new_f32(total, 2, x, where, "total", stream)
     ws, ws_bytes = _loss_scratch(workspace, x, w, 1, where, stream)
-    _check(LIB.fbl_linear_ce_fwd(dt, order, M, K, w.shape[1], _ptr(x), ldx, _ptr(w), ldw, _ptr(labels), ignore_index, _ptr(loss),
-                                 _ptr(lse), _ptr(total), _mean_ptr(mean, where), _ptr(ws), ws_bytes,
-                                 _launch_stream(stream)), "fbl_linear_ce_fwd")
+    _call("fbl_linear_ce_fwd", x, stream, dt, order, M, K, w.shape[1], _ptr(x), ldx, _ptr(w), ldw, _ptr(labels),
+          ignore_index, _ptr(loss), _ptr(lse), _ptr(total), _mean_ptr(mean, where), _ptr(ws), ws_bytes)
     return loss, lse, total
 
 
@@ -1195,9 +1201,9 @@ def linear_ce_bwd(dloss, x, w, labels, lse, total=None, ignore_index: int = -100
     gstride = _dloss(dloss, M, where)
     dx, lddx, dw, lddw = _head_grads(x, w, dx, dw, need_dx, need_dw, order, where, stream)
     ws, ws_bytes = _loss_scratch(workspace, x, w, 1, where, stream)
-    _check(LIB.fbl_linear_ce_bwd(dt, order, M, K, w.shape[1], _ptr(dloss), gstride, _ptr(total), _ptr(x), ldx, _ptr(w), ldw,
-                                 _ptr(labels), ignore_index, _ptr(lse), _ptr(dx), lddx, _ptr(dw), lddw, _ptr(ws), ws_bytes,
-                                 _launch_stream(stream)), "fbl_linear_ce_bwd")
+    _call("fbl_linear_ce_bwd", x, stream, dt, order, M, K, w.shape[1], _ptr(dloss), gstride, _ptr(total), _ptr(x),
+          ldx, _ptr(w), ldw, _ptr(labels), ignore_index, _ptr(lse), _ptr(dx), lddx, _ptr(dw), lddw, _ptr(ws),
+          ws_bytes)
     return dx, dw
 
 
@@ -1239,9 +1245,9 @@ def linear_kd_fwd(x, w, index, logits, temperature: float = 1.0, loss=None, lse=
         prob = _empty((M, top), torch.float32, x, stream)
     _contiguous(prob, where, "prob", (M, top))
     ws, ws_bytes = _loss_scratch(workspace, x, w, top, where, stream)
-    _check(LIB.fbl_linear_kd_fwd(dt, order, M, K, w.shape[1], top, _ptr(x), ldx, _ptr(w), ldw, _ptr(index), ldi, ldt,
-                                 _ptr(logits), ldl, float(temperature), _ptr(prob), _ptr(loss), _ptr(lse), _ptr(total),
-                                 _mean_ptr(mean, where), _ptr(ws), ws_bytes, _launch_stream(stream)), "fbl_linear_kd_fwd")
+    _call("fbl_linear_kd_fwd", x, stream, dt, order, M, K, w.shape[1], top, _ptr(x), ldx, _ptr(w), ldw, _ptr(index),
+          ldi, ldt, _ptr(logits), ldl, float(temperature), _ptr(prob), _ptr(loss), _ptr(lse), _ptr(total),
+          _mean_ptr(mean, where), _ptr(ws), ws_bytes)
     return loss, lse, prob, total
 
 
@@ -1277,7 +1283,7 @@ def linear_kd_bwd(dloss, x, w, index, prob, lse, temperature: float = 1.0, total
     gstride = _dloss(dloss, M, where)
     dx, lddx, dw, lddw = _head_grads(x, w, dx, dw, need_dx, need_dw, order, where, stream)
     ws, ws_bytes = _loss_scratch(workspace, x, w, top, where, stream)
-    _check(LIB.fbl_linear_kd_bwd(dt, order, M, K, w.shape[1], top, _ptr(dloss), gstride, _ptr(total), _ptr(x), ldx, _ptr(w), ldw,
-                                 _ptr(index), ldi, float(temperature), _ptr(prob), _ptr(lse), _ptr(dx), lddx, _ptr(dw), lddw,
-                                 _ptr(ws), ws_bytes, _launch_stream(stream)), "fbl_linear_kd_bwd")
+    _call("fbl_linear_kd_bwd", x, stream, dt, order, M, K, w.shape[1], top, _ptr(dloss), gstride, _ptr(total),
+          _ptr(x), ldx, _ptr(w), ldw, _ptr(index), ldi, float(temperature), _ptr(prob), _ptr(lse), _ptr(dx), lddx,
+          _ptr(dw), lddw, _ptr(ws), ws_bytes)
     return dx, dw

@@ -248,3 +248,11 @@ def test_losses_binding_refuses_host_tensors_and_layouts():
     with pytest.raises(fbl.FblError) as e:
         head(torch.zeros(1, 100).expand(64, 100), x, "")  # one row for all
     assert e.value.status == F.FBL_ERR_LAYOUT
+
+
+def test_linear_width_limits():
+    n = ctypes.c_size_t()
+    f = LIB.fbl_linear_bwd_workspace
+    assert f(F32, 1, 8, (1 << 26) + 1, ctypes.byref(n)) == F.FBL_ERR_UNSUPPORTED
+    assert f(F32, 1, (1 << 26) + 1, 8, ctypes.byref(n)) == F.FBL_ERR_UNSUPPORTED
+    assert f(F32, 1, 8, 1 << 26, ctypes.byref(n)) == F.FBL_OK
