@@ -52,11 +52,12 @@ fbl_status check_weight(const Shape& s, const void* w, int64_t ld) {
     return s.es() == 2 ? (v.aligned16() ? FBL_OK : FBL_ERR_ALIGN) : (v.natural() ? FBL_OK : FBL_ERR_ALIGN);
 }
 
-// Vocabulary entries of a forward launch: all of them, or as many rows of a large table as a span holds.
+// Vocabulary entries of a forward launch: all of them, or as many rows of a large table as a span holds, or columns
+// as keep a launch's threads below 2^32 (at most 2^34 logits; tiles are of 16 a thread at least).
 int64_t forward_piece(const Shape& s, int64_t ldw) {
-    if (!s.table()) return s.V;
-    const int64_t rows = ((kSpan - 1) / s.es() - s.K) / ldw + 1;
-    return rows >= s.V ? s.V : rows / 256 * 256;
+    int64_t most = std::max<int64_t>(256, ((int64_t)1 << 34) / s.M);
+    if (s.table()) most = std::min(most, ((kSpan - 1) / s.es() - s.K) / ldw + 1);
+    return most >= s.V ? s.V : most / 256 * 256;
 }
 
 // Vocabulary entries of a piece of the backward.  dz [M][piece] goes through memory twice and dX's fp32

@@ -284,6 +284,34 @@ def test_pieces_of_the_vocabulary(table, dt):
     assert torch.equal(one[0], dx) and one[1] is None and torch.equal(two[1], dw) and two[0] is None
 
 
+def test_more_tiles_than_a_launch_holds():
+    """2^20 rows of 2^19 logits: 2^23 tiles of 512 threads would be 2^32, one more than a launch may have.  64 rows'
+    loss and dx against float64."""
+    dt = torch.bfloat16
+    M, K, V = 1 << 20, 8, 1 << 19
+    note(f"ce M={M} K={K} V={V}")
+    g = torch.Generator("cuda").manual_seed(5)
+    x, w = (torch.randn(s, generator=g, device="cuda").to(dt) for s in ((M, K), (K, V)))
+    lab = torch.randint(0, V, (M,), generator=g, device="cuda")
+    loss, lse, total = fbl.linear_ce_fwd(x, w, lab)
+    dx, _ = fbl.linear_ce_bwd(torch.ones((), device="cuda"), x, w, lab, lse, None, need_dw=False)
+    at = torch.linspace(0, M - 1, 64, device="cuda").long()
+    xd, wd, ld = x[at].double(), w.double(), lab[at]
+    z = xd @ wd
+    ref = torch.logsumexp(z, 1)
+    picked = z.gather(1, ld[:, None])[:, 0]
+    # K + 16 roundings of a logit, the sums of exponentials (2^-17), lse's and the loss' own
+    zb = (K + 16) * 2.0 ** -24 * (xd.abs() @ wd.abs()).amax(1)
+    bound = 2 * zb + 2.0 ** -17 + 2.0 ** -20 * (ref.abs() + picked.abs())
+    assert bool(((loss[at].double() - (ref - picked)).abs() <= bound).all())
+    z.sub_(ref[:, None]).exp_()
+    z.scatter_add_(1, ld[:, None], torch.full((64, 1), -1.0, dtype=torch.float64, device="cuda"))
+    want, mag = z @ wd.t(), z.abs() @ wd.abs().t()
+    bound = HALF[dt] * want.abs() + mag * (HALF[dt] + 2.0 ** -15 + zb.amax() * 2 + (V + 16) * 2.0 ** -24)
+    assert bool(((dx[at].double() - want).abs() <= bound).all())
+    assert total[1] == M
+
+
 @pytest.mark.parametrize("reduction", ["mean", "sum", "none"])
 def test_autograd(reduction):
     from paper_2607_21624_amd import autograd as ag
