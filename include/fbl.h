@@ -18,6 +18,10 @@
  * gradients, also for LoRA adapters) read the same token-major activations
  * in place, and Q, K, V can be views of one packed projection output
  * (fbl_layout_packed_qkv).
+ * Around them, for a whole block's training step: layer norm (fbl_layer_norm_*), linear
+ * layers with bias, activation and residual (fbl_linear_*), and the softmax cross entropy
+ * and distillation losses of a linear head without its logits in memory
+ * (fbl_linear_ce_*, fbl_linear_kd_*).
  *
  * Conventions shared by every entry point.
  *  - Element (b, h, s, i) of a tensor described by an fbl_layout L is at
@@ -66,7 +70,7 @@ typedef enum {
     FBL_ERR_LAYOUT = 4,      /* a tile-legality check failed (strides, tile shape)  */
     FBL_ERR_ALIGN = 5,       /* base pointer or row stride not 16-byte aligned      */
     FBL_ERR_UNSUPPORTED = 6, /* shape, head dim or mask combination not implemented  */
-    FBL_ERR_WORKSPACE = 7,   /* workspace NULL or below fbl_attn_bwd_workspace_min  */
+    FBL_ERR_WORKSPACE = 7,   /* workspace NULL or smaller than the call needs      */
     FBL_ERR_HIP = 8,         /* the HIP runtime reported an error at launch         */
     FBL_ERR_ARG = 9          /* other invalid argument (non-finite scale, aliasing) */
 } fbl_status;
@@ -680,7 +684,8 @@ fbl_status fbl_linear_bwd(int32_t dtype, uint32_t act, int64_t M, int64_t K, int
  *
  * Cross entropy (fbl_linear_ce_*), labels int64 [M]:
  *   loss[m] = lse[m] - z[m, labels[m]],   lse[m] = log sum_v exp(z[m, v])
- * A row whose label is `ignore` does not count: loss 0, no gradient.
+ * A row whose label is `ignore` does not count: loss 0, no gradient.  (Its x still enters dW's sums, times 0,
+ * and must be finite there.)
  *
  * Distillation from a teacher's top logits (fbl_linear_kd_*), index int64 [M, top] (row
  * stride ldi) and logits [M, top] (row stride ldl, of logits_dtype), temperature T > 0, top up to 1024:
@@ -704,8 +709,9 @@ fbl_status fbl_linear_bwd(int32_t dtype, uint32_t act, int64_t M, int64_t K, int
  * products; dx is summed over the pieces in fp32.
  *
  * Workspace: fbl_linear_loss_workspace bytes for W's row stride, 16-byte aligned, the
- * same for all four calls (top 1 for cross entropy); nothing is kept in it between calls.  Its
- * size stays about 128 MiB of dz plus small lists and M K fp32 sums.
+ * same for all four calls (top 1 for cross entropy); nothing is kept in it between calls.  It holds
+ * about 128 MiB of dz and M K fp32 sums (up to 8 of them where workgroups share dX's contraction), or 8 bytes
+ * for each row and 256 vocabulary entries where that is more, and small lists.
  * fp32: any extents, natural alignment.  bf16: 16-byte aligned pointers and rows, K a multiple
  * of 8, for FBL_HEAD_KV V too; any number of tokens.  x, dx and a FBL_HEAD_KV W below 2 GiB
  * (fp32 sums of dx included: M K below 2^29); a table may be larger.  Outputs and workspace overlap

@@ -14,12 +14,14 @@ Modules
              to cross-check ``attention``.
   proj       the projection matrix products around attention: Y = X W and its
              data and weight gradients.
+  train      layer norm, linear layers with bias, activation and residual, and
+             the softmax cross entropy and distillation losses of a linear head.
   layout     the logical (b, h, s, i) -> physical offset map of a token-major
              tensor, built by the reshape-then-transpose chain itself, also
              for Q, K, V split out of one packed projection output.
 
 Pins (tests/test_oracle.py, tests/test_oracle_cross.py, tests/test_oracle_proj.py,
-tests/test_layout_oracle.py) tie each function to
+tests/test_oracle_train.py, tests/test_layout_oracle.py) tie each function to
 something other than itself: brute force, float64 torch SDPA with autograd,
 central finite differences, closed forms, invariants and the paper's own
 layout examples.  Each function's docstring names the pin(s).

@@ -1,8 +1,7 @@
-"""torch.autograd wrappers over the C ABI: attention and projection products
-usable inside an ordinary training step.  Argument marshalling only -- every
-forward and backward runs in the library's kernels (fbl_attn_fwd /
-fbl_attn_bwd, fbl_proj); torch provides the tensors, the stream and the
-autograd graph.
+"""torch.autograd wrappers over the C ABI: attention, linear layers, layer norm and
+the losses of a linear head, usable inside an ordinary training step.  Argument
+marshalling only -- every forward and backward runs in the library's kernels;
+torch provides the tensors, the stream and the autograd graph.
 
   attention(q, k, v, Hq, Hkv, scale=None, causal=False, kv_len=None) -> O
       q [B, S_q, Hq*d], k and v [B, S_kv, Hkv*d], token-major (any row
@@ -32,6 +31,11 @@ inner stride (any row stride), like every tensor the kernels read.  Autograd
 can hand over a broadcast view (the gradient of a plain .sum(), inner stride
 0); such a gradient is rejected with FblError, and the caller makes it
 contiguous (or backpropagates a materialised tensor) instead.
+
+Capturing a backward pass into a graph: run a step on the capturing stream first and
+let go of every eager loss or output of the same leaves.  While one lives, torch
+keeps the leaves' accumulation on that graph's stream, and a capture that meets another
+stream ends with an error or the process.
 """
 import math
 

@@ -17,14 +17,17 @@ constexpr int64_t kMaxWidth = (int64_t)1 << 26;  // of a layer: a launch of 32 t
 
 size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 
+template <int ACT>
+hipError_t run_act(int f32, int grad, int tile, const fbl::LinearArgs& p, hipStream_t s) {
+    return f32 ? fbl::launch_linear_gemm_f32<ACT>(grad, p, s) : fbl::launch_linear_gemm<ACT>(grad, tile, p, s);
+}
 hipError_t run_linear_gemm(int f32, int act, int grad, int tile, const fbl::LinearArgs& p, hipStream_t s) {
     switch (act) {
-        case FBL_ACT_NONE: return f32 ? fbl::launch_linear_gemm_f32<fbl::kActNone>(grad, p, s) : fbl::launch_linear_gemm<fbl::kActNone>(grad, tile, p, s);
-        case FBL_ACT_RELU: return f32 ? fbl::launch_linear_gemm_f32<fbl::kActRelu>(grad, p, s) : fbl::launch_linear_gemm<fbl::kActRelu>(grad, tile, p, s);
-        case FBL_ACT_GELU: return f32 ? fbl::launch_linear_gemm_f32<fbl::kActGelu>(grad, p, s) : fbl::launch_linear_gemm<fbl::kActGelu>(grad, tile, p, s);
-        case FBL_ACT_GELU_TANH:
-            return f32 ? fbl::launch_linear_gemm_f32<fbl::kActGeluTanh>(grad, p, s) : fbl::launch_linear_gemm<fbl::kActGeluTanh>(grad, tile, p, s);
-        default: return f32 ? fbl::launch_linear_gemm_f32<fbl::kActSilu>(grad, p, s) : fbl::launch_linear_gemm<fbl::kActSilu>(grad, tile, p, s);
+        case FBL_ACT_NONE: return run_act<fbl::kActNone>(f32, grad, tile, p, s);
+        case FBL_ACT_RELU: return run_act<fbl::kActRelu>(f32, grad, tile, p, s);
+        case FBL_ACT_GELU: return run_act<fbl::kActGelu>(f32, grad, tile, p, s);
+        case FBL_ACT_GELU_TANH: return run_act<fbl::kActGeluTanh>(f32, grad, tile, p, s);
+        default: return run_act<fbl::kActSilu>(f32, grad, tile, p, s);
     }
 }
 
@@ -40,7 +43,6 @@ ActGrid act_grid(int f32, int64_t M, int64_t N) {
     const int64_t rows = ((M + want - 1) / want + 3) / 4 * 4;
     return {rows, (int)((M + rows - 1) / rows)};
 }
-
 
 // A product of few rows whose contraction `splits` workgroups a tile share, their planes, and what follows it.
 hipError_t run_shared(int f32, int act, int grad, int splits, const fbl::LinearArgs& p, float* planes, hipStream_t s) {

@@ -39,8 +39,11 @@ namespace fbl {
 
 hipError_t launch_proj_gemm(int a_kmajor, int b_nmajor, int tile, const GemmArgs& p, hipStream_t stream) {
     if (tile < 0 || tile >= kGemmTileCount) return hipErrorInvalidValue;
-    if (a_kmajor) return b_nmajor ? launch_gemm_tile<true, true, PlainStore>(tile, p, stream) : launch_gemm_tile<true, false, PlainStore>(tile, p, stream);
-    return b_nmajor ? launch_gemm_tile<false, true, PlainStore>(tile, p, stream) : launch_gemm_tile<false, false, PlainStore>(tile, p, stream);
+    if (a_kmajor)
+        return b_nmajor ? launch_gemm_tile<true, true, PlainStore>(tile, p, stream)
+                        : launch_gemm_tile<true, false, PlainStore>(tile, p, stream);
+    return b_nmajor ? launch_gemm_tile<false, true, PlainStore>(tile, p, stream)
+                    : launch_gemm_tile<false, false, PlainStore>(tile, p, stream);
 }
 
 }  // namespace fbl

@@ -24,7 +24,8 @@ namespace {
 hipError_t launch_f32(int a_kmajor, int b_nmajor, int tile, const GemmArgs& p, hipStream_t stream) {
     if (a_kmajor && b_nmajor) return hipErrorInvalidValue;  // no product reads both that way
     if (a_kmajor) return launch_f32_tile<true, false, PlainStoreF32>(tile, p, stream);
-    return b_nmajor ? launch_f32_tile<false, true, PlainStoreF32>(tile, p, stream) : launch_f32_tile<false, false, PlainStoreF32>(tile, p, stream);
+    return b_nmajor ? launch_f32_tile<false, true, PlainStoreF32>(tile, p, stream)
+                    : launch_f32_tile<false, false, PlainStoreF32>(tile, p, stream);
 }
 
 }  // namespace
