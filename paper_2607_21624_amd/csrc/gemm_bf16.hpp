@@ -1,7 +1,7 @@
 // gemm_bf16.hpp -- the kernel of the bf16 matrix products, gfx950: the projection
 // products (proj_gemm.hip, whose head describes the products, the operand reads and
 // the partial tiles) and the products with something fused behind them
-// (linear_gemm.hip, head_gemm.hip).
+// (linear_gemm.hpp, head_gemm.hip).
 #pragma once
 
 #include <array>
@@ -369,9 +369,9 @@ proj_gemm_bf16(typename EP::Args p) {
 
 // A wavefront's accumulators by rows: f(m, n, v, d) gets 8 consecutive columns n .. n+7 of row m and what
 // d = ahead(m, n) has loaded for them, neighbouring lanes the next 8, so that whole 128-byte lines are
-// loaded and stored beside them.  (As they stand a lane has 4 columns of a row and the lanes 32 rows: a layer that writes y and z that
-// way and reads a residual spends as long on it as on a contraction of 1500.  4096 x 8192 from 2048,
-// GELU: 208 us, 140 through here.)  Each 32 rows go through LDS, 32 x (32 TN + 4) floats of
+// loaded and stored beside them.  (As they stand a lane has 4 columns of a row and the lanes 32 rows: a layer
+// that writes y and z that way and reads a residual spends as long on it as on a contraction of 1500.  4096 x
+// 8192 from 2048, GELU: 208 us, 140 through here.)  Each 32 rows go through LDS, 32 x (32 TN + 4) floats of
 // the wavefront's own; the pitch puts 16 rows' writes on different banks.  The loads beside 32 rows
 // are all issued before the first store (no load is moved over a store to what might be the same memory).
 struct Nothing {};

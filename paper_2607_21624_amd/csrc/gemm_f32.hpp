@@ -1,6 +1,6 @@
 // gemm_f32.hpp -- the kernel of the fp32 matrix products, gfx950: the projection
 // products (proj_gemm_f32.hip, whose head describes it) and the products with
-// something fused behind them (linear_gemm.hip, head_gemm.hip).
+// something fused behind them (linear_gemm.hpp, head_gemm.hip).
 #pragma once
 
 #include <algorithm>

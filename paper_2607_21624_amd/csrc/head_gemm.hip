@@ -310,7 +310,9 @@ constexpr int kSplitTileF32 = 4;
 }  // namespace
 
 // Tiles whose wavefronts each have the whole contraction, of 32, 64, 128 and 256 tokens: the one of least modelled
-// time (gemm_cost.hpp); fp32: 128 x 128 where that makes two workgroups for each CU, else 64 x 64.
+// time (gemm_cost.hpp).  Two workgroups a CU, so that one's exponentials and stores run beside the other's products,
+// do not pay for their narrower tiles: 4096 x 1024 x 50257 forward 451 us with 256 x 256, 495 with 256 x 128 or 128 x
+// 256 in steps of 32, 581 with 128 x 128; dz 141, 159, 156 and 171 a piece.  fp32: 128 x 128 where that makes two workgroups for each CU, else 64 x 64.
 int head_tile(int f32, int table, int64_t M, int64_t V, int64_t K) {
     if (f32) return ((M + 127) / 128) * ((V + 127) / 128) >= 512 ? 0 : 2;
     int best = 19;
