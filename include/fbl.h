@@ -645,13 +645,14 @@ fbl_status fbl_layer_norm_bwd(int32_t dtype, int64_t M, int64_t N, const void* d
  *
  * fbl_linear_bwd gives, from dy [M, N], any of (NULL: not wanted)
  *   dx = (dz . w^T) * xact'(xz),   dw = x^T . dz,   dbias = sum over rows of dz,
- *   dz = dy * act'(z)
+ *   dz = dy * act'(z),   dxbias = sum over rows of dx
  * xact and xz [M, K] are the activation and pre-activation that made x, where the
- * caller wants the gradient of that pre-activation at once (FBL_ACT_NONE: x's own).
+ * caller wants the gradient of that pre-activation at once (FBL_ACT_NONE: x's own); dxbias [K]
+ * (needs dx) is then the gradient of the bias in it.
  * The residual's gradient is dy.  dz is rounded to the storage type before the
- * products; the bias' gradient sums it in fp32 unrounded.  x may be NULL without dw, w without dx,
+ * products; dbias and dxbias sum dz and dx in fp32 unrounded.  x may be NULL without dw, w without dx,
  * z with act NONE.  The workspace (16-byte aligned, fbl_linear_bwd_workspace
- * bytes) is needed where act is not NONE or dbias is wanted, else it may be NULL; with it, workgroups share the
+ * bytes) is needed where act is not NONE or dbias or dxbias is wanted, else it may be NULL; with it, workgroups share the
  * contraction of dx for a few tokens.
  *
  * Row strides in elements, at least the width.  fp32: any extents, natural
@@ -672,8 +673,8 @@ fbl_status fbl_linear_fwd_workspace(int32_t dtype, int64_t M, int64_t K, int64_t
 fbl_status fbl_linear_bwd_workspace(int32_t dtype, int64_t M, int64_t K, int64_t N, size_t* bytes);
 fbl_status fbl_linear_bwd(int32_t dtype, uint32_t act, int64_t M, int64_t K, int64_t N, const void* dy, int64_t lddy,
                           const void* x, int64_t ldx, const void* w, int64_t ldw, const void* z, int64_t ldz,
-                          uint32_t xact, const void* xz, int64_t ldxz, void* dx, int64_t lddx, void* dw, int64_t lddw,
-                          void* dbias, void* ws, size_t ws_bytes, void* stream);
+                          uint32_t xact, const void* xz, int64_t ldxz, void* dx, int64_t lddx, void* dxbias,
+                          void* dw, int64_t lddw, void* dbias, void* ws, size_t ws_bytes, void* stream);
 
 /*
  * Softmax losses of a linear head, logits z = x [M, K] . W over a vocabulary of V, without

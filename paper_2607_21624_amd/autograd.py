@@ -15,7 +15,7 @@ torch provides the tensors, the stream and the autograd graph.
       act "none", "relu", "gelu", "gelu_tanh" or "silu", residual [..., N].
   mlp(x, w1, b1, w2, b2, act="gelu", residual=None) -> act(x @ w1 + b1) @ w2 + b2 + residual
       a block's feed-forward part; its backward takes the activation's
-      derivative in the epilogue of the data gradient.  b1, b2 may be None.
+      derivative and b1's gradient in the epilogue of the data gradient.  b1, b2 may be None.
   layer_norm(x, weight=None, bias=None, eps=1e-5) -> y
       x [..., N] (rows one strided matrix), weight and bias [N]; gradients to all three.
   linear_cross_entropy(x, w, labels, ignore_index=-100, reduction="mean") -> loss
@@ -201,10 +201,11 @@ class _Mlp(torch.autograd.Function):
         if first or second:
             dy2 = _matrix_of(_unit(dy, "mlp"), "mlp: the incoming gradient")
             # the hidden layer's gradient arrives as that of its pre-activation
+            db1 = torch.empty(w1.shape[1], dtype=w1.dtype, device=w1.device) if need[2] else None
             dz, dw2, db2 = _f.linear_bwd(dy2, h, w2, need_dx=first, need_dw=need[3], need_bias=need[4],
-                                         x_act=act if first else "none", x_z=z if first else None)
-            if first:
-                dx, dw1, db1 = _f.linear_bwd(dz, x2, w1, need_dx=need[0], need_dw=need[1], need_bias=need[2])
+                                         x_act=act if first else "none", x_z=z if first else None, dxbias=db1)
+            if need[0] or need[1]:
+                dx, dw1, _ = _f.linear_bwd(dz, x2, w1, need_dx=need[0], need_dw=need[1], need_bias=False)
         return dx.view(xshape) if need[0] else None, dw1, db1, dw2, db2, dy if need[5] else None, None
 
 

@@ -74,9 +74,10 @@ int forward_tile(int64_t M, int64_t K, int64_t N) {
 }
 size_t few_ws(int splits, int64_t M, int64_t N) { return splits > 1 ? (size_t)splits * (size_t)M * (size_t)N * 4 : 0; }
 
-// Workspace of the backward: partial sums of the bias' gradient, dz, planes of dx.
+// Workspace of the backward: partial sums of the bias' gradient, dz, planes of dx, partial sums of dx (as many rows
+// of them as any tile writes, linear_grad_groups, or one for each of a few tokens).
 struct LinearWs {
-    size_t dz, planes, total;
+    size_t dz, planes, sums, total;
     int splits;
 };
 LinearWs linear_ws(int f32, int64_t M, int64_t K, int64_t N) {
@@ -84,7 +85,8 @@ LinearWs linear_ws(int f32, int64_t M, int64_t K, int64_t N) {
     w.splits = few_splits(f32, M, N, K);
     w.dz = align256((size_t)act_grid(f32, M, N).groups * (size_t)N * 4);
     w.planes = w.dz + align256((size_t)M * (size_t)N * (f32 ? 4 : 2));
-    w.total = w.planes + few_ws(w.splits, M, K);
+    w.sums = w.planes + align256(few_ws(w.splits, M, K));
+    w.total = w.sums + (size_t)(w.splits > 1 ? M : M / 32 + 4) * (size_t)K * 4;
     return w;
 }
 
@@ -160,32 +162,32 @@ fbl_status fbl_linear_bwd_workspace(int32_t dtype, int64_t M, int64_t K, int64_t
 
 fbl_status fbl_linear_bwd(int32_t dtype, uint32_t act, int64_t M, int64_t K, int64_t N, const void* dy, int64_t lddy,
                           const void* x, int64_t ldx, const void* w, int64_t ldw, const void* z, int64_t ldz,
-                          uint32_t xact, const void* xz, int64_t ldxz, void* dx, int64_t lddx, void* dw, int64_t lddw,
-                          void* dbias, void* ws, size_t ws_bytes, void* stream) {
+                          uint32_t xact, const void* xz, int64_t ldxz, void* dx, int64_t lddx, void* dxbias,
+                          void* dw, int64_t lddw, void* dbias, void* ws, size_t ws_bytes, void* stream) {
     fbl_status st = linear_shape(dtype, act, M, K, N);
     if (st != FBL_OK) return st;
     if (xact > FBL_ACT_SILU) return FBL_ERR_ARG;
-    if (!dy || (dw && !x) || (dx && !w)) return FBL_ERR_NULL;
+    if (!dy || (dw && !x) || (dx && !w) || (dxbias && !dx)) return FBL_ERR_NULL;
     const bool has_act = act != FBL_ACT_NONE, has_xact = dx && xact != FBL_ACT_NONE;
     if ((has_act && !z) || (has_xact && !xz)) return FBL_ERR_NULL;
     const int es = (int)fbl::dtype_size(dtype), f32 = es == 4;
     const RowsView vdy{dy, M, N, lddy, es}, vx{dw ? x : nullptr, M, K, ldx, es}, vw{dx ? w : nullptr, K, N, ldw, es},
         vz{has_act ? z : nullptr, M, N, ldz, es}, vxz{has_xact ? xz : nullptr, M, K, ldxz, es}, vdx{dx, M, K, lddx, es},
         vdw{dw, K, N, lddw, es};
-    const RowsView vdb{dbias, 1, N, N, es};
+    const RowsView vdb{dbias, 1, N, N, es}, vdxb{dxbias, 1, K, K, es};
     for (const RowsView* v : {&vdy, &vx, &vw, &vz, &vxz, &vdx, &vdw})
         if ((st = fbl::check_operand(*v)) != FBL_OK) return st;
-    if (!vdb.natural()) return FBL_ERR_ALIGN;
+    if (!vdb.natural() || !vdxb.natural()) return FBL_ERR_ALIGN;
     if (es == 2 && ((dx && (N % 8 || K % 4)) || (dw && N % 4))) return FBL_ERR_UNSUPPORTED;
     // what is needed of the workspace: partial sums for the bias, dz where an activation makes it
     const LinearWs lw = linear_ws(f32, M, K, N);
     const bool pass = has_act ? (dx || dw || dbias) : dbias != nullptr, shared = dx && lw.splits > 1 && ws;
-    const size_t need = pass || shared ? lw.total : 0;
+    const size_t need = pass || shared || dxbias ? lw.total : 0;
     if (need && (!ws || ws_bytes < need)) return FBL_ERR_WORKSPACE;
     const RowsView vws{need ? ws : nullptr, 1, (int64_t)need, (int64_t)need + 1, 1};
     if (vws.begin() % 16) return FBL_ERR_ALIGN;
-    const RowsView* outs[] = {&vdx, &vdw, &vdb, &vws};
-    for (int i = 0; i < 4; ++i) {
+    const RowsView* outs[] = {&vdx, &vdw, &vdb, &vdxb, &vws};
+    for (int i = 0; i < 5; ++i) {
         for (const RowsView* in : {&vdy, &vx, &vw, &vz, &vxz})
             if (overlap(*outs[i], *in)) return FBL_ERR_ARG;
         for (int j = 0; j < i; ++j)
@@ -211,10 +213,15 @@ fbl_status fbl_linear_bwd(int32_t dtype, uint32_t act, int64_t M, int64_t K, int
         fbl::product(p, FBL_PROJ_BWD_DATA, g, vw, vdx, M, K, N);
         const int tile = f32 ? 0 : fbl::proj_auto_tile(FBL_PROJ_BWD_DATA, M, K, N);
         if (has_xact) p.z = const_cast<void*>(xz), p.ldz = ldxz, p.z_bytes = fbl::load_span(vxz);
+        if (dxbias) p.sums = reinterpret_cast<float*>(static_cast<char*>(ws) + lw.sums);
         const int a = has_xact ? (int)xact : FBL_ACT_NONE;
         e = shared ? run_shared(f32, a, 1, lw.splits, p, reinterpret_cast<float*>(static_cast<char*>(ws) + lw.planes), s)
-            : f32 && !has_xact ? fbl::launch_proj_gemm_f32(0, 1, p, s)
+            : f32 && !has_xact && !dxbias ? fbl::launch_proj_gemm_f32(0, 1, p, s)
                    : run_linear_gemm(f32, a, 1, tile, p, s);
+        if (e == hipSuccess && dxbias) {
+            const int64_t groups = shared ? M : fbl::linear_grad_groups(f32, tile, p);
+            e = fbl::launch_column_sums(f32, p.sums, (int)groups, 1, (int)K, dxbias, nullptr, s);
+        }
     }
     if (e == hipSuccess && dw) {
         fbl::LinearArgs p{};

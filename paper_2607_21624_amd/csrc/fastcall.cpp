@@ -495,23 +495,23 @@ PyObject* linear_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
-// linear_bwd(dy, x, w, z, act, dx, dw, dbias, workspace, stream, need_dx, need_dw, need_bias, x_act, x_z)
+// linear_bwd(dy, x, w, z, act, dx, dw, dbias, workspace, stream, need_dx, need_dw, need_bias, x_act, x_z, dxbias)
 PyObject* linear_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     HANDLE_TH_ERRORS
-    if (n != 15) Py_RETURN_NONE;
+    if (n != 16) Py_RETURN_NONE;
     Args g{a};
     const Tensor *dy = g.tensor(0), *x = g.tensor(1), *w = g.tensor(2), *z = g.tensor_or_none(3);
     const uint32_t act = g.act(4), xact = g.act(13);
     const Tensor *dx = g.tensor_or_none(5), *dw = g.tensor_or_none(6), *db = g.tensor_or_none(7), *ws = g.tensor_or_none(8);
     g.no_stream(9);
     const bool need_x = g.flag(10), need_w = g.flag(11), need_b = g.flag(12);
-    const Tensor* xz = g.tensor_or_none(14);
+    const Tensor *xz = g.tensor_or_none(14), *dxb = g.tensor_or_none(15);
     if (!g.ready() || x->dim() != 2 || w->dim() != 2 || dtype_code(*x) < 0) Py_RETURN_NONE;
     const int64_t M = x->size(0), K = x->size(1), N = w->size(1);
     const at::ScalarType dt = x->scalar_type();
     const int code = dtype_code(*x);
     if (!matrix(x, M, K, dt) || !matrix(w, K, N, dt) || !matrix(dy, M, N, dt) || !matrix(z, M, N, dt) || !matrix(xz, M, K, dt) ||
-        !matrix(dx, M, K, dt) || !matrix(dw, K, N, dt) || !vector(db, N, dt))
+        !matrix(dx, M, K, dt) || !matrix(dw, K, N, dt) || !vector(db, N, dt) || !vector(dxb, K, dt))
         Py_RETURN_NONE;
     Tensor mx, mw, mb;
     if (!dx && need_x) mx = empty({M, K}, dt, *x), dx = &mx;
@@ -519,17 +519,17 @@ PyObject* linear_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (!db && need_b) mb = empty({N}, dt, *x), db = &mb;
     Scratch sc;
     size_t need = 0;
-    if (act != FBL_ACT_NONE || db || ws || (dx && M <= 128)) {
+    if (act != FBL_ACT_NONE || db || dxb || ws || (dx && M <= 128)) {
         if (!ws && fbl_linear_bwd_workspace(code, M, K, N, &need) != FBL_OK) Py_RETURN_NONE;
         if (!sc.set(ws, need, *x)) Py_RETURN_NONE;
     }
     void *s = g.stream(), *py = data(dy), *px = data(x), *pw = data(w), *pz = data(z), *pxz = data(xz), *pdx = data(dx),
-         *pdw = data(dw), *pdb = data(db);
+         *pdw = data(dw), *pdb = data(db), *pdxb = data(dxb);
     const int64_t ldy = row_stride(dy), ldx = row_stride(x), ldw = row_stride(w), ldz = row_stride(z), ldxz = row_stride(xz),
                   lddx = row_stride(dx), lddw = row_stride(dw);
     const fbl_status st = unlocked([&] {
-        return fbl_linear_bwd(code, act, M, K, N, py, ldy, px, ldx, pw, ldw, pz, ldz, xact, pxz, ldxz, pdx, lddx, pdw, lddw, pdb,
-                              sc.p, sc.bytes, s);
+        return fbl_linear_bwd(code, act, M, K, N, py, ldy, px, ldx, pw, ldw, pz, ldz, xact, pxz, ldxz, pdx, lddx, pdxb, pdw, lddw,
+                              pdb, sc.p, sc.bytes, s);
     });
     if (st != FBL_OK) Py_RETURN_NONE;
     return tuple_of<3>({object_or_none(a[5], mx), object_or_none(a[6], mw), object_or_none(a[7], mb)});

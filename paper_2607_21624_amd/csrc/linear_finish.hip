@@ -29,6 +29,7 @@ __global__ __launch_bounds__(256) void linear_finish(LinearArgs p, const float* 
     if constexpr (GRAD) {
         if constexpr (ACT != kActNone) z *= act_grad<ACT, sizeof(T) == 2>((float)static_cast<const T*>(p.z)[m * p.ldz + n]);
         static_cast<T*>(p.c)[m * p.ldc + n] = (T)z;
+        if (p.sums) p.sums[at] = z;  // every row a block of its own
         return;
     }
     if (p.bias) z += (float)static_cast<const T*>(p.bias)[n];

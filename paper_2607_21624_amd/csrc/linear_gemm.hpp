@@ -5,10 +5,12 @@
 //
 //   forward        z = X W + bias;  y = act(z) + residual   (z stored too where the backward needs it)
 //   data gradient  dX = (dZ W^T) act'(zp)                   (zp: the layer before's z)
+//                  and the sums of dX's columns over a tile's rows, that layer's bias gradient
 //
 // The tile loops are those of the projection products; the epilogue works on the
 // accumulators where they are, so the layer writes y once and reads nothing back: a
-// separate pass over y would cost 2 to 3 times its bytes again.  bf16: the sums stay in
+// separate pass over y would cost 2 to 3 times its bytes again.  The sums of dX are taken here, unrounded, for the same
+// reason (4096 x 8192: a pass over dX 13 us).  bf16: the sums stay in
 // fp32 up to the one rounding of y and of z each.
 #include "act.hpp"
 #include "gemm_bf16.hpp"
@@ -29,7 +31,8 @@ struct LinearEp {
         const __amdgpu_buffer_rsrc_t rc = span(p.c, p.c_bytes), rz = span(p.z, p.z_bytes), rr = span(p.res, p.res_bytes);
         const bool has_res = p.res != nullptr, has_z = p.z != nullptr;
         // every turn is at the same columns
-        const int nb = n0 + wn * C::TN * 32 + (threadIdx.x & 63) % (4 * C::TN) * 8;
+        constexpr int LANES = 4 * C::TN;
+        const int nb = n0 + wn * C::TN * 32 + (threadIdx.x & 63) % LANES * 8;
         float b[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         if (!GRAD && p.bias) {
             const bf16x8 x = load8(span(p.bias, (uint32_t)p.N * 2), (uint32_t)nb * 2);  // past N: 0
@@ -52,11 +55,15 @@ struct LinearEp {
                 store8(rc, offset(m, n, p.ldc), v, n, p.N);
             });
         };
+        float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};  // of the lane's columns over its rows
         if constexpr (GRAD && ACT != kActNone) {
             rows([&](int m, int n) __attribute__((always_inline)) { return load8(rz, offset(m, n, p.ldz)); },
-                 [](float (&v)[8], const bf16x8& z) __attribute__((always_inline)) {
+                 [&](float (&v)[8], const bf16x8& z) __attribute__((always_inline)) {
 #pragma unroll
-                     for (int e = 0; e < 8; ++e) v[e] *= act_grad<ACT, true>((float)z[e]);
+                     for (int e = 0; e < 8; ++e) {
+                         v[e] *= act_grad<ACT, true>((float)z[e]);
+                         s[e] += v[e];  // rows past M: products of zeros
+                     }
                  });
         } else if (!GRAD && has_res) {
             rows([&](int m, int n) __attribute__((always_inline)) { return load8(rr, offset(m, n, p.ldr)); },
@@ -66,7 +73,25 @@ struct LinearEp {
                  });
         } else {
             rows([](int, int) __attribute__((always_inline)) { return Nothing{}; },
-                 [](float (&)[8], Nothing) __attribute__((always_inline)) {});
+                 [&](float (&v)[8], Nothing) __attribute__((always_inline)) {
+                     if constexpr (GRAD) {
+#pragma unroll
+                         for (int e = 0; e < 8; ++e) s[e] += v[e];
+                     }
+                 });
+        }
+        if constexpr (GRAD) {
+            if (!p.sums) return;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+#pragma unroll
+                for (int d = LANES; d < 64; d *= 2) s[e] += __shfl_xor(s[e], d);
+            }
+            float* const out = p.sums + (int64_t)(m0 / C::BM * C::WM + wm) * p.N + nb;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                if ((threadIdx.x & 63) < LANES && nb + 4 * h < p.N)  // N is a multiple of 4
+                    *reinterpret_cast<f32x4*>(out + 4 * h) = f32x4{s[4 * h], s[4 * h + 1], s[4 * h + 2], s[4 * h + 3]};
         }
     }
 
@@ -84,6 +109,7 @@ struct LinearEp {
         for (int tn = 0; tn < C::TN; ++tn) {
             const int n = n0 + (wn * C::TN + tn) * 32 + (lane & 31);
             const float b = GRAD ? 0.f : load(rb, n < p.N ? (uint32_t)n * 4 : kNowhere);
+            float s = 0.f;
 #pragma unroll
             for (int tm = 0; tm < C::TM; ++tm) {
                 const auto offset = [&](int r, int64_t ld) __attribute__((always_inline)) {
@@ -100,6 +126,7 @@ struct LinearEp {
                     float v = acc[tm][tn][r];
                     if constexpr (GRAD) {
                         if constexpr (ACT != kActNone) v *= act_grad<ACT, false>(x[r]);
+                        s += v;  // rows past M: products of zeros
                     } else {
                         v += b;
                         if (has_z) __builtin_amdgcn_raw_buffer_store_b32(__float_as_int(v), rz, offset(r, p.ldz), 0, 0);
@@ -108,6 +135,10 @@ struct LinearEp {
                     }
                     __builtin_amdgcn_raw_buffer_store_b32(__float_as_int(v), rc, offset(r, p.ldc), 0, 0);
                 }
+            }
+            if constexpr (GRAD) {
+                s += other_half(s);
+                if (p.sums && g == 0 && n < p.N) p.sums[(int64_t)(m0 / C::t.bm * C::t.wm + wm) * p.N + n] = s;
             }
         }
     }
@@ -122,6 +153,15 @@ hipError_t launch_linear_gemm<FBL_ACT>(int grad, int tile, const LinearArgs& p, 
 }
 
 #if FBL_ACT == 0
+int64_t linear_grad_groups(int f32, int tile, const LinearArgs& p) {
+    if (f32) {
+        const F32Tile& t = kF32Tiles[f32_tile(p)];
+        return ((int64_t)p.M + t.bm - 1) / t.bm * t.wm;
+    }
+    const GemmTile& t = kGemmTiles[tile];
+    return ((int64_t)p.M + t.bm - 1) / t.bm * t.wm;
+}
+
 // A weight gradient, its tiles written by rows.
 hipError_t launch_weight_gemm(int tile, const LinearArgs& p, hipStream_t stream) {
     return launch_gemm_tile<true, false, LinearEp<kActNone, false>>(tile, p, stream);

@@ -117,6 +117,7 @@ struct LinearArgs : GemmArgs {
     void* z;
     int64_t ldr, ldz;
     uint32_t res_bytes, z_bytes;
+    float* sums;  // data gradient: [groups][N] sums of c down blocks of rows (linear_grad_groups), or nullptr
 };
 
 // dz = dy act'(z) over M x N; part, where not nullptr, gets [groups][N] sums down blocks of `rows` rows.

@@ -201,7 +201,7 @@ def _load() -> ctypes.CDLL:
     lib.fbl_linear_bwd_workspace.argtypes = [i32, i64, i64, i64, sizep]
     lib.fbl_linear_bwd_workspace.restype = ctypes.c_int
     lib.fbl_linear_bwd.argtypes = [i32, u32, i64, i64, i64, vp, i64, vp, i64, vp, i64, vp, i64, u32, vp, i64, vp, i64, vp,
-                                   i64, vp, vp, size, vp]
+                                   vp, i64, vp, vp, size, vp]
     lib.fbl_linear_bwd.restype = ctypes.c_int
     lib.fbl_linear_loss_workspace.argtypes = [i32, u32] + [i64] * 5 + [sizep]
     lib.fbl_linear_loss_workspace.restype = ctypes.c_int
@@ -1032,16 +1032,19 @@ def linear_bwd_workspace(x, w) -> int:
 
 
 def linear_bwd(dy, x, w, z=None, act: str = "none", dx=None, dw=None, dbias=None, workspace=None, stream=None,
-               need_dx: bool = True, need_dw: bool = True, need_bias: bool = True, x_act: str = "none", x_z=None):
+               need_dx: bool = True, need_dw: bool = True, need_bias: bool = True, x_act: str = "none", x_z=None, dxbias=None):
     """Gradients of linear_fwd: returns (dx, dw, dbias), each None where not needed.  z is the
     forward's pre-activation (None for act "none"); the residual's gradient is dy.  Where x
-    itself is x_act(x_z), dx can be the gradient of x_z."""
-    done = _FAST.linear_bwd(dy, x, w, z, act, dx, dw, dbias, workspace, stream, need_dx, need_dw, need_bias, x_act, x_z)
+    itself is x_act(x_z), dx can be the gradient of x_z; dxbias [K], where given, receives the
+    sums of dx over its rows, then the gradient of the bias in x_z."""
+    done = _FAST.linear_bwd(dy, x, w, z, act, dx, dw, dbias, workspace, stream, need_dx, need_dw, need_bias, x_act, x_z,
+                            dxbias)
     if done is not None:
         return done
     import torch
     where = "linear_bwd"
-    _check_device(where, stream, dy=dy, x=x, w=w, z=z, dx=dx, dw=dw, dbias=dbias, workspace=workspace, x_z=x_z)
+    _check_device(where, stream, dy=dy, x=x, w=w, z=z, dx=dx, dw=dw, dbias=dbias, workspace=workspace, x_z=x_z,
+                  dxbias=dxbias)
     ldx = _matrix(x, where, "x")
     M, K = x.shape
     dt, code, xcode = _dtype_code(x), _act_code(act, where), _act_code(x_act, where)
@@ -1061,12 +1064,13 @@ def linear_bwd(dy, x, w, z=None, act: str = "none", dx=None, dw=None, dbias=None
     lddx = 0 if dx is None else _matrix(dx, where, "dx", (M, K), x)
     lddw = 0 if dw is None else _matrix(dw, where, "dw", (K, N), x)
     _vector(dbias, where, "dbias", N, x.dtype)
+    _vector(dxbias, where, "dxbias", K, x.dtype)
     ws, ws_bytes = None, 0
-    if code != FBL_ACT_NONE or dbias is not None or workspace is not None or (dx is not None and M <= 128):
+    if code != FBL_ACT_NONE or dbias is not None or dxbias is not None or workspace is not None or (dx is not None and M <= 128):
         need = 0 if workspace is not None else linear_bwd_workspace(x, w)
         ws, ws_bytes = _scratch(workspace, need, where, x, stream)
     _call("fbl_linear_bwd", x, stream, dt, code, M, K, N, _ptr(dy), lddy, _ptr(x), ldx, _ptr(w), ldw, _ptr(z), ldz,
-          xcode, _ptr(x_z), ldxz, _ptr(dx), lddx, _ptr(dw), lddw, _ptr(dbias), _ptr(ws), ws_bytes)
+          xcode, _ptr(x_z), ldxz, _ptr(dx), lddx, _ptr(dxbias), _ptr(dw), lddw, _ptr(dbias), _ptr(ws), ws_bytes)
     return dx, dw, dbias
 
 

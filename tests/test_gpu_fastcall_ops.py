@@ -65,6 +65,7 @@ def test_native_equals_general(monkeypatch, dt):
             _both(monkeypatch, lambda: pkg.linear_fwd(x, w1, b1, act, r, z=z))
             _both(monkeypatch, lambda: pkg.linear_bwd(r, x, w1, z, act))
             _both(monkeypatch, lambda: pkg.linear_bwd(r, x, w1, x_act=act, x_z=x, need_bias=False, need_dw=False))
+            _both(monkeypatch, lambda: pkg.linear_bwd(r, x, w1, x_act=act, x_z=x, dxbias=torch.empty_like(x[0])))
     _both(monkeypatch, lambda: pkg.linear_fwd(g(4, 4096, scale=0) + 1, g(4096, 128, scale=0) + 1))  # shared contraction
     one = torch.ones((), device="cuda")
     for w in (g(64, 200), g(200, 64).t(), g(200, 80)[:, :64].t(), g(64, 208)[:, :200]):

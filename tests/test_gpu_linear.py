@@ -224,6 +224,35 @@ def test_gradient_of_the_previous_pre_activation(M, K, N, act, dt):
     check("dxz", got, prod * d, np.abs(d) * _sum_bound(ref[4], ref[1].T) + np.abs(prod) * 2.0 ** -20 * (1 + np.abs(xzr)))
 
 
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("act", ["none", "gelu"])
+@pytest.mark.parametrize("M,K,N", [(1, 264, 64), (3, 12, 264), (40, 1028, 8200), (77, 260, 64), (300, 100, 384), (1000, 2052, 200),
+                                   (4096, 512, 264), (2000, 8192, 64), (1001, 8192, 64), (2050, 1000, 2048),
+                                   (2050, 256, 512), (1000, 64, 256), (4100, 8200, 128), (4096, 4096, 1024)])
+def test_sums_of_the_data_gradient(M, K, N, act, dt):
+    """dxbias: dx summed over its rows before its rounding, with tiles of every kind and with shared contractions.
+    Each dx is off by its product's bound and act's; then M fp32 additions."""
+    dt = DTYPES[dt]
+    rng = np.random.default_rng(M + N)
+    xz, xzr = rounded(rng, (M, K), dt)
+    (x, w, _, _, dy), ref = _case(M, K, N, dt, "none", False, False)
+    buf = torch.full((K + 8,), 7.0, dtype=dt, device="cuda")
+    new = lambda t: padded(t, -K % 8)[0]  # rows of whole 16-byte chunks
+    kw = dict(need_dw=False, need_bias=False, x_act=act, x_z=None if act == "none" else new(xz))
+    dx = fbl.linear_bwd(dy, new(x), w, dx=new(torch.zeros_like(x)), dxbias=buf[:K], **kw)[0]
+    assert torch.equal(dx, fbl.linear_bwd(dy, new(x), w, dx=new(torch.zeros_like(x)), **kw)[0]) or (dt == torch.float32 and act == "none")
+    assert bool((buf[K:] == 7.0).all())
+    d = oracle.act_grad(xzr, act) if act != "none" else np.ones_like(xzr)
+    prod = ref[4] @ ref[1].T
+    off = np.abs(d) * _sum_bound(ref[4], ref[1].T) + (0 if act == "none" else np.abs(prod) * 2.0 ** -20 * (1 + np.abs(xzr)))
+    dxr = prod * d
+    check("dx", dx, dxr, off)
+    check("dxbias", buf[:K], dxr.sum(0), off.sum(0) + (M + 16) * 2.0 ** -24 * np.abs(dxr).sum(0))
+    again = torch.empty(K, dtype=dt, device="cuda")
+    fbl.linear_bwd(dy, new(x), w, dx=new(torch.zeros_like(x)), dxbias=again, **kw)
+    assert torch.equal(again, buf[:K])
+
+
 @pytest.mark.parametrize("act", ACTS)
 def test_extreme_pre_activations(act):
     """z far out on both sides: saturated values and derivatives of 0 and 1, nothing non-finite."""
@@ -264,8 +293,9 @@ def test_autograd_and_mlp():
     h = fbl.linear_fwd(t["x"].view(M, K), t["w1"], t["b1"], "gelu", z=z)
     y2 = fbl.linear_fwd(h, t["w2"], t["b2"], residual=t["r"].view(M, K))
     assert torch.equal(y.view(M, K), y2)
-    dz, dw2, db2 = fbl.linear_bwd(t["dy"].view(M, K), h, t["w2"], x_act="gelu", x_z=z)
-    dx, dw1, db1 = fbl.linear_bwd(dz, t["x"].view(M, K), t["w1"])
+    db1 = torch.empty(N, dtype=dt, device="cuda")
+    dz, dw2, db2 = fbl.linear_bwd(t["dy"].view(M, K), h, t["w2"], x_act="gelu", x_z=z, dxbias=db1)
+    dx, dw1, _ = fbl.linear_bwd(dz, t["x"].view(M, K), t["w1"])
     for k, g in (("x", dx), ("w1", dw1), ("b1", db1), ("w2", dw2), ("b2", db2), ("r", t["dy"])):
         assert torch.equal(leaf[k].grad, g.view_as(t[k])), k
     f = {k: v.double().cpu().numpy().reshape(-1, v.shape[-1]) if v.dim() > 1 else v.double().cpu().numpy() for k, v in t.items()}

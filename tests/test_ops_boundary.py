@@ -89,8 +89,8 @@ def lin_fwd(**kw):
 
 def lin_bwd(**kw):
     return LIB.fbl_linear_bwd(*_merge(dict(dt=BF16, act=2, M=8, K=64, N=64, dy=at(1), lddy=64, x=at(2), ldx=64, w=at(3),
-                                           ldw=64, z=at(4), ldz=64, xact=3, xz=at(5), ldxz=64, dx=at(6), lddx=64, dw=at(7),
-                                           lddw=64, dbias=at(8), ws=at(9), ws_bytes=1 << 19, stream=None), kw))
+                                           ldw=64, z=at(4), ldz=64, xact=3, xz=at(5), ldxz=64, dx=at(6), lddx=64, dxbias=None,
+                                           dw=at(7), lddw=64, dbias=at(8), ws=at(9), ws_bytes=1 << 19, stream=None), kw))
 
 
 @pytest.mark.parametrize("kw,status", [
@@ -115,7 +115,10 @@ def test_linear_fwd_refusals(kw, status):
     (dict(ws_bytes=1000), F.FBL_ERR_WORKSPACE), (dict(ws=at(9, 8)), F.FBL_ERR_ALIGN), (dict(lddx=32), F.FBL_ERR_LAYOUT),
     (dict(dbias=at(8, 1)), F.FBL_ERR_ALIGN), (dict(N=68, lddy=72, ldw=72, ldz=72, lddw=72), F.FBL_ERR_UNSUPPORTED),
     (dict(dx=at(1)), F.FBL_ERR_ARG), (dict(dw=at(6)), F.FBL_ERR_ARG), (dict(dbias=at(7)), F.FBL_ERR_ARG),
-    (dict(ws=at(5)), F.FBL_ERR_ARG), (dict(dx=at(5)), F.FBL_ERR_ARG),
+    (dict(ws=at(5)), F.FBL_ERR_ARG), (dict(dx=at(5)), F.FBL_ERR_ARG), (dict(dxbias=at(10, 1)), F.FBL_ERR_ALIGN),
+    (dict(dxbias=at(6)), F.FBL_ERR_ARG), (dict(dxbias=at(8)), F.FBL_ERR_ARG), (dict(dxbias=at(3)), F.FBL_ERR_ARG),
+    (dict(dxbias=at(10), dx=None), F.FBL_ERR_NULL), (dict(dxbias=at(9)), F.FBL_ERR_ARG),
+    (dict(act=0, dbias=None, dxbias=at(10), ws=None), F.FBL_ERR_WORKSPACE),
 ])
 def test_linear_bwd_refusals(kw, status):
     assert lin_bwd(**kw) == status
