@@ -157,12 +157,12 @@ struct HeadFwd {
     static FBL_DEV void done(const Args& p, uint32_t, f32x16 (&acc)[C::TN][C::TM], int m0, int n0, int wm, int wn) {
         extern __shared__ __attribute__((aligned(1024))) unsigned char gemm_smem[];
         constexpr int BM = C::BM, BN = C::BN;
-        head_stats<C::TN, C::TM, C::WN, BM, 64 * C::NW>(p, acc, (float2*)gemm_smem, n0 + wn * C::TN * 32,
+        head_stats<C::TN, C::TM, C::WN, BM, 64 * C::WM * C::WN>(p, acc, (float2*)gemm_smem, n0 + wn * C::TN * 32,
                                                         m0 + wm * C::TM * 32, wn, wm * C::TM * 32, n0 / BN, m0);
     }
     template <typename C>
     static FBL_DEV void done(const Args& p, float* smem, f32x16 (&acc)[C::TM][C::TN], int m0, int n0, int wm, int wn) {
-        head_stats<C::TM, C::TN, C::t.wm, C::t.bn, C::NT>(p, acc, (float2*)smem, m0 + wm * C::TM * 32, n0 + wn * C::TN * 32,
+        head_stats<C::TM, C::TN, C::t.wm, C::t.bn, 64 * C::t.wm * C::t.wn>(p, acc, (float2*)smem, m0 + wm * C::TM * 32, n0 + wn * C::TN * 32,
                                                           wm, wn * C::TN * 32, m0 / C::t.bm, n0);
     }
 };
@@ -273,16 +273,35 @@ struct SumPieces {
     }
 };
 
-template <typename T>
+// c = sum of the planes times *scale, in a fixed order.  A thread adds an element's planes; where there are many, SLICES
+// threads take every SLICES-th each, for a chain of loads as much shorter, and their sums are added one after the
+// other.
+template <typename T, int SLICES>
 __global__ __launch_bounds__(256) void sum_planes(const float* planes, int splits, int64_t M, int64_t N, const float* scale,
                                                   T* c, int64_t ldc) {
-    const int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    constexpr int COLS = 256 / SLICES;
+    __shared__ float part[SLICES][COLS];
+    const int l = threadIdx.x % COLS, r = threadIdx.x / COLS;
+    const int64_t n = (int64_t)blockIdx.x * COLS + l, at = n < N ? n : N - 1;
     const float f = scale ? *scale : 1.f;
-    if (n >= N) return;
     for (int64_t m = blockIdx.y; m < M; m += gridDim.y) {
+        const auto plane = [&](int i) { return planes[((int64_t)i * M + m) * N + at]; };
         float s = 0.f;
-        for (int i = 0; i < splits; ++i) s += planes[((int64_t)i * M + m) * N + n];
-        c[m * ldc + n] = (T)(s * f);
+        int i = r;
+        for (; i + 3 * SLICES < splits; i += 4 * SLICES) {
+            const float a = plane(i), b = plane(i + SLICES), d = plane(i + 2 * SLICES), e = plane(i + 3 * SLICES);
+            s += a, s += b, s += d, s += e;
+        }
+        for (; i < splits; i += SLICES) s += plane(i);
+        if constexpr (SLICES > 1) {
+            __syncthreads();
+            part[r][l] = s;
+            __syncthreads();
+            if (r > 0) continue;
+#pragma unroll
+            for (int k = 1; k < SLICES; ++k) s += part[k][l];
+        }
+        if (n < N) c[m * ldc + n] = (T)(s * f);
     }
 }
 
@@ -290,6 +309,8 @@ template <typename EP>
 hipError_t launch_head(int f32, int table, HeadArgs& p, hipStream_t s) {
     if (!f32) {  // C = X W: tokens are the rows
         switch (p.shape) {
+            case 9: return table ? launch_gemm_bf16<9, false, true, EP>(p, s) : launch_gemm_bf16<9, false, false, EP>(p, s);
+            case 16: return table ? launch_gemm_bf16<16, false, true, EP>(p, s) : launch_gemm_bf16<16, false, false, EP>(p, s);
             case 15: return table ? launch_gemm_bf16<15, false, true, EP>(p, s) : launch_gemm_bf16<15, false, false, EP>(p, s);
             case 6: return table ? launch_gemm_bf16<6, false, true, EP>(p, s) : launch_gemm_bf16<6, false, false, EP>(p, s);
             case 4: return table ? launch_gemm_bf16<4, false, true, EP>(p, s) : launch_gemm_bf16<4, false, false, EP>(p, s);
@@ -298,8 +319,13 @@ hipError_t launch_head(int f32, int table, HeadArgs& p, hipStream_t s) {
     }
     // C = W^T X^T: the vocabulary is the rows, so that tokens lie along the lanes here too
     std::swap(p.a, p.b), std::swap(p.lda, p.ldb), std::swap(p.a_bytes, p.b_bytes), std::swap(p.M, p.N);
-    if (p.shape == 2) return table ? launch_gemm_f32<2, false, true, EP>(p, s) : launch_gemm_f32<2, true, true, EP>(p, s);
-    return table ? launch_gemm_f32<0, false, true, EP>(p, s) : launch_gemm_f32<0, true, true, EP>(p, s);
+    switch (p.shape) {
+        case 2: return table ? launch_gemm_f32<2, false, true, EP>(p, s) : launch_gemm_f32<2, true, true, EP>(p, s);
+        case 3: return table ? launch_gemm_f32<3, false, true, EP>(p, s) : launch_gemm_f32<3, true, true, EP>(p, s);
+        case 4: return table ? launch_gemm_f32<4, false, true, EP>(p, s) : launch_gemm_f32<4, true, true, EP>(p, s);
+        case 5: return table ? launch_gemm_f32<5, false, true, EP>(p, s) : launch_gemm_f32<5, true, true, EP>(p, s);
+        default: return table ? launch_gemm_f32<0, false, true, EP>(p, s) : launch_gemm_f32<0, true, true, EP>(p, s);
+    }
 }
 
 // The tile of a split product: as narrow as the few rows that split one.
@@ -309,14 +335,23 @@ constexpr int kSplitTileF32 = 4;
 
 }  // namespace
 
-// Tiles whose wavefronts each have the whole contraction, of 32, 64, 128 and 256 tokens: the one of least modelled
-// time (gemm_cost.hpp).  Two workgroups a CU, so that one's exponentials and stores run beside the other's products,
-// do not pay for their narrower tiles: 4096 x 1024 x 50257 forward 451 us with 256 x 256, 495 with 256 x 128 or 128 x
-// 256 in steps of 32, 581 with 128 x 128; dz 141, 159, 156 and 171 a piece.  fp32: 128 x 128 where that makes two workgroups for each CU, else 64 x 64.
+// bf16: of tiles of 32, 64, 128 and 256 tokens, the narrower two also with a contraction split among their wavefronts,
+// the one of least modelled time (gemm_cost.hpp; 4 tokens x 3600 x 288 forward 25.2 us without the split ones, 17.0
+// with, 16 x 8192 x 128 43.1 and 24.5, 300 x 4096 x 1000 28.0 and 19.8).  Two workgroups a CU, so that one's exponentials
+// and stores run beside the other's products, do not pay for their narrower tiles: 4096 x 1024 x 50257 forward 451
+// us with 256 x 256, 495 with 256 x 128 or 128 x 256 in steps of 32, 581 with 128 x 128; dz 141, 159, 156 and 171 a
+// piece.
+// fp32: 128 x 128 where that makes two workgroups for each CU; 64 x 64 with more than 320 of them (300 x 2000 x 5000
+// forward 88.4 us, 91.1 with 64 x 32 on half a step a wavefront, 85.5 with 32 x 32 on a quarter, but 1000 x 700 x 4000
+// 71, 85 and 84); 64 x 32 down to 160 (250 x 500 x 5003 30.6, 29.0 and 32.3); below, 32 x 32 on a quarter, or for 1024
+// and more on an eighth (500 x 512 x 1000 22.4, 17.7, 16.6 and 17.5; 128 x 2048 x 1024 53, 35, 27 and 23).
 int head_tile(int f32, int table, int64_t M, int64_t V, int64_t K) {
-    if (f32) return ((M + 127) / 128) * ((V + 127) / 128) >= 512 ? 0 : 2;
+    if (f32) {
+        const auto tiles = [&](int64_t n) { return ((M + n - 1) / n) * ((V + n - 1) / n); };
+        return tiles(128) >= 512 ? 0 : tiles(64) > 320 ? 2 : tiles(64) > 160 ? 3 : K < 1024 ? 4 : 5;
+    }
     int best = 19;
-    for (int t : {4, 6, 15})
+    for (int t : {4, 6, 15, 9, 16})
         if (gemm_cost(t, table, M, V, K) < gemm_cost(best, table, M, V, K)) best = t;
     return best;
 }
@@ -374,10 +409,14 @@ hipError_t launch_sum_gemm_f32(int b_nmajor, const SumArgs& p, hipStream_t s) {
 
 hipError_t launch_sum_planes(int f32, const float* planes, int splits, int64_t M, int64_t N, const float* scale, void* c,
                              int64_t ldc, hipStream_t s) {
-    const dim3 grid((unsigned)((N + 255) / 256), (unsigned)std::min<int64_t>(M, 4096));
-    if (f32) hipLaunchKernelGGL(sum_planes<float>, grid, dim3(256), 0, s, planes, splits, M, N, scale, (float*)c, ldc);
-    else hipLaunchKernelGGL(sum_planes<bf16>, grid, dim3(256), 0, s, planes, splits, M, N, scale, (bf16*)c, ldc);
-    return hipGetLastError();
+    const auto run = [&](auto kernel, int cols, auto* out) {
+        const dim3 grid((unsigned)((N + cols - 1) / cols), (unsigned)std::min<int64_t>(M, 4096));
+        hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, planes, splits, M, N, scale, out, ldc);
+        return hipGetLastError();
+    };
+    const bool many = splits >= 16;
+    if (f32) return many ? run(sum_planes<float, 8>, 32, (float*)c) : run(sum_planes<float, 1>, 256, (float*)c);
+    return many ? run(sum_planes<bf16, 8>, 32, (bf16*)c) : run(sum_planes<bf16, 1>, 256, (bf16*)c);
 }
 
 }  // namespace fbl

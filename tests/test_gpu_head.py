@@ -118,6 +118,15 @@ def test_ce_f32(M, K, V, table):
     _ce(M, K, V, torch.float32, table, ignored=0.0 if M < 10 else 0.2)
 
 
+@pytest.mark.parametrize("table", [False, True])
+@pytest.mark.parametrize("M,K,V,dt", [(4, 3600, 288, "bf16"), (16, 8192, 128, "bf16"), (100, 2048, 1000, "bf16"),
+                                      (300, 4096, 1000, "bf16"), (2, 64, 60824, "bf16"), (5, 1100, 300, "f32"),
+                                      (70, 1030, 333, "f32"), (130, 40, 5003, "f32"), (3, 40, 30011, "f32")])
+def test_ce_few_tiles(M, K, V, dt, table):
+    """A contraction split among a tile's wavefronts, a vocabulary among workgroups: many planes of dX."""
+    _ce(M, K, V, DTYPES[dt], table)
+
+
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
 def test_ce_per_row_gradient(dt):
     _ce(70, 64, 520, DTYPES[dt], True, dloss=np.random.default_rng(0).normal(size=70).astype(np.float32))
