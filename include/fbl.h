@@ -653,7 +653,7 @@ fbl_status fbl_layer_norm_bwd(int32_t dtype, int64_t M, int64_t N, const void* d
  * products; dbias and dxbias sum dz and dx in fp32 unrounded.  x may be NULL without dw, w without dx,
  * z with act NONE.  The workspace (16-byte aligned, fbl_linear_bwd_workspace
  * bytes) is needed where act is not NONE or dbias or dxbias is wanted, else it may be NULL; with it, workgroups share the
- * contraction of dx for a few tokens.
+ * contraction of dx for a few tokens and of a small dw for many.
  *
  * Row strides in elements, at least the width.  fp32: any extents, natural
  * alignment.  bf16: 16-byte aligned pointers (bias too) and rows; forward K a

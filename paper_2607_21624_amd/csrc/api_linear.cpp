@@ -78,14 +78,15 @@ size_t few_ws(int splits, int64_t M, int64_t N) { return splits > 1 ? (size_t)sp
 // of them as any tile writes, linear_grad_groups, or one for each of a few tokens).
 struct LinearWs {
     size_t dz, planes, sums, total;
-    int splits;
+    int splits, wsplits;  // of dx and of dw: the planes are used by one after the other
 };
 LinearWs linear_ws(int f32, int64_t M, int64_t K, int64_t N) {
     LinearWs w;
     w.splits = few_splits(f32, M, N, K);
     w.dz = align256((size_t)act_grid(f32, M, N).groups * (size_t)N * 4);
     w.planes = w.dz + align256((size_t)M * (size_t)N * (f32 ? 4 : 2));
-    w.sums = w.planes + align256(few_ws(w.splits, M, K));
+    w.wsplits = fbl::weight_splits(f32, M, K, N, f32 ? 0 : fbl::weight_tile(M, K, N));
+    w.sums = w.planes + align256(std::max(few_ws(w.splits, M, K), few_ws(w.wsplits, K, N)));
     w.total = w.sums + (size_t)(w.splits > 1 ? M : M / 32 + 4) * (size_t)K * 4;
     return w;
 }
@@ -181,8 +182,9 @@ fbl_status fbl_linear_bwd(int32_t dtype, uint32_t act, int64_t M, int64_t K, int
     if (es == 2 && ((dx && (N % 8 || K % 4)) || (dw && N % 4))) return FBL_ERR_UNSUPPORTED;
     // what is needed of the workspace: partial sums for the bias, dz where an activation makes it
     const LinearWs lw = linear_ws(f32, M, K, N);
-    const bool pass = has_act ? (dx || dw || dbias) : dbias != nullptr, shared = dx && lw.splits > 1 && ws;
-    const size_t need = pass || shared || dxbias ? lw.total : 0;
+    const bool pass = has_act ? (dx || dw || dbias) : dbias != nullptr, shared = dx && lw.splits > 1 && ws,
+               wshared = dw && lw.wsplits > 1 && ws;
+    const size_t need = pass || shared || wshared || dxbias ? lw.total : 0;
     if (need && (!ws || ws_bytes < need)) return FBL_ERR_WORKSPACE;
     const RowsView vws{need ? ws : nullptr, 1, (int64_t)need, (int64_t)need + 1, 1};
     if (vws.begin() % 16) return FBL_ERR_ALIGN;
@@ -223,7 +225,15 @@ fbl_status fbl_linear_bwd(int32_t dtype, uint32_t act, int64_t M, int64_t K, int
             e = fbl::launch_column_sums(f32, p.sums, (int)groups, 1, (int)K, dxbias, nullptr, s);
         }
     }
-    if (e == hipSuccess && dw) {
+    if (e == hipSuccess && wshared) {
+        fbl::SumArgs q{};
+        fbl::product(q, FBL_PROJ_BWD_WEIGHT, vx, g, vdw, M, K, N);
+        q.sum = reinterpret_cast<float*>(static_cast<char*>(ws) + lw.planes), q.lds = N;
+        q.sum_bytes = (uint32_t)(K * N * 4);
+        q.first = 1, q.splits = lw.wsplits, q.share = (int)(((M + q.splits - 1) / q.splits + 63) / 64 * 64);
+        e = fbl::launch_weight_shares(f32, q, s);
+        if (e == hipSuccess) e = fbl::launch_sum_planes(f32, q.sum, q.splits, K, N, nullptr, dw, lddw, s);
+    } else if (e == hipSuccess && dw) {
         fbl::LinearArgs p{};
         fbl::product(p, FBL_PROJ_BWD_WEIGHT, vx, g, vdw, M, K, N);
         e = f32 ? fbl::launch_proj_gemm_f32(1, 0, p, s) : fbl::launch_weight_gemm(fbl::weight_tile(M, K, N), p, s);

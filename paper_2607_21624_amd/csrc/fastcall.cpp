@@ -519,7 +519,7 @@ PyObject* linear_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (!db && need_b) mb = empty({N}, dt, *x), db = &mb;
     Scratch sc;
     size_t need = 0;
-    if (act != FBL_ACT_NONE || db || dxb || ws || (dx && M <= 128)) {
+    if (act != FBL_ACT_NONE || db || dxb || ws || (dx && M <= 128) || (dw && K * N <= 1 << 19)) {
         if (!ws && fbl_linear_bwd_workspace(code, M, K, N, &need) != FBL_OK) Py_RETURN_NONE;
         if (!sc.set(ws, need, *x)) Py_RETURN_NONE;
     }

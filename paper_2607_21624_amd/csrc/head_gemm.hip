@@ -380,6 +380,32 @@ int sum_splits(int f32, int b_nmajor, int64_t M, int64_t N, int64_t kc, int tile
     return (int)std::max<int64_t>(1, std::min<int64_t>((want + tiles / 2) / tiles, kc / (f32 ? 256 : 512)));
 }
 
+// A small weight gradient has few tiles and all tokens for its contraction.  Its shares are of 128 x 128 tiles, or 64 x
+// 64 for a narrow layer (fp32: 64 x 64), up to two workgroups a CU in all, with 512 tokens each at least (fp32 256): bf16
+// where the model has them 10% below, fp32 from 2048 tokens (alone and shared, us: bf16 32768 tokens 128 x 128 75 and
+// 24, 8192 tokens 256 x 256 22.1 and 14.4, 8027 tokens 328 x 320 24.9 and 20.0; fp32 32768 tokens 128 x 128 199 and 28,
+// 8192 tokens 256 x 256 52 and 18, 4096 tokens 512 x 1024 52 and 49, 2048 tokens 256 x 256 15.7 and 12.0).
+static int weight_split_tile(int f32, int64_t K, int64_t N) { return f32 ? 2 : K <= 64 || N <= 64 ? 7 : 4; }
+
+int weight_splits(int f32, int64_t M, int64_t K, int64_t N, int tile) {
+    if (K * N > kWeightSplitMax) return 1;
+    const int t = weight_split_tile(f32, K, N), bm = f32 ? kF32Tiles[t].bm : kGemmTiles[t].bm,
+              bn = f32 ? kF32Tiles[t].bn : kGemmTiles[t].bn;
+    const int64_t rows = (K + bm - 1) / bm, tiles = rows * ((N + bn - 1) / bn);
+    const int64_t s = std::min<int64_t>(512 / tiles, M / (f32 ? 256 : 512));
+    if (s < 2) return 1;
+    if (f32) return M >= 2048 ? (int)s : 1;
+    const double shared = gemm_cost(t, 2, rows * bm * s, N, M / s) + 3.0 + 8.0 * (double)(s * K * N) / 4.5e6;
+    return shared < 0.9 * gemm_cost(tile, 2, K, N, M) ? (int)s : 1;
+}
+
+hipError_t launch_weight_shares(int f32, const SumArgs& p, hipStream_t s) {
+    using EP = SumPieces<true>;
+    const int t = weight_split_tile(f32, p.M, p.N);
+    if (f32) return launch_gemm_f32<2, true, false, EP>(p, s, p.splits);
+    return t == 4 ? launch_gemm_bf16<4, true, false, EP>(p, s, p.splits) : launch_gemm_bf16<7, true, false, EP>(p, s, p.splits);
+}
+
 hipError_t launch_sum_gemm(int a_kmajor, int b_nmajor, int tile, const SumArgs& p, hipStream_t s) {
     if (p.splits > 1) {
         const auto run = [&](auto bt_c) {

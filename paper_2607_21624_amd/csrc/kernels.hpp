@@ -136,6 +136,10 @@ hipError_t launch_sum_gemm(int a_kmajor, int b_nmajor, int tile, const SumArgs& 
 hipError_t launch_sum_gemm_f32(int b_nmajor, const SumArgs& p, hipStream_t stream);
 // Workgroups that should share the contraction kc of an M x N product's tiles, which alone would run with `tile` (bf16).
 int sum_splits(int f32, int b_nmajor, int64_t M, int64_t N, int64_t kc, int tile);
+// The same for a weight gradient of K x N over M tokens (bf16: alone with `tile`), and its launch for p.splits > 1.
+constexpr int64_t kWeightSplitMax = (int64_t)1 << 19;  // K N
+int weight_splits(int f32, int64_t M, int64_t K, int64_t N, int tile);
+hipError_t launch_weight_shares(int f32, const SumArgs& p, hipStream_t stream);
 // C [M][ldc] = scale * the sum of the planes [splits][M][N] (scale nullptr: 1).
 hipError_t launch_sum_planes(int f32, const float* planes, int splits, int64_t M, int64_t N, const float* scale, void* c,
                              int64_t ldc, hipStream_t stream);

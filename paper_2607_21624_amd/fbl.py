@@ -1066,7 +1066,8 @@ def linear_bwd(dy, x, w, z=None, act: str = "none", dx=None, dw=None, dbias=None
     _vector(dbias, where, "dbias", N, x.dtype)
     _vector(dxbias, where, "dxbias", K, x.dtype)
     ws, ws_bytes = None, 0
-    if code != FBL_ACT_NONE or dbias is not None or dxbias is not None or workspace is not None or (dx is not None and M <= 128):
+    if code != FBL_ACT_NONE or dbias is not None or dxbias is not None or workspace is not None \
+            or (dx is not None and M <= 128) or (dw is not None and K * N <= 1 << 19):
         need = 0 if workspace is not None else linear_bwd_workspace(x, w)
         ws, ws_bytes = _scratch(workspace, need, where, x, stream)
     _call("fbl_linear_bwd", x, stream, dt, code, M, K, N, _ptr(dy), lddy, _ptr(x), ldx, _ptr(w), ldw, _ptr(z), ldz,

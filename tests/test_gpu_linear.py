@@ -77,7 +77,7 @@ def _run(M, K, N, dt, act, bias=True, residual=True, tile=-1):
 
 
 @pytest.mark.parametrize("act", ACTS)
-@pytest.mark.parametrize("M,K,N", [(1, 64, 64), (3, 256, 520), (33, 72, 200), (200, 512, 264), (1001, 128, 96), (257, 1024, 768)])
+@pytest.mark.parametrize("M,K,N", [(1, 64, 64), (3, 256, 520), (33, 72, 200), (200, 512, 264), (1001, 128, 96), (257, 1024, 768), (9000, 72, 136)])
 def test_bf16(M, K, N, act):
     _run(M, K, N, torch.bfloat16, act)
 
@@ -222,6 +222,21 @@ def test_gradient_of_the_previous_pre_activation(M, K, N, act, dt):
     d = oracle.act_grad(xzr, act)
     prod = ref[4] @ ref[1].T
     check("dxz", got, prod * d, np.abs(d) * _sum_bound(ref[4], ref[1].T) + np.abs(prod) * 2.0 ** -20 * (1 + np.abs(xzr)))
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("M,K,N", [(8200, 64, 72), (9001, 132, 260), (4099, 256, 264), (20000, 8, 16)])
+def test_small_weights_of_many_tokens(M, K, N, dt):
+    """dw with its contraction shared among workgroups; written between the guards of a larger matrix."""
+    dt = DTYPES[dt]
+    (x, w, _, _, dy), ref = _case(M, K, N, dt, "none", False, False)
+    row = lambda t: padded(t, 8 + -t.shape[1] % 8)[0]
+    view, buf = padded(torch.zeros(K, N, dtype=dt, device="cuda"), 8 + -N % 8, 9.0)
+    dx, dw, _ = fbl.linear_bwd(row(dy), row(x), row(w), dw=view, need_dx=False, need_bias=False)
+    check("dw", dw, ref[0].T @ ref[4], _sum_bound(ref[0].T, ref[4]))
+    assert bool((buf[:, N:] == 9.0).all()) and bool((buf[-1] == 9.0).all())
+    again = fbl.linear_bwd(row(dy), row(x), row(w), dw=row(torch.zeros_like(w)), need_dx=False, need_bias=False)[1]
+    assert torch.equal(again, dw)
 
 
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
