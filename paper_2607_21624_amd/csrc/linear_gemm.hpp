@@ -42,6 +42,7 @@ struct LinearEp {
         const auto offset = [&](int m, int n, int64_t ld) __attribute__((always_inline)) {
             return m < p.M && n < p.N ? (uint32_t)(((int64_t)m * ld + n) * 2) : kNowhere;
         };
+        float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};  // of the lane's columns over its rows
         const auto rows = [&](auto&& ahead, auto&& beside) __attribute__((always_inline)) {
             by_rows<C>(lds, acc, m0, n0, wm, wn, ahead, [&](int m, int n, float (&v)[8], const auto& x) __attribute__((always_inline)) {
                 if constexpr (!GRAD) {
@@ -52,18 +53,18 @@ struct LinearEp {
                     for (int e = 0; e < 8; ++e) v[e] = act<ACT, true>(v[e]);
                 }
                 beside(v, x);
+                if constexpr (GRAD) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) s[e] += m < p.M ? v[e] : 0.f;
+                }
                 store8(rc, offset(m, n, p.ldc), v, n, p.N);
             });
         };
-        float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};  // of the lane's columns over its rows
         if constexpr (GRAD && ACT != kActNone) {
             rows([&](int m, int n) __attribute__((always_inline)) { return load8(rz, offset(m, n, p.ldz)); },
-                 [&](float (&v)[8], const bf16x8& z) __attribute__((always_inline)) {
+                 [](float (&v)[8], const bf16x8& z) __attribute__((always_inline)) {
 #pragma unroll
-                     for (int e = 0; e < 8; ++e) {
-                         v[e] *= act_grad<ACT, true>((float)z[e]);
-                         s[e] += v[e];  // rows past M: products of zeros
-                     }
+                     for (int e = 0; e < 8; ++e) v[e] *= act_grad<ACT, true>((float)z[e]);
                  });
         } else if (!GRAD && has_res) {
             rows([&](int m, int n) __attribute__((always_inline)) { return load8(rr, offset(m, n, p.ldr)); },
@@ -73,12 +74,7 @@ struct LinearEp {
                  });
         } else {
             rows([](int, int) __attribute__((always_inline)) { return Nothing{}; },
-                 [&](float (&v)[8], Nothing) __attribute__((always_inline)) {
-                     if constexpr (GRAD) {
-#pragma unroll
-                         for (int e = 0; e < 8; ++e) s[e] += v[e];
-                     }
-                 });
+                 [](float (&)[8], Nothing) __attribute__((always_inline)) {});
         }
         if constexpr (GRAD) {
             if (!p.sums) return;
@@ -126,7 +122,7 @@ struct LinearEp {
                     float v = acc[tm][tn][r];
                     if constexpr (GRAD) {
                         if constexpr (ACT != kActNone) v *= act_grad<ACT, false>(x[r]);
-                        s += v;  // rows past M: products of zeros
+                        s += offset(r, 0) != kNowhere ? v : 0.f;
                     } else {
                         v += b;
                         if (has_z) __builtin_amdgcn_raw_buffer_store_b32(__float_as_int(v), rz, offset(r, p.ldz), 0, 0);

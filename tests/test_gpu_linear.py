@@ -266,6 +266,10 @@ def test_sums_of_the_data_gradient(M, K, N, act, dt):
     again = torch.empty(K, dtype=dt, device="cuda")
     fbl.linear_bwd(dy, new(x), w, dx=new(torch.zeros_like(x)), dxbias=again, **kw)
     assert torch.equal(again, buf[:K])
+    # an infinite weight: that column alone, infinite of one sign, and no nan from rows behind the last
+    w[1, 0] = float("inf")
+    fbl.linear_bwd(dy.abs() + 1, new(x), w, dx=new(torch.zeros_like(x)), need_dw=False, need_bias=False, dxbias=again)
+    assert again[1] == float("inf") and bool(again.isfinite().sum() == K - 1)
 
 
 @pytest.mark.parametrize("act", ACTS)
