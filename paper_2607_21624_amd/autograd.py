@@ -37,12 +37,28 @@ let go of every eager loss or output of the same leaves.  While one lives, torch
 keeps the leaves' accumulation on that graph's stream, and a capture that meets another
 stream ends with an error or the process.
 """
+import functools
 import math
 
 import torch
 from torch.autograd.function import once_differentiable
 
 from . import fbl as _f
+
+
+def _first_order(backward):
+    """A backward in the library's kernels, of which autograd knows no derivative: its gradients under
+    create_graph may be read, but differentiating them raises.  once_differentiable marks them so only where an
+    incoming gradient requires grad; without one (the gradient of a weighted sum) they would count as
+    constants, though they depend on what the forward saved, and a penalty on them would drop out unseen."""
+    once = once_differentiable(backward)
+
+    @functools.wraps(backward)
+    def marked(ctx, *grads):
+        if torch.is_grad_enabled():
+            grads = tuple(g if g.requires_grad else g.detach().requires_grad_() for g in grads)
+        return once(ctx, *grads)
+    return marked
 
 
 def _unit(t, what: str):
@@ -71,6 +87,7 @@ class _Attention(torch.autograd.Function):
         return o
 
     @staticmethod
+    @_first_order
     def backward(ctx, do):
         q, k, v, o, lse, kv = ctx.saved_tensors
         Hq, Hkv, scale, causal, has_kv = ctx.cfg
@@ -94,6 +111,7 @@ class _AttentionPacked(torch.autograd.Function):
         return o
 
     @staticmethod
+    @_first_order
     def backward(ctx, do):
         qkv, o, lse = ctx.saved_tensors
         Hq, Hkv, scale, causal = ctx.cfg
@@ -117,6 +135,7 @@ class _Linear(torch.autograd.Function):
         return y.view(*x.shape[:-1], w.shape[1])
 
     @staticmethod
+    @_first_order
     def backward(ctx, dy):
         x2, w = ctx.saved_tensors
         dy = _unit(dy, "linear")
@@ -153,7 +172,7 @@ class _LinearAct(torch.autograd.Function):
         return y.view(*x.shape[:-1], N)
 
     @staticmethod
-    @once_differentiable
+    @_first_order
     def backward(ctx, dy):
         x2, w, z = ctx.saved_tensors
         xshape, act = ctx.cfg
@@ -191,7 +210,7 @@ class _Mlp(torch.autograd.Function):
         return y.view(*x.shape[:-1], w2.shape[1])
 
     @staticmethod
-    @once_differentiable
+    @_first_order
     def backward(ctx, dy):
         x2, w1, w2, z, h = ctx.saved_tensors
         xshape, act = ctx.cfg
@@ -223,7 +242,7 @@ class _LayerNorm(torch.autograd.Function):
         return y.view(x.shape)
 
     @staticmethod
-    @once_differentiable
+    @_first_order
     def backward(ctx, dy):
         x2, mean, rstd, weight = ctx.saved_tensors
         dy2 = _matrix_of(_unit(dy, "layer_norm"), "layer_norm: the incoming gradient")
@@ -272,7 +291,7 @@ class _LinearCrossEntropy(torch.autograd.Function):
         return _reduced(loss, total, mean, reduction, x.shape[:-1])
 
     @staticmethod
-    @once_differentiable
+    @_first_order
     def backward(ctx, dloss):
         x2, w, labels, lse, total = ctx.saved_tensors
         xshape, ignore_index, reduction = ctx.cfg
@@ -303,7 +322,7 @@ class _LinearDistillation(torch.autograd.Function):
         return _reduced(loss, total, mean, reduction, x.shape[:-1])
 
     @staticmethod
-    @once_differentiable
+    @_first_order
     def backward(ctx, dloss):
         x2, w, index, prob, lse, total = ctx.saved_tensors
         xshape, temperature, reduction = ctx.cfg
