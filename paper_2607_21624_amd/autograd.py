@@ -78,6 +78,13 @@ def _matrix_of(t, what: str):
                                              f"contiguous") from None
 
 
+def _rows_of(x, width):
+    """A new [..., width] tensor beside x [..., K], and it as a matrix of rows for the library to write.  (A function
+    that returned a view of the matrix would have an output that torch lets nobody change in place.)"""
+    out = torch.empty((*x.shape[:-1], width), dtype=x.dtype, device=x.device)
+    return out, out if out.dim() == 2 else out.view(-1, width)
+
+
 class _Attention(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, Hq, Hkv, scale, causal, kv_len):
@@ -129,10 +136,11 @@ class _Linear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, w):
         x2 = x.reshape(-1, x.shape[-1])  # a view for token-major activations
-        y = _f.proj(_f.FBL_PROJ_FWD, x2, w)
+        y, y2 = _rows_of(x, w.shape[-1])
+        _f.proj(_f.FBL_PROJ_FWD, x2, w, out=y2)
         ctx.save_for_backward(x2, w)
         ctx.xshape = x.shape
-        return y.view(*x.shape[:-1], w.shape[1])
+        return y
 
     @staticmethod
     @_first_order
@@ -166,10 +174,11 @@ class _LinearAct(torch.autograd.Function):
         z = None
         if act != "none" and any(ctx.needs_input_grad[:3]):
             z = torch.empty((x2.shape[0], N), dtype=x.dtype, device=x.device)
-        y = _f.linear_fwd(x2, w, bias, act, res2, z=z)
+        y, y2 = _rows_of(x, N)
+        _f.linear_fwd(x2, w, bias, act, res2, out=y2, z=z)
         ctx.save_for_backward(x2, w, z)
         ctx.cfg = (x.shape, act)
-        return y.view(*x.shape[:-1], N)
+        return y
 
     @staticmethod
     @_first_order
@@ -204,10 +213,11 @@ class _Mlp(torch.autograd.Function):
         if act != "none" and any(ctx.needs_input_grad[:3]):
             z = torch.empty((x2.shape[0], w1.shape[1]), dtype=x.dtype, device=x.device)
         h = _f.linear_fwd(x2, w1, b1, act, z=z)
-        y = _f.linear_fwd(h, w2, b2, residual=res2)
+        y, y2 = _rows_of(x, w2.shape[1])
+        _f.linear_fwd(h, w2, b2, residual=res2, out=y2)
         ctx.save_for_backward(x2, w1, w2, z, h)
         ctx.cfg = (x.shape, act)
-        return y.view(*x.shape[:-1], w2.shape[1])
+        return y
 
     @staticmethod
     @_first_order
@@ -236,10 +246,11 @@ class _LayerNorm(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, bias, eps):
         x2 = _matrix_of(x, "layer_norm")
-        y, mean, rstd = _f.layer_norm_fwd(x2, weight, bias, eps)
+        y, y2 = _rows_of(x, x.shape[-1])
+        _, mean, rstd = _f.layer_norm_fwd(x2, weight, bias, eps, out=y2)
         ctx.save_for_backward(x2, mean, rstd, weight)
         ctx.xshape = x.shape
-        return y.view(x.shape)
+        return y
 
     @staticmethod
     @_first_order
@@ -260,10 +271,18 @@ def _reduction(reduction, where: str):
         raise _f.FblError(_f.FBL_ERR_ARG, f"{where}: reduction {reduction!r}, there are mean, sum and none")
 
 
-def _reduced(loss, total, mean, reduction, shape):
+def _reduced(x, reduction):
+    """The loss to return, a tensor of its own that may be changed in place, and the argument by which the library
+    writes it: the mean, the first number of total (in whose memory the sum stands), or every row's."""
+    new = functools.partial(torch.empty, dtype=torch.float32, device=x.device)
     if reduction == "mean":
-        return mean
-    return total[0] if reduction == "sum" else loss.view(shape)
+        mean = new(())
+        return mean, {"mean": mean}
+    if reduction == "sum":
+        total = new(2)
+        return new(0).set_(total.untyped_storage(), 0, (), ()), {"total": total}
+    loss = new(x.shape[:-1])
+    return loss, {"loss": loss.view(-1)}
 
 
 def _loss_grad(dloss, reduction, M: int):
@@ -284,11 +303,11 @@ class _LinearCrossEntropy(torch.autograd.Function):
             raise _f.FblError(_f.FBL_ERR_SHAPE, f"{where}: labels have shape {tuple(labels.shape)}, need "
                                                 f"{tuple(x.shape[:-1])}")
         labels2 = labels.reshape(-1)
-        mean = torch.empty((), dtype=torch.float32, device=x.device)
-        loss, lse, total = _f.linear_ce_fwd(x2, w, labels2, ignore_index, mean=mean)
-        ctx.save_for_backward(x2, w, labels2, lse, total)
+        result, out = _reduced(x, reduction)
+        _, lse, total = _f.linear_ce_fwd(x2, w, labels2, ignore_index, **out)
+        ctx.save_for_backward(x2, w, labels2, lse, total if reduction == "mean" else None)
         ctx.cfg = (x.shape, ignore_index, reduction)
-        return _reduced(loss, total, mean, reduction, x.shape[:-1])
+        return result
 
     @staticmethod
     @_first_order
@@ -296,8 +315,8 @@ class _LinearCrossEntropy(torch.autograd.Function):
         x2, w, labels, lse, total = ctx.saved_tensors
         xshape, ignore_index, reduction = ctx.cfg
         need = ctx.needs_input_grad
-        dx, dw = _f.linear_ce_bwd(_loss_grad(dloss, reduction, x2.shape[0]), x2, w, labels, lse,
-                                  total if reduction == "mean" else None, ignore_index, need_dx=need[0], need_dw=need[1])
+        dx, dw = _f.linear_ce_bwd(_loss_grad(dloss, reduction, x2.shape[0]), x2, w, labels, lse, total, ignore_index,
+                                  need_dx=need[0], need_dw=need[1])
         return dx.view(xshape) if need[0] else None, dw, None, None, None
 
 
@@ -315,11 +334,11 @@ class _LinearDistillation(torch.autograd.Function):
             raise _f.FblError(_f.FBL_ERR_SHAPE, f"{where}: index {tuple(index.shape)} and logits {tuple(logits.shape)} need "
                                                 f"the shape {tuple(x.shape[:-1])} + (top,)")
         index2, logits2 = _matrix_of(index, where), _matrix_of(logits, where)
-        mean = torch.empty((), dtype=torch.float32, device=x.device)
-        loss, lse, prob, total = _f.linear_kd_fwd(x2, w, index2, logits2, temperature, mean=mean)
-        ctx.save_for_backward(x2, w, index2, prob, lse, total)
+        result, out = _reduced(x, reduction)
+        _, lse, prob, total = _f.linear_kd_fwd(x2, w, index2, logits2, temperature, **out)
+        ctx.save_for_backward(x2, w, index2, prob, lse, total if reduction == "mean" else None)
         ctx.cfg = (x.shape, temperature, reduction)
-        return _reduced(loss, total, mean, reduction, x.shape[:-1])
+        return result
 
     @staticmethod
     @_first_order
@@ -327,8 +346,8 @@ class _LinearDistillation(torch.autograd.Function):
         x2, w, index, prob, lse, total = ctx.saved_tensors
         xshape, temperature, reduction = ctx.cfg
         need = ctx.needs_input_grad
-        dx, dw = _f.linear_kd_bwd(_loss_grad(dloss, reduction, x2.shape[0]), x2, w, index, prob, lse, temperature,
-                                  total if reduction == "mean" else None, need_dx=need[0], need_dw=need[1])
+        dx, dw = _f.linear_kd_bwd(_loss_grad(dloss, reduction, x2.shape[0]), x2, w, index, prob, lse, temperature, total,
+                                  need_dx=need[0], need_dw=need[1])
         return dx.view(xshape) if need[0] else None, dw, None, None, None, None
 
 

@@ -61,7 +61,8 @@ def _stand_ins():
         loss = _into(loss, (M,), f32, 2.0)
         total = _into(total, (2,), f32, float(M))
         total[0] *= 2
-        mean.fill_(2.0)
+        if mean is not None:
+            mean.fill_(2.0)
         return loss, torch.zeros(M), total
 
     def linear_ce_fwd(x, w, labels, ignore_index, loss=None, total=None, mean=None):
@@ -137,3 +138,22 @@ def test_second_derivatives_are_refused(name, constant):
         assert torch.equal(a.detach(), b)
         with pytest.raises(RuntimeError, match="once_differentiable"):
             (a * a).sum().backward(retain_graph=True)
+
+
+@pytest.mark.parametrize("name", [n for n in FUNCTIONS if "attention" not in n])  # attention's backward reads its output
+def test_results_may_be_changed_in_place(name):
+    """loss /= steps, or a layer's output scaled where it stands: allowed, with the gradient that goes with it."""
+    f, shapes = FUNCTIONS[name]
+    leaves = [_randn(*s) for s in shapes]
+    for lead in (leaves, [t if t.dim() < 3 else t[0] for t in leaves]):  # [..., K] of three dimensions and of two
+        if lead is not leaves and ("cross" in name or "distillation" in name):
+            continue
+        out = f(*lead)
+        value = out.detach().clone()
+        want = torch.autograd.grad(out, lead, torch.ones_like(out) / 2)
+        out = f(*lead)
+        assert not out._is_view()
+        out /= 2
+        assert torch.equal(out.detach(), value / 2)
+        for a, b in zip(torch.autograd.grad(out, lead, torch.ones_like(out)), want):
+            assert torch.equal(a, b)
