@@ -302,7 +302,7 @@ class _LinearCrossEntropy(torch.autograd.Function):
         if labels.shape != x.shape[:-1]:
             raise _f.FblError(_f.FBL_ERR_SHAPE, f"{where}: labels have shape {tuple(labels.shape)}, need "
                                                 f"{tuple(x.shape[:-1])}")
-        labels2 = labels.reshape(-1)
+        labels2 = labels.reshape(-1).contiguous()
         result, out = _reduced(x, reduction)
         _, lse, total = _f.linear_ce_fwd(x2, w, labels2, ignore_index, **out)
         ctx.save_for_backward(x2, w, labels2, lse, total if reduction == "mean" else None)

@@ -66,6 +66,7 @@ def _stand_ins():
         return loss, torch.zeros(M), total
 
     def linear_ce_fwd(x, w, labels, ignore_index, loss=None, total=None, mean=None):
+        assert labels.shape == (len(x),) and labels.is_contiguous()
         return losses(x, loss, total, mean)
 
     def grads(g, x, w, total, need_dx, need_dw):
@@ -157,3 +158,11 @@ def test_results_may_be_changed_in_place(name):
         assert torch.equal(out.detach(), value / 2)
         for a, b in zip(torch.autograd.grad(out, lead, torch.ones_like(out)), want):
             assert torch.equal(a, b)
+
+
+def test_labels_of_any_strides():
+    """Labels of a view are copied, whether or not they could be one strided row."""
+    ids = torch.arange(B * (S + 1) * 2).view(B, S + 1, 2) % V
+    for labels in (ids[:, 1:, 0], ids[:, :S, 1], ids[:1, :1, :1].expand(B, S, 1)[..., 0]):
+        ag.linear_cross_entropy(torch.randn(B, S, K), torch.randn(K, V), labels)
+    ag.linear_cross_entropy(torch.randn(S, K), torch.randn(K, V), ids[0, :S, 0])
