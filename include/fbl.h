@@ -641,7 +641,8 @@ fbl_status fbl_layer_norm_bwd(int32_t dtype, int64_t M, int64_t N, const void* d
  *   FBL_ACT_SILU       z / (1 + exp(-z))
  * tile: as fbl_proj's for the product (FBL_PROJ_FWD, M, K, N); AUTO for fp32.
  * ws: NULL, or fbl_linear_fwd_workspace bytes (16-byte aligned), with which tile AUTO lets several
- * workgroups share the contraction of a few tokens' tiles (serving: 0 bytes where it does not).
+ * workgroups share the contraction of a few tokens' tiles (serving: 0 bytes where it does not), whatever fbl_proj_tune
+ * chose.  Sizes of workspaces are functions of the shape.
  *
  * fbl_linear_bwd gives, from dy [M, N], any of (NULL: not wanted)
  *   dx = (dz . w^T) * xact'(xz),   dw = x^T . dz,   dbias = sum over rows of dz,

@@ -1257,19 +1257,27 @@ int32_t default_tile(const ProjPlan& pl) {
 
 }  // namespace
 
-int fbl::proj_auto_tile(uint32_t op, int64_t M, int64_t K, int64_t N) {
-    const int32_t t = tuned_tile(op, M, K, N);
-    if (t >= 0) return t;
+int fbl::proj_untuned_tile(uint32_t op, int64_t M, int64_t K, int64_t N) {
     ProjPlan pl;
     proj_shape(op, M, K, N, pl);
     return default_tile(pl);
 }
 
-int fbl::weight_tile(int64_t M, int64_t K, int64_t N) {
-    const int t = proj_auto_tile(FBL_PROJ_BWD_WEIGHT, M, K, N);
+int fbl::proj_auto_tile(uint32_t op, int64_t M, int64_t K, int64_t N) {
+    const int32_t t = tuned_tile(op, M, K, N);
+    return t >= 0 ? t : proj_untuned_tile(op, M, K, N);
+}
+
+int fbl::weight_untuned_tile(int64_t M, int64_t K, int64_t N) {
+    const int t = proj_untuned_tile(FBL_PROJ_BWD_WEIGHT, M, K, N);
     // written by rows, 8 wavefronts are ahead of the 4 that lead the plain products' order (2048 x 8192 from
     // 4096: 120 and 127 us)
-    return t == 18 && tuned_tile(FBL_PROJ_BWD_WEIGHT, M, K, N) < 0 ? 19 : t;
+    return t == 18 ? 19 : t;
+}
+
+int fbl::weight_tile(int64_t M, int64_t K, int64_t N) {
+    const int32_t t = tuned_tile(FBL_PROJ_BWD_WEIGHT, M, K, N);
+    return t >= 0 ? t : weight_untuned_tile(M, K, N);
 }
 
 extern "C" {

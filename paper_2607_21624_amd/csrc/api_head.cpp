@@ -95,9 +95,9 @@ struct HeadWs {
     size_t weight, row, scale, dz, sum, bwd;            // backward
     int splits;                                         // of dX's contraction
 };
-// Tile of dX over a contraction of kc entries.
-int dx_tile(const Shape& s, int64_t kc) {
-    return s.table() ? fbl::proj_auto_tile(FBL_PROJ_FWD, s.M, kc, s.K) : fbl::proj_auto_tile(FBL_PROJ_BWD_DATA, s.M, s.K, kc);
+// Tile of dX over a contraction of kc entries: chosen by `choose`, for a launch or (untuned) for the workspace's layout.
+int dx_tile(int (*choose)(uint32_t, int64_t, int64_t, int64_t), const Shape& s, int64_t kc) {
+    return s.table() ? choose(FBL_PROJ_FWD, s.M, kc, s.K) : choose(FBL_PROJ_BWD_DATA, s.M, s.K, kc);
 }
 
 HeadWs head_ws(const Shape& s, int64_t ldw) {
@@ -114,7 +114,7 @@ HeadWs head_ws(const Shape& s, int64_t ldw) {
     w.dz = w.scale + 256;
     w.sum = w.dz + align256((size_t)s.M * (size_t)padded64(bp) * (size_t)s.es());
     const size_t plane = (size_t)s.M * (size_t)s.K * 4;
-    w.splits = fbl::sum_splits(s.f32(), !s.table(), s.M, s.K, bp, s.f32() ? 0 : dx_tile(s, bp));
+    w.splits = fbl::sum_splits(s.f32(), !s.table(), s.M, s.K, bp, s.f32() ? 0 : dx_tile(fbl::proj_untuned_tile, s, bp));
     w.bwd = w.sum + (w.splits > 1 ? align256((size_t)w.splits * plane) : bp < s.V && !s.f32() ? align256(plane) : 0);
     return w;
 }
@@ -295,7 +295,7 @@ fbl_status head_bwd(const Shape& s, const float* dloss, int64_t dloss_stride, co
                 q.sum = reinterpret_cast<float*>(base + lay.sum), q.lds = s.K;
                 q.sum_bytes = (uint32_t)(s.M * s.K * 4);
             }
-            const int tile = s.f32() ? 0 : dx_tile(s, kc);
+            const int tile = s.f32() ? 0 : dx_tile(fbl::proj_auto_tile, s, kc);
             e = s.f32() ? fbl::launch_sum_gemm_f32(!s.table(), q, hs) : fbl::launch_sum_gemm(0, !s.table(), tile, q, hs);
             if (e == hipSuccess && last && lay.splits > 1)
                 e = fbl::launch_sum_planes(s.f32(), q.sum, lay.splits, s.M, s.K, scale, dx, lddx, hs);

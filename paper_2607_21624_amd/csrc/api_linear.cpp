@@ -74,7 +74,8 @@ int forward_tile(int64_t M, int64_t K, int64_t N) {
 }
 size_t few_ws(int splits, int64_t M, int64_t N) { return splits > 1 ? (size_t)splits * (size_t)M * (size_t)N * 4 : 0; }
 
-// Workspace of the backward: partial sums of the bias' gradient, dz, planes of dx, partial sums of dx (as many rows
+// Workspace of the backward, a function of the shape (a caller may keep it while fbl_proj_tune's choices come and
+// go): partial sums of the bias' gradient, dz, planes of dx, partial sums of dx (as many rows
 // of them as any tile writes, linear_grad_groups, or one for each of a few tokens).
 struct LinearWs {
     size_t dz, planes, sums, total;
@@ -85,7 +86,7 @@ LinearWs linear_ws(int f32, int64_t M, int64_t K, int64_t N) {
     w.splits = few_splits(f32, M, N, K);
     w.dz = align256((size_t)act_grid(f32, M, N).groups * (size_t)N * 4);
     w.planes = w.dz + align256((size_t)M * (size_t)N * (f32 ? 4 : 2));
-    w.wsplits = fbl::weight_splits(f32, M, K, N, f32 ? 0 : fbl::weight_tile(M, K, N));
+    w.wsplits = fbl::weight_splits(f32, M, K, N, f32 ? 0 : fbl::weight_untuned_tile(M, K, N));
     w.sums = w.planes + align256(std::max(few_ws(w.splits, M, K), few_ws(w.wsplits, K, N)));
     w.total = w.sums + (size_t)(w.splits > 1 ? M : M / 32 + 4) * (size_t)K * 4;
     return w;

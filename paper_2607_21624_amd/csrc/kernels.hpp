@@ -151,6 +151,9 @@ hipError_t launch_head_grad_rows(const HeadRowArgs& a, hipStream_t stream);     
 int proj_auto_tile(uint32_t op, int64_t M, int64_t K, int64_t N);
 // The same for a weight gradient whose tiles are written by rows.
 int weight_tile(int64_t M, int64_t K, int64_t N);
+// Both as they are without fbl_proj_tune: functions of the shape, by which workspaces are laid out.
+int proj_untuned_tile(uint32_t op, int64_t M, int64_t K, int64_t N);
+int weight_untuned_tile(int64_t M, int64_t K, int64_t N);
 
 // Diagnostic: offsets of a token-major tensor computed by the device index map.
 hipError_t launch_layout_map(const TokMap& m, int B, int H, int S, int D, int64_t* out, hipStream_t stream);
