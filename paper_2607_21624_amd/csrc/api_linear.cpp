@@ -79,13 +79,15 @@ size_t few_ws(int splits, int64_t M, int64_t N) { return splits > 1 ? (size_t)sp
 // of them as any tile writes, linear_grad_groups, or one for each of a few tokens).
 struct LinearWs {
     size_t dz, planes, sums, total;
+    int64_t ldz;          // of dz: bf16 rows of whole 16-byte chunks, as every operand that the products stage
     int splits, wsplits;  // of dx and of dw: the planes are used by one after the other
 };
 LinearWs linear_ws(int f32, int64_t M, int64_t K, int64_t N) {
     LinearWs w;
     w.splits = few_splits(f32, M, N, K);
     w.dz = align256((size_t)act_grid(f32, M, N).groups * (size_t)N * 4);
-    w.planes = w.dz + align256((size_t)M * (size_t)N * (f32 ? 4 : 2));
+    w.ldz = f32 ? N : (N + 7) / 8 * 8;
+    w.planes = w.dz + align256((size_t)M * (size_t)w.ldz * (f32 ? 4 : 2));
     w.wsplits = fbl::weight_splits(f32, M, K, N, f32 ? 0 : fbl::weight_untuned_tile(M, K, N));
     w.sums = w.planes + align256(std::max(few_ws(w.splits, M, K), few_ws(w.wsplits, K, N)));
     w.total = w.sums + (size_t)(w.splits > 1 ? M : M / 32 + 4) * (size_t)K * 4;
@@ -205,8 +207,9 @@ fbl_status fbl_linear_bwd(int32_t dtype, uint32_t act, int64_t M, int64_t K, int
         a.dy = dy, a.z = z, a.lddy = lddy, a.ldz = ldz, a.M = M, a.N = (int)N, a.rows = ag.rows, a.groups = ag.groups;
         a.part = dbias ? static_cast<float*>(ws) : nullptr;
         if (has_act) {
-            g = RowsView{static_cast<char*>(ws) + lw.dz, M, N, N, es};
-            a.dz = const_cast<void*>(g.p), a.lddz = N;
+            // (its span is at most dy's, whose rows are as long at least)
+            g = RowsView{static_cast<char*>(ws) + lw.dz, M, N, lw.ldz, es};
+            a.dz = const_cast<void*>(g.p), a.lddz = g.ld;
         }
         e = fbl::launch_linear_act_bwd(f32, (int)act, a, s);
         if (e == hipSuccess && dbias) e = fbl::launch_column_sums(f32, a.part, a.groups, 1, (int)N, dbias, nullptr, s);
