@@ -712,8 +712,10 @@ fbl_status fbl_linear_bwd(int32_t dtype, uint32_t act, int64_t M, int64_t K, int
  *
  * Workspace: fbl_linear_loss_workspace bytes for W's row stride, 16-byte aligned, the
  * same for all four calls (top 1 for cross entropy); nothing is kept in it between calls.  It holds
- * about 128 MiB of dz and M K fp32 sums (up to 8 of them where workgroups share dX's contraction), or 8 bytes
- * for each row and 256 vocabulary entries where that is more, and small lists.
+ * a piece of dz: all of it, 128 MiB, or 4096 vocabulary entries for each row where that is more (from 16384 rows
+ * bf16, 8192 fp32; below 2 GiB); M K fp32 sums, or as many of them as workgroups share dX's contraction, 64 MiB at
+ * most then; or for the forward 8 bytes for each row and tile of 32 to 256 entries where that is more; and 8 bytes for
+ * each of M top targets.
  * fp32: any extents, natural alignment.  bf16: 16-byte aligned pointers and rows, K a multiple
  * of 8, for FBL_HEAD_KV V too; any number of tokens.  x, dx and a FBL_HEAD_KV W below 2 GiB
  * (fp32 sums of dx included: M K below 2^29); a table may be larger.  Outputs and workspace overlap

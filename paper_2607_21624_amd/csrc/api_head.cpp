@@ -63,7 +63,10 @@ int64_t forward_piece(const Shape& s, int64_t ldw) {
 // Vocabulary entries of a piece of the backward.  dz [M][piece] goes through memory twice and dX's fp32
 // sums once a piece, so pieces are large, up to 128 MiB of dz; of those, the width whose tiles
 // fill the CUs' rounds best.  (4096 tokens, K 1024, V 50257: 3 pieces of 16384 and one of 1105 make 13 rounds of dz
-// and 4 of dW, 4 pieces of 12800 make 16 and 4.)
+// and 4 of dW, 4 pieces of 12800 make 15 and 4.)  Many tokens still get 4096 entries, for more memory: with 128 MiB
+// of dz in half or a quarter of them the sums' traffic costs more than that is worth (backward, ms, with 4096 and with
+// 128 MiB: 32768 tokens, K 2048, V 128256 51.0 and 55.0; K 4096, V 32000 23.2 and 26.8; K 1024, V 50257 11.3 and
+// 13.6; 65536 tokens, K 1024 22.7 and 34.9; fp32 16384 tokens, K 512, V 50257 20.7 and 22.4).
 int64_t backward_piece(const Shape& s, int64_t ldw) {
     int64_t most = std::max<int64_t>(4096, ((int64_t)128 << 20) / (s.M * s.es()));
     most = std::min(most, std::max<int64_t>(64, (kSpan - 1) / (s.M * s.es()) - 64));

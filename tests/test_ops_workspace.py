@@ -24,3 +24,23 @@ def test_rows_of_dz_are_whole_chunks(N):
     # sums over blocks of rows: at most 512 rows of N + 4 fp32, and roundings to 256 bytes
     assert size(N + 4) - size(N) <= 512 * 4 * 4 + 3 * 256
     assert size(N) >= M * (N + 4) * 2
+
+
+@pytest.mark.parametrize("table", [False, True])
+@pytest.mark.parametrize("dt,es", [(F.FBL_BF16, 2), (F.FBL_F32, 4)])
+@pytest.mark.parametrize("M", [1, 16, 100, 128, 129, 700, 4096, 8192, 16384, 32768, 65536, 131072])
+@pytest.mark.parametrize("K,V", [(64, 50256), (1024, 50256), (2048, 128256), (512, 1000)])
+def test_losses_workspace_is_within_its_bound(K, V, M, dt, es, table):
+    """A piece of dz, sums of dX, the forward's parts and the targets' lists, as the header states them."""
+    if not table and K * V * es >= 1 << 31:
+        return
+    for top in (1, 50):
+        got = _size(LIB.fbl_linear_loss_workspace, dt, F.FBL_HEAD_VK if table else F.FBL_HEAD_KV, M, K, V, top, K if table else V)
+        rows = M * es
+        dz = min(rows * (V + 63), max(128 << 20, 4096 * rows) + 64 * rows, 1 << 31)
+        sums = max(M * K * 4, 64 << 20)
+        parts = M * 8 * (-(-V // 32) + 16)
+        lists = 2 * M * top * 4 + 3 * 8 * M
+        assert got <= max(dz + sums, parts) + lists + 4096
+        if M >= 4096 and rows * V > 256 << 20:  # and pieces are not small
+            assert got >= 32 << 20
