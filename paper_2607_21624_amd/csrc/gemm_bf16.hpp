@@ -450,7 +450,7 @@ hipError_t launch_gemm_bf16(const typename EP::Args& p, hipStream_t stream, int 
 }
 
 template <typename EP>
-using GemmLauncher = hipError_t (*)(const typename EP::Args&, hipStream_t, int);
+using GemmLauncher = hipError_t (*)(const typename EP::Args&, hipStream_t, int splits);
 
 template <bool AT, bool BT, typename EP, int... I>
 constexpr std::array<GemmLauncher<EP>, sizeof...(I)> gemm_launchers(std::integer_sequence<int, I...>) {
@@ -458,9 +458,9 @@ constexpr std::array<GemmLauncher<EP>, sizeof...(I)> gemm_launchers(std::integer
 }
 
 template <bool AT, bool BT, typename EP>
-hipError_t launch_gemm_tile(int tile, const typename EP::Args& p, hipStream_t stream, int splits = 1) {
+hipError_t launch_gemm_tile(int tile, const typename EP::Args& p, hipStream_t stream) {
     static constexpr auto table = gemm_launchers<AT, BT, EP>(std::make_integer_sequence<int, kGemmTileCount>{});
-    return table[tile](p, stream, splits);
+    return table[tile](p, stream, 1);
 }
 
 }  // namespace

@@ -262,7 +262,7 @@ hipError_t launch_gemm_f32(const typename EP::Args& p, hipStream_t stream, int s
 }
 
 template <typename EP>
-using F32Launcher = hipError_t (*)(const typename EP::Args&, hipStream_t, int);
+using F32Launcher = hipError_t (*)(const typename EP::Args&, hipStream_t, int splits);
 
 template <bool AT, bool BT, typename EP, int... I>
 constexpr std::array<F32Launcher<EP>, sizeof...(I)> f32_launchers(std::integer_sequence<int, I...>) {
@@ -270,9 +270,9 @@ constexpr std::array<F32Launcher<EP>, sizeof...(I)> f32_launchers(std::integer_s
 }
 
 template <bool AT, bool BT, typename EP>
-hipError_t launch_f32_tile(int tile, const typename EP::Args& p, hipStream_t stream, int splits = 1) {
+hipError_t launch_f32_tile(int tile, const typename EP::Args& p, hipStream_t stream) {
     static constexpr auto table = f32_launchers<AT, BT, EP>(std::make_integer_sequence<int, kF32TileCount>{});
-    return table[tile](p, stream, splits);
+    return table[tile](p, stream, 1);
 }
 
 // The tile of a product: least rounds x area x cost, where rounds is the number
