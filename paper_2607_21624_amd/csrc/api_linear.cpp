@@ -66,8 +66,10 @@ int few_splits(int f32, int64_t M, int64_t K, int64_t N) {
     return (f32 ? M <= 128 && K >= 1024 : M <= 64 ? K > 2048 : M <= 128 && K >= 8192) ? fbl::sum_splits(f32, 0, M, N, K, 0) : 1;
 }
 // The tile of a bf16 forward that is not shared.  Up to 32 tokens and 8192 columns that is 32 x 32 on four
-// wavefronts, whose many workgroups have the most loads on the way (1 token, 2048 x 8192: 11.3 us, 16.9 with the
-// products' own choice below 32 rows; 4096 x 12288: 37.7 and 34.5).
+// wavefronts, whose many workgroups have the most loads on the way; wider, the 32 x 128 of the products' own choice
+// covers the CUs too and reads x less often (us, cold weights, 32 x 32 and own choice: 1 token 512 x 8192 4.3 and
+// 5.2, 2048 x 8192 10.9 and 16.5, 2048 x 8200 12.7 and 16.9, 512 x 12288 6.0 and 5.7, 2048 x 12288 18.4 and 17.0,
+// 2048 x 32768 29.9 and 22.7; 17 tokens 2048 x 8192 11.6 and 16.9, 2048 x 12288 19.8 and 17.5).
 int forward_tile(int64_t M, int64_t K, int64_t N) {
     if (M <= 32 && N <= 8192 && fbl_proj_tuned_tile(FBL_PROJ_FWD, M, K, N) < 0) return 16;
     return fbl::proj_auto_tile(FBL_PROJ_FWD, M, K, N);
