@@ -694,8 +694,8 @@ fbl_status fbl_linear_bwd(int32_t dtype, uint32_t act, int64_t M, int64_t K, int
  *   p = softmax(logits / T) over the row's entries, q = softmax(z / T) over the vocabulary
  *   loss[m] = T^2 sum_j p_j (log p_j - log q_{index_j}),   lse = log sum exp(z / T)
  * A negative index is an absent entry, a logit of -inf one of weight 0; a row without
- * any other does not count.  An index that stands in a row twice counts with
- * both weights.  prob [M, top] float32 receives p, for the backward.
+ * any other does not count (of its x, what is said above).  An index that stands in a row twice counts with
+ * both weights.  prob [M, top] float32 receives p, for the backward.  The teacher's logits get no gradient.
  *
  * A label or index of V and more (or a label below 0 that is not `ignore`) gives
  * its row a loss and gradients of nan.

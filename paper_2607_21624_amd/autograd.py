@@ -24,10 +24,14 @@ torch provides the tensors, the stream and the autograd graph.
       int64; gradients to x and w.  loss float32: the mean over the rows not
       labelled ignore_index, their "sum", or every row's ("none", [...]).
   linear_distillation(x, w, index, logits, temperature=1.0, reduction="mean") -> loss
-      the same from a teacher's top logits: index int64 and logits [..., top].
+      the same from a teacher's top logits: index int64 and logits [..., top].  The
+      teacher is a constant: logits that require grad get no gradient from here.
+
+Gradients are those of the first order: taken with create_graph they hold their
+values, and differentiating them raises an error.
 
 The incoming gradient is read in place, never copied: it must have unit
-inner stride (any row stride), like every tensor the kernels read.  Autograd
+inner stride (any row stride from the width on), like every tensor the kernels read.  Autograd
 can hand over a broadcast view (the gradient of a plain .sum(), inner stride
 0); such a gradient is rejected with FblError, and the caller makes it
 contiguous (or backpropagates a materialised tensor) instead.

@@ -1231,7 +1231,8 @@ def linear_kd_fwd(x, w, index, logits, temperature: float = 1.0, loss=None, lse=
     """Distillation from a teacher's top logits on the student's logits x w, which are never kept: index int64 and
     logits (float32 or bfloat16) [M, top] are the teacher's, loss[m] = T^2 sum p (log p - log q) with p = softmax(logits /
     T) over the row's entries and q = softmax(x w / T) over the vocabulary.  A negative index is an absent entry; a
-    row without entries does not count.  Returns (loss, lse, prob, total); prob float32 [M, top]."""
+    row without entries does not count.  The teacher is a constant: there is no gradient of its logits.  Returns (loss,
+    lse, prob, total); prob float32 [M, top]."""
     done = _FAST.linear_kd_fwd(x, w, index, logits, temperature, loss, lse, prob, total, mean, workspace, stream)
     if done is not None:
         return done
