@@ -207,7 +207,9 @@ struct HeadGrad {
 // The factor of a mean's or sum's gradient is the same for every row, so bf16 keeps it out of dz: dz's
 // largest entries, -1 at the labels, are then exact, where g, a constant, rounded would be off by the same
 // 2^-9 in every row (4096 x 1024 x 50257: error of dx 0.28% of its norm, 0.17% of
-// which are the result's own rounding).
+// which are the result's own rounding).  A factor of each row's own, and distillation's weights of the targets, are
+// in dz and rounded with it: one rounding of an operand that the matrix instructions take in 16 bits (2048 x 2048 x
+// 128256, 32 targets a row: 0.23%).
 template <bool SPLIT>
 struct SumPieces {
     using Args = SumArgs;

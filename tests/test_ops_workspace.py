@@ -44,3 +44,19 @@ def test_losses_workspace_is_within_its_bound(K, V, M, dt, es, table):
         assert got <= max(dz + sums, parts) + lists + 4096
         if M >= 4096 and rows * V > 256 << 20:  # and pieces are not small
             assert got >= 32 << 20
+
+
+@pytest.mark.parametrize("dt,es", [(F.FBL_BF16, 2), (F.FBL_F32, 4)])
+def test_nothing_is_shared_where_the_binding_brings_no_workspace(dt, es):
+    """The binding asks for a forward's workspace up to 128 tokens, and for a plain backward's up to 128 tokens or
+    weights of 2^19; what the library could share beyond that it would leave alone, unnoticed.  There no size may have
+    room for planes (two of them at least): a block of bias sums, dz and dx's sums are all."""
+    for M in (129, 136, 200, 256, 300, 512, 1000, 4096, 8192, 100000):
+        for K in (64, 512, 1032, 2048, 4096, 8192, 16384):
+            for N in (64, 264, 1024, 4096, 8200, 32768):
+                if M * max(K, N) * es >= 1 << 31:
+                    continue
+                assert _size(LIB.fbl_linear_fwd_workspace, dt, M, K, N) == 0
+                if K * N > 1 << 19:
+                    most = 512 * N * 4 + M * N * es + (M // 32 + 4) * K * 4 + 3 * 256
+                    assert _size(LIB.fbl_linear_bwd_workspace, dt, M, K, N) <= most, (M, K, N)
