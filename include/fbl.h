@@ -742,6 +742,58 @@ fbl_status fbl_linear_kd_bwd(int32_t dtype, uint32_t order, int64_t M, int64_t K
                              const float* lse, void* dx, int64_t lddx, void* dw, int64_t lddw, void* ws, size_t ws_bytes,
                              void* stream);
 
+/*
+ * Norms of queries and keys for each head, and their rotation by position (rotary embedding), in one pass over the
+ * projection's output, between fbl_proj and fbl_attn_fwd: for every head row x of D values
+ *   h = x r w,  r = 1 / sqrt(mean(x^2) + eps)        (norm NULL: h = x; w NULL: ones)
+ *   y = h with dims / 2 pairs (a, b) of its first dims values turned by t = position * frequency of the pair:
+ *       (a cos t - b sin t, b cos t + a sin t)       (rot NULL: y = h)
+ * Pair j is (h[j], h[j + dims / 2]), or with `neighbours` (h[2j], h[2j + 1]); values from dims on do not turn.
+ *
+ * fbl_rotary: turns [dims / 2] holds the frequencies as fbl_rotary_turns makes them (device memory): turns a position in
+ * 64-bit fixed point, 2^64 a whole turn, so that t is exact to 2^-33 turns for any frequency up to 2^31
+ * positions from 0 and a position may be any int64.  fbl_rotary_turns (host) takes radians a position.
+ * positions: int64 device memory, token s of sequence b at axis a is positions[a * stride_axis + b * stride_batch + s *
+ * stride_token] (strides in elements, 0 allowed); NULL: s itself.  With several axes (time, height, width of
+ * images and video) pair j turns by its own axis' position, axes[j] (host memory, with the struct).
+ * fbl_head_norm: weights [D] of the tensors' type, one for all query heads, one for all key heads.
+ *
+ * q, k and their outputs are token-major tensors given by layout descriptors (views of a packed projection for
+ * instance); k (with its descriptor and output) may be NULL.  An output may be exactly its own input, in place.
+ * The backward takes the gradients gq, gk of the outputs and gives
+ *   dq, dk (each may be exactly gq, gk, in place), and where not NULL the sums over tokens and heads
+ *   dq_weight, dk_weight [D] = g x r,   g = the gradient turned back;   dx = r (g w - x r mean(g w x r))
+ * from the forward's inputs q, k (needed with norm alone, else NULL).  The workspace, fbl_qk_norm_rotary_bwd_workspace
+ * bytes (4-byte aligned), is needed where a weight's gradient is wanted.  All sums run in a fixed order, in fp32.
+ * Checks: D 32, 64 or 128 and dims a multiple of 16 (FBL_ERR_UNSUPPORTED), descriptors as fbl_attn_fwd's, 16-byte
+ * aligned tensors, at most 2^31 - 1 tokens, 1 to FBL_ROTARY_MAX_AXES axes, finite eps >= 0 (FBL_ERR_ARG), nothing written
+ * overlapping anything else (FBL_ERR_ARG), neither rot nor norm (FBL_ERR_ARG).
+ */
+#define FBL_ROTARY_MAX_AXES 4
+typedef struct {
+    const uint64_t* turns;
+    const int64_t* positions;
+    int64_t stride_axis, stride_batch, stride_token;
+    int32_t dims, neighbours, num_axes, reserved; /* reserved: zero */
+    uint8_t axes[64];
+} fbl_rotary;
+typedef struct {
+    const void* q_weight;
+    const void* k_weight;
+    float eps;
+    uint32_t reserved; /* zero */
+} fbl_head_norm;
+fbl_status fbl_rotary_turns(const double* frequencies, int64_t n, uint64_t* turns);
+fbl_status fbl_qk_norm_rotary_fwd(const fbl_layout* lq, const void* q, const fbl_layout* lk, const void* k,
+                                  const fbl_rotary* rot, const fbl_head_norm* norm, const fbl_layout* lqo, void* qo,
+                                  const fbl_layout* lko, void* ko, void* stream);
+fbl_status fbl_qk_norm_rotary_bwd_workspace(const fbl_layout* lq, const fbl_layout* lk, size_t* bytes);
+fbl_status fbl_qk_norm_rotary_bwd(const fbl_layout* lgq, const void* gq, const fbl_layout* lgk, const void* gk,
+                                  const fbl_layout* lq, const void* q, const fbl_layout* lk, const void* k,
+                                  const fbl_rotary* rot, const fbl_head_norm* norm, const fbl_layout* ldq, void* dq,
+                                  const fbl_layout* ldk, void* dk, void* dq_weight, void* dk_weight, void* ws,
+                                  size_t ws_bytes, void* stream);
+
 /* Static, human-readable name of a status code. */
 const char* fbl_status_str(fbl_status s);
 

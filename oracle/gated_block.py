@@ -1,0 +1,89 @@
+"""Norms of queries and keys with their rotation, the gated feed-forward part and clipping by the global norm in float64
+numpy: the textbook definitions written out (test infrastructure)."""
+import math
+
+import numpy as np
+
+from .train import act, act_grad
+
+
+# ------------------------------------------------------- per-head norm and rotation
+def _pairs(D, dims, neighbours):
+    """Index arrays (a, b) of the dims / 2 pairs of a head."""
+    j = np.arange(dims // 2)
+    return (2 * j, 2 * j + 1) if neighbours else (j, j + dims // 2)
+
+
+def angles(positions, frequencies, axes=None):
+    """[B, S, dims / 2] angles from positions [B, S] or [axes, B, S]."""
+    p = np.asarray(positions)
+    p = p[None] if p.ndim == 2 else p
+    axes = [0] * len(frequencies) if axes is None else axes
+    # the whole turns go out of the product before it is rounded to float64
+    return np.stack([np.vectorize(lambda n: math.remainder(float(n) * f, 2 * math.pi), otypes=[np.float64])(p[a])
+                     for a, f in zip(axes, frequencies)], axis=-1)
+
+
+def rotate(x, angle, neighbours=False):
+    """x [B, S, H, D] with its first 2 * angle.shape[-1] values turned."""
+    x = np.asarray(x, dtype=np.float64)
+    if angle is None:
+        return x
+    a, b = _pairs(x.shape[-1], 2 * angle.shape[-1], neighbours)
+    c, s = np.cos(angle)[:, :, None], np.sin(angle)[:, :, None]
+    y = x.copy()
+    y[..., a] = x[..., a] * c - x[..., b] * s
+    y[..., b] = x[..., b] * c + x[..., a] * s
+    return y
+
+
+def qk_norm_rotary_fwd(x, angle=None, neighbours=False, w=None, eps=None):
+    """y of x [B, S, H, D]; eps None: no norm; angle None: no rotation."""
+    x = np.asarray(x, dtype=np.float64)
+    if eps is not None:
+        x = x / np.sqrt((x * x).mean(axis=-1, keepdims=True) + eps)
+        if w is not None:
+            x = x * np.asarray(w, dtype=np.float64)
+    return rotate(x, angle, neighbours)
+
+
+def qk_norm_rotary_bwd(dy, x, angle=None, neighbours=False, w=None, eps=None):
+    """(dx, dw)."""
+    g = rotate(dy, None if angle is None else -angle, neighbours)
+    if eps is None:
+        return g, None
+    x = np.asarray(x, dtype=np.float64)
+    r = 1.0 / np.sqrt((x * x).mean(axis=-1, keepdims=True) + eps)
+    xh = x * r
+    dw = (g * xh).sum(axis=(0, 1, 2))
+    if w is not None:
+        g = g * np.asarray(w, dtype=np.float64)
+    return r * (g - xh * (g * xh).mean(axis=-1, keepdims=True)), dw
+
+
+# ---------------------------------------------------------------- gated feed-forward
+def gated_fwd(x, w, b=None, kind="silu"):
+    """(h, z): z = x w + b for w [K, 2F], gate then up;  h = act(gate) up."""
+    x, w = np.asarray(x, dtype=np.float64), np.asarray(w, dtype=np.float64)
+    z = x @ w
+    if b is not None:
+        z = z + np.asarray(b, dtype=np.float64)
+    F = w.shape[1] // 2
+    return act(z[:, :F], kind) * z[:, F:], z
+
+
+def gated_bwd(dh, z, kind="silu"):
+    """dz [M, 2F] from dh [M, F]."""
+    dh, z = np.asarray(dh, dtype=np.float64), np.asarray(z, dtype=np.float64)
+    F = dh.shape[1]
+    gate, up = z[:, :F], z[:, F:]
+    return np.concatenate([dh * up * act_grad(gate, kind), dh * act(gate, kind)], axis=1)
+
+
+# ------------------------------------------------------------------------- clipping
+def grad_norm(grads):
+    return math.sqrt(math.fsum(float((np.asarray(g, dtype=np.float64) ** 2).sum()) for g in grads))
+
+
+def clip_scale(norm, limit):
+    return min(1.0, limit / (norm + 1e-6))

@@ -6,9 +6,16 @@ torch provides the tensors, the stream and the autograd graph.
   attention(q, k, v, Hq, Hkv, scale=None, causal=False, kv_len=None) -> O
       q [B, S_q, Hq*d], k and v [B, S_kv, Hkv*d], token-major (any row
       stride, inner stride 1); gradients flow to q, k and v.
-  attention_packed(qkv, Hq, Hkv, scale=None, causal=False) -> O
+  attention_packed(qkv, Hq, Hkv, scale=None, causal=False, turns=None, positions=None, axes=None,
+                   neighbours=False, q_weight=None, k_weight=None, eps=None) -> O
       qkv [B, S, (Hq + 2 Hkv) d], the packed output of a fused QKV
-      projection; its gradient is one packed tensor of the same shape.
+      projection; its gradient is one packed tensor of the same shape.  With turns or eps queries and
+      keys are normed for each head and turned by their positions on the way, as by qk_norm_rotary.
+  qk_norm_rotary(q, k, Hq, Hkv, turns=None, positions=None, axes=None, neighbours=False,
+                 q_weight=None, k_weight=None, eps=None) -> (q', k')
+      norms of each head of q [B, S, Hq d] and k [B, S, Hkv d] (eps; weights [d]) and their rotation by
+      position (turns: fbl.rotary_turns; positions int64 [S], [B, S] or [axes, B, S]); gradients to q, k and the
+      weights.  k may be None, and is then None in the result.
   linear(x, w, bias=None, act="none", residual=None) -> act(x @ w + bias) + residual
       x [..., K] (rows contiguous), w [K, N]; gradients x and w by the data-
       and weight-gradient products, no transposed copy of either.  bias [N],
@@ -60,7 +67,7 @@ def _first_order(backward):
     @functools.wraps(backward)
     def marked(ctx, *grads):
         if torch.is_grad_enabled():
-            grads = tuple(g if g.requires_grad else g.detach().requires_grad_() for g in grads)
+            grads = tuple(g if g is None or g.requires_grad else g.detach().requires_grad_() for g in grads)
         return once(ctx, *grads)
     return marked
 
@@ -130,10 +137,77 @@ class _AttentionPacked(torch.autograd.Function):
         return dqkv, None, None, None, None
 
 
-def attention_packed(qkv, Hq: int, Hkv: int, scale=None, causal: bool = False):
+class _AttentionPackedRotary(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, qkv, Hq, Hkv, scale, causal, turns, positions, axes, neighbours, q_weight, k_weight, eps):
+        q, k, v = _packed_views(qkv, Hq, Hkv, "attention_packed")
+        qk = torch.empty((*qkv.shape[:2], q.shape[2] + k.shape[2]), dtype=qkv.dtype, device=qkv.device)
+        qr, kr = qk[..., :q.shape[2]], qk[..., q.shape[2]:]
+        _f.qk_norm_rotary_fwd(q, k, Hq, Hkv, turns, positions, axes, neighbours, q_weight, k_weight, eps, qr, kr)
+        o, lse = _f.attn_fwd(qr, kr, v, Hq, Hkv, scale, causal)
+        ctx.save_for_backward(qkv, qk, o, lse, turns, positions, q_weight, k_weight)
+        ctx.cfg = (Hq, Hkv, scale, causal, axes, neighbours, eps)
+        return o
+
+    @staticmethod
+    @_first_order
+    def backward(ctx, do):
+        qkv, qk, o, lse, turns, positions, q_weight, k_weight = ctx.saved_tensors
+        Hq, Hkv, scale, causal, axes, neighbours, eps = ctx.cfg
+        q, k, v = _packed_views(qkv, Hq, Hkv, "attention_packed")
+        dqkv = torch.empty(qkv.shape, dtype=qkv.dtype, device=qkv.device)
+        dq, dk, dv = _packed_views(dqkv, Hq, Hkv, "attention_packed")
+        _f.attn_bwd(qk[..., :q.shape[2]], qk[..., q.shape[2]:], v, o, _unit(do, "attention_packed"), lse, Hq, Hkv, scale, causal,
+                    dq=dq, dk=dk, dv=dv)
+        # the gradients of what attention read become those of the projection where they lie
+        need = ctx.needs_input_grad[9] or ctx.needs_input_grad[10]
+        _, _, dqw, dkw = _f.qk_norm_rotary_bwd(dq, dk, q, k, Hq, Hkv, turns, positions, axes, neighbours, q_weight, k_weight,
+                                               eps, dq=dq, dk=dk, need_weights=need)
+        return (dqkv,) + (None,) * 8 + (dqw, dkw, None)
+
+
+def _packed_views(qkv, Hq: int, Hkv: int, where: str):
+    """Q, K and V in a packed [B, S, (Hq + 2 Hkv) d] tensor."""
+    if qkv.dim() != 3 or qkv.shape[2] % (Hq + 2 * Hkv):
+        raise _f.FblError(_f.FBL_ERR_SHAPE, f"{where}: qkv has shape {tuple(qkv.shape)}, needs [B, S, ({Hq} + 2 * {Hkv}) d]")
+    d = qkv.shape[2] // (Hq + 2 * Hkv)
+    return qkv[..., :Hq * d], qkv[..., Hq * d:(Hq + Hkv) * d], qkv[..., (Hq + Hkv) * d:]
+
+
+def attention_packed(qkv, Hq: int, Hkv: int, scale=None, causal: bool = False, turns=None, positions=None, axes=None,
+                     neighbours: bool = False, q_weight=None, k_weight=None, eps=None):
     if scale is None:
         scale = 1.0 / math.sqrt(qkv.shape[-1] // (Hq + 2 * Hkv))
-    return _AttentionPacked.apply(qkv, Hq, Hkv, float(scale), bool(causal))
+    if turns is None and eps is None and all(t is None for t in (positions, axes, q_weight, k_weight)):
+        return _AttentionPacked.apply(qkv, Hq, Hkv, float(scale), bool(causal))
+    return _AttentionPackedRotary.apply(qkv, Hq, Hkv, float(scale), bool(causal), turns, positions, axes, bool(neighbours),
+                                        q_weight, k_weight, eps)
+
+
+class _QkNormRotary(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, Hq, Hkv, turns, positions, axes, neighbours, q_weight, k_weight, eps):
+        y = _f.qk_norm_rotary_fwd(q, k, Hq, Hkv, turns, positions, axes, neighbours, q_weight, k_weight, eps)
+        ctx.save_for_backward(q if eps is not None else None, k if eps is not None else None, turns, positions, q_weight,
+                              k_weight)
+        ctx.cfg = (Hq, Hkv, axes, neighbours, eps)
+        return y
+
+    @staticmethod
+    @_first_order
+    def backward(ctx, gq, gk):
+        q, k, turns, positions, q_weight, k_weight = ctx.saved_tensors
+        Hq, Hkv, axes, neighbours, eps = ctx.cfg
+        gq, gk = _unit(gq, "qk_norm_rotary"), None if gk is None else _unit(gk, "qk_norm_rotary")
+        need = ctx.needs_input_grad[8] or ctx.needs_input_grad[9]
+        dq, dk, dqw, dkw = _f.qk_norm_rotary_bwd(gq, gk, q, k, Hq, Hkv, turns, positions, axes, neighbours, q_weight,
+                                                 k_weight, eps, need_weights=need)
+        return dq, dk, None, None, None, None, None, None, dqw, dkw, None
+
+
+def qk_norm_rotary(q, k, Hq: int, Hkv: int, turns=None, positions=None, axes=None, neighbours: bool = False, q_weight=None,
+                   k_weight=None, eps=None):
+    return _QkNormRotary.apply(q, k, Hq, Hkv, turns, positions, axes, bool(neighbours), q_weight, k_weight, eps)
 
 
 class _Linear(torch.autograd.Function):

@@ -107,6 +107,11 @@ bool layer_norm_wide(int f32, int N);  // a row takes 16 wavefronts
 hipError_t launch_column_sums(int f32, const float* part, int groups, int K, int N, void* out0, void* out1,
                               hipStream_t stream);
 
+// Norms of queries and keys and their rotation (qk_norm_rotary.hip), D 32, 64 or 128; forward, or with `bwd` the
+// gradients.  rotary_rows: heads that a wavefront has room for in a step.
+int rotary_rows(int f32, int D);
+hipError_t launch_qk_norm_rotary(int f32, int D, int neighbours, int norm, int bwd, const RotaryArgs& p, hipStream_t stream);
+
 // Products with a linear layer's epilogue (linear_gemm.hpp), ACT of act.hpp: the forward, or with
 // `grad` the data gradient times act'.  bf16 with `tile` of kGemmTiles; fp32 with its own choice.
 template <int ACT>

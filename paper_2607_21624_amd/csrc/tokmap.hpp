@@ -74,6 +74,31 @@ struct BwdArgs {
     int dq_tile = 7;
 };
 
+// Norms of queries and keys for each head and their rotation (qk_norm_rotary.hip).  Of what a call does
+// not have the pointers are nullptr: keys (Hkv 0), weights, x in a backward without norm.
+struct RotaryArgs {
+    const void *q, *k;    // x
+    const void *gq, *gk;  // backward: dy
+    void *oq, *ok;        // y, or dx
+    TokMap mq, mk, mgq, mgk, moq, mok;
+    const void *wq, *wk;
+    float eps;
+    int B, S, Hq, Hkv;
+    // dims (0: no rotation) of a head's values turn; turns [dims / 2], 2^64 a turn a position; positions [axis][b][s]
+    // by strides, nullptr: s; axes: 2 bits for each pair
+    int dims, num_axes;
+    const uint64_t* turns;
+    const int64_t* pos;
+    int64_t pos_axis, pos_batch, pos_token;
+    uint64_t axes[2];
+    // a wavefront's step is `heads` heads (a power of two) of as many tokens as its rows have room for, a group; a
+    // group's heads are `parts` items of `per` steps
+    int heads, per, parts;
+    int64_t groups;
+    int workgroups;
+    float* sums;  // backward: [workgroups][2][D] partial sums of the weights' gradients, or nullptr
+};
+
 // Matrix product C[M, N] = sum_k A(m, k) B(k, n), bf16 operands, row-major
 // storage with leading dimensions in elements.  A is stored [M, K] (or [K, M]
 // when read k-major), B [K, N] (or [N, K] when read n-major); a_bytes/b_bytes

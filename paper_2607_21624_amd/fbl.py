@@ -72,6 +72,7 @@ EXPORTED = ("fbl_layout_desc", "fbl_layout_packed_qkv", "fbl_layout_offset", "fb
             "fbl_proj_float_tile", "fbl_proj_tune_reset", "fbl_layer_norm_fwd", "fbl_layer_norm_bwd_workspace",
             "fbl_layer_norm_bwd", "fbl_linear_fwd", "fbl_linear_fwd_workspace", "fbl_linear_bwd_workspace", "fbl_linear_bwd",
             "fbl_linear_loss_workspace", "fbl_linear_ce_fwd", "fbl_linear_ce_bwd", "fbl_linear_kd_fwd", "fbl_linear_kd_bwd",
+            "fbl_rotary_turns", "fbl_qk_norm_rotary_fwd", "fbl_qk_norm_rotary_bwd_workspace", "fbl_qk_norm_rotary_bwd",
             "fbl_status_str")
 
 
@@ -90,6 +91,23 @@ class Layout(ctypes.Structure):
 class Mask(ctypes.Structure):
     """Mirror of fbl_mask."""
     _fields_ = [("kind", ctypes.c_uint32), ("reserved", ctypes.c_uint32), ("kv_len", ctypes.c_void_p)]
+
+
+FBL_ROTARY_MAX_AXES = 4
+
+
+class RotaryArgs(ctypes.Structure):
+    """Mirror of fbl_rotary."""
+    _fields_ = [("turns", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("stride_axis", ctypes.c_int64),
+                ("stride_batch", ctypes.c_int64), ("stride_token", ctypes.c_int64), ("dims", ctypes.c_int32),
+                ("neighbours", ctypes.c_int32), ("num_axes", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("axes", ctypes.c_uint8 * 64)]
+
+
+class HeadNormArgs(ctypes.Structure):
+    """Mirror of fbl_head_norm."""
+    _fields_ = [("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("eps", ctypes.c_float),
+                ("reserved", ctypes.c_uint32)]
 
 
 class FblError(RuntimeError):
@@ -216,6 +234,15 @@ def _load() -> ctypes.CDLL:
     lib.fbl_linear_kd_bwd.argtypes = [i32, u32, i64, i64, i64, i64, vp, i64, vp, vp, i64, vp, i64, vp, i64, f32, vp, vp, vp,
                                       i64, vp, i64, vp, size, vp]
     lib.fbl_linear_kd_bwd.restype = ctypes.c_int
+    lib.fbl_rotary_turns.argtypes = [P(ctypes.c_double), i64, P(ctypes.c_uint64)]
+    lib.fbl_rotary_turns.restype = ctypes.c_int
+    L, R, H = P(Layout), P(RotaryArgs), P(HeadNormArgs)
+    lib.fbl_qk_norm_rotary_fwd.argtypes = [L, vp, L, vp, R, H, L, vp, L, vp, vp]
+    lib.fbl_qk_norm_rotary_fwd.restype = ctypes.c_int
+    lib.fbl_qk_norm_rotary_bwd_workspace.argtypes = [L, L, sizep]
+    lib.fbl_qk_norm_rotary_bwd_workspace.restype = ctypes.c_int
+    lib.fbl_qk_norm_rotary_bwd.argtypes = [L, vp, L, vp, L, vp, L, vp, R, H, L, vp, L, vp, vp, vp, vp, size, vp]
+    lib.fbl_qk_norm_rotary_bwd.restype = ctypes.c_int
     lib.fbl_status_str.argtypes = [ctypes.c_int]
     lib.fbl_status_str.restype = ctypes.c_char_p
     return lib
@@ -1293,3 +1320,154 @@ def linear_kd_bwd(dloss, x, w, index, prob, lse, temperature: float = 1.0, total
           _ptr(x), ldx, _ptr(w), ldw, _ptr(index), ldi, float(temperature), _ptr(prob), _ptr(lse), _ptr(dx), lddx,
           _ptr(dw), lddw, _ptr(ws), ws_bytes)
     return dx, dw
+
+
+# ---------------------- norms of queries and keys for each head, and their rotation
+def rotary_frequencies(dims: int, base: float = 10000.0):
+    """Radians a position of each of dims / 2 pairs: base ** (-2 j / dims)."""
+    return [base ** (-2.0 * j / dims) for j in range(dims // 2)]
+
+
+def rotary_turns(frequencies, device="cuda"):
+    """The plan of a rotation that a program makes once: int64 [dims / 2] on `device`, the frequencies (radians a
+    position, any sequence of floats) as turns of 64-bit fixed point."""
+    import torch
+    f = [float(x) for x in frequencies]
+    out = (ctypes.c_uint64 * max(len(f), 1))()
+    _check(LIB.fbl_rotary_turns((ctypes.c_double * max(len(f), 1))(*f), len(f), out), "fbl_rotary_turns")
+    return torch.tensor([x - (1 << 64) if x >> 63 else x for x in out], dtype=torch.int64, device=device)
+
+
+def _rotary(turns, positions, axes, neighbours: bool, B: int, S: int, where: str):
+    """fbl_rotary of a call, None where nothing turns.  Both are read by address: what does not agree with
+    the tensors would be read past its end."""
+    import torch
+    if turns is None:
+        if positions is not None or axes is not None:
+            raise FblError(FBL_ERR_ARG, f"{where}: positions and axes need turns")
+        return None
+    if turns.dtype != torch.int64:
+        raise FblError(FBL_ERR_DTYPE, f"{where}: turns is {turns.dtype}, needs torch.int64")
+    if turns.dim() != 1 or not turns.is_contiguous():
+        raise FblError(FBL_ERR_LAYOUT, f"{where}: turns must be one contiguous dimension of dims / 2, as rotary_turns makes it")
+    r = RotaryArgs(turns=turns.data_ptr(), dims=2 * turns.numel(), neighbours=bool(neighbours), num_axes=1)
+    if turns.numel() > 64:
+        raise FblError(FBL_ERR_SHAPE, f"{where}: {turns.numel()} pairs do not fit a head of at most 128")
+    if axes is not None:
+        axes = [int(a) for a in axes]
+        if len(axes) != turns.numel():
+            raise FblError(FBL_ERR_SHAPE, f"{where}: {len(axes)} axes for {turns.numel()} pairs")
+        if positions is None or positions.dim() != 3:
+            raise FblError(FBL_ERR_SHAPE, f"{where}: axes need positions [axes, B, S]")
+        if axes and not 0 <= min(axes) <= max(axes) < min(positions.shape[0], FBL_ROTARY_MAX_AXES):
+            raise FblError(FBL_ERR_ARG, f"{where}: axes must be 0 .. {min(positions.shape[0], FBL_ROTARY_MAX_AXES) - 1}")
+        r.axes[:len(axes)] = axes
+    if positions is not None:
+        if positions.dtype != torch.int64:
+            raise FblError(FBL_ERR_DTYPE, f"{where}: positions is {positions.dtype}, needs torch.int64")
+        want = {1: (S,), 2: (B, S), 3: (positions.shape[0], B, S)}.get(positions.dim())
+        if want is None or tuple(positions.shape) != want or positions.shape[0] == 0:
+            raise FblError(FBL_ERR_SHAPE, f"{where}: positions has shape {tuple(positions.shape)}, needs {(S,)}, {(B, S)} or "
+                                          f"{('axes', B, S)}")
+        if positions.dim() == 3:
+            if axes is None and positions.shape[0] > 1:
+                raise FblError(FBL_ERR_ARG, f"{where}: positions of {positions.shape[0]} axes need axes, the axis of each pair")
+            if positions.shape[0] > FBL_ROTARY_MAX_AXES:
+                raise FblError(FBL_ERR_ARG, f"{where}: {positions.shape[0]} axes, there are at most {FBL_ROTARY_MAX_AXES}")
+            r.num_axes = positions.shape[0]
+        st = positions.stride()
+        r.positions = positions.data_ptr()
+        r.stride_token = st[-1]
+        r.stride_batch = st[-2] if positions.dim() >= 2 else 0
+        r.stride_axis = st[0] if positions.dim() == 3 else 0
+    return r
+
+
+def _head_norm(q_weight, k_weight, eps, D: int, dtype, where: str):
+    """fbl_head_norm of a call, None without a norm."""
+    if eps is None:
+        if q_weight is not None or k_weight is not None:
+            raise FblError(FBL_ERR_ARG, f"{where}: weights need a norm: give eps")
+        return None
+    _vector(q_weight, where, "q_weight", D, dtype)
+    _vector(k_weight, where, "k_weight", D, dtype)
+    return HeadNormArgs(q_weight=_ptr(q_weight), k_weight=_ptr(k_weight), eps=float(eps))
+
+
+def _ref(x):
+    return None if x is None else ctypes.byref(x)
+
+
+def _heads_out(out, like, stream):
+    """`out`, or a new contiguous tensor of like's shape."""
+    return _empty(like.shape, like.dtype, like, stream) if out is None else out
+
+
+def qk_norm_rotary_fwd(q, k, Hq: int, Hkv: int, turns=None, positions=None, axes=None, neighbours: bool = False,
+                       q_weight=None, k_weight=None, eps: Optional[float] = None, q_out=None, k_out=None, stream=None):
+    """Norms of each head of q [B, S, Hq d] and k [B, S, Hkv d] (k may be None) and their rotation by position, d 32, 64 or
+    128: returns (q', k').  eps: of the norm, x / sqrt(mean(x^2) + eps) * weight, None for none; the weights
+    [d] may be None.  turns: rotary_turns of dims / 2 frequencies, None for no rotation; positions: int64 [S], [B, S] or
+    [axes, B, S], None for 0 .. S - 1; axes: with several, the axis of each pair.  The pairs are the halves of the first
+    dims values, or neighbours.  q_out and k_out may be q and k themselves."""
+    where = "qk_norm_rotary_fwd"
+    _check_device(where, stream, q=q, k=k, turns=turns, positions=positions, q_weight=q_weight, k_weight=k_weight,
+                  q_out=q_out, k_out=k_out)
+    lq, lk = _layout(q, Hq), None if k is None else _layout(k, Hkv)
+    B, S = q.shape[:2]
+    rot = _rotary(turns, positions, axes, neighbours, B, S, where)
+    norm = _head_norm(q_weight, k_weight, eps, lq.D, q.dtype, where)
+    q_out = _heads_out(q_out, q, stream)
+    if k is not None:
+        k_out = _heads_out(k_out, k, stream)
+    lqo, lko = _layout(q_out, Hq), None if k_out is None else _layout(k_out, Hkv)
+    _call("fbl_qk_norm_rotary_fwd", q, stream, _ref(lq), _ptr(q), _ref(lk), _ptr(k), _ref(rot), _ref(norm), _ref(lqo),
+          _ptr(q_out), _ref(lko), _ptr(k_out))
+    return q_out, k_out
+
+
+def qk_norm_rotary_bwd_workspace(q, k, Hq: int, Hkv: int) -> int:
+    """Bytes of qk_norm_rotary_bwd's workspace where a weight's gradient is wanted."""
+    n = ctypes.c_size_t(0)
+    _check(LIB.fbl_qk_norm_rotary_bwd_workspace(_ref(_layout(q, Hq)), _ref(None if k is None else _layout(k, Hkv)),
+                                                ctypes.byref(n)), "fbl_qk_norm_rotary_bwd_workspace")
+    return int(n.value)
+
+
+def qk_norm_rotary_bwd(dq_out, dk_out, q, k, Hq: int, Hkv: int, turns=None, positions=None, axes=None,
+                       neighbours: bool = False, q_weight=None, k_weight=None, eps: Optional[float] = None, dq=None, dk=None,
+                       dq_weight=None, dk_weight=None, workspace=None, stream=None, need_weights: bool = True):
+    """Gradients of qk_norm_rotary_fwd from those of its results (dk_out None without keys): returns (dq, dk, dq_weight,
+    dk_weight), the weights' None where there is no weight or need_weights is False.  q and k are the forward's inputs,
+    needed with a norm (else they may be None).  dq and dk may be dq_out and dk_out themselves."""
+    where = "qk_norm_rotary_bwd"
+    if eps is None:
+        q = k = None
+    elif q is None or (k is None) != (dk_out is None):
+        raise FblError(FBL_ERR_NULL, f"{where}: a norm's backward needs the forward's inputs")
+    _check_device(where, stream, dq_out=dq_out, dk_out=dk_out, q=q, k=k, turns=turns, positions=positions, q_weight=q_weight,
+                  k_weight=k_weight, dq=dq, dk=dk, dq_weight=dq_weight, dk_weight=dk_weight, workspace=workspace)
+    lgq, lgk = _layout(dq_out, Hq), None if dk_out is None else _layout(dk_out, Hkv)
+    lq, lk = None if q is None else _layout(q, Hq), None if k is None else _layout(k, Hkv)
+    B, S = dq_out.shape[:2]
+    rot = _rotary(turns, positions, axes, neighbours, B, S, where)
+    norm = _head_norm(q_weight, k_weight, eps, lgq.D, dq_out.dtype, where)
+    dq = _heads_out(dq, dq_out, stream)
+    if dk_out is not None:
+        dk = _heads_out(dk, dk_out, stream)
+    if need_weights:
+        if dq_weight is None and q_weight is not None:
+            dq_weight = _empty(lgq.D, dq_out.dtype, dq_out, stream)
+        if dk_weight is None and k_weight is not None and dk_out is not None:
+            dk_weight = _empty(lgq.D, dq_out.dtype, dq_out, stream)
+    _vector(dq_weight, where, "dq_weight", lgq.D, dq_out.dtype)
+    _vector(dk_weight, where, "dk_weight", lgq.D, dq_out.dtype)
+    ws, ws_bytes = None, 0
+    if dq_weight is not None or dk_weight is not None:
+        need = 0 if workspace is not None else qk_norm_rotary_bwd_workspace(dq_out, dk_out, Hq, Hkv)
+        ws, ws_bytes = _scratch(workspace, need, where, dq_out, stream)
+    ldq, ldk = _layout(dq, Hq), None if dk is None else _layout(dk, Hkv)
+    _call("fbl_qk_norm_rotary_bwd", dq_out, stream, _ref(lgq), _ptr(dq_out), _ref(lgk), _ptr(dk_out), _ref(lq), _ptr(q),
+          _ref(lk), _ptr(k), _ref(rot), _ref(norm), _ref(ldq), _ptr(dq), _ref(ldk), _ptr(dk), _ptr(dq_weight),
+          _ptr(dk_weight), _ptr(ws), ws_bytes)
+    return dq, dk, dq_weight, dk_weight
