@@ -19,5 +19,6 @@ from .fbl import (  # noqa: F401
     FBL_ACT_NONE, FBL_ACT_RELU, FBL_ACT_GELU, FBL_ACT_GELU_TANH, FBL_ACT_SILU, ACTIVATIONS, linear_fwd, linear_fwd_workspace, linear_bwd, linear_bwd_workspace,
     FBL_HEAD_KV, FBL_HEAD_VK, linear_loss_workspace, linear_ce_fwd, linear_ce_bwd, linear_kd_fwd, linear_kd_bwd,
     layer_norm_fwd, layer_norm_bwd, layer_norm_bwd_workspace,
+    gated_fwd, gated_fwd_workspace, gated_bwd, gated_bwd_workspace,
     rotary_frequencies, rotary_turns, qk_norm_rotary_fwd, qk_norm_rotary_bwd, qk_norm_rotary_bwd_workspace,
 )

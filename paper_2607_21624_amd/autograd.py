@@ -23,6 +23,10 @@ torch provides the tensors, the stream and the autograd graph.
   mlp(x, w1, b1, w2, b2, act="gelu", residual=None) -> act(x @ w1 + b1) @ w2 + b2 + residual
       a block's feed-forward part; its backward takes the activation's
       derivative and b1's gradient in the epilogue of the data gradient.  b1, b2 may be None.
+  gated_mlp(x, w1, b1, w2, b2, act="silu", residual=None) -> (act(gate) * up) @ w2 + b2 + residual
+      with (gate, up) = x @ w1 + b1: a gated feed-forward part.  x [..., K], w1 [K, 2F] and b1 [2F] hold gate, then
+      up columns, w2 [F, N]; b1, b2 may be None.  Both projections, the activation and the product are one
+      kernel, and its backward's.
   layer_norm(x, weight=None, bias=None, eps=1e-5) -> y
       x [..., N] (rows one strided matrix), weight and bias [N]; gradients to all three.
   linear_cross_entropy(x, w, labels, ignore_index=-100, reduction="mean") -> loss
@@ -318,6 +322,48 @@ class _Mlp(torch.autograd.Function):
 
 def mlp(x, w1, b1, w2, b2, act: str = "gelu", residual=None):
     return _Mlp.apply(x, w1, b1, w2, b2, residual, act)
+
+
+class _GatedMlp(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, w1, b1, w2, b2, residual, act):
+        x2 = _matrix_of(x, "gated_mlp")
+        res2 = None
+        if residual is not None:
+            if residual.shape != (*x.shape[:-1], w2.shape[1]):
+                raise _f.FblError(_f.FBL_ERR_SHAPE, f"gated_mlp: residual has shape {tuple(residual.shape)}, needs "
+                                                    f"{(*x.shape[:-1], w2.shape[1])}")
+            res2 = _matrix_of(residual, "gated_mlp: residual")
+        z = None
+        if any(ctx.needs_input_grad[:3]):
+            z = torch.empty((x2.shape[0], w1.shape[1]), dtype=x.dtype, device=x.device)
+        h = _f.gated_fwd(x2, w1, b1, act, z=z)
+        y, y2 = _rows_of(x, w2.shape[1])
+        _f.linear_fwd(h, w2, b2, residual=res2, out=y2)
+        ctx.save_for_backward(x2, w1, w2, z, h)
+        ctx.cfg = (x.shape, act)
+        return y
+
+    @staticmethod
+    @_first_order
+    def backward(ctx, dy):
+        x2, w1, w2, z, h = ctx.saved_tensors
+        xshape, act = ctx.cfg
+        need = ctx.needs_input_grad
+        dx = dw1 = db1 = dw2 = db2 = None
+        if any(need[:5]):
+            dy2 = _matrix_of(_unit(dy, "gated_mlp"), "gated_mlp: the incoming gradient")
+            if any(need[:3]):
+                dz, db1 = _f.gated_bwd(dy2, w2, z, act, need_bias=need[2])
+                if need[0] or need[1]:
+                    dx, dw1, _ = _f.linear_bwd(dz, x2, w1, need_dx=need[0], need_dw=need[1], need_bias=False)
+            if need[3] or need[4]:
+                _, dw2, db2 = _f.linear_bwd(dy2, h, w2, need_dx=False, need_dw=need[3], need_bias=need[4])
+        return dx.view(xshape) if need[0] else None, dw1, db1, dw2, db2, dy if need[5] else None, None
+
+
+def gated_mlp(x, w1, b1, w2, b2, act: str = "silu", residual=None):
+    return _GatedMlp.apply(x, w1, b1, w2, b2, residual, act)
 
 
 class _LayerNorm(torch.autograd.Function):

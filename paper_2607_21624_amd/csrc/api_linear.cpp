@@ -8,14 +8,49 @@
 #include "kernels.hpp"
 #include "products.hpp"
 
+using fbl::align256;
+using fbl::few_splits;
+using fbl::few_ws;
+using fbl::forward_tile;
+using fbl::kMaxWidth;
 using fbl::overlap;
 using fbl::RowsView;
 
+namespace fbl {
+
+// Workgroups that share the contraction of a few tokens' tiles.  A tile alone has too few of w's bytes on the
+// way, and the longer its contraction the more that costs; sharing it costs a second launch and the planes
+// (cold weights, us, alone and shared: bf16, 1 token 4096 x 4096 18.3 and 12.3, 8192 x 2048 31.4 and 12.1, 2048 x
+// 8192 11.3 and 12.1, 1024 x 4096 6.8 and 8.9; 64 tokens 4096 x 4096 20.1 and 15.1, 128 tokens 22.7 and 25.0, but
+// 8192 x 2048 33.6 and 25.4; fp32, 12 tokens 4096 x 4096 38 and 23, 1024 x 1024 11.6 and 7.7, 96 tokens 60 and 52).
+// The data gradient, whose contraction is N, the same (dx, bf16, 1 token 2048 x 8192 25.1 and 11.9, 64 tokens 25.1 and
+// 14.9; fp32, 1 token 57 and 19, 128 tokens 59 and 52, 200 tokens 92 and 89, but 1024 x 1024 9.4 and 12.1).
+int few_splits(int f32, int64_t M, int64_t K, int64_t N) {
+    if (M * N >= (int64_t)1 << 29) return 1;  // a plane's offsets
+    return (f32 ? M <= 128 && K >= 1024 : M <= 64 ? K > 2048 : M <= 128 && K >= 8192) ? sum_splits(f32, 0, M, N, K, 0) : 1;
+}
+
+// The tile of a bf16 forward that is not shared.  Up to 32 tokens and 8192 columns that is 32 x 32 on four
+// wavefronts, whose many workgroups have the most loads on the way; wider, the 32 x 128 of the products' own choice
+// covers the CUs too and reads x less often (us, cold weights, 32 x 32 and own choice: 1 token 512 x 8192 4.3 and
+// 5.2, 2048 x 8192 10.9 and 16.5, 2048 x 8200 12.7 and 16.9, 512 x 12288 6.0 and 5.7, 2048 x 12288 18.4 and 17.0,
+// 2048 x 32768 29.9 and 22.7; 17 tokens 2048 x 8192 11.6 and 16.9, 2048 x 12288 19.8 and 17.5).
+int forward_tile(int64_t M, int64_t K, int64_t N) {
+    if (M <= 32 && N <= 8192 && fbl_proj_tuned_tile(FBL_PROJ_FWD, M, K, N) < 0) return 16;
+    return proj_auto_tile(FBL_PROJ_FWD, M, K, N);
+}
+
+hipError_t launch_shares(int f32, int grad, int splits, const GemmArgs& p, float* planes, hipStream_t s) {
+    SumArgs q{};
+    static_cast<GemmArgs&>(q) = p;
+    q.sum = planes, q.lds = p.N, q.sum_bytes = (uint32_t)((int64_t)p.M * p.N * 4);
+    q.first = 1, q.splits = splits, q.share = (int)((((int64_t)p.K + splits - 1) / splits + 63) / 64 * 64);
+    return f32 ? launch_sum_gemm_f32(grad, q, s) : launch_sum_gemm(0, grad, 0, q, s);
+}
+
+}  // namespace fbl
+
 namespace {
-
-constexpr int64_t kMaxWidth = (int64_t)1 << 26;  // of a layer: a launch of 32 threads a column keeps below 2^32
-
-size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 template <int ACT>
 hipError_t run_act(int f32, int grad, int tile, const fbl::LinearArgs& p, hipStream_t s) {
@@ -46,35 +81,9 @@ ActGrid act_grid(int f32, int64_t M, int64_t N) {
 
 // A product of few rows whose contraction `splits` workgroups a tile share, their planes, and what follows it.
 hipError_t run_shared(int f32, int act, int grad, int splits, const fbl::LinearArgs& p, float* planes, hipStream_t s) {
-    fbl::SumArgs q{};
-    static_cast<fbl::GemmArgs&>(q) = p;
-    q.sum = planes, q.lds = p.N, q.sum_bytes = (uint32_t)((int64_t)p.M * p.N * 4);
-    q.first = 1, q.splits = splits, q.share = (int)((((int64_t)p.K + splits - 1) / splits + 63) / 64 * 64);
-    const hipError_t e = f32 ? fbl::launch_sum_gemm_f32(grad, q, s) : fbl::launch_sum_gemm(0, grad, 0, q, s);
+    const hipError_t e = fbl::launch_shares(f32, grad, splits, p, planes, s);
     return e == hipSuccess ? fbl::launch_linear_finish(f32, act, grad, p, planes, splits, s) : e;
 }
-
-// Workgroups that share the contraction of a few tokens' tiles.  A tile alone has too few of w's bytes on the
-// way, and the longer its contraction the more that costs; sharing it costs a second launch and the planes
-// (cold weights, us, alone and shared: bf16, 1 token 4096 x 4096 18.3 and 12.3, 8192 x 2048 31.4 and 12.1, 2048 x
-// 8192 11.3 and 12.1, 1024 x 4096 6.8 and 8.9; 64 tokens 4096 x 4096 20.1 and 15.1, 128 tokens 22.7 and 25.0, but
-// 8192 x 2048 33.6 and 25.4; fp32, 12 tokens 4096 x 4096 38 and 23, 1024 x 1024 11.6 and 7.7, 96 tokens 60 and 52).
-// The data gradient, whose contraction is N, the same (dx, bf16, 1 token 2048 x 8192 25.1 and 11.9, 64 tokens 25.1 and
-// 14.9; fp32, 1 token 57 and 19, 128 tokens 59 and 52, 200 tokens 92 and 89, but 1024 x 1024 9.4 and 12.1).
-int few_splits(int f32, int64_t M, int64_t K, int64_t N) {
-    if (M * N >= (int64_t)1 << 29) return 1;  // a plane's offsets
-    return (f32 ? M <= 128 && K >= 1024 : M <= 64 ? K > 2048 : M <= 128 && K >= 8192) ? fbl::sum_splits(f32, 0, M, N, K, 0) : 1;
-}
-// The tile of a bf16 forward that is not shared.  Up to 32 tokens and 8192 columns that is 32 x 32 on four
-// wavefronts, whose many workgroups have the most loads on the way; wider, the 32 x 128 of the products' own choice
-// covers the CUs too and reads x less often (us, cold weights, 32 x 32 and own choice: 1 token 512 x 8192 4.3 and
-// 5.2, 2048 x 8192 10.9 and 16.5, 2048 x 8200 12.7 and 16.9, 512 x 12288 6.0 and 5.7, 2048 x 12288 18.4 and 17.0,
-// 2048 x 32768 29.9 and 22.7; 17 tokens 2048 x 8192 11.6 and 16.9, 2048 x 12288 19.8 and 17.5).
-int forward_tile(int64_t M, int64_t K, int64_t N) {
-    if (M <= 32 && N <= 8192 && fbl_proj_tuned_tile(FBL_PROJ_FWD, M, K, N) < 0) return 16;
-    return fbl::proj_auto_tile(FBL_PROJ_FWD, M, K, N);
-}
-size_t few_ws(int splits, int64_t M, int64_t N) { return splits > 1 ? (size_t)splits * (size_t)M * (size_t)N * 4 : 0; }
 
 // Workspace of the backward, a function of the shape (a caller may keep it while fbl_proj_tune's choices come and
 // go): partial sums of the bias' gradient, dz, planes of dx, partial sums of dx (as many rows

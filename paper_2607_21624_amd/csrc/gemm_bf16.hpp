@@ -77,6 +77,16 @@ struct GemmCfg {
 // the contraction is split): acc[tn][tm] is the C^T tile of rows m0 + (wm * TM + tm) *
 // 32 + lane % 32 and columns n0 + (wn * TN + tn) * 32 + acc_row(register, lane / 32).
 // The loads have all landed; LDS is free once the wavefronts have met at a barrier.
+//
+// EP::kPairs (where there is one, and true): the weight [K, 2F] holds two matrices side by side, and a tile's columns are
+// 8 of the one, 8 of the other, 8 of the one ..: p.N is 2F, and tile column n is column n0 / 2 + 8 (n / 16) + n % 8 of
+// matrix n / 8 % 2.  A 16-byte load is 8 columns, so only the loads' addresses know; and the accumulators of a column's pair are
+// in one lane, four registers apart.
+template <typename EP, typename = void>
+struct PairsOf : std::false_type {};
+template <typename EP>
+struct PairsOf<EP, std::enable_if_t<EP::kPairs>> : std::true_type {};
+
 struct PlainStore {
     using Args = GemmArgs;
     static constexpr bool kByRows = false;  // done uses by_rows
@@ -90,6 +100,8 @@ proj_gemm_bf16(typename EP::Args p) {
     using TA = typename C::TA;
     using TB = typename C::TB;
     constexpr int TM = C::TM, TN = C::TN, KCW = C::KCW;
+    constexpr bool PAIRS = PairsOf<EP>::value;
+    static_assert(!PAIRS || !BT, "columns of pairs along B's stored rows");
     extern __shared__ __attribute__((aligned(1024))) unsigned char gemm_smem[];
     const uint32_t lds = lds_addr(gemm_smem);
     if constexpr (EP::kSplits) take_share<2, AT, BT>(p);
@@ -111,14 +123,20 @@ proj_gemm_bf16(typename EP::Args p) {
     typename TA::Dma da;
     typename TB::Dma db;
     da.init((uint32_t)(p.lda * 2), wave, lane);
-    db.init((uint32_t)(p.ldb * 2), wave, lane);
+    if constexpr (PAIRS) {
+        const uint32_t second = (uint32_t)p.N;  // bytes from one matrix to the other
+        db.init((uint32_t)(p.ldb * 2), wave, lane,
+                [&](int c) __attribute__((always_inline)) { return (uint32_t)(c >> 1) * 16u + (c & 1 ? second : 0u); });
+    } else {
+        db.init((uint32_t)(p.ldb * 2), wave, lane);
+    }
     auto a_off = [&](int s) __attribute__((always_inline)) {
         const int k0 = s * BK;
         return (uint32_t)((AT ? (int64_t)k0 * p.lda + m0 : (int64_t)m0 * p.lda + k0) * 2);
     };
     auto b_off = [&](int s) __attribute__((always_inline)) {
         const int k0 = s * BK;
-        return (uint32_t)((BT ? (int64_t)n0 * p.ldb + k0 : (int64_t)k0 * p.ldb + n0) * 2);
+        return (uint32_t)((BT ? (int64_t)n0 * p.ldb + k0 : (int64_t)k0 * p.ldb + (PAIRS ? n0 / 2 : n0)) * 2);
     };
     auto issue = [&](int s, int buf) __attribute__((always_inline)) {
         da.issue(lds + buf * C::STAGE, ra, a_off(s), wave);

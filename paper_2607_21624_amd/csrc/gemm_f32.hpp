@@ -46,10 +46,15 @@ struct FTile {
     f32x4 x[PER];
     uint32_t voff[PER];
     FBL_DEV void init(uint32_t row_bytes) {
+        init(row_bytes, [](int c) __attribute__((always_inline)) { return (uint32_t)c * 16u; });
+    }
+    // ... chunk c of a row lies `col(c)` bytes behind the row's origin
+    template <typename F>
+    FBL_DEV void init(uint32_t row_bytes, F&& col) {
 #pragma unroll
         for (int j = 0; j < PER; ++j) {
             const int q = (int)threadIdx.x + j * NT;
-            voff[j] = (uint32_t)(q / CPR) * row_bytes + (uint32_t)(q % CPR) * 16u;
+            voff[j] = (uint32_t)(q / CPR) * row_bytes + col(q % CPR);
         }
     }
     FBL_DEV void load(__amdgpu_buffer_rsrc_t rs, uint32_t origin) {
@@ -120,6 +125,12 @@ struct F32Cfg {
 // the contraction is split): acc[tm][tn] is the tile of rows m0 + (wm * TM + tm) * 32 +
 // acc_row(register, lane / 32) and columns n0 + (wn * TN + tn) * 32 + lane % 32.  LDS is
 // free once the wavefronts have met at a barrier.
+// EP::kPairs: as in gemm_bf16.hpp; a column's pair is eight lanes apart.
+template <typename EP, typename = void>
+struct PairsOfF32 : std::false_type {};
+template <typename EP>
+struct PairsOfF32<EP, std::enable_if_t<EP::kPairs>> : std::true_type {};
+
 struct PlainStoreF32 {
     using Args = GemmArgs;
     static constexpr bool kSplits = false;  // gridDim.y workgroups share a tile's contraction (take_share)
@@ -132,6 +143,8 @@ __global__ __launch_bounds__((F32Cfg<I, AT, BT>::NT), 2) void proj_gemm_f32(type
     using TB = typename C::TB;
     constexpr F32Tile t = C::t;
     constexpr int TM = C::TM, TN = C::TN;
+    constexpr bool PAIRS = PairsOfF32<EP>::value;
+    static_assert(!PAIRS || !BT, "columns of pairs along B's stored rows");
     extern __shared__ __attribute__((aligned(16))) float f32_smem[];
     if constexpr (EP::kSplits) take_share<4, AT, BT>(p);
 
@@ -154,11 +167,18 @@ __global__ __launch_bounds__((F32Cfg<I, AT, BT>::NT), 2) void proj_gemm_f32(type
     TA ta;
     TB tb;
     ta.init((uint32_t)(p.lda * 4));
-    tb.init((uint32_t)(p.ldb * 4));
+    if constexpr (PAIRS) {
+        const uint32_t second = (uint32_t)p.N * 2u;  // bytes from one matrix to the other
+        tb.init((uint32_t)(p.ldb * 4), [&](int c) __attribute__((always_inline)) {
+            return (uint32_t)((c >> 2) * 2 + (c & 1)) * 16u + (c & 2 ? second : 0u);
+        });
+    } else {
+        tb.init((uint32_t)(p.ldb * 4));
+    }
     auto load = [&](int s) __attribute__((always_inline)) {
         const int k0 = s * t.bk;
         ta.load(ra, (uint32_t)((AT ? (int64_t)k0 * p.lda + m0 : (int64_t)m0 * p.lda + k0) * 4));
-        tb.load(rb, (uint32_t)((BT ? (int64_t)n0 * p.ldb + k0 : (int64_t)k0 * p.ldb + n0) * 4));
+        tb.load(rb, (uint32_t)((BT ? (int64_t)n0 * p.ldb + k0 : (int64_t)k0 * p.ldb + (PAIRS ? n0 / 2 : n0)) * 4));
     };
     auto store = [&](int s) __attribute__((always_inline)) {
         float* stage = f32_smem + (s & 1) * C::STAGE;

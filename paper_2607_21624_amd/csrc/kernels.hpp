@@ -121,11 +121,20 @@ template <int ACT>
 hipError_t launch_linear_gemm_f32(int grad, const LinearArgs& p, hipStream_t stream);
 // Rows of LinearArgs::sums that a data gradient with p's extents writes, one for each wavefront's rows of a tile
 // (tile: of the launch, bf16), at most M / 32 + 4.
-int64_t linear_grad_groups(int f32, int tile, const LinearArgs& p);
+int64_t linear_grad_groups(int f32, int tile, const GemmArgs& p);
 // y and z of a forward product, or with `grad` dx of a data gradient, from its planes (launch_sum_gemm), for few rows
 // (linear_finish.hip); p.sums: M rows.
 hipError_t launch_linear_finish(int f32, int act, int grad, const LinearArgs& p, const float* planes, int splits,
                                 hipStream_t stream);
+// The gated layer's products (gated_gemm.hpp): the forward, or with `grad` the data gradient.
+template <int ACT>
+hipError_t launch_gated_gemm(int grad, int tile, const GatedArgs& p, hipStream_t stream);
+template <int ACT>
+hipError_t launch_gated_gemm_f32(int grad, const GatedArgs& p, hipStream_t stream);
+// The same from a product's planes [splits][M][2F], or of the data gradient [splits][M][F] (gated_finish.hip); p.sums: M
+// rows.
+hipError_t launch_gated_finish(int f32, int act, int grad, const GatedArgs& p, const float* planes, int splits,
+                               hipStream_t stream);
 hipError_t launch_linear_act_bwd(int f32, int act, const LinearActArgs& a, hipStream_t stream);
 
 // Softmax losses of a linear head (head_gemm.hip, head_rows.hip); table: the weight is stored

@@ -149,7 +149,7 @@ hipError_t launch_linear_gemm<FBL_ACT>(int grad, int tile, const LinearArgs& p, 
 }
 
 #if FBL_ACT == 0
-int64_t linear_grad_groups(int f32, int tile, const LinearArgs& p) {
+int64_t linear_grad_groups(int f32, int tile, const GemmArgs& p) {
     if (f32) {
         const F32Tile& t = kF32Tiles[f32_tile(p)];
         return ((int64_t)p.M + t.bm - 1) / t.bm * t.wm;

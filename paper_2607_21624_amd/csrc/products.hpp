@@ -2,6 +2,8 @@
 // losses: checks and kernel arguments (host).
 #pragma once
 
+#include <hip/hip_runtime.h>
+
 #include "rows_check.hpp"
 #include "tokmap.hpp"
 
@@ -37,5 +39,19 @@ inline void product(GemmArgs& p, uint32_t op, const RowsView& a, const RowsView&
     p.a_bytes = load_span(a), p.b_bytes = load_span(b);
     p.c_bytes = (uint32_t)c.bytes();
 }
+
+constexpr int64_t kMaxWidth = (int64_t)1 << 26;  // of a layer: a launch of 32 threads a column keeps below 2^32
+
+inline size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
+
+// A few tokens' layer (api_linear.cpp): how many workgroups share the contraction K of a tile of M x N outputs, the bytes of
+// their planes, and the product alone, its shares in `planes` (grad: B stored n-major).
+int few_splits(int f32, int64_t M, int64_t K, int64_t N);
+inline size_t few_ws(int splits, int64_t M, int64_t N) {
+    return splits > 1 ? (size_t)splits * (size_t)M * (size_t)N * 4 : 0;
+}
+hipError_t launch_shares(int f32, int grad, int splits, const GemmArgs& p, float* planes, hipStream_t s);
+// The tile of a bf16 forward that is not shared.
+int forward_tile(int64_t M, int64_t K, int64_t N);
 
 }  // namespace fbl

@@ -203,12 +203,17 @@ struct DmaPlan {
     static_assert(INSTS >= 1, "a tile is at least one 1 KB load");
     uint32_t voff[PER_WAVE];
     FBL_DEV void init(uint32_t row_bytes, int wave, int lane) {
+        init(row_bytes, wave, lane, [](int c) __attribute__((always_inline)) { return (uint32_t)c * 16u; });
+    }
+    // ... chunk c of a row lies `col(c)` bytes behind the row's origin
+    template <typename F>
+    FBL_DEV void init(uint32_t row_bytes, int wave, int lane, F&& col) {
 #pragma unroll
         for (int j = 0; j < PER_WAVE; ++j) {
             const int q = ((j * NWAVES + wave) % INSTS) * 64 + lane;
             const int r = q / G::CPR;
             const int c = (q % G::CPR) ^ G::swz(r);
-            voff[j] = (uint32_t)r * row_bytes + (uint32_t)c * 16u;
+            voff[j] = (uint32_t)r * row_bytes + col(c);
         }
     }
     // Loads rows row0.. of the tile at LDS byte address `tile`.

@@ -145,6 +145,17 @@ struct LinearArgs : GemmArgs {
     float* sums;  // data gradient: [groups][N] sums of c down blocks of rows (linear_grad_groups), or nullptr
 };
 
+// A gated layer's product with its epilogue (gated_gemm.hpp); z [M][2F], gate columns, then up columns.
+// Forward: N is 2F, C is h = act(gate) up of z = A B + bias, z stored where given.  Data gradient: N is F, the product is
+// the gradient of h, C [M][2F] that of the given z.
+struct GatedArgs : GemmArgs {
+    const void* bias;
+    void* z;
+    int64_t ldz;
+    uint32_t z_bytes;
+    float* sums;  // data gradient: [groups][2F] sums of C down blocks of rows (linear_grad_groups), or nullptr
+};
+
 // dz = dy act'(z) over M x N; part, where not nullptr, gets [groups][N] sums down blocks of `rows` rows.
 struct LinearActArgs {
     const void* dy;

@@ -73,7 +73,7 @@ EXPORTED = ("fbl_layout_desc", "fbl_layout_packed_qkv", "fbl_layout_offset", "fb
             "fbl_layer_norm_bwd", "fbl_linear_fwd", "fbl_linear_fwd_workspace", "fbl_linear_bwd_workspace", "fbl_linear_bwd",
             "fbl_linear_loss_workspace", "fbl_linear_ce_fwd", "fbl_linear_ce_bwd", "fbl_linear_kd_fwd", "fbl_linear_kd_bwd",
             "fbl_rotary_turns", "fbl_qk_norm_rotary_fwd", "fbl_qk_norm_rotary_bwd_workspace", "fbl_qk_norm_rotary_bwd",
-            "fbl_status_str")
+            "fbl_gated_fwd", "fbl_gated_fwd_workspace", "fbl_gated_bwd_workspace", "fbl_gated_bwd", "fbl_status_str")
 
 
 class Layout(ctypes.Structure):
@@ -243,6 +243,14 @@ def _load() -> ctypes.CDLL:
     lib.fbl_qk_norm_rotary_bwd_workspace.restype = ctypes.c_int
     lib.fbl_qk_norm_rotary_bwd.argtypes = [L, vp, L, vp, L, vp, L, vp, R, H, L, vp, L, vp, vp, vp, vp, size, vp]
     lib.fbl_qk_norm_rotary_bwd.restype = ctypes.c_int
+    lib.fbl_gated_fwd.argtypes = [i32, u32, i64, i64, i64, vp, i64, vp, i64, vp, vp, i64, vp, i64, i32, vp, size, vp]
+    lib.fbl_gated_fwd.restype = ctypes.c_int
+    lib.fbl_gated_fwd_workspace.argtypes = [i32, i64, i64, i64, sizep]
+    lib.fbl_gated_fwd_workspace.restype = ctypes.c_int
+    lib.fbl_gated_bwd_workspace.argtypes = [i32, i64, i64, i64, sizep]
+    lib.fbl_gated_bwd_workspace.restype = ctypes.c_int
+    lib.fbl_gated_bwd.argtypes = [i32, u32, i64, i64, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, i32, vp, size, vp]
+    lib.fbl_gated_bwd.restype = ctypes.c_int
     lib.fbl_status_str.argtypes = [ctypes.c_int]
     lib.fbl_status_str.restype = ctypes.c_char_p
     return lib
@@ -1100,6 +1108,90 @@ def linear_bwd(dy, x, w, z=None, act: str = "none", dx=None, dw=None, dbias=None
     _call("fbl_linear_bwd", x, stream, dt, code, M, K, N, _ptr(dy), lddy, _ptr(x), ldx, _ptr(w), ldw, _ptr(z), ldz,
           xcode, _ptr(x_z), ldxz, _ptr(dx), lddx, _ptr(dxbias), _ptr(dw), lddw, _ptr(dbias), _ptr(ws), ws_bytes)
     return dx, dw, dbias
+
+
+# ------------------------------------------------------------------ gated layers
+def _gated_width(w, where: str) -> int:
+    if w.dim() != 2 or w.shape[1] % 2:
+        raise FblError(FBL_ERR_SHAPE, f"{where}: w has shape {tuple(w.shape)}, needs [K, 2 F], gate then up columns")
+    return w.shape[1] // 2
+
+
+def gated_fwd_workspace(x, w) -> int:
+    """Bytes of gated_fwd's workspace for x [M, K] and w [K, 2F]: 0 but for a few tokens."""
+    n = ctypes.c_size_t(0)
+    _check(LIB.fbl_gated_fwd_workspace(_dtype_code(x), *x.shape, _gated_width(w, "gated_fwd_workspace"), ctypes.byref(n)),
+           "fbl_gated_fwd_workspace")
+    return int(n.value)
+
+
+def gated_fwd(x, w, bias=None, act: str = "silu", out=None, z=None, tile: int = FBL_GEMM_TILE_AUTO, workspace=None,
+              stream=None):
+    """h = act(gate) * up with (gate, up) = x w + bias for x [M, K], w [K, 2F] and bias [2F], gate then up columns (any row
+    strides, one storage type), act one of ACTIVATIONS.  z [M, 2F], where given, receives the pre-activations,
+    which gated_bwd needs.  workspace: gated_fwd_workspace bytes, allocated where they are needed and it is None.
+    Returns h [M, F]."""
+    import torch
+    where = "gated_fwd"
+    _check_device(where, stream, x=x, w=w, bias=bias, out=out, z=z, workspace=workspace)
+    ldx = _matrix(x, where, "x")
+    M, K = x.shape
+    dt, code = _dtype_code(x), _act_code(act, where)
+    ldw = _matrix(w, where, "w", None, x)
+    F = _gated_width(w, where)
+    if w.shape[0] != K:
+        raise FblError(FBL_ERR_SHAPE, f"{where}: x {tuple(x.shape)} and w {tuple(w.shape)} do not agree")
+    _vector(bias, where, "bias", 2 * F, x.dtype)
+    ldz = 0 if z is None else _matrix(z, where, "z", (M, 2 * F), x)
+    if out is None:
+        out = _empty((M, F), x.dtype, x, stream)
+    ldh = _matrix(out, where, "out", (M, F), x)
+    ws, ws_bytes = None, 0
+    need = gated_fwd_workspace(x, w) if workspace is None and M <= 128 and tile == FBL_GEMM_TILE_AUTO else 0
+    if workspace is not None or need:
+        ws, ws_bytes = _scratch(workspace, need, where, x, stream)
+    _call("fbl_gated_fwd", x, stream, dt, code, M, K, F, _ptr(x), ldx, _ptr(w), ldw, _ptr(bias), _ptr(out), ldh, _ptr(z),
+          ldz, tile, _ptr(ws), ws_bytes)
+    return out
+
+
+def gated_bwd_workspace(dy, w_down) -> int:
+    """Bytes of gated_bwd's workspace for dy [M, N] and w_down [F, N]."""
+    n = ctypes.c_size_t(0)
+    _check(LIB.fbl_gated_bwd_workspace(_dtype_code(dy), dy.shape[0], *w_down.shape, ctypes.byref(n)),
+           "fbl_gated_bwd_workspace")
+    return int(n.value)
+
+
+def gated_bwd(dy, w_down, z, act: str = "silu", dz=None, dbias=None, tile: int = FBL_GEMM_TILE_AUTO, workspace=None,
+              stream=None, need_bias: bool = True):
+    """Gradient of a gated layer's pre-activations from that of the block's result: dy [M, N], w_down [F, N] and the
+    forward's z [M, 2F] give dz [M, 2F] and the sums of dz over its rows, dbias [2F].  Returns (dz, dbias), dbias None
+    where not needed.  dx and dw are linear_bwd's of dz."""
+    import torch
+    where = "gated_bwd"
+    _check_device(where, stream, dy=dy, w_down=w_down, z=z, dz=dz, dbias=dbias, workspace=workspace)
+    lddy = _matrix(dy, where, "dy")
+    M, N = dy.shape
+    dt, code = _dtype_code(dy), _act_code(act, where)
+    ldwd = _matrix(w_down, where, "w_down", None, dy)
+    F = w_down.shape[0]
+    if w_down.shape[1] != N:
+        raise FblError(FBL_ERR_SHAPE, f"{where}: dy {tuple(dy.shape)} and w_down {tuple(w_down.shape)} do not agree")
+    ldz = _matrix(z, where, "z", (M, 2 * F), dy)
+    if dz is None:
+        dz = _empty((M, 2 * F), dy.dtype, dy, stream)
+    lddz = _matrix(dz, where, "dz", (M, 2 * F), dy)
+    if dbias is None and need_bias:
+        dbias = _empty(2 * F, dy.dtype, dy, stream)
+    _vector(dbias, where, "dbias", 2 * F, dy.dtype)
+    ws, ws_bytes = None, 0
+    if dbias is not None or workspace is not None or M <= 128:
+        need = 0 if workspace is not None else gated_bwd_workspace(dy, w_down)
+        ws, ws_bytes = _scratch(workspace, need, where, dy, stream)
+    _call("fbl_gated_bwd", dy, stream, dt, code, M, F, N, _ptr(dy), lddy, _ptr(w_down), ldwd, _ptr(z), ldz, _ptr(dz), lddz,
+          _ptr(dbias), tile, _ptr(ws), ws_bytes)
+    return dz, dbias
 
 
 # ------------------------------------- losses of a linear head over a vocabulary
