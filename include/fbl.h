@@ -825,6 +825,35 @@ fbl_status fbl_gated_bwd(int32_t dtype, uint32_t act, int64_t M, int64_t F, int6
                          const void* w_down, int64_t ldwd, const void* z, int64_t ldz, void* dz, int64_t lddz, void* dbias,
                          int32_t tile, void* ws, size_t ws_bytes, void* stream);
 
+/*
+ * The end of a training step: the global norm of a list of gradients, and the gradients clipped by it.
+ *   norm = sqrt(sum of squares over all values of all tensors)
+ *   out  = g * min(1, limit / (norm + 1e-6))
+ * fbl_grad describes one tensor: n values of `dtype` (FBL_F32 or FBL_BF16, which a list may mix) in one piece at p, and
+ * where clipping writes them, `out`: p itself, or other memory of the same size.  n may be 0 (p is then not read).  The
+ * list (host memory) is not kept.
+ *   fbl_grad_norm       norm (float32, device memory); `out` is not looked at
+ *   fbl_grad_clip       out from a norm that is given: the program's own, or of gradients that lie on several devices
+ *   fbl_clip_grad_norm  both
+ * In place, a norm within the limit leaves the gradients untouched.  The norm is summed in float64 in a fixed order and
+ * rounded once; it does not overflow before its own value does.  An infinite norm makes the scale 0 (an infinite
+ * gradient then nan), a norm of nan everything nan.  Workspace: fbl_grad_norm_workspace bytes for `count` tensors, 8-byte
+ * aligned; nothing is kept in it.  A launch takes 112 tensors.
+ * Checks: count >= 1, limit >= 0 (FBL_ERR_ARG; infinity: no clipping), pointers aligned to their element, no two tensors,
+ * outputs, norm or workspace sharing a byte (FBL_ERR_ARG; the same tensor twice is one such case), 2^45 bytes at most.
+ */
+typedef struct {
+    const void* p;
+    void* out;
+    int64_t n;
+    int32_t dtype, reserved; /* reserved: zero */
+} fbl_grad;
+fbl_status fbl_grad_norm_workspace(int64_t count, size_t* bytes);
+fbl_status fbl_grad_norm(int64_t count, const fbl_grad* grads, float* norm, void* ws, size_t ws_bytes, void* stream);
+fbl_status fbl_grad_clip(int64_t count, const fbl_grad* grads, const float* norm, float limit, void* stream);
+fbl_status fbl_clip_grad_norm(int64_t count, const fbl_grad* grads, float limit, float* norm, void* ws, size_t ws_bytes,
+                              void* stream);
+
 /* Static, human-readable name of a status code. */
 const char* fbl_status_str(fbl_status s);
 

@@ -20,5 +20,6 @@ from .fbl import (  # noqa: F401
     FBL_HEAD_KV, FBL_HEAD_VK, linear_loss_workspace, linear_ce_fwd, linear_ce_bwd, linear_kd_fwd, linear_kd_bwd,
     layer_norm_fwd, layer_norm_bwd, layer_norm_bwd_workspace,
     gated_fwd, gated_fwd_workspace, gated_bwd, gated_bwd_workspace,
+    grad_norm, grad_norm_workspace, clip_grads, clip_grad_norm,
     rotary_frequencies, rotary_turns, qk_norm_rotary_fwd, qk_norm_rotary_bwd, qk_norm_rotary_bwd_workspace,
 )

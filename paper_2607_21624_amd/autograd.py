@@ -37,6 +37,9 @@ torch provides the tensors, the stream and the autograd graph.
   linear_distillation(x, w, index, logits, temperature=1.0, reduction="mean") -> loss
       the same from a teacher's top logits: index int64 and logits [..., top].  The
       teacher is a constant: logits that require grad get no gradient from here.
+  clip_grad_norm_(parameters, limit) -> norm
+      the norm of all parameters' .grad (those that are not None), which are scaled in place where it is above
+      the limit: grad * min(1, limit / (norm + 1e-6)).  norm float32, of the gradients as they were.
 
 Gradients are those of the first order: taken with create_graph they hold their
 values, and differentiating them raises an error.
@@ -477,3 +480,10 @@ class _LinearDistillation(torch.autograd.Function):
 
 def linear_distillation(x, w, index, logits, temperature: float = 1.0, reduction: str = "mean"):
     return _LinearDistillation.apply(x, w, index, logits, float(temperature), reduction)
+
+
+def clip_grad_norm_(parameters, limit: float):
+    grads = [p.grad for p in ([parameters] if isinstance(parameters, torch.Tensor) else parameters) if p.grad is not None]
+    norm = _f.clip_grad_norm(grads, limit)
+    torch.autograd.graph.increment_version(grads)  # changed in place
+    return norm

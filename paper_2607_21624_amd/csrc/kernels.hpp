@@ -137,6 +137,13 @@ hipError_t launch_gated_finish(int f32, int act, int grad, const GatedArgs& p, c
                                hipStream_t stream);
 hipError_t launch_linear_act_bwd(int f32, int act, const LinearActArgs& a, hipStream_t stream);
 
+// Sums of squares of a list's tensors, one for each workgroup; the norm from n of them; out = g min(1, limit / (norm +
+// 1e-6)), the norm being that of n sums, which is then written where norm is not nullptr, or, sums nullptr, norm's.
+hipError_t launch_grad_squares(const GradList& a, double* sums, int workgroups, hipStream_t stream);
+hipError_t launch_grad_norm(const double* sums, int n, float* norm, hipStream_t stream);
+hipError_t launch_grad_scale(const GradList& a, const double* sums, int n, float* norm, float limit, int workgroups,
+                             hipStream_t stream);
+
 // Softmax losses of a linear head (head_gemm.hip, head_rows.hip); table: the weight is stored
 // [V, K], else [K, V].
 constexpr int kHeadMaxTop = 1024;

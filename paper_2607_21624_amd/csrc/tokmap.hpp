@@ -156,6 +156,21 @@ struct GatedArgs : GemmArgs {
     float* sums;  // data gradient: [groups][2F] sums of C down blocks of rows (linear_grad_groups), or nullptr
 };
 
+// Tensors of one launch over a list of gradients (grad_clip.hip), by value in its arguments: `first` chunks of kGradChunk
+// bytes come before each, and first[count] = chunks.
+constexpr int kGradChunk = 32768;
+constexpr int kGradTensors = 112;
+struct GradList {
+    struct {
+        const void* p;
+        void* out;
+        int64_t n : 62, f32 : 2;
+    } t[kGradTensors];
+    int first[kGradTensors + 1];
+    int count, chunks;
+};
+static_assert(sizeof(GradList) <= 3584, "a launch's arguments end at 4 KB");
+
 // dz = dy act'(z) over M x N; part, where not nullptr, gets [groups][N] sums down blocks of `rows` rows.
 struct LinearActArgs {
     const void* dy;

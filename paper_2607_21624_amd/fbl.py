@@ -73,7 +73,8 @@ EXPORTED = ("fbl_layout_desc", "fbl_layout_packed_qkv", "fbl_layout_offset", "fb
             "fbl_layer_norm_bwd", "fbl_linear_fwd", "fbl_linear_fwd_workspace", "fbl_linear_bwd_workspace", "fbl_linear_bwd",
             "fbl_linear_loss_workspace", "fbl_linear_ce_fwd", "fbl_linear_ce_bwd", "fbl_linear_kd_fwd", "fbl_linear_kd_bwd",
             "fbl_rotary_turns", "fbl_qk_norm_rotary_fwd", "fbl_qk_norm_rotary_bwd_workspace", "fbl_qk_norm_rotary_bwd",
-            "fbl_gated_fwd", "fbl_gated_fwd_workspace", "fbl_gated_bwd_workspace", "fbl_gated_bwd", "fbl_status_str")
+            "fbl_gated_fwd", "fbl_gated_fwd_workspace", "fbl_gated_bwd_workspace", "fbl_gated_bwd",
+            "fbl_grad_norm_workspace", "fbl_grad_norm", "fbl_grad_clip", "fbl_clip_grad_norm", "fbl_status_str")
 
 
 class Layout(ctypes.Structure):
@@ -108,6 +109,12 @@ class HeadNormArgs(ctypes.Structure):
     """Mirror of fbl_head_norm."""
     _fields_ = [("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("eps", ctypes.c_float),
                 ("reserved", ctypes.c_uint32)]
+
+
+class Grad(ctypes.Structure):
+    """Mirror of fbl_grad."""
+    _fields_ = [("p", ctypes.c_void_p), ("out", ctypes.c_void_p), ("n", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
 
 
 class FblError(RuntimeError):
@@ -251,6 +258,14 @@ def _load() -> ctypes.CDLL:
     lib.fbl_gated_bwd_workspace.restype = ctypes.c_int
     lib.fbl_gated_bwd.argtypes = [i32, u32, i64, i64, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, i32, vp, size, vp]
     lib.fbl_gated_bwd.restype = ctypes.c_int
+    lib.fbl_grad_norm_workspace.argtypes = [i64, sizep]
+    lib.fbl_grad_norm_workspace.restype = ctypes.c_int
+    lib.fbl_grad_norm.argtypes = [i64, P(Grad), vp, vp, size, vp]
+    lib.fbl_grad_norm.restype = ctypes.c_int
+    lib.fbl_grad_clip.argtypes = [i64, P(Grad), vp, f32, vp]
+    lib.fbl_grad_clip.restype = ctypes.c_int
+    lib.fbl_clip_grad_norm.argtypes = [i64, P(Grad), f32, vp, vp, size, vp]
+    lib.fbl_clip_grad_norm.restype = ctypes.c_int
     lib.fbl_status_str.argtypes = [ctypes.c_int]
     lib.fbl_status_str.restype = ctypes.c_char_p
     return lib
@@ -1563,3 +1578,95 @@ def qk_norm_rotary_bwd(dq_out, dk_out, q, k, Hq: int, Hkv: int, turns=None, posi
           _ref(lk), _ptr(k), _ref(rot), _ref(norm), _ref(ldq), _ptr(dq), _ref(ldk), _ptr(dk), _ptr(dq_weight),
           _ptr(dk_weight), _ptr(ws), ws_bytes)
     return dq, dk, dq_weight, dk_weight
+
+
+# ------------------------------------------------- the global norm of gradients
+def _dense(t) -> bool:
+    """Whether a tensor's values lie in one piece of memory, in any order of its dimensions."""
+    if t.is_contiguous():
+        return True
+    step = 1
+    for stride, size in sorted((st, n) for st, n in zip(t.stride(), t.shape) if n > 1):
+        if stride != step:
+            return False
+        step *= size
+    return True
+
+
+def _grad_list(grads, out, where: str):
+    """(fbl_grad array, the first tensor) of a list of gradients and of the tensors that receive them."""
+    import torch
+    grads = list(grads)
+    out = grads if out is None else list(out)
+    if not grads:
+        raise FblError(FBL_ERR_SHAPE, f"{where}: no gradients")
+    if len(out) != len(grads):
+        raise FblError(FBL_ERR_SHAPE, f"{where}: {len(out)} outputs for {len(grads)} gradients")
+    a = (Grad * len(grads))()
+    first = grads[0]
+    for i, (g, o) in enumerate(zip(grads, out)):
+        for name, t in (("grads", g), ("out", o)):
+            if not isinstance(t, torch.Tensor) or t.layout != torch.strided:
+                raise FblError(FBL_ERR_ARG, f"{where}: {name}[{i}] must be a plain tensor")
+            if not t.is_cuda or t.device != first.device:
+                raise FblError(FBL_ERR_ARG, f"{where}: {name}[{i}] is on {t.device}, all must be on one GPU"
+                                            + (f", grads[0] is on {first.device}" if first.is_cuda else ""))
+        if not _dense(g):
+            raise FblError(FBL_ERR_LAYOUT, f"{where}: grads[{i}] has gaps, shape {tuple(g.shape)} strides {g.stride()}")
+        if o is not g:
+            if o.dtype != g.dtype:
+                raise FblError(FBL_ERR_DTYPE, f"{where}: out[{i}] is {o.dtype}, needs {g.dtype}")
+            if o.shape != g.shape or any(x != y for x, y, n in zip(o.stride(), g.stride(), g.shape) if n > 1):
+                raise FblError(FBL_ERR_SHAPE, f"{where}: out[{i}] has shape {tuple(o.shape)} strides {o.stride()}, needs "
+                                              f"{tuple(g.shape)} {g.stride()}")
+        a[i].p, a[i].out, a[i].n, a[i].dtype = g.data_ptr(), o.data_ptr(), g.numel(), _dtype_code(g)
+    return a, first
+
+
+def _norm_out(norm, like, where: str, stream):
+    import torch
+    if norm is None:
+        return _empty((), torch.float32, like, stream)
+    if norm.dtype != torch.float32 or norm.numel() != 1:
+        raise FblError(FBL_ERR_SHAPE, f"{where}: norm must be one float32")
+    return norm
+
+
+def grad_norm_workspace(grads) -> int:
+    """Bytes of grad_norm's and clip_grad_norm's workspace."""
+    n = ctypes.c_size_t(0)
+    _check(LIB.fbl_grad_norm_workspace(len(grads), ctypes.byref(n)), "fbl_grad_norm_workspace")
+    return int(n.value)
+
+
+def grad_norm(grads, norm=None, workspace=None, stream=None):
+    """The norm of all values of a list of tensors (float32 and bfloat16, each in one piece of memory): one
+    float32 on their device."""
+    where = "grad_norm"
+    a, like = _grad_list(grads, None, where)
+    norm = _norm_out(norm, like, where, stream)
+    _check_device(where, stream, grads=like, norm=norm, workspace=workspace)
+    ws, ws_bytes = _scratch(workspace, 0 if workspace is not None else grad_norm_workspace(a), where, like, stream)
+    _call("fbl_grad_norm", like, stream, len(a), a, _ptr(norm), _ptr(ws), ws_bytes)
+    return norm
+
+
+def clip_grads(grads, norm, limit: float, out=None, stream=None) -> None:
+    """Every gradient times min(1, limit / (norm + 1e-6)), in place or into the tensors of `out`; norm is one float32 on
+    their device (grad_norm's, or the program's own)."""
+    where = "clip_grads"
+    a, like = _grad_list(grads, out, where)
+    norm = _norm_out(norm, like, where, stream)
+    _check_device(where, stream, grads=like, norm=norm)
+    _call("fbl_grad_clip", like, stream, len(a), a, _ptr(norm), float(limit))
+
+
+def clip_grad_norm(grads, limit: float, out=None, norm=None, workspace=None, stream=None):
+    """grad_norm and clip_grads by it in one call: returns the norm of the gradients as they were."""
+    where = "clip_grad_norm"
+    a, like = _grad_list(grads, out, where)
+    norm = _norm_out(norm, like, where, stream)
+    _check_device(where, stream, grads=like, norm=norm, workspace=workspace)
+    ws, ws_bytes = _scratch(workspace, 0 if workspace is not None else grad_norm_workspace(a), where, like, stream)
+    _call("fbl_clip_grad_norm", like, stream, len(a), a, float(limit), _ptr(norm), _ptr(ws), ws_bytes)
+    return norm
