@@ -32,7 +32,7 @@ void plan(fbl::RotaryArgs& p, int f32, int64_t D, bool sums) {
     p.per = (int)((steps + parts - 1) / parts);
     p.parts = (steps + p.per - 1) / p.per;
     const int64_t wgs = (p.groups * p.parts + 3) / 4;
-    p.workgroups = (int)std::min<int64_t>(wgs, sums ? 1024 : 4096);
+    p.workgroups = (int)std::min<int64_t>(wgs, sums ? 768 : 2560);
 }
 
 // Extents and layouts of queries and (where there) keys.

@@ -87,23 +87,26 @@ struct HeadRow {
     static constexpr int b(int i) { return NEIGHBOURS ? 2 * i + 1 : V + i; }
 };
 
+// A lane's two chunks of a head's row as they are stored, and as numbers.
 template <typename T>
-FBL_DEV void load2(float (&x)[2 * Chunk<T>::V], const T* p, int c0, int c1) {
-    using C = Chunk<T>;
-    const C u = *reinterpret_cast<const C*>(p + c0), v = *reinterpret_cast<const C*>(p + c1);
+struct Two {
+    static constexpr int V = Chunk<T>::V;
+    Chunk<T> c[2];
+    FBL_DEV void load(const T* p, int c0, int c1) {
+        c[0] = *reinterpret_cast<const Chunk<T>*>(p + c0);
+        c[1] = *reinterpret_cast<const Chunk<T>*>(p + c1);
+    }
+    FBL_DEV void store(T* p, int c0, int c1) const {
+        *reinterpret_cast<Chunk<T>*>(p + c0) = c[0];
+        *reinterpret_cast<Chunk<T>*>(p + c1) = c[1];
+    }
+    FBL_DEV float operator[](int e) const { return (float)c[e / V].v[e % V]; }
+    FBL_DEV void set(int e, float x) { c[e / V].v[e % V] = (T)x; }
+    FBL_DEV void clear() {
 #pragma unroll
-    for (int e = 0; e < C::V; ++e) x[e] = (float)u.v[e], x[C::V + e] = (float)v.v[e];
-}
-template <typename T>
-FBL_DEV void store2(const float (&x)[2 * Chunk<T>::V], T* p, int c0, int c1) {
-    using C = Chunk<T>;
-    C u, v;
-#pragma unroll
-    for (int e = 0; e < C::V; ++e) u.v[e] = (T)x[e], v.v[e] = (T)x[C::V + e];
-    *reinterpret_cast<C*>(p + c0) = u;
-    *reinterpret_cast<C*>(p + c1) = v;
-}
-
+        for (int e = 0; e < 2 * V; ++e) set(e, 0.f);
+    }
+};
 // (a, b) by the angle, or BACK by its negative
 template <typename H, bool BACK, int V>
 FBL_DEV void rotate(float (&x)[2 * V], const float (&c)[V], const float (&s)[V]) {
@@ -116,7 +119,7 @@ FBL_DEV void rotate(float (&x)[2 * V], const float (&c)[V], const float (&s)[V])
 }
 
 template <typename T, int D, bool NEIGHBOURS, bool NORM, bool BWD>
-__global__ __launch_bounds__(256) void qk_norm_rotary(RotaryArgs p) {
+__global__ __launch_bounds__(256, (NORM && BWD ? 3 : 5)) void qk_norm_rotary(RotaryArgs p) {
     using H = HeadRow<T, D, NEIGHBOURS>;
     constexpr int V = H::V, LANES = H::LANES, ROWS = H::ROWS;
     constexpr bool SUMS = NORM && BWD;
@@ -126,106 +129,143 @@ __global__ __launch_bounds__(256) void qk_norm_rotary(RotaryArgs p) {
     const bool turns = 2 * pair < p.dims;  // the lane's pairs, all or none (dims are whole lanes)
     const int hsub = sub & (p.heads - 1), tsub = sub / p.heads;  // heads: a power of two, up to ROWS
     const int H_all = p.Hq + p.Hkv;
-    const int64_t tokens = (int64_t)p.B * p.S;
+    const uint32_t tokens = (uint32_t)p.B * (uint32_t)p.S, per_group = ROWS / p.heads;
 
-    // weights of the lane's columns
-    float w[2][2 * V];
+    // A wavefront's items: blocks of `per` steps of heads of a group of tokens.  While one step is computed the next one's
+    // rows, and its tokens' positions, are on the way.
+    struct Step {
+        int64_t item;
+        int h0;
+        int b, s;   // of the lane's token
+        bool there;
+    };
+    const int64_t items = p.groups * p.parts, stride = (int64_t)gridDim.x * 4;
+    Two<T> nx, ng;
+    int64_t at[4];
+    const auto enter = [&](Step& k, int64_t item) __attribute__((always_inline)) {
+        k.item = item;
+        const uint32_t group = (uint32_t)(item / p.parts), part = (uint32_t)(item - (int64_t)group * p.parts);
+        const uint32_t token = group * per_group + tsub;
+        k.there = token < tokens;
+        k.b = k.there ? (int)(token / (uint32_t)p.S) : 0;
+        k.s = k.there ? (int)(token - (uint32_t)k.b * (uint32_t)p.S) : 0;
+        k.h0 = (int)part * p.per * p.heads;
+        if (!p.dims) return;
+#pragma unroll
+        for (int a = 0; a < 4; ++a)
+            if (a < p.num_axes) at[a] = p.pos ? p.pos[a * p.pos_axis + k.b * p.pos_batch + k.s * p.pos_token] : k.s;
+    };
+    const auto fetch = [&](const Step& k) __attribute__((always_inline)) {
+        const int h = k.h0 + hsub;
+        if (!k.there || h >= H_all) return;
+        const bool key = h >= p.Hq;
+        const int hk = key ? h - p.Hq : h;
+        if (!BWD || NORM) nx.load(static_cast<const T*>(key ? p.k : p.q) + (key ? p.mk : p.mq).offset(k.b, hk, k.s, 0), c0, c1);
+        if (BWD) ng.load(static_cast<const T*>(key ? p.gk : p.gq) + (key ? p.mgk : p.mgq).offset(k.b, hk, k.s, 0), c0, c1);
+    };
+    Step cur{}, next{};
+    next.item = (int64_t)blockIdx.x * 4 + wave;
+    if (next.item < items) {
+        enter(next, next.item);
+        fetch(next);
+    }
+
+    // weights and frequencies in LDS: in registers, unpacked for every step, they are what keeps a third wavefront out
+    __shared__ T lw[2][D] __attribute__((aligned(16)));
+    __shared__ uint64_t lfreq[D / 2] __attribute__((aligned(16)));
+    if (NORM && threadIdx.x < 2 * D) {
+        const int k = threadIdx.x / D, c = threadIdx.x % D;
+        const T* const wp = static_cast<const T*>(k ? p.wk : p.wq);
+        lw[k][c] = wp ? wp[c] : (T)1.f;
+    }
+    if (2 * (int)threadIdx.x < p.dims) lfreq[threadIdx.x] = p.turns[threadIdx.x];
+    __syncthreads();
     float sum[2][2 * V];
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        const T* wp = static_cast<const T*>(k ? p.wk : p.wq);
+    for (int k = 0; k < 2; ++k)
 #pragma unroll
-        for (int e = 0; e < 2 * V; ++e) w[k][e] = 1.f, sum[k][e] = 0.f;
-        if (NORM && wp) {
-#pragma unroll
-            for (int e = 0; e < V; ++e) w[k][e] = (float)wp[c0 + e], w[k][V + e] = (float)wp[c1 + e];
-        }
-    }
-    uint64_t freq[V];
-    int axis[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        freq[i] = turns ? p.turns[pair + i] : 0;
-        axis[i] = (int)(p.axes[(pair + i) / 32] >> (pair + i) % 32 * 2) & 3;
-    }
+        for (int e = 0; e < 2 * V; ++e) sum[k][e] = 0.f;
+    float cs[V], sn[V];
+    cur.item = -1;
 
-    // a wavefront's items: blocks of `per` steps of heads of a group of tokens
-    const int64_t items = p.groups * p.parts;
-    for (int64_t item = (int64_t)blockIdx.x * 4 + wave; item < items; item += (int64_t)gridDim.x * 4) {
-        const int64_t group = item / p.parts;
-        const int part = (int)(item - group * p.parts);
-        const int64_t token = group * (ROWS / p.heads) + tsub;
-        const bool there = token < tokens;
-        const int64_t b = there ? token / p.S : 0, s = there ? token - b * p.S : 0;
-        float cs[V], sn[V];
-        if (p.dims) {
-            int64_t at[4] = {s, s, s, s};
-            if (p.pos) {
-#pragma unroll
-                for (int a = 0; a < 4; ++a)
-                    if (a < p.num_axes) at[a] = p.pos[a * p.pos_axis + b * p.pos_batch + s * p.pos_token];
-            }
+    while (next.item < items) {
+        const bool entered = cur.item != next.item;
+        cur = next;
+        Two<T> x = nx, g = ng;
+        if (entered && turns) {
+            int first = pair;
+            asm volatile("" : "+v"(first));  // read anew for every token, not kept over the loop
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 int64_t n = at[0];
-                if (p.num_axes > 1) n = axis[i] == 0 ? at[0] : axis[i] == 1 ? at[1] : axis[i] == 2 ? at[2] : at[3];
-                turned<sizeof(T) == 2>((int32_t)((uint64_t)n * freq[i] >> 32), cs[i], sn[i]);
+                if (p.num_axes > 1) {
+                    const int a = (int)(p.axes[D > 64 ? (pair + i) / 32 : 0] >> (pair + i) % 32 * 2) & 3;
+                    n = a == 0 ? at[0] : a == 1 ? at[1] : a == 2 ? at[2] : at[3];
+                }
+                turned<sizeof(T) == 2>((int32_t)((uint64_t)n * lfreq[first + i] >> 32), cs[i], sn[i]);
             }
+        }
+        next.h0 += p.heads;
+        if (next.h0 >= min(H_all, (int)(cur.item % p.parts + 1) * p.per * p.heads)) {
+            next.item += stride;
+            if (next.item < items) enter(next, next.item);
+        }
+        if (next.item < items) fetch(next);
+
+        const int h = cur.h0 + hsub;
+        const bool live = cur.there && h < H_all, key = h >= p.Hq;
+        if (!live) {
+            x.clear();
+            g.clear();
+        }
+        float r = 1.f;
+        if constexpr (NORM) {
+            float q = 0.f;
+#pragma unroll
+            for (int e = 0; e < 2 * V; ++e) q = __builtin_fmaf(x[e], x[e], q);
+            r = 1.f / sqrtf(group_sum<LANES>(q) * (1.f / D) + p.eps);
+            if (!live) r = 0.f;  // (eps may be 0)
+        }
+        float y[2 * V];
+        if constexpr (!BWD) {
+#pragma unroll
+            for (int e = 0; e < 2 * V; ++e) y[e] = x[e];
+            if constexpr (NORM) {
+                Two<T> wh;
+                wh.load(lw[key], c0, c1);
+#pragma unroll
+                for (int e = 0; e < 2 * V; ++e) y[e] *= r * wh[e];
+            }
+            if (turns) rotate<H, false, V>(y, cs, sn);  // (an infinite value that does not turn stays alone)
         } else {
 #pragma unroll
-            for (int i = 0; i < V; ++i) cs[i] = 1.f, sn[i] = 0.f;
-        }
-        const int h1 = min(H_all, (part + 1) * p.per * p.heads);
-        for (int h0 = part * p.per * p.heads; h0 < h1; h0 += p.heads) {
-            const int h = h0 + hsub;
-            const bool live = there && h < H_all, key = h >= p.Hq;
-            const int hk = key ? h - p.Hq : h;
-            float x[2 * V], g[2 * V];
-#pragma unroll
-            for (int e = 0; e < 2 * V; ++e) x[e] = g[e] = 0.f;
-            if (live) {
-                if (!BWD || NORM)
-                    load2<T>(x, static_cast<const T*>(key ? p.k : p.q) + (key ? p.mk : p.mq).offset((int)b, hk, (int)s, 0), c0, c1);
-                if (BWD)
-                    load2<T>(g, static_cast<const T*>(key ? p.gk : p.gq) + (key ? p.mgk : p.mgq).offset((int)b, hk, (int)s, 0), c0, c1);
-            }
-            float r = 1.f;
+            for (int e = 0; e < 2 * V; ++e) y[e] = g[e];
+            if (turns) rotate<H, true, V>(y, cs, sn);
             if constexpr (NORM) {
-                float q = 0.f;
+                Two<T> wh;
+                wh.load(lw[key], c0, c1);
+                const int first = cur.h0, last = min(H_all, cur.h0 + p.heads) - 1;
+                const bool all_q = last < p.Hq, all_k = first >= p.Hq;  // the same for the wavefront
+                float m = 0.f;
 #pragma unroll
-                for (int e = 0; e < 2 * V; ++e) q = __builtin_fmaf(x[e], x[e], q);
-                r = 1.f / sqrtf(group_sum<LANES>(q) * (1.f / D) + p.eps);
-                if (!live) r = 0.f;  // (eps may be 0)
-            }
-            if constexpr (!BWD) {
-                if constexpr (NORM) {
-#pragma unroll
-                    for (int e = 0; e < 2 * V; ++e) x[e] *= r * (key ? w[1][e] : w[0][e]);
+                for (int e = 0; e < 2 * V; ++e) {
+                    const float t = y[e] * (x[e] * r);
+                    if (all_q) sum[0][e] += t;
+                    else if (all_k) sum[1][e] += t;
+                    else sum[0][e] += key ? 0.f : t, sum[1][e] += key ? t : 0.f;
+                    m = __builtin_fmaf(t, wh[e], m);
                 }
-                if (turns) rotate<H, false, V>(x, cs, sn);  // (an infinite value that does not turn stays alone)
-            } else {
-                if (turns) rotate<H, true, V>(g, cs, sn);
-                if constexpr (NORM) {
-                    float m = 0.f;
+                m = group_sum<LANES>(m) * (1.f / D);
 #pragma unroll
-                    for (int e = 0; e < 2 * V; ++e) {
-                        const float xh = x[e] * r, t = g[e] * xh;
-                        sum[0][e] += key ? 0.f : t;
-                        sum[1][e] += key ? t : 0.f;
-                        g[e] *= key ? w[1][e] : w[0][e];
-                        m = __builtin_fmaf(g[e], xh, m);
-                        x[e] = xh;
-                    }
-                    m = group_sum<LANES>(m) * (1.f / D);
-#pragma unroll
-                    for (int e = 0; e < 2 * V; ++e) x[e] = r * (g[e] - x[e] * m);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 2 * V; ++e) x[e] = g[e];
-                }
+                for (int e = 0; e < 2 * V; ++e) y[e] = r * (y[e] * wh[e] - x[e] * r * m);
             }
-            if (live)
-                store2<T>(x, static_cast<T*>(key ? p.ok : p.oq) + (key ? p.mok : p.moq).offset((int)b, hk, (int)s, 0), c0, c1);
+        }
+        if (live) {
+            Two<T> o;
+#pragma unroll
+            for (int e = 0; e < 2 * V; ++e) o.set(e, y[e]);
+            const int hk = key ? h - p.Hq : h;
+            o.store(static_cast<T*>(key ? p.ok : p.oq) + (key ? p.mok : p.moq).offset(cur.b, hk, cur.s, 0), c0, c1);
         }
     }
 
