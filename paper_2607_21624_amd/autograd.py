@@ -357,9 +357,9 @@ class _GatedMlp(torch.autograd.Function):
         if any(need[:5]):
             dy2 = _matrix_of(_unit(dy, "gated_mlp"), "gated_mlp: the incoming gradient")
             if any(need[:3]):
-                dz, db1 = _f.gated_bwd(dy2, w2, z, act, need_bias=need[2])
-                if need[0] or need[1]:
-                    dx, dw1, _ = _f.linear_bwd(dz, x2, w1, need_dx=need[0], need_dw=need[1], need_bias=False)
+                dz, db1, dx = _f.gated_bwd(dy2, w2, z, act, w=w1 if need[0] else None, need_bias=need[2])
+                if need[1]:
+                    _, dw1, _ = _f.linear_bwd(dz, x2, w1, need_dx=False, need_bias=False)
             if need[3] or need[4]:
                 _, dw2, db2 = _f.linear_bwd(dy2, h, w2, need_dx=False, need_dw=need[3], need_bias=need[4])
         return dx.view(xshape) if need[0] else None, dw1, db1, dw2, db2, dy if need[5] else None, None

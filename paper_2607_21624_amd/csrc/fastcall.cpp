@@ -26,6 +26,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <vector>
 
 #include "../../include/fbl.h"
 
@@ -716,6 +717,280 @@ PyObject* linear_kd_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// ---------------------- norms and rotation of queries and keys, gated layers, clipping
+// How a call turns and norms: its arguments from `turns` to `eps` (seven), as the binding's _rotary and _head_norm
+// read them.
+struct Turning {
+    fbl_rotary rot{};
+    fbl_head_norm norm{};
+    const fbl_rotary* prot = nullptr;
+    const fbl_head_norm* pnorm = nullptr;
+    const Tensor *wq = nullptr, *wk = nullptr;
+    bool set(Args& g, int i, int64_t B, int64_t S, int64_t D, at::ScalarType dt) {
+        const Tensor *turns = g.tensor_or_none(i), *pos = g.tensor_or_none(i + 1);
+        PyObject* axes = g.a[i + 2];
+        const bool neighbours = g.flag(i + 3);
+        wq = g.tensor_or_none(i + 4), wk = g.tensor_or_none(i + 5);
+        const bool has_norm = g.a[i + 6] != Py_None;
+        const float eps = has_norm ? g.real(i + 6) : 0.f;
+        if (!g.ok || !vector(wq, D, dt) || !vector(wk, D, dt) || (!has_norm && (wq || wk))) return false;
+        if (has_norm) {
+            norm.q_weight = data(wq), norm.k_weight = data(wk), norm.eps = eps;
+            pnorm = &norm;
+        }
+        if (!turns) return !pos && axes == Py_None;
+        const int64_t pairs = turns->numel();
+        if (turns->scalar_type() != at::kLong || turns->dim() != 1 || !turns->is_contiguous() || pairs < 1 || pairs > 64) return false;
+        rot.turns = static_cast<const uint64_t*>(turns->data_ptr()), rot.dims = (int32_t)(2 * pairs), rot.neighbours = neighbours;
+        rot.num_axes = 1;
+        prot = &rot;
+        if (!pos) return axes == Py_None;
+        const int64_t dim = pos->dim();
+        if (pos->scalar_type() != at::kLong || dim < 1 || dim > 3 || pos->size(dim - 1) != S || (dim > 1 && pos->size(dim - 2) != B))
+            return false;
+        rot.positions = static_cast<const int64_t*>(pos->data_ptr());
+        rot.stride_token = pos->stride(dim - 1), rot.stride_batch = dim > 1 ? pos->stride(dim - 2) : 0;
+        if (dim == 3) {
+            const int64_t n = pos->size(0);
+            if (n < 1 || n > FBL_ROTARY_MAX_AXES || (n > 1 && axes == Py_None)) return false;
+            rot.num_axes = (int32_t)n, rot.stride_axis = pos->stride(0);
+        }
+        if (axes == Py_None) return true;
+        if (dim != 3 || !PyTuple_CheckExact(axes) || PyTuple_GET_SIZE(axes) != pairs) return false;
+        for (int64_t k = 0; k < pairs; ++k) {
+            PyObject* o = PyTuple_GET_ITEM(axes, k);
+            const long v = PyLong_CheckExact(o) ? PyLong_AsLong(o) : -1;
+            if (v == -1 && PyErr_Occurred()) PyErr_Clear();
+            if (v < 0 || v >= rot.num_axes) return false;
+            rot.axes[k] = (uint8_t)v;
+        }
+        return true;
+    }
+};
+
+// qk_norm_rotary_fwd(q, k, Hq, Hkv, turns, positions, axes, neighbours, q_weight, k_weight, eps, q_out, k_out, stream)
+PyObject* qk_norm_rotary_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (n != 14) Py_RETURN_NONE;
+    Args g{a};
+    const Tensor *q = g.tensor(0), *k = g.tensor_or_none(1);
+    const int64_t Hq = g.integer(2), Hkv = g.integer(3);
+    const Tensor *qo = g.tensor_or_none(11), *ko = g.tensor_or_none(12);
+    g.no_stream(13);
+    fbl_layout lq, lk, lqo, lko;
+    if (!g.ready() || !layout(q, Hq, &lq) || (k && !layout(k, Hkv, &lk)) || (!k && ko)) Py_RETURN_NONE;
+    Turning t;
+    if (!t.set(g, 4, lq.B, lq.S, lq.D, q->scalar_type()) || !g.ready()) Py_RETURN_NONE;
+    Tensor mq, mk;
+    if (!qo) mq = empty(q->sizes(), q->scalar_type(), *q), qo = &mq;
+    if (k && !ko) mk = empty(k->sizes(), k->scalar_type(), *q), ko = &mk;
+    if (!layout(qo, Hq, &lqo) || (k && !layout(ko, Hkv, &lko))) Py_RETURN_NONE;
+    void *s = g.stream(), *pq = data(q), *pk = data(k), *pqo = data(qo), *pko = data(ko);
+    const fbl_status st = unlocked([&] {
+        return fbl_qk_norm_rotary_fwd(&lq, pq, k ? &lk : nullptr, pk, t.prot, t.pnorm, &lqo, pqo, k ? &lko : nullptr, pko, s);
+    });
+    if (st != FBL_OK) Py_RETURN_NONE;
+    return tuple_of<2>({object_of(a[11], mq), object_or_none(a[12], mk)});
+    END_HANDLE_TH_ERRORS
+}
+
+// qk_norm_rotary_bwd(dq_out, dk_out, q, k, Hq, Hkv, turns, positions, axes, neighbours, q_weight, k_weight, eps, dq, dk,
+//                    dq_weight, dk_weight, workspace, stream, need_weights)
+PyObject* qk_norm_rotary_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (n != 20) Py_RETURN_NONE;
+    Args g{a};
+    const Tensor *gq = g.tensor(0), *gk = g.tensor_or_none(1);
+    const int64_t Hq = g.integer(4), Hkv = g.integer(5);
+    const bool norm = a[12] != Py_None;
+    const Tensor *q = norm ? g.tensor(2) : nullptr, *k = norm ? g.tensor_or_none(3) : nullptr;
+    const Tensor *dq = g.tensor_or_none(13), *dk = g.tensor_or_none(14), *dqw = g.tensor_or_none(15), *dkw = g.tensor_or_none(16);
+    const Tensor* ws = g.tensor_or_none(17);
+    g.no_stream(18);
+    const bool need = g.flag(19);
+    fbl_layout lgq, lgk, lq, lk, ldq, ldk;
+    if (!g.ready() || !layout(gq, Hq, &lgq) || (gk && !layout(gk, Hkv, &lgk)) || (!gk && dk)) Py_RETURN_NONE;
+    if (norm && (!layout(q, Hq, &lq) || !k != !gk || (k && !layout(k, Hkv, &lk)))) Py_RETURN_NONE;
+    Turning t;
+    const at::ScalarType dt = gq->scalar_type();
+    if (!t.set(g, 6, lgq.B, lgq.S, lgq.D, dt) || !vector(dqw, lgq.D, dt) || !vector(dkw, lgq.D, dt) || !g.ready()) Py_RETURN_NONE;
+    Tensor mq, mk, mqw, mkw;
+    if (!dq) mq = empty(gq->sizes(), dt, *gq), dq = &mq;
+    if (gk && !dk) mk = empty(gk->sizes(), gk->scalar_type(), *gq), dk = &mk;
+    if (need && !dqw && t.wq) mqw = empty({lgq.D}, dt, *gq), dqw = &mqw;
+    if (need && !dkw && t.wk && gk) mkw = empty({lgq.D}, dt, *gq), dkw = &mkw;
+    if (!layout(dq, Hq, &ldq) || (gk && !layout(dk, Hkv, &ldk))) Py_RETURN_NONE;
+    Scratch sc;
+    size_t bytes = 0;
+    if (dqw || dkw) {
+        if (!ws && fbl_qk_norm_rotary_bwd_workspace(&lgq, gk ? &lgk : nullptr, &bytes) != FBL_OK) Py_RETURN_NONE;
+        if (!sc.set(ws, bytes, *gq)) Py_RETURN_NONE;
+    }
+    void *s = g.stream(), *pgq = data(gq), *pgk = data(gk), *pq = data(q), *pk = data(k), *pdq = data(dq), *pdk = data(dk),
+         *pdqw = data(dqw), *pdkw = data(dkw);
+    const fbl_status st = unlocked([&] {
+        return fbl_qk_norm_rotary_bwd(&lgq, pgq, gk ? &lgk : nullptr, pgk, q ? &lq : nullptr, pq, k ? &lk : nullptr, pk, t.prot, t.pnorm,
+                                      &ldq, pdq, gk ? &ldk : nullptr, pdk, pdqw, pdkw, sc.p, sc.bytes, s);
+    });
+    if (st != FBL_OK) Py_RETURN_NONE;
+    return tuple_of<4>({object_of(a[13], mq), object_or_none(a[14], mk), object_or_none(a[15], mqw), object_or_none(a[16], mkw)});
+    END_HANDLE_TH_ERRORS
+}
+
+// gated_fwd(x, w, bias, act, out, z, tile, workspace, stream)
+PyObject* gated_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (n != 9) Py_RETURN_NONE;
+    Args g{a};
+    const Tensor *x = g.tensor(0), *w = g.tensor(1), *b = g.tensor_or_none(2);
+    const uint32_t act = g.act(3);
+    const Tensor *out = g.tensor_or_none(4), *z = g.tensor_or_none(5);
+    const int64_t tile = g.integer(6);
+    const Tensor* ws = g.tensor_or_none(7);
+    g.no_stream(8);
+    if (!g.ready() || x->dim() != 2 || w->dim() != 2 || w->size(1) % 2 || dtype_code(*x) < 0) Py_RETURN_NONE;
+    const int64_t M = x->size(0), K = x->size(1), F = w->size(1) / 2;
+    const at::ScalarType dt = x->scalar_type();
+    const int code = dtype_code(*x);
+    if (!matrix(x, M, K, dt) || !matrix(w, K, 2 * F, dt) || !vector(b, 2 * F, dt) || !matrix(out, M, F, dt) || !matrix(z, M, 2 * F, dt))
+        Py_RETURN_NONE;
+    Tensor mo;
+    if (!out) mo = empty({M, F}, dt, *x), out = &mo;
+    Scratch sc;
+    size_t need = 0;
+    if (!ws && tile == FBL_GEMM_TILE_AUTO && M <= 128 && fbl_gated_fwd_workspace(code, M, K, F, &need) != FBL_OK) Py_RETURN_NONE;
+    if (!sc.set(ws, need, *x)) Py_RETURN_NONE;
+    void *s = g.stream(), *px = data(x), *pw = data(w), *pb = data(b), *po = data(out), *pz = data(z);
+    const int64_t ldx = row_stride(x), ldw = row_stride(w), ldo = row_stride(out), ldz = row_stride(z);
+    const fbl_status st = unlocked([&] {
+        return fbl_gated_fwd(code, act, M, K, F, px, ldx, pw, ldw, pb, po, ldo, pz, ldz, (int32_t)tile, sc.p, sc.bytes, s);
+    });
+    if (st != FBL_OK) Py_RETURN_NONE;
+    return object_of(a[4], mo);
+    END_HANDLE_TH_ERRORS
+}
+
+// gated_bwd(dy, w_down, z, act, dz, dbias, w, dx, tile, workspace, stream, need_bias)
+PyObject* gated_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (n != 12) Py_RETURN_NONE;
+    Args g{a};
+    const Tensor *dy = g.tensor(0), *wd = g.tensor(1), *z = g.tensor(2);
+    const uint32_t act = g.act(3);
+    const Tensor *dz = g.tensor_or_none(4), *db = g.tensor_or_none(5), *w = g.tensor_or_none(6), *dx = g.tensor_or_none(7);
+    const int64_t tile = g.integer(8);
+    const Tensor* ws = g.tensor_or_none(9);
+    g.no_stream(10);
+    const bool need_b = g.flag(11);
+    if (!g.ready() || dy->dim() != 2 || wd->dim() != 2 || (w && w->dim() != 2) || (dx && !w) || dtype_code(*dy) < 0) Py_RETURN_NONE;
+    const int64_t M = dy->size(0), N = dy->size(1), F = wd->size(0), K = w ? w->size(0) : N;
+    const at::ScalarType dt = dy->scalar_type();
+    const int code = dtype_code(*dy);
+    if (!matrix(dy, M, N, dt) || !matrix(wd, F, N, dt) || !matrix(z, M, 2 * F, dt) || !matrix(dz, M, 2 * F, dt) || !vector(db, 2 * F, dt) ||
+        !matrix(w, K, 2 * F, dt) || !matrix(dx, M, K, dt))
+        Py_RETURN_NONE;
+    Tensor mz, mb, mx;
+    if (!dz) mz = empty({M, 2 * F}, dt, *dy), dz = &mz;
+    if (!db && need_b) mb = empty({2 * F}, dt, *dy), db = &mb;
+    if (w && !dx) mx = empty({M, K}, dt, *dy), dx = &mx;
+    Scratch sc;
+    size_t need = 0;
+    if (db || ws || dx || M <= 128) {
+        if (!ws && fbl_gated_bwd_workspace(code, M, K, F, N, &need) != FBL_OK) Py_RETURN_NONE;
+        if (!sc.set(ws, need, *dy)) Py_RETURN_NONE;
+    }
+    void *s = g.stream(), *py = data(dy), *pwd = data(wd), *pz = data(z), *pdz = data(dz), *pdb = data(db), *pw = data(w), *pdx = data(dx);
+    const int64_t ldy = row_stride(dy), ldwd = row_stride(wd), ldz = row_stride(z), lddz = row_stride(dz), ldw = row_stride(w),
+                  lddx = row_stride(dx);
+    const fbl_status st = unlocked([&] {
+        return fbl_gated_bwd(code, act, M, K, F, N, py, ldy, pwd, ldwd, pz, ldz, pdz, lddz, pdb, pw, ldw, pdx, lddx, (int32_t)tile, sc.p,
+                             sc.bytes, s);
+    });
+    if (st != FBL_OK) Py_RETURN_NONE;
+    return tuple_of<3>({object_of(a[4], mz), object_or_none(a[5], mb), object_or_none(a[7], mx)});
+    END_HANDLE_TH_ERRORS
+}
+
+// A list (or tuple) of gradients and of the tensors that receive them, as the binding's _grad_list reads it.
+struct Grads {
+    std::vector<fbl_grad> list;
+    const Tensor* first = nullptr;
+    static Py_ssize_t size(PyObject* o) {
+        return PyList_CheckExact(o) ? PyList_GET_SIZE(o) : PyTuple_CheckExact(o) ? PyTuple_GET_SIZE(o) : -1;
+    }
+    static PyObject* item(PyObject* o, Py_ssize_t i) { return PyList_CheckExact(o) ? PyList_GET_ITEM(o, i) : PyTuple_GET_ITEM(o, i); }
+    bool set(Args& g, PyObject* grads, PyObject* out) {
+        const Py_ssize_t n = size(grads);
+        if (n < 1 || (out != Py_None && size(out) != n)) return false;
+        list.resize((size_t)n);
+        for (Py_ssize_t i = 0; i < n; ++i) {
+            PyObject* const given = item(grads, i);
+            const Tensor* t = plain(given);
+            if (!t || t->layout() != c10::kStrided || dtype_code(*t) < 0 || !t->is_non_overlapping_and_dense()) return false;
+            if (g.device < 0) g.device = t->device().index();
+            if (t->device().index() != g.device) return false;
+            if (!first) first = t;
+            fbl_grad& e = list[(size_t)i];
+            e = fbl_grad{t->data_ptr(), t->data_ptr(), t->numel(), dtype_code(*t), 0};
+            if (out == Py_None) continue;
+            const Tensor* o = plain(item(out, i));
+            if (!o || o->scalar_type() != t->scalar_type() || o->sizes() != t->sizes() || o->strides() != t->strides() ||
+                o->device().index() != g.device)
+                return false;
+            e.out = o->data_ptr();
+        }
+        return true;
+    }
+};
+bool one_float(const Tensor* t) { return !t || (t->scalar_type() == at::kFloat && t->numel() == 1); }
+
+// grad_norm(grads, norm, workspace, stream)
+PyObject* grad_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (n != 4) Py_RETURN_NONE;
+    Args g{a};
+    const Tensor *norm = g.tensor_or_none(1), *ws = g.tensor_or_none(2);
+    g.no_stream(3);
+    Grads l;
+    if (!g.ok || !l.set(g, a[0], Py_None) || !g.ready() || !one_float(norm)) Py_RETURN_NONE;
+    Tensor made;
+    if (!norm) made = empty({}, at::kFloat, *l.first), norm = &made;
+    Scratch sc;
+    size_t need = 0;
+    const int64_t count = (int64_t)l.list.size();
+    if ((!ws && fbl_grad_norm_workspace(count, &need) != FBL_OK) || !sc.set(ws, need, *l.first)) Py_RETURN_NONE;
+    void* s = g.stream();
+    float* pn = data<float>(norm);
+    const fbl_status st = unlocked([&] { return fbl_grad_norm(count, l.list.data(), pn, sc.p, sc.bytes, s); });
+    if (st != FBL_OK) Py_RETURN_NONE;
+    return object_of(a[1], made);
+    END_HANDLE_TH_ERRORS
+}
+
+// clip_grad_norm(grads, limit, out, norm, workspace, stream)
+PyObject* clip_grad_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (n != 6) Py_RETURN_NONE;
+    Args g{a};
+    const float limit = g.real(1);
+    const Tensor *norm = g.tensor_or_none(3), *ws = g.tensor_or_none(4);
+    g.no_stream(5);
+    Grads l;
+    if (!g.ok || !l.set(g, a[0], a[2]) || !g.ready() || !one_float(norm)) Py_RETURN_NONE;
+    Tensor made;
+    if (!norm) made = empty({}, at::kFloat, *l.first), norm = &made;
+    Scratch sc;
+    size_t need = 0;
+    const int64_t count = (int64_t)l.list.size();
+    if ((!ws && fbl_grad_norm_workspace(count, &need) != FBL_OK) || !sc.set(ws, need, *l.first)) Py_RETURN_NONE;
+    void* s = g.stream();
+    float* pn = data<float>(norm);
+    const fbl_status st = unlocked([&] { return fbl_clip_grad_norm(count, l.list.data(), limit, pn, sc.p, sc.bytes, s); });
+    if (st != FBL_OK) Py_RETURN_NONE;
+    return object_of(a[3], made);
+    END_HANDLE_TH_ERRORS
+}
+
 PyMethodDef kMethods[] = {
     {"attn_fwd", (PyCFunction)(void (*)())attn_fwd, METH_FASTCALL, nullptr},
     {"attn_bwd", (PyCFunction)(void (*)())attn_bwd, METH_FASTCALL, nullptr},
@@ -730,6 +1005,12 @@ PyMethodDef kMethods[] = {
     {"linear_ce_bwd", (PyCFunction)(void (*)())linear_ce_bwd, METH_FASTCALL, nullptr},
     {"linear_kd_fwd", (PyCFunction)(void (*)())linear_kd_fwd, METH_FASTCALL, nullptr},
     {"linear_kd_bwd", (PyCFunction)(void (*)())linear_kd_bwd, METH_FASTCALL, nullptr},
+    {"qk_norm_rotary_fwd", (PyCFunction)(void (*)())qk_norm_rotary_fwd, METH_FASTCALL, nullptr},
+    {"qk_norm_rotary_bwd", (PyCFunction)(void (*)())qk_norm_rotary_bwd, METH_FASTCALL, nullptr},
+    {"gated_fwd", (PyCFunction)(void (*)())gated_fwd, METH_FASTCALL, nullptr},
+    {"gated_bwd", (PyCFunction)(void (*)())gated_bwd, METH_FASTCALL, nullptr},
+    {"grad_norm", (PyCFunction)(void (*)())grad_norm, METH_FASTCALL, nullptr},
+    {"clip_grad_norm", (PyCFunction)(void (*)())clip_grad_norm, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};

@@ -254,9 +254,10 @@ def _load() -> ctypes.CDLL:
     lib.fbl_gated_fwd.restype = ctypes.c_int
     lib.fbl_gated_fwd_workspace.argtypes = [i32, i64, i64, i64, sizep]
     lib.fbl_gated_fwd_workspace.restype = ctypes.c_int
-    lib.fbl_gated_bwd_workspace.argtypes = [i32, i64, i64, i64, sizep]
+    lib.fbl_gated_bwd_workspace.argtypes = [i32, i64, i64, i64, i64, sizep]
     lib.fbl_gated_bwd_workspace.restype = ctypes.c_int
-    lib.fbl_gated_bwd.argtypes = [i32, u32, i64, i64, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, i32, vp, size, vp]
+    lib.fbl_gated_bwd.argtypes = [i32, u32, i64, i64, i64, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, i64, vp, i64, i32,
+                                  vp, size, vp]
     lib.fbl_gated_bwd.restype = ctypes.c_int
     lib.fbl_grad_norm_workspace.argtypes = [i64, sizep]
     lib.fbl_grad_norm_workspace.restype = ctypes.c_int
@@ -278,7 +279,8 @@ LIB = _load()
 # any argument that is not a plain one, any error -- and the Python below then
 # makes the call with every check.
 _NATIVE = ("attn_fwd", "attn_bwd", "attn_fwd_packed", "attn_bwd_packed", "proj", "layer_norm_fwd", "layer_norm_bwd",
-           "linear_fwd", "linear_bwd", "linear_ce_fwd", "linear_ce_bwd", "linear_kd_fwd", "linear_kd_bwd")
+           "linear_fwd", "linear_bwd", "linear_ce_fwd", "linear_ce_bwd", "linear_kd_fwd", "linear_kd_bwd", "qk_norm_rotary_fwd",
+           "qk_norm_rotary_bwd", "gated_fwd", "gated_bwd", "grad_norm", "clip_grad_norm")
 
 
 def _load_native():
@@ -1146,6 +1148,9 @@ def gated_fwd(x, w, bias=None, act: str = "silu", out=None, z=None, tile: int = 
     strides, one storage type), act one of ACTIVATIONS.  z [M, 2F], where given, receives the pre-activations,
     which gated_bwd needs.  workspace: gated_fwd_workspace bytes, allocated where they are needed and it is None.
     Returns h [M, F]."""
+    done = _FAST.gated_fwd(x, w, bias, act, out, z, tile, workspace, stream)
+    if done is not None:
+        return done
     import torch
     where = "gated_fwd"
     _check_device(where, stream, x=x, w=w, bias=bias, out=out, z=z, workspace=workspace)
@@ -1170,22 +1175,26 @@ def gated_fwd(x, w, bias=None, act: str = "silu", out=None, z=None, tile: int = 
     return out
 
 
-def gated_bwd_workspace(dy, w_down) -> int:
-    """Bytes of gated_bwd's workspace for dy [M, N] and w_down [F, N]."""
+def gated_bwd_workspace(dy, w_down, w=None) -> int:
+    """Bytes of gated_bwd's workspace for dy [M, N], w_down [F, N] and, where dx is wanted, w [K, 2F]."""
     n = ctypes.c_size_t(0)
-    _check(LIB.fbl_gated_bwd_workspace(_dtype_code(dy), dy.shape[0], *w_down.shape, ctypes.byref(n)),
-           "fbl_gated_bwd_workspace")
+    _check(LIB.fbl_gated_bwd_workspace(_dtype_code(dy), dy.shape[0], w_down.shape[1] if w is None else w.shape[0],
+                                       *w_down.shape, ctypes.byref(n)), "fbl_gated_bwd_workspace")
     return int(n.value)
 
 
-def gated_bwd(dy, w_down, z, act: str = "silu", dz=None, dbias=None, tile: int = FBL_GEMM_TILE_AUTO, workspace=None,
-              stream=None, need_bias: bool = True):
+def gated_bwd(dy, w_down, z, act: str = "silu", dz=None, dbias=None, w=None, dx=None, tile: int = FBL_GEMM_TILE_AUTO,
+              workspace=None, stream=None, need_bias: bool = True):
     """Gradient of a gated layer's pre-activations from that of the block's result: dy [M, N], w_down [F, N] and the
-    forward's z [M, 2F] give dz [M, 2F] and the sums of dz over its rows, dbias [2F].  Returns (dz, dbias), dbias None
-    where not needed.  dx and dw are linear_bwd's of dz."""
+    forward's z [M, 2F] give dz [M, 2F], the sums of dz over its rows, dbias [2F], and with the layer's w [K, 2F] the
+    gradient of its input, dx [M, K].  Returns (dz, dbias, dx), dbias None where not needed and dx without w.  dw is
+    linear_bwd's of dz."""
+    done = _FAST.gated_bwd(dy, w_down, z, act, dz, dbias, w, dx, tile, workspace, stream, need_bias)
+    if done is not None:
+        return done
     import torch
     where = "gated_bwd"
-    _check_device(where, stream, dy=dy, w_down=w_down, z=z, dz=dz, dbias=dbias, workspace=workspace)
+    _check_device(where, stream, dy=dy, w_down=w_down, z=z, dz=dz, dbias=dbias, w=w, dx=dx, workspace=workspace)
     lddy = _matrix(dy, where, "dy")
     M, N = dy.shape
     dt, code = _dtype_code(dy), _act_code(act, where)
@@ -1200,13 +1209,24 @@ def gated_bwd(dy, w_down, z, act: str = "silu", dz=None, dbias=None, tile: int =
     if dbias is None and need_bias:
         dbias = _empty(2 * F, dy.dtype, dy, stream)
     _vector(dbias, where, "dbias", 2 * F, dy.dtype)
+    K, ldw, lddx = N, 0, 0
+    if w is None and dx is not None:
+        raise FblError(FBL_ERR_NULL, f"{where}: dx needs the layer's w")
+    if w is not None:
+        ldw = _matrix(w, where, "w", None, dy)
+        K = w.shape[0]
+        if w.shape[1] != 2 * F:
+            raise FblError(FBL_ERR_SHAPE, f"{where}: w {tuple(w.shape)} and w_down {tuple(w_down.shape)} do not agree")
+        if dx is None:
+            dx = _empty((M, K), dy.dtype, dy, stream)
+        lddx = _matrix(dx, where, "dx", (M, K), dy)
     ws, ws_bytes = None, 0
-    if dbias is not None or workspace is not None or M <= 128:
-        need = 0 if workspace is not None else gated_bwd_workspace(dy, w_down)
+    if dbias is not None or workspace is not None or dx is not None or M <= 128:
+        need = 0 if workspace is not None else gated_bwd_workspace(dy, w_down, w)
         ws, ws_bytes = _scratch(workspace, need, where, dy, stream)
-    _call("fbl_gated_bwd", dy, stream, dt, code, M, F, N, _ptr(dy), lddy, _ptr(w_down), ldwd, _ptr(z), ldz, _ptr(dz), lddz,
-          _ptr(dbias), tile, _ptr(ws), ws_bytes)
-    return dz, dbias
+    _call("fbl_gated_bwd", dy, stream, dt, code, M, K, F, N, _ptr(dy), lddy, _ptr(w_down), ldwd, _ptr(z), ldz, _ptr(dz),
+          lddz, _ptr(dbias), _ptr(w), ldw, _ptr(dx), lddx, tile, _ptr(ws), ws_bytes)
+    return dz, dbias, dx
 
 
 # ------------------------------------- losses of a linear head over a vocabulary
@@ -1517,6 +1537,10 @@ def qk_norm_rotary_fwd(q, k, Hq: int, Hkv: int, turns=None, positions=None, axes
     [d] may be None.  turns: rotary_turns of dims / 2 frequencies, None for no rotation; positions: int64 [S], [B, S] or
     [axes, B, S], None for 0 .. S - 1; axes: with several, the axis of each pair.  The pairs are the halves of the first
     dims values, or neighbours.  q_out and k_out may be q and k themselves."""
+    done = _FAST.qk_norm_rotary_fwd(q, k, Hq, Hkv, turns, positions, axes, neighbours, q_weight, k_weight, eps, q_out, k_out,
+                                    stream)
+    if done is not None:
+        return done
     where = "qk_norm_rotary_fwd"
     _check_device(where, stream, q=q, k=k, turns=turns, positions=positions, q_weight=q_weight, k_weight=k_weight,
                   q_out=q_out, k_out=k_out)
@@ -1547,6 +1571,10 @@ def qk_norm_rotary_bwd(dq_out, dk_out, q, k, Hq: int, Hkv: int, turns=None, posi
     """Gradients of qk_norm_rotary_fwd from those of its results (dk_out None without keys): returns (dq, dk, dq_weight,
     dk_weight), the weights' None where there is no weight or need_weights is False.  q and k are the forward's inputs,
     needed with a norm (else they may be None).  dq and dk may be dq_out and dk_out themselves."""
+    done = _FAST.qk_norm_rotary_bwd(dq_out, dk_out, q, k, Hq, Hkv, turns, positions, axes, neighbours, q_weight, k_weight, eps,
+                                    dq, dk, dq_weight, dk_weight, workspace, stream, need_weights)
+    if done is not None:
+        return done
     where = "qk_norm_rotary_bwd"
     if eps is None:
         q = k = None
@@ -1642,6 +1670,9 @@ def grad_norm_workspace(grads) -> int:
 def grad_norm(grads, norm=None, workspace=None, stream=None):
     """The norm of all values of a list of tensors (float32 and bfloat16, each in one piece of memory): one
     float32 on their device."""
+    done = _FAST.grad_norm(grads, norm, workspace, stream)
+    if done is not None:
+        return done
     where = "grad_norm"
     a, like = _grad_list(grads, None, where)
     norm = _norm_out(norm, like, where, stream)
@@ -1663,6 +1694,9 @@ def clip_grads(grads, norm, limit: float, out=None, stream=None) -> None:
 
 def clip_grad_norm(grads, limit: float, out=None, norm=None, workspace=None, stream=None):
     """grad_norm and clip_grads by it in one call: returns the norm of the gradients as they were."""
+    done = _FAST.clip_grad_norm(grads, limit, out, norm, workspace, stream)
+    if done is not None:
+        return done
     where = "clip_grad_norm"
     a, like = _grad_list(grads, out, where)
     norm = _norm_out(norm, like, where, stream)
