@@ -806,28 +806,25 @@ fbl_status fbl_qk_norm_rotary_bwd(const fbl_layout* lgq, const void* gq, const f
  * fbl_gated_bwd takes the gradient dy [M, N] of the block's result and w_down [F, N], its second weight, and gives
  *   dz [M, 2F] = (dh * up * act'(gate),  dh * act(gate)),   dh = dy . w_down^T  (never stored)
  *   dbias [2F] (NULL: not wanted) = sums over rows of dz, unrounded
- *   dx [M, K] (NULL: not wanted, w is then not read) = dz . w^T
- * of which fbl_linear_bwd makes dw = x^T . dz, and from h and dy the gradients of w_down and of its bias.  dz is rounded to
- * the storage type.  The workspace (16-byte aligned, fbl_gated_bwd_workspace bytes) is needed where dbias is wanted,
- * else it may be NULL; with it, workgroups share the contractions of dz and dx for a few tokens, and that of dx where its own
- * tiles are few.
+ * of which fbl_linear_bwd makes dx = dz . w^T and dw = x^T . dz, and from h and dy the gradients of w_down and of its bias.
+ * The workspace (16-byte aligned, fbl_gated_bwd_workspace bytes) is needed where dbias is wanted, else it may be NULL; with it,
+ * workgroups share the contraction for a few tokens.
  *
  * Row strides in elements, at least the width.  fp32: any extents, natural alignment.  bf16: 16-byte aligned
  * pointers (bias too) and rows, K, F and N multiples of 8; any number of tokens M.  K, N and 2F at most 2^26, operands
  * below 2 GiB each (FBL_ERR_UNSUPPORTED), outputs and workspace overlapping nothing (FBL_ERR_ARG).  tile: as fbl_proj's
- * of the products (FBL_PROJ_FWD, M, K, 2F) and (FBL_PROJ_BWD_DATA, M, F, N) and of dx; AUTO for fp32, and for shared
- * contractions.
+ * of the products (FBL_PROJ_FWD, M, K, 2F) and (FBL_PROJ_BWD_DATA, M, F, N), of which AUTO takes the tuned one too; AUTO for
+ * fp32, and for shared contractions.
  * All sums run in a fixed order.
  */
 fbl_status fbl_gated_fwd(int32_t dtype, uint32_t act, int64_t M, int64_t K, int64_t F, const void* x, int64_t ldx,
                          const void* w, int64_t ldw, const void* bias, void* h, int64_t ldh, void* z, int64_t ldz,
                          int32_t tile, void* ws, size_t ws_bytes, void* stream);
 fbl_status fbl_gated_fwd_workspace(int32_t dtype, int64_t M, int64_t K, int64_t F, size_t* bytes);
-fbl_status fbl_gated_bwd_workspace(int32_t dtype, int64_t M, int64_t K, int64_t F, int64_t N, size_t* bytes);
-fbl_status fbl_gated_bwd(int32_t dtype, uint32_t act, int64_t M, int64_t K, int64_t F, int64_t N, const void* dy,
-                         int64_t lddy, const void* w_down, int64_t ldwd, const void* z, int64_t ldz, void* dz, int64_t lddz,
-                         void* dbias, const void* w, int64_t ldw, void* dx, int64_t lddx, int32_t tile, void* ws,
-                         size_t ws_bytes, void* stream);
+fbl_status fbl_gated_bwd_workspace(int32_t dtype, int64_t M, int64_t F, int64_t N, size_t* bytes);
+fbl_status fbl_gated_bwd(int32_t dtype, uint32_t act, int64_t M, int64_t F, int64_t N, const void* dy, int64_t lddy,
+                         const void* w_down, int64_t ldwd, const void* z, int64_t ldz, void* dz, int64_t lddz, void* dbias,
+                         int32_t tile, void* ws, size_t ws_bytes, void* stream);
 
 /*
  * The end of a training step: the global norm of a list of gradients, and the gradients clipped by it.
@@ -839,7 +836,7 @@ fbl_status fbl_gated_bwd(int32_t dtype, uint32_t act, int64_t M, int64_t K, int6
  *   fbl_grad_norm       norm (float32, device memory); `out` is not looked at
  *   fbl_grad_clip       out from a norm that is given: the program's own, or of gradients that lie on several devices
  *   fbl_clip_grad_norm  both
- * In place, a norm within the limit leaves the gradients untouched.  The norm is summed in float64 in a fixed order and
+ * In place, a norm within the limit leaves the gradients untouched (in a list of both, written unchanged).  The norm is summed in float64 in a fixed order and
  * rounded once; it does not overflow before its own value does.  An infinite norm makes the scale 0 (an infinite
  * gradient then nan), a norm of nan everything nan.  Workspace: fbl_grad_norm_workspace bytes for `count` tensors, 8-byte
  * aligned; nothing is kept in it.  A launch takes 112 tensors.

@@ -54,25 +54,16 @@ int gated_tile(int grad, int64_t M, int64_t cols, int64_t kc) {
     return grad ? fbl::proj_auto_tile(op, M, K, N) : fbl::forward_tile(M, K, N);
 }
 
-// Workgroups that share the contraction 2F of a tile of dx: a few tokens', and (bf16) where its own tiles fill
-// half of the CUs (4096 x 2048 from 16384: 337 us alone).
-int dx_splits(int f32, int64_t M, int64_t K, int64_t F) {
-    if (M <= 128) return few_splits(f32, M, 2 * F, K);
-    if (f32 || M * K >= (int64_t)1 << 29) return 1;
-    return fbl::sum_splits(0, 1, M, K, 2 * F, fbl::proj_untuned_tile(FBL_PROJ_BWD_DATA, M, K, 2 * F));
-}
-
-// Workspace of the backward, a function of the shape: planes of dh, then of dx, and partial sums of dz (as many
-// rows of them as any tile writes, linear_grad_groups, or one for each of a few tokens).
+// Workspace of the data gradient, a function of the shape: planes of dh, and partial sums of dz (as many rows of them as any
+// tile writes, linear_grad_groups, or one for each of a few tokens).
 struct GatedWs {
     size_t sums, total;
-    int splits, xsplits;
+    int splits;
 };
-GatedWs gated_ws(int f32, int64_t M, int64_t K, int64_t F, int64_t N) {
+GatedWs gated_ws(int f32, int64_t M, int64_t F, int64_t N) {
     GatedWs w;
     w.splits = few_splits(f32, M, N, F);
-    w.xsplits = dx_splits(f32, M, K, F);
-    w.sums = align256(std::max(few_ws(w.splits, M, F), few_ws(w.xsplits, M, K)));
+    w.sums = align256(few_ws(w.splits, M, F));
     w.total = w.sums + (size_t)(w.splits > 1 ? M : M / 32 + 4) * 2 * (size_t)F * 4;
     return w;
 }
@@ -136,40 +127,37 @@ fbl_status fbl_gated_fwd(int32_t dtype, uint32_t act, int64_t M, int64_t K, int6
     return e == hipSuccess ? FBL_OK : FBL_ERR_HIP;
 }
 
-fbl_status fbl_gated_bwd_workspace(int32_t dtype, int64_t M, int64_t K, int64_t F, int64_t N, size_t* bytes) {
+fbl_status fbl_gated_bwd_workspace(int32_t dtype, int64_t M, int64_t F, int64_t N, size_t* bytes) {
     if (!bytes) return FBL_ERR_NULL;
-    fbl_status st = gated_shape(dtype, FBL_ACT_NONE, M, N, F);
-    if (st == FBL_OK) st = gated_shape(dtype, FBL_ACT_NONE, M, K, F);
-    if (st == FBL_OK) *bytes = gated_ws(dtype == FBL_F32, M, K, F, N).total;
+    const fbl_status st = gated_shape(dtype, FBL_ACT_NONE, M, N, F);
+    if (st == FBL_OK) *bytes = gated_ws(dtype == FBL_F32, M, F, N).total;
     return st;
 }
 
-fbl_status fbl_gated_bwd(int32_t dtype, uint32_t act, int64_t M, int64_t K, int64_t F, int64_t N, const void* dy,
-                         int64_t lddy, const void* wd, int64_t ldwd, const void* z, int64_t ldz, void* dz, int64_t lddz,
-                         void* dbias, const void* w, int64_t ldw, void* dx, int64_t lddx, int32_t tile, void* ws,
-                         size_t ws_bytes, void* stream) {
+fbl_status fbl_gated_bwd(int32_t dtype, uint32_t act, int64_t M, int64_t F, int64_t N, const void* dy, int64_t lddy,
+                         const void* wd, int64_t ldwd, const void* z, int64_t ldz, void* dz, int64_t lddz, void* dbias,
+                         int32_t tile, void* ws, size_t ws_bytes, void* stream) {
     fbl_status st = gated_shape(dtype, act, M, N, F);
-    if (st == FBL_OK) st = gated_shape(dtype, act, M, K, F);
     if (st != FBL_OK) return st;
-    if (!dy || !wd || !z || !dz || (dx && !w)) return FBL_ERR_NULL;
+    if (!dy || !wd || !z || !dz) return FBL_ERR_NULL;
     const int es = (int)fbl::dtype_size(dtype), f32 = es == 4;
     const RowsView vdy{dy, M, N, lddy, es}, vwd{wd, F, N, ldwd, es}, vz{z, M, 2 * F, ldz, es}, vdz{dz, M, 2 * F, lddz, es},
-        vdb{dbias, 1, 2 * F, 2 * F, es}, vw{dx ? w : nullptr, K, 2 * F, ldw, es}, vdx{dx, M, K, lddx, es};
-    for (const RowsView* v : {&vdy, &vwd, &vz, &vdz, &vw, &vdx})
+        vdb{dbias, 1, 2 * F, 2 * F, es};
+    for (const RowsView* v : {&vdy, &vwd, &vz, &vdz})
         if ((st = fbl::check_operand(*v)) != FBL_OK) return st;
     if (!vdb.natural()) return FBL_ERR_ALIGN;
-    if (es == 2 && (N % 8 || F % 8 || (dx && K % 8))) return FBL_ERR_UNSUPPORTED;
+    if (es == 2 && (N % 8 || F % 8)) return FBL_ERR_UNSUPPORTED;
     if (tile < FBL_GEMM_TILE_AUTO || tile >= fbl::kGemmTileCount || (es == 4 && tile != FBL_GEMM_TILE_AUTO))
         return FBL_ERR_ARG;
-    const GatedWs gw = gated_ws(f32, M, K, F, N);
-    const bool any = ws && tile == FBL_GEMM_TILE_AUTO, shared = any && gw.splits > 1, xshared = any && dx && gw.xsplits > 1;
-    const size_t need = shared || xshared || dbias ? gw.total : 0;
+    const GatedWs gw = gated_ws(f32, M, F, N);
+    const bool shared = ws && tile == FBL_GEMM_TILE_AUTO && gw.splits > 1;
+    const size_t need = shared || dbias ? gw.total : 0;
     if (need && (!ws || ws_bytes < need)) return FBL_ERR_WORKSPACE;
     const RowsView vws{need ? ws : nullptr, 1, (int64_t)need, (int64_t)need + 1, 1};
     if (vws.begin() % 16) return FBL_ERR_ALIGN;
-    const RowsView* outs[] = {&vdz, &vdb, &vdx, &vws};
-    for (int i = 0; i < 4; ++i) {
-        for (const RowsView* in : {&vdy, &vwd, &vz, &vw})
+    const RowsView* outs[] = {&vdz, &vdb, &vws};
+    for (int i = 0; i < 3; ++i) {
+        for (const RowsView* in : {&vdy, &vwd, &vz})
             if (overlap(*outs[i], *in)) return FBL_ERR_ARG;
         for (int j = 0; j < i; ++j)
             if (overlap(*outs[i], *outs[j])) return FBL_ERR_ARG;
@@ -180,26 +168,13 @@ fbl_status fbl_gated_bwd(int32_t dtype, uint32_t act, int64_t M, int64_t K, int6
     p.c_bytes = (uint32_t)vdz.bytes();
     p.z = const_cast<void*>(z), p.ldz = ldz, p.z_bytes = fbl::load_span(vz);
     if (dbias) p.sums = reinterpret_cast<float*>(static_cast<char*>(ws) + gw.sums);
-    float* const planes = static_cast<float*>(ws);
-    const int ztile = f32 ? 0 : tile == FBL_GEMM_TILE_AUTO ? gated_tile(1, M, F, N) : tile;
+    if (!f32 && tile == FBL_GEMM_TILE_AUTO) tile = gated_tile(1, M, F, N);
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    hipError_t e = shared ? run_shared(f32, (int)act, 1, gw.splits, p, planes, s) : run_gated_gemm(f32, (int)act, 1, ztile, p, s);
+    hipError_t e = shared ? run_shared(f32, (int)act, 1, gw.splits, p, static_cast<float*>(ws), s)
+                          : run_gated_gemm(f32, (int)act, 1, tile, p, s);
     if (e == hipSuccess && dbias) {
-        const int64_t groups = shared ? M : fbl::linear_grad_groups(f32, ztile, p);
+        const int64_t groups = shared ? M : fbl::linear_grad_groups(f32, tile, p);
         e = fbl::launch_column_sums(f32, p.sums, (int)groups, 1, (int)(2 * F), dbias, nullptr, s);
-    }
-    if (e == hipSuccess && dx) {
-        fbl::LinearArgs q{};
-        fbl::product(q, FBL_PROJ_BWD_DATA, vdz, vw, vdx, M, K, 2 * F);
-        const int xtile = f32 ? 0 : tile == FBL_GEMM_TILE_AUTO ? fbl::proj_auto_tile(FBL_PROJ_BWD_DATA, M, K, 2 * F) : tile;
-        if (xshared) {
-            e = fbl::launch_shares(f32, 1, gw.xsplits, q, planes, s);
-            if (e == hipSuccess)
-                e = M <= 128 ? fbl::launch_linear_finish(f32, fbl::kActNone, 1, q, planes, gw.xsplits, s)
-                             : fbl::launch_sum_planes(f32, planes, gw.xsplits, M, K, nullptr, dx, lddx, s);
-        } else {
-            e = f32 ? fbl::launch_proj_gemm_f32(0, 1, q, s) : fbl::launch_linear_gemm<fbl::kActNone>(1, xtile, q, s);
-        }
     }
     return e == hipSuccess ? FBL_OK : FBL_ERR_HIP;
 }

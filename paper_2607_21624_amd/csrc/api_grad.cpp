@@ -12,7 +12,7 @@ namespace {
 
 using fbl::GradList;
 
-constexpr int kWorkgroups = 2048;  // of a launch: eight a CU
+constexpr int kWorkgroups = 1024;  // of a launch: their sums are added by every workgroup that clips (85 M values within the limit: 2048 41, 1024 38 us)
 constexpr int64_t kMostBytes = (int64_t)1 << 45;  // of a list: its chunks count to 2^30
 
 int64_t launches(int64_t count) { return (count + fbl::kGradTensors - 1) / fbl::kGradTensors; }
@@ -57,13 +57,14 @@ template <typename F>
 fbl_status for_lists(int64_t count, const fbl_grad* g, bool outs, F&& f) {
     for (int64_t i = 0; i < count;) {
         GradList a;
-        a.count = 0;
+        a.count = 0, a.in_place = 1;
         int64_t chunks = 0;
         for (; i < count && a.count < fbl::kGradTensors; ++i) {
             if (g[i].n == 0) continue;
             const int64_t bytes = g[i].n * fbl::dtype_size(g[i].dtype);
             auto& t = a.t[a.count];
             t.p = g[i].p, t.out = outs ? g[i].out : nullptr, t.n = g[i].n, t.f32 = g[i].dtype == FBL_F32;
+            if (t.out != t.p) a.in_place = 0;
             a.first[a.count++] = (int)chunks;
             chunks += (bytes + fbl::kGradChunk - 1) / fbl::kGradChunk;
         }

@@ -870,44 +870,40 @@ PyObject* gated_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
-// gated_bwd(dy, w_down, z, act, dz, dbias, w, dx, tile, workspace, stream, need_bias)
+// gated_bwd(dy, w_down, z, act, dz, dbias, tile, workspace, stream, need_bias)
 PyObject* gated_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     HANDLE_TH_ERRORS
-    if (n != 12) Py_RETURN_NONE;
+    if (n != 10) Py_RETURN_NONE;
     Args g{a};
     const Tensor *dy = g.tensor(0), *wd = g.tensor(1), *z = g.tensor(2);
     const uint32_t act = g.act(3);
-    const Tensor *dz = g.tensor_or_none(4), *db = g.tensor_or_none(5), *w = g.tensor_or_none(6), *dx = g.tensor_or_none(7);
-    const int64_t tile = g.integer(8);
-    const Tensor* ws = g.tensor_or_none(9);
-    g.no_stream(10);
-    const bool need_b = g.flag(11);
-    if (!g.ready() || dy->dim() != 2 || wd->dim() != 2 || (w && w->dim() != 2) || (dx && !w) || dtype_code(*dy) < 0) Py_RETURN_NONE;
-    const int64_t M = dy->size(0), N = dy->size(1), F = wd->size(0), K = w ? w->size(0) : N;
+    const Tensor *dz = g.tensor_or_none(4), *db = g.tensor_or_none(5);
+    const int64_t tile = g.integer(6);
+    const Tensor* ws = g.tensor_or_none(7);
+    g.no_stream(8);
+    const bool need_b = g.flag(9);
+    if (!g.ready() || dy->dim() != 2 || wd->dim() != 2 || dtype_code(*dy) < 0) Py_RETURN_NONE;
+    const int64_t M = dy->size(0), N = dy->size(1), F = wd->size(0);
     const at::ScalarType dt = dy->scalar_type();
     const int code = dtype_code(*dy);
-    if (!matrix(dy, M, N, dt) || !matrix(wd, F, N, dt) || !matrix(z, M, 2 * F, dt) || !matrix(dz, M, 2 * F, dt) || !vector(db, 2 * F, dt) ||
-        !matrix(w, K, 2 * F, dt) || !matrix(dx, M, K, dt))
+    if (!matrix(dy, M, N, dt) || !matrix(wd, F, N, dt) || !matrix(z, M, 2 * F, dt) || !matrix(dz, M, 2 * F, dt) || !vector(db, 2 * F, dt))
         Py_RETURN_NONE;
-    Tensor mz, mb, mx;
+    Tensor mz, mb;
     if (!dz) mz = empty({M, 2 * F}, dt, *dy), dz = &mz;
     if (!db && need_b) mb = empty({2 * F}, dt, *dy), db = &mb;
-    if (w && !dx) mx = empty({M, K}, dt, *dy), dx = &mx;
     Scratch sc;
     size_t need = 0;
-    if (db || ws || dx || M <= 128) {
-        if (!ws && fbl_gated_bwd_workspace(code, M, K, F, N, &need) != FBL_OK) Py_RETURN_NONE;
+    if (db || ws || M <= 128) {
+        if (!ws && fbl_gated_bwd_workspace(code, M, F, N, &need) != FBL_OK) Py_RETURN_NONE;
         if (!sc.set(ws, need, *dy)) Py_RETURN_NONE;
     }
-    void *s = g.stream(), *py = data(dy), *pwd = data(wd), *pz = data(z), *pdz = data(dz), *pdb = data(db), *pw = data(w), *pdx = data(dx);
-    const int64_t ldy = row_stride(dy), ldwd = row_stride(wd), ldz = row_stride(z), lddz = row_stride(dz), ldw = row_stride(w),
-                  lddx = row_stride(dx);
+    void *s = g.stream(), *py = data(dy), *pwd = data(wd), *pz = data(z), *pdz = data(dz), *pdb = data(db);
+    const int64_t ldy = row_stride(dy), ldwd = row_stride(wd), ldz = row_stride(z), lddz = row_stride(dz);
     const fbl_status st = unlocked([&] {
-        return fbl_gated_bwd(code, act, M, K, F, N, py, ldy, pwd, ldwd, pz, ldz, pdz, lddz, pdb, pw, ldw, pdx, lddx, (int32_t)tile, sc.p,
-                             sc.bytes, s);
+        return fbl_gated_bwd(code, act, M, F, N, py, ldy, pwd, ldwd, pz, ldz, pdz, lddz, pdb, (int32_t)tile, sc.p, sc.bytes, s);
     });
     if (st != FBL_OK) Py_RETURN_NONE;
-    return tuple_of<3>({object_of(a[4], mz), object_or_none(a[5], mb), object_or_none(a[7], mx)});
+    return tuple_of<2>({object_of(a[4], mz), object_or_none(a[5], mb)});
     END_HANDLE_TH_ERRORS
 }
 

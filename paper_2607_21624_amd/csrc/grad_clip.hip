@@ -4,7 +4,7 @@
 //
 // Bound by memory: the norm reads every value once, clipping reads and writes it once more, or does
 // neither where it is in place and the norm is within the limit.  The list travels in the kernel's arguments, so that a
-// call copies nothing and can be captured.  Tensors are cut into chunks of 32 KB; a workgroup walks every gridDim-th of
+// call copies nothing and can be captured.  Tensors are cut into chunks of 16 KB; a workgroup walks every gridDim-th of
 // them.  Squares are summed in float64: no square overflows or vanishes, and a sum of 2^30 terms keeps fp32's digits.
 // Each workgroup leaves one sum; whoever needs the norm adds them in the same fixed order.  Clipping walks the chunks from
 // the last one back, since the end of what the norm has read is what the last-level cache still holds.
@@ -15,7 +15,7 @@ namespace fbl {
 
 namespace {
 
-constexpr int kLoads = 8;                      // 16-byte loads of a thread and chunk
+constexpr int kLoads = 4;                      // 16-byte loads of a thread and chunk
 constexpr int kChunkBytes = 256 * 16 * kLoads;
 static_assert(kChunkBytes == kGradChunk, "chunks as the host counts them");
 
@@ -60,9 +60,10 @@ struct Share {
             for (int k = 0; k < kLoads; ++k) x[k].fetch(p, at(k), left);
 #pragma unroll
             for (int k = 0; k < kLoads; ++k) x[k].settle(at(k), left);
-        } else {
+        } else {  // the first thread's alone
 #pragma unroll
-            for (int k = 0; k < kLoads; ++k) x[k].template fetch<true>(p, at(k), left);
+            for (int k = 1; k < kLoads; ++k) x[k] = P{};
+            x[0].template fetch<true>(p, at(0), left);
         }
     }
 };
@@ -127,9 +128,9 @@ __global__ __launch_bounds__(256) void grad_scale(GradList a, const double* sums
     if (sums && norm && blockIdx.x == 0 && threadIdx.x == 0) norm[0] = x;
     const double ratio = (double)limit / ((double)x + 1e-6);
     const float scale = ratio >= 1.0 ? 1.f : (float)ratio;  // (a norm that is nan makes everything nan)
+    if (scale == 1.f && a.in_place) return;
     for (int c = a.chunks - 1 - (int)blockIdx.x; c >= 0; c -= gridDim.x) {
         const int t = tensor_of(a, c);
-        if (scale == 1.f && a.t[t].out == a.t[t].p) continue;
         const int64_t at = (int64_t)(c - a.first[t]) * kChunkBytes;
         if (a.t[t].f32) scaled<float>(a.t[t].p, a.t[t].out, at / 4, a.t[t].n, scale);
         else scaled<bf16>(a.t[t].p, a.t[t].out, at / 2, a.t[t].n, scale);

@@ -37,6 +37,19 @@ FBL_DEV float group_sum(float x) {
     return x;
 }
 
+// Sum over the lanes of a wavefront that have the same place in groups of LANES, the same value in each: rotations
+// within 16 lanes, then the row swaps.
+template <int LANES>
+FBL_DEV float place_sum(float x) {
+    if constexpr (LANES <= 2) x += dpp<0x122>(x);  // row_ror 2
+    if constexpr (LANES <= 4) x += dpp<0x124>(x);  // row_ror 4
+    if constexpr (LANES <= 8) x += dpp<0x128>(x);  // row_ror 8
+    auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+    p = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(p[0]) + __uint_as_float(p[1]);
+}
+
 // Cosine and sine of f / 2^32 turns.
 template <bool FAST>
 FBL_DEV void turned(int32_t f, float& c, float& s) {
@@ -276,8 +289,7 @@ __global__ __launch_bounds__(256, (NORM && BWD ? 3 : 5)) void qk_norm_rotary(Rot
         for (int k = 0; k < 2; ++k)
 #pragma unroll
             for (int e = 0; e < 2 * V; ++e) {
-#pragma unroll
-                for (int d = LANES; d < 64; d *= 2) sum[k][e] += __shfl_xor(sum[k][e], d);
+                sum[k][e] = place_sum<LANES>(sum[k][e]);
                 if (lane < LANES) part[wave][k][(e < V ? c0 : c1) + e % V] = sum[k][e];
             }
         __syncthreads();

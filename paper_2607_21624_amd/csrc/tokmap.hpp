@@ -158,7 +158,7 @@ struct GatedArgs : GemmArgs {
 
 // Tensors of one launch over a list of gradients (grad_clip.hip), by value in its arguments: `first` chunks of kGradChunk
 // bytes come before each, and first[count] = chunks.
-constexpr int kGradChunk = 32768;
+constexpr int kGradChunk = 16384;
 constexpr int kGradTensors = 112;
 struct GradList {
     struct {
@@ -168,6 +168,7 @@ struct GradList {
     } t[kGradTensors];
     int first[kGradTensors + 1];
     int count, chunks;
+    int in_place;  // every tensor's output is itself
 };
 static_assert(sizeof(GradList) <= 3584, "a launch's arguments end at 4 KB");
 

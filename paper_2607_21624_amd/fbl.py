@@ -254,10 +254,9 @@ def _load() -> ctypes.CDLL:
     lib.fbl_gated_fwd.restype = ctypes.c_int
     lib.fbl_gated_fwd_workspace.argtypes = [i32, i64, i64, i64, sizep]
     lib.fbl_gated_fwd_workspace.restype = ctypes.c_int
-    lib.fbl_gated_bwd_workspace.argtypes = [i32, i64, i64, i64, i64, sizep]
+    lib.fbl_gated_bwd_workspace.argtypes = [i32, i64, i64, i64, sizep]
     lib.fbl_gated_bwd_workspace.restype = ctypes.c_int
-    lib.fbl_gated_bwd.argtypes = [i32, u32, i64, i64, i64, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, i64, vp, i64, i32,
-                                  vp, size, vp]
+    lib.fbl_gated_bwd.argtypes = [i32, u32, i64, i64, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, i32, vp, size, vp]
     lib.fbl_gated_bwd.restype = ctypes.c_int
     lib.fbl_grad_norm_workspace.argtypes = [i64, sizep]
     lib.fbl_grad_norm_workspace.restype = ctypes.c_int
@@ -1175,26 +1174,25 @@ def gated_fwd(x, w, bias=None, act: str = "silu", out=None, z=None, tile: int = 
     return out
 
 
-def gated_bwd_workspace(dy, w_down, w=None) -> int:
-    """Bytes of gated_bwd's workspace for dy [M, N], w_down [F, N] and, where dx is wanted, w [K, 2F]."""
+def gated_bwd_workspace(dy, w_down) -> int:
+    """Bytes of gated_bwd's workspace for dy [M, N] and w_down [F, N]."""
     n = ctypes.c_size_t(0)
-    _check(LIB.fbl_gated_bwd_workspace(_dtype_code(dy), dy.shape[0], w_down.shape[1] if w is None else w.shape[0],
-                                       *w_down.shape, ctypes.byref(n)), "fbl_gated_bwd_workspace")
+    _check(LIB.fbl_gated_bwd_workspace(_dtype_code(dy), dy.shape[0], *w_down.shape, ctypes.byref(n)),
+           "fbl_gated_bwd_workspace")
     return int(n.value)
 
 
-def gated_bwd(dy, w_down, z, act: str = "silu", dz=None, dbias=None, w=None, dx=None, tile: int = FBL_GEMM_TILE_AUTO,
-              workspace=None, stream=None, need_bias: bool = True):
+def gated_bwd(dy, w_down, z, act: str = "silu", dz=None, dbias=None, tile: int = FBL_GEMM_TILE_AUTO, workspace=None,
+              stream=None, need_bias: bool = True):
     """Gradient of a gated layer's pre-activations from that of the block's result: dy [M, N], w_down [F, N] and the
-    forward's z [M, 2F] give dz [M, 2F], the sums of dz over its rows, dbias [2F], and with the layer's w [K, 2F] the
-    gradient of its input, dx [M, K].  Returns (dz, dbias, dx), dbias None where not needed and dx without w.  dw is
-    linear_bwd's of dz."""
-    done = _FAST.gated_bwd(dy, w_down, z, act, dz, dbias, w, dx, tile, workspace, stream, need_bias)
+    forward's z [M, 2F] give dz [M, 2F] and the sums of dz over its rows, dbias [2F].  Returns (dz, dbias), dbias None
+    where not needed.  dx and dw are linear_bwd's of dz."""
+    done = _FAST.gated_bwd(dy, w_down, z, act, dz, dbias, tile, workspace, stream, need_bias)
     if done is not None:
         return done
     import torch
     where = "gated_bwd"
-    _check_device(where, stream, dy=dy, w_down=w_down, z=z, dz=dz, dbias=dbias, w=w, dx=dx, workspace=workspace)
+    _check_device(where, stream, dy=dy, w_down=w_down, z=z, dz=dz, dbias=dbias, workspace=workspace)
     lddy = _matrix(dy, where, "dy")
     M, N = dy.shape
     dt, code = _dtype_code(dy), _act_code(act, where)
@@ -1209,24 +1207,13 @@ def gated_bwd(dy, w_down, z, act: str = "silu", dz=None, dbias=None, w=None, dx=
     if dbias is None and need_bias:
         dbias = _empty(2 * F, dy.dtype, dy, stream)
     _vector(dbias, where, "dbias", 2 * F, dy.dtype)
-    K, ldw, lddx = N, 0, 0
-    if w is None and dx is not None:
-        raise FblError(FBL_ERR_NULL, f"{where}: dx needs the layer's w")
-    if w is not None:
-        ldw = _matrix(w, where, "w", None, dy)
-        K = w.shape[0]
-        if w.shape[1] != 2 * F:
-            raise FblError(FBL_ERR_SHAPE, f"{where}: w {tuple(w.shape)} and w_down {tuple(w_down.shape)} do not agree")
-        if dx is None:
-            dx = _empty((M, K), dy.dtype, dy, stream)
-        lddx = _matrix(dx, where, "dx", (M, K), dy)
     ws, ws_bytes = None, 0
-    if dbias is not None or workspace is not None or dx is not None or M <= 128:
-        need = 0 if workspace is not None else gated_bwd_workspace(dy, w_down, w)
+    if dbias is not None or workspace is not None or M <= 128:
+        need = 0 if workspace is not None else gated_bwd_workspace(dy, w_down)
         ws, ws_bytes = _scratch(workspace, need, where, dy, stream)
-    _call("fbl_gated_bwd", dy, stream, dt, code, M, K, F, N, _ptr(dy), lddy, _ptr(w_down), ldwd, _ptr(z), ldz, _ptr(dz),
-          lddz, _ptr(dbias), _ptr(w), ldw, _ptr(dx), lddx, tile, _ptr(ws), ws_bytes)
-    return dz, dbias, dx
+    _call("fbl_gated_bwd", dy, stream, dt, code, M, F, N, _ptr(dy), lddy, _ptr(w_down), ldwd, _ptr(z), ldz, _ptr(dz), lddz,
+          _ptr(dbias), tile, _ptr(ws), ws_bytes)
+    return dz, dbias
 
 
 # ------------------------------------- losses of a linear head over a vocabulary

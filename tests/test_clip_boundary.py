@@ -59,10 +59,10 @@ def test_refusals(f, kw, status):
 @pytest.mark.parametrize("f", [both, norm_of])
 def test_workspace_refusals(f):
     n = ctypes.c_size_t()
-    assert LIB.fbl_grad_norm_workspace(3, ctypes.byref(n)) == F.FBL_OK and n.value == 2048 * 8
+    assert LIB.fbl_grad_norm_workspace(3, ctypes.byref(n)) == F.FBL_OK and n.value == 1024 * 8
     assert f(ws=None) == F.FBL_ERR_WORKSPACE and f(ws_bytes=n.value - 1) == F.FBL_ERR_WORKSPACE
     assert f(ws=at(9, 4)) == F.FBL_ERR_ALIGN and f(ws=at(1)) == F.FBL_ERR_ARG and f(ws=at(8) - 8) == F.FBL_ERR_ARG
-    assert LIB.fbl_grad_norm_workspace(113, ctypes.byref(n)) == F.FBL_OK and n.value == 2 * 2048 * 8
+    assert LIB.fbl_grad_norm_workspace(113, ctypes.byref(n)) == F.FBL_OK and n.value == 2 * 1024 * 8
     assert LIB.fbl_grad_norm_workspace(0, ctypes.byref(n)) == F.FBL_ERR_SHAPE
     assert LIB.fbl_grad_norm_workspace(3, None) == F.FBL_ERR_NULL
 

@@ -54,23 +54,16 @@ def _check_bwd(dz, db, dy, wd, z, act):
         check("dbias", db, ref.sum(0), (len(dy) + 16) * 2.0 ** -24 * (np.abs(ref) + bound).sum(0) + bound.sum(0))
 
 
-def _check_dx(dx, dz, w):
-    """From dz as it was rounded: a product alone."""
-    d = dz.double().cpu().numpy()
-    check("dx", dx, d @ w.T, _sum_bound(d, w.T))
-
-
 def _run(M, K, F, N, dt, act, bias=True, tile=-1):
     (x, xr), (w, wr), (b, br), (wd, wdr), (z, zr), (dy, dyr) = _inputs(M, K, F, N, dt, bias)
     zo = torch.full((M, 2 * F), float("nan"), dtype=dt, device="cuda")
     h = fbl.gated_fwd(x, w, b, act, z=zo, tile=tile)
     only = fbl.gated_fwd(x, w, b, act, tile=tile)
-    dz, db, dx = fbl.gated_bwd(dy, wd, z, act, w=w, need_bias=bias, tile=tile)
+    dz, db = fbl.gated_bwd(dy, wd, z, act, need_bias=bias, tile=tile)
     torch.cuda.synchronize()
     _check_fwd(h, zo, xr, wr, br, act)
     assert torch.equal(h, only)
     _check_bwd(dz, db, dyr, wdr, zr, act)
-    _check_dx(dx, dz, wr)
     assert (db is None) == (not bias)
 
 
@@ -103,13 +96,11 @@ def test_every_tile(tile):
     zo, zbuf = padded(torch.zeros(M, 2 * F, dtype=torch.bfloat16, device="cuda"), 8, 7.0)
     dz, dbuf = padded(torch.zeros(M, 2 * F, dtype=torch.bfloat16, device="cuda"), 8, 7.0)
     fbl.gated_fwd(x, w, b, "gelu", out=h, z=zo, tile=tile)
-    dx, xbuf = padded(torch.zeros(M, K, dtype=torch.bfloat16, device="cuda"), 8, 7.0)
-    _, db, _ = fbl.gated_bwd(dy, wd, zin, "gelu", dz=dz, w=w, dx=dx, tile=tile)
+    _, db = fbl.gated_bwd(dy, wd, zin, "gelu", dz=dz, tile=tile)
     torch.cuda.synchronize()
     _check_fwd(h, zo, xr, wr, br, "gelu")
     _check_bwd(dz, db, dyr, wdr, zr, "gelu")
-    _check_dx(dx, dz, wr)
-    for buf, n in ((hbuf, F), (zbuf, 2 * F), (dbuf, 2 * F), (xbuf, K)):
+    for buf, n in ((hbuf, F), (zbuf, 2 * F), (dbuf, 2 * F)):
         assert torch.all(buf[:, n:] == 7.0) and torch.all(buf[-1] == 7.0)
 
 
@@ -132,21 +123,20 @@ def test_shared_contractions(dt):
         F = F + odd
         x, w, wd, z, dy = (padded(t, 8)[0] for t in (x, w, wd, z, dy))
         new = lambda n: padded(torch.zeros(M, n, dtype=dt, device="cuda"), 8, 7.0)
-        need, back = fbl.gated_fwd_workspace(x, w), fbl.gated_bwd_workspace(dy, wd, w)
+        need, back = fbl.gated_fwd_workspace(x, w), fbl.gated_bwd_workspace(dy, wd)
         assert need > 0 and need % (M * 2 * F * 4) == 0
-        (h, hbuf), (zo, zbuf), (dz, dbuf), (dx, xbuf) = new(F), new(2 * F), new(2 * F), new(K + odd)
+        (h, hbuf), (zo, zbuf), (dz, dbuf) = new(F), new(2 * F), new(2 * F)
         fbl.gated_fwd(x, w, b, "silu", out=h, z=zo)
-        _, db, _ = fbl.gated_bwd(dy, wd, z, "silu", dz=dz, w=w, dx=dx)
+        _, db = fbl.gated_bwd(dy, wd, z, "silu", dz=dz)
         _check_fwd(h, zo, xr, wr, br, "silu")
         _check_bwd(dz, db, dyr, wdr, zr, "silu")
-        _check_dx(dx, dz, wr)
-        for buf, n in ((hbuf, F), (zbuf, 2 * F), (dbuf, 2 * F), (xbuf, K + odd)):
+        for buf, n in ((hbuf, F), (zbuf, 2 * F), (dbuf, 2 * F)):
             assert torch.all(buf[:, n:] == 7.0) and torch.all(buf[-1] == 7.0)
         ws = torch.full((max(need, back) + 64,), 0xff, dtype=torch.uint8, device="cuda")
         assert torch.equal(h, fbl.gated_fwd(x, w, b, "silu", out=new(F)[0], workspace=ws[:need]))
         assert torch.all(ws[need:] == 0xff)
-        again = fbl.gated_bwd(dy, wd, z, "silu", dz=new(2 * F)[0], w=w, workspace=ws[:back])
-        assert torch.equal(again[0], dz) and torch.equal(again[1], db) and torch.equal(again[2], dx) and torch.all(ws[max(need, back):] == 0xff)
+        again = fbl.gated_bwd(dy, wd, z, "silu", dz=new(2 * F)[0], workspace=ws[:back])
+        assert torch.equal(again[0], dz) and torch.equal(again[1], db) and torch.all(ws[max(need, back):] == 0xff)
         alone = fbl.gated_bwd(dy, wd, z, "silu", dz=new(2 * F)[0], need_bias=False)
         assert torch.equal(alone[0], dz) and alone[1] is None
         side, got = torch.cuda.Stream(), new(F)[0]
@@ -155,31 +145,9 @@ def test_shared_contractions(dt):
         torch.cuda.synchronize()
         assert torch.equal(h, got)
         for f in (lambda: fbl.gated_fwd(x, w, b, "silu", workspace=ws[:need - 16]),
-                  lambda: fbl.gated_bwd(dy, wd, z, "silu", w=w, workspace=ws[:back - 16])):
+                  lambda: fbl.gated_bwd(dy, wd, z, "silu", workspace=ws[:back - 16])):
             with pytest.raises(fbl.FblError):
                 f()
-
-
-def test_dx_of_few_tiles_is_shared():
-    """dx whose 256 x 256 tiles fill half of the CUs: the contraction is shared, the same way each time, and a workspace
-    that is not brought leaves it alone."""
-    M, K, F, N = 4000, 2040, 8200, 64
-    rng = np.random.default_rng(5)
-    dt = torch.bfloat16
-    w, wr = rounded(rng, (K, 2 * F), dt, K ** -0.5)
-    wd, _ = rounded(rng, (F, N), dt, N ** -0.5)
-    z, _ = rounded(rng, (M, 2 * F), dt)
-    dy, _ = rounded(rng, (M, N), dt)
-    note("shared dx of many tokens")
-    need = fbl.gated_bwd_workspace(dy, wd, w)
-    assert need >= 2 * M * K * 4  # two planes at least
-    some = np.r_[0:40, 3900:4000]  # (of both ends)
-    dx, xbuf = padded(torch.zeros(M, K, dtype=dt, device="cuda"), 8, 7.0)
-    dz, _, _ = fbl.gated_bwd(dy, wd, z, w=w, dx=dx, need_bias=False)
-    _check_dx(dx[some], dz[some], wr)
-    assert torch.all(xbuf[:, K:] == 7.0) and torch.all(xbuf[-1] == 7.0)
-    ws = torch.full((need,), 0xff, dtype=torch.uint8, device="cuda")
-    assert torch.equal(fbl.gated_bwd(dy, wd, z, w=w, workspace=ws)[2], dx)
 
 
 @pytest.mark.parametrize("dt,gap", [("bf16", 8), ("f32", 3)])
@@ -189,7 +157,7 @@ def test_strided_operands(dt, gap):
     (x, _), (w, _), (b, _), (wd, _), (z, _), (dy, _) = _inputs(75, 88, 104, 72, dt, True)
     zo = torch.empty_like(z)
     h = fbl.gated_fwd(x, w, b, "gelu_tanh", z=zo)
-    dz, db, dx = fbl.gated_bwd(dy, wd, z, "gelu_tanh")
+    dz, db = fbl.gated_bwd(dy, wd, z, "gelu_tanh")
     view = lambda t: padded(t, gap)[0]
     zv = view(torch.zeros_like(zo))
     assert torch.equal(h, fbl.gated_fwd(view(x), view(w), b, "gelu_tanh", z=zv, out=view(torch.zeros_like(h))))
@@ -247,8 +215,8 @@ def test_autograd(dt, lead):
         z = torch.empty(x2.shape[0], 2 * F, dtype=dtype, device="cuda")
         h = fbl.gated_fwd(x2, w1, b1, "silu", z=z)
         y2 = fbl.linear_fwd(h, w2, b2, residual=r2)
-        dz, db1, dx = fbl.gated_bwd(dy2, w2, z, "silu", w=w1)
-        _, dw1, _ = fbl.linear_bwd(dz, x2, w1, need_dx=False, need_bias=False)
+        dz, db1 = fbl.gated_bwd(dy2, w2, z, "silu")
+        dx, dw1, _ = fbl.linear_bwd(dz, x2, w1, need_bias=False)
         _, dw2, db2 = fbl.linear_bwd(dy2, h, w2, need_dx=False)
     for a, b in zip((y, *got), (y2, dx, dw1, db1, dw2, db2, dy)):
         assert torch.equal(a.reshape(b.shape), b)
