@@ -797,14 +797,14 @@ fbl_status fbl_qk_norm_rotary_bwd(const fbl_layout* lgq, const void* gq, const f
 /*
  * A gated layer, the first part of a gated feed-forward block (its second is fbl_linear_fwd with the block's bias and
  * residual): both projections, the activation and their product in one kernel.
- *   z = x [M, K] . w [K, 2F] + bias [2F],   h [M, F] = act(gate) * up
- * gate is columns 0 .. F - 1 of z, up columns F .. 2F - 1 (w, bias and z hold the two side by side; act as
- * fbl_linear_fwd's).  bias may be NULL; z [M, 2F], where not NULL, receives the pre-activations that the backward needs,
- * rounded to the storage type (h is made from them unrounded).  ws: NULL, or fbl_gated_fwd_workspace bytes (16-byte
+ *   (gate, up) = x [M, K] . w [K, 2F] + bias [2F],   h [M, F] = act(gate) * up
+ * gate is columns 0 .. F - 1, up columns F .. 2F - 1 (w and bias hold the two side by side; act as fbl_linear_fwd's).
+ * bias may be NULL.  factors [M, 2F], where not NULL, receives what the backward needs, the derivatives of h by gate and by
+ * up, (up * act'(gate), act(gate)), rounded to the storage type.  ws: NULL, or fbl_gated_fwd_workspace bytes (16-byte
  * aligned), with which several workgroups share the contraction of a few tokens' tiles (0 bytes where they do not).
  *
  * fbl_gated_bwd takes the gradient dy [M, N] of the block's result and w_down [F, N], its second weight, and gives
- *   dz [M, 2F] = (dh * up * act'(gate),  dh * act(gate)),   dh = dy . w_down^T  (never stored)
+ *   dz [M, 2F] = dh * factors, for gate and for up,   dh = dy . w_down^T  (never stored)
  *   dbias [2F] (NULL: not wanted) = sums over rows of dz, unrounded
  * of which fbl_linear_bwd makes dx = dz . w^T and dw = x^T . dz, and from h and dy the gradients of w_down and of its bias.
  * The workspace (16-byte aligned, fbl_gated_bwd_workspace bytes) is needed where dbias is wanted, else it may be NULL; with it,
@@ -818,13 +818,13 @@ fbl_status fbl_qk_norm_rotary_bwd(const fbl_layout* lgq, const void* gq, const f
  * All sums run in a fixed order.
  */
 fbl_status fbl_gated_fwd(int32_t dtype, uint32_t act, int64_t M, int64_t K, int64_t F, const void* x, int64_t ldx,
-                         const void* w, int64_t ldw, const void* bias, void* h, int64_t ldh, void* z, int64_t ldz,
-                         int32_t tile, void* ws, size_t ws_bytes, void* stream);
+                         const void* w, int64_t ldw, const void* bias, void* h, int64_t ldh, void* factors,
+                         int64_t ldf, int32_t tile, void* ws, size_t ws_bytes, void* stream);
 fbl_status fbl_gated_fwd_workspace(int32_t dtype, int64_t M, int64_t K, int64_t F, size_t* bytes);
 fbl_status fbl_gated_bwd_workspace(int32_t dtype, int64_t M, int64_t F, int64_t N, size_t* bytes);
-fbl_status fbl_gated_bwd(int32_t dtype, uint32_t act, int64_t M, int64_t F, int64_t N, const void* dy, int64_t lddy,
-                         const void* w_down, int64_t ldwd, const void* z, int64_t ldz, void* dz, int64_t lddz, void* dbias,
-                         int32_t tile, void* ws, size_t ws_bytes, void* stream);
+fbl_status fbl_gated_bwd(int32_t dtype, int64_t M, int64_t F, int64_t N, const void* dy, int64_t lddy, const void* w_down,
+                         int64_t ldwd, const void* factors, int64_t ldf, void* dz, int64_t lddz, void* dbias, int32_t tile,
+                         void* ws, size_t ws_bytes, void* stream);
 
 /*
  * The end of a training step: the global norm of a list of gradients, and the gradients clipped by it.

@@ -72,12 +72,17 @@ def gated_fwd(x, w, b=None, kind="silu"):
     return act(z[:, :F], kind) * z[:, F:], z
 
 
-def gated_bwd(dh, z, kind="silu"):
+def gated_factors(z, kind="silu"):
+    """The derivatives of h by gate and by up [M, 2F]."""
+    z = np.asarray(z, dtype=np.float64)
+    F = z.shape[1] // 2
+    return np.concatenate([z[:, F:] * act_grad(z[:, :F], kind), act(z[:, :F], kind)], axis=1)
+
+
+def gated_bwd(dh, factors):
     """dz [M, 2F] from dh [M, F]."""
-    dh, z = np.asarray(dh, dtype=np.float64), np.asarray(z, dtype=np.float64)
-    F = dh.shape[1]
-    gate, up = z[:, :F], z[:, F:]
-    return np.concatenate([dh * up * act_grad(gate, kind), dh * act(gate, kind)], axis=1)
+    dh, factors = np.asarray(dh, dtype=np.float64), np.asarray(factors, dtype=np.float64)
+    return np.concatenate([dh, dh], axis=1) * factors
 
 
 # ------------------------------------------------------------------------- clipping

@@ -349,32 +349,31 @@ class _GatedMlp(torch.autograd.Function):
                 raise _f.FblError(_f.FBL_ERR_SHAPE, f"gated_mlp: residual has shape {tuple(residual.shape)}, needs "
                                                     f"{(*x.shape[:-1], w2.shape[1])}")
             res2 = _matrix_of(residual, "gated_mlp: residual")
-        z = None
+        factors = None
         if any(ctx.needs_input_grad[:3]):
-            z = _wide(x2.shape[0], w1.shape[1], x)
-        h = _f.gated_fwd(x2, w1, b1, act, z=z)
+            factors = _wide(x2.shape[0], w1.shape[1], x)
+        h = _f.gated_fwd(x2, w1, b1, act, factors=factors)
         y, y2 = _rows_of(x, w2.shape[1])
         _f.linear_fwd(h, w2, b2, residual=res2, out=y2)
-        ctx.save_for_backward(x2, w1, w2, z, h)
-        ctx.cfg = (x.shape, act)
+        ctx.save_for_backward(x2, w1, w2, factors, h)
+        ctx.xshape = x.shape
         return y
 
     @staticmethod
     @_first_order
     def backward(ctx, dy):
-        x2, w1, w2, z, h = ctx.saved_tensors
-        xshape, act = ctx.cfg
+        x2, w1, w2, factors, h = ctx.saved_tensors
         need = ctx.needs_input_grad
         dx = dw1 = db1 = dw2 = db2 = None
         if any(need[:5]):
             dy2 = _matrix_of(_unit(dy, "gated_mlp"), "gated_mlp: the incoming gradient")
             if any(need[:3]):
-                dz, db1 = _f.gated_bwd(dy2, w2, z, act, dz=_wide(*z.shape, z), need_bias=need[2])
+                dz, db1 = _f.gated_bwd(dy2, w2, factors, dz=_wide(*factors.shape, factors), need_bias=need[2])
                 if need[0] or need[1]:
                     dx, dw1, _ = _f.linear_bwd(dz, x2, w1, need_dx=need[0], need_dw=need[1], need_bias=False)
             if need[3] or need[4]:
                 _, dw2, db2 = _f.linear_bwd(dy2, h, w2, need_dx=False, need_dw=need[3], need_bias=need[4])
-        return dx.view(xshape) if need[0] else None, dw1, db1, dw2, db2, dy if need[5] else None, None
+        return dx.view(ctx.xshape) if need[0] else None, dw1, db1, dw2, db2, dy if need[5] else None, None
 
 
 def gated_mlp(x, w1, b1, w2, b2, act: str = "silu", residual=None):

@@ -17,7 +17,7 @@ OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libfbl.so")
 ACTS = ["none", "relu", "gelu", "gelu_tanh", "silu"]
 SOURCES = ["head_gemm.hip", *(f"{layer}_gemm_{a}.hip" for layer in ("linear", "gated") for a in ACTS), "attn_streams.hip", "attn_rows_f32.hip", "attn_fwd_bf16.hip", "attn_bwd.hip", "attn_bwd_kv.hip", "attn_bwd_q.hip", "attn_bwd_dq.hip", "proj_gemm.hip",
-           "proj_gemm_f32.hip", "layout_map.hip", "noalloc.hip", "layer_norm.hip", "column_sums.hip", "linear_act.hip", "linear_finish.hip", "gated_finish.hip", "head_rows.hip", "qk_norm_rotary.hip", "grad_clip.hip",
+           "proj_gemm_f32.hip", "layout_map.hip", "noalloc.hip", "layer_norm.hip", "column_sums.hip", "linear_act.hip", "linear_finish.hip", "gated_grad.hip", "gated_finish.hip", "head_rows.hip", "qk_norm_rotary.hip", "grad_clip.hip",
            "api.cpp", "api_norm.cpp", "api_linear.cpp", "api_head.cpp", "api_rotary.cpp", "api_gated.cpp", "api_grad.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

@@ -16,22 +16,17 @@ using fbl::RowsView;
 namespace {
 
 template <int ACT>
-hipError_t run_act(int f32, int grad, int tile, const fbl::GatedArgs& p, hipStream_t s) {
-    return f32 ? fbl::launch_gated_gemm_f32<ACT>(grad, p, s) : fbl::launch_gated_gemm<ACT>(grad, tile, p, s);
+hipError_t run_act(int f32, int tile, const fbl::GatedArgs& p, hipStream_t s) {
+    return f32 ? fbl::launch_gated_gemm_f32<ACT>(p, s) : fbl::launch_gated_gemm<ACT>(tile, p, s);
 }
-hipError_t run_gated_gemm(int f32, int act, int grad, int tile, const fbl::GatedArgs& p, hipStream_t s) {
+hipError_t run_gated_gemm(int f32, int act, int tile, const fbl::GatedArgs& p, hipStream_t s) {
     switch (act) {
-        case FBL_ACT_NONE: return run_act<fbl::kActNone>(f32, grad, tile, p, s);
-        case FBL_ACT_RELU: return run_act<fbl::kActRelu>(f32, grad, tile, p, s);
-        case FBL_ACT_GELU: return run_act<fbl::kActGelu>(f32, grad, tile, p, s);
-        case FBL_ACT_GELU_TANH: return run_act<fbl::kActGeluTanh>(f32, grad, tile, p, s);
-        default: return run_act<fbl::kActSilu>(f32, grad, tile, p, s);
+        case FBL_ACT_NONE: return run_act<fbl::kActNone>(f32, tile, p, s);
+        case FBL_ACT_RELU: return run_act<fbl::kActRelu>(f32, tile, p, s);
+        case FBL_ACT_GELU: return run_act<fbl::kActGelu>(f32, tile, p, s);
+        case FBL_ACT_GELU_TANH: return run_act<fbl::kActGeluTanh>(f32, tile, p, s);
+        default: return run_act<fbl::kActSilu>(f32, tile, p, s);
     }
-}
-
-hipError_t run_shared(int f32, int act, int grad, int splits, const fbl::GatedArgs& p, float* planes, hipStream_t s) {
-    const hipError_t e = fbl::launch_shares(f32, grad, splits, p, planes, s);
-    return e == hipSuccess ? fbl::launch_gated_finish(f32, act, grad, p, planes, splits, s) : e;
 }
 
 // The tile of a bf16 product of `cols` columns over a contraction kc: the forward's (2F columns) or the data gradient's
@@ -90,23 +85,23 @@ fbl_status fbl_gated_fwd_workspace(int32_t dtype, int64_t M, int64_t K, int64_t 
 }
 
 fbl_status fbl_gated_fwd(int32_t dtype, uint32_t act, int64_t M, int64_t K, int64_t F, const void* x, int64_t ldx,
-                         const void* w, int64_t ldw, const void* bias, void* h, int64_t ldh, void* z, int64_t ldz,
-                         int32_t tile, void* ws, size_t ws_bytes, void* stream) {
+                         const void* w, int64_t ldw, const void* bias, void* h, int64_t ldh, void* factors,
+                         int64_t ldf, int32_t tile, void* ws, size_t ws_bytes, void* stream) {
     fbl_status st = gated_shape(dtype, act, M, K, F);
     if (st != FBL_OK) return st;
     if (!x || !w || !h) return FBL_ERR_NULL;
     const int es = (int)fbl::dtype_size(dtype), f32 = es == 4;
     const RowsView vx{x, M, K, ldx, es}, vw{w, K, 2 * F, ldw, es}, vb{bias, 1, 2 * F, (2 * F + 7) / 8 * 8, es},
-        vh{h, M, F, ldh, es}, vz{z, M, 2 * F, ldz, es};
-    for (const RowsView* v : {&vx, &vw, &vb, &vh, &vz})
+        vh{h, M, F, ldh, es}, vf{factors, M, 2 * F, ldf, es};
+    for (const RowsView* v : {&vx, &vw, &vb, &vh, &vf})
         if ((st = fbl::check_operand(*v)) != FBL_OK) return st;
     if (es == 2 && (K % 8 || F % 8)) return FBL_ERR_UNSUPPORTED;
     if (tile < FBL_GEMM_TILE_AUTO || tile >= fbl::kGemmTileCount || (es == 4 && tile != FBL_GEMM_TILE_AUTO))
         return FBL_ERR_ARG;
-    for (const RowsView* out : {&vh, &vz})
+    for (const RowsView* out : {&vh, &vf})
         for (const RowsView* in : {&vx, &vw, &vb})
             if (overlap(*out, *in)) return FBL_ERR_ARG;
-    if (overlap(vh, vz)) return FBL_ERR_ARG;
+    if (overlap(vh, vf)) return FBL_ERR_ARG;
     // with a workspace for the shares of it
     const int splits = ws && tile == FBL_GEMM_TILE_AUTO ? few_splits(f32, M, K, 2 * F) : 1;
     if (splits > 1) {
@@ -114,16 +109,22 @@ fbl_status fbl_gated_fwd(int32_t dtype, uint32_t act, int64_t M, int64_t K, int6
         if (ws_bytes < need) return FBL_ERR_WORKSPACE;
         const RowsView vws{ws, 1, (int64_t)need, (int64_t)need, 1};
         if (vws.begin() % 16) return FBL_ERR_ALIGN;
-        for (const RowsView* v : {&vx, &vw, &vb, &vh, &vz})
+        for (const RowsView* v : {&vx, &vw, &vb, &vh, &vf})
             if (overlap(vws, *v)) return FBL_ERR_ARG;
     }
     fbl::GatedArgs p{};
     fbl::product(p, FBL_PROJ_FWD, vx, vw, vh, M, K, 2 * F);
-    p.bias = bias, p.z = z, p.ldz = ldz, p.z_bytes = z ? (uint32_t)vz.bytes() : 0;
+    p.bias = bias, p.factors = factors, p.ldf = ldf, p.f_bytes = factors ? (uint32_t)vf.bytes() : 0;
     const hipStream_t s = static_cast<hipStream_t>(stream);
     if (!f32 && tile == FBL_GEMM_TILE_AUTO) tile = gated_tile(0, M, 2 * F, K);
-    const hipError_t e = splits > 1 ? run_shared(f32, (int)act, 0, splits, p, static_cast<float*>(ws), s)
-                                    : run_gated_gemm(f32, (int)act, 0, tile, p, s);
+    hipError_t e;
+    if (splits > 1) {
+        float* const planes = static_cast<float*>(ws);
+        e = fbl::launch_shares(f32, 0, splits, p, planes, s);
+        if (e == hipSuccess) e = fbl::launch_gated_finish(f32, (int)act, p, planes, splits, s);
+    } else {
+        e = run_gated_gemm(f32, (int)act, tile, p, s);
+    }
     return e == hipSuccess ? FBL_OK : FBL_ERR_HIP;
 }
 
@@ -134,16 +135,16 @@ fbl_status fbl_gated_bwd_workspace(int32_t dtype, int64_t M, int64_t F, int64_t 
     return st;
 }
 
-fbl_status fbl_gated_bwd(int32_t dtype, uint32_t act, int64_t M, int64_t F, int64_t N, const void* dy, int64_t lddy,
-                         const void* wd, int64_t ldwd, const void* z, int64_t ldz, void* dz, int64_t lddz, void* dbias,
+fbl_status fbl_gated_bwd(int32_t dtype, int64_t M, int64_t F, int64_t N, const void* dy, int64_t lddy, const void* wd,
+                         int64_t ldwd, const void* factors, int64_t ldf, void* dz, int64_t lddz, void* dbias,
                          int32_t tile, void* ws, size_t ws_bytes, void* stream) {
-    fbl_status st = gated_shape(dtype, act, M, N, F);
+    fbl_status st = gated_shape(dtype, FBL_ACT_NONE, M, N, F);
     if (st != FBL_OK) return st;
-    if (!dy || !wd || !z || !dz) return FBL_ERR_NULL;
+    if (!dy || !wd || !factors || !dz) return FBL_ERR_NULL;
     const int es = (int)fbl::dtype_size(dtype), f32 = es == 4;
-    const RowsView vdy{dy, M, N, lddy, es}, vwd{wd, F, N, ldwd, es}, vz{z, M, 2 * F, ldz, es}, vdz{dz, M, 2 * F, lddz, es},
+    const RowsView vdy{dy, M, N, lddy, es}, vwd{wd, F, N, ldwd, es}, vf{factors, M, 2 * F, ldf, es}, vdz{dz, M, 2 * F, lddz, es},
         vdb{dbias, 1, 2 * F, 2 * F, es};
-    for (const RowsView* v : {&vdy, &vwd, &vz, &vdz})
+    for (const RowsView* v : {&vdy, &vwd, &vf, &vdz})
         if ((st = fbl::check_operand(*v)) != FBL_OK) return st;
     if (!vdb.natural()) return FBL_ERR_ALIGN;
     if (es == 2 && (N % 8 || F % 8)) return FBL_ERR_UNSUPPORTED;
@@ -157,7 +158,7 @@ fbl_status fbl_gated_bwd(int32_t dtype, uint32_t act, int64_t M, int64_t F, int6
     if (vws.begin() % 16) return FBL_ERR_ALIGN;
     const RowsView* outs[] = {&vdz, &vdb, &vws};
     for (int i = 0; i < 3; ++i) {
-        for (const RowsView* in : {&vdy, &vwd, &vz})
+        for (const RowsView* in : {&vdy, &vwd, &vf})
             if (overlap(*outs[i], *in)) return FBL_ERR_ARG;
         for (int j = 0; j < i; ++j)
             if (overlap(*outs[i], *outs[j])) return FBL_ERR_ARG;
@@ -166,12 +167,18 @@ fbl_status fbl_gated_bwd(int32_t dtype, uint32_t act, int64_t M, int64_t F, int6
     fbl::GatedArgs p{};
     fbl::product(p, FBL_PROJ_BWD_DATA, vdy, vwd, vdh, M, F, N);
     p.c_bytes = (uint32_t)vdz.bytes();
-    p.z = const_cast<void*>(z), p.ldz = ldz, p.z_bytes = fbl::load_span(vz);
+    p.factors = const_cast<void*>(factors), p.ldf = ldf, p.f_bytes = fbl::load_span(vf);
     if (dbias) p.sums = reinterpret_cast<float*>(static_cast<char*>(ws) + gw.sums);
     if (!f32 && tile == FBL_GEMM_TILE_AUTO) tile = gated_tile(1, M, F, N);
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    hipError_t e = shared ? run_shared(f32, (int)act, 1, gw.splits, p, static_cast<float*>(ws), s)
-                          : run_gated_gemm(f32, (int)act, 1, tile, p, s);
+    hipError_t e;
+    if (shared) {
+        float* const planes = static_cast<float*>(ws);
+        e = fbl::launch_shares(f32, 1, gw.splits, p, planes, s);
+        if (e == hipSuccess) e = fbl::launch_gated_grad_finish(f32, p, planes, gw.splits, s);
+    } else {
+        e = fbl::launch_gated_grad(f32, tile, p, s);
+    }
     if (e == hipSuccess && dbias) {
         const int64_t groups = shared ? M : fbl::linear_grad_groups(f32, tile, p);
         e = fbl::launch_column_sums(f32, p.sums, (int)groups, 1, (int)(2 * F), dbias, nullptr, s);

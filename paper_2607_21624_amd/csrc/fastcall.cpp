@@ -837,14 +837,14 @@ PyObject* qk_norm_rotary_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
-// gated_fwd(x, w, bias, act, out, z, tile, workspace, stream)
+// gated_fwd(x, w, bias, act, out, factors, tile, workspace, stream)
 PyObject* gated_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     HANDLE_TH_ERRORS
     if (n != 9) Py_RETURN_NONE;
     Args g{a};
     const Tensor *x = g.tensor(0), *w = g.tensor(1), *b = g.tensor_or_none(2);
     const uint32_t act = g.act(3);
-    const Tensor *out = g.tensor_or_none(4), *z = g.tensor_or_none(5);
+    const Tensor *out = g.tensor_or_none(4), *f = g.tensor_or_none(5);
     const int64_t tile = g.integer(6);
     const Tensor* ws = g.tensor_or_none(7);
     g.no_stream(8);
@@ -852,7 +852,7 @@ PyObject* gated_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int64_t M = x->size(0), K = x->size(1), F = w->size(1) / 2;
     const at::ScalarType dt = x->scalar_type();
     const int code = dtype_code(*x);
-    if (!matrix(x, M, K, dt) || !matrix(w, K, 2 * F, dt) || !vector(b, 2 * F, dt) || !matrix(out, M, F, dt) || !matrix(z, M, 2 * F, dt))
+    if (!matrix(x, M, K, dt) || !matrix(w, K, 2 * F, dt) || !vector(b, 2 * F, dt) || !matrix(out, M, F, dt) || !matrix(f, M, 2 * F, dt))
         Py_RETURN_NONE;
     Tensor mo;
     if (!out) mo = empty({M, F}, dt, *x), out = &mo;
@@ -860,33 +860,32 @@ PyObject* gated_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     size_t need = 0;
     if (!ws && tile == FBL_GEMM_TILE_AUTO && M <= 128 && fbl_gated_fwd_workspace(code, M, K, F, &need) != FBL_OK) Py_RETURN_NONE;
     if (!sc.set(ws, need, *x)) Py_RETURN_NONE;
-    void *s = g.stream(), *px = data(x), *pw = data(w), *pb = data(b), *po = data(out), *pz = data(z);
-    const int64_t ldx = row_stride(x), ldw = row_stride(w), ldo = row_stride(out), ldz = row_stride(z);
+    void *s = g.stream(), *px = data(x), *pw = data(w), *pb = data(b), *po = data(out), *pf = data(f);
+    const int64_t ldx = row_stride(x), ldw = row_stride(w), ldo = row_stride(out), ldf = row_stride(f);
     const fbl_status st = unlocked([&] {
-        return fbl_gated_fwd(code, act, M, K, F, px, ldx, pw, ldw, pb, po, ldo, pz, ldz, (int32_t)tile, sc.p, sc.bytes, s);
+        return fbl_gated_fwd(code, act, M, K, F, px, ldx, pw, ldw, pb, po, ldo, pf, ldf, (int32_t)tile, sc.p, sc.bytes, s);
     });
     if (st != FBL_OK) Py_RETURN_NONE;
     return object_of(a[4], mo);
     END_HANDLE_TH_ERRORS
 }
 
-// gated_bwd(dy, w_down, z, act, dz, dbias, tile, workspace, stream, need_bias)
+// gated_bwd(dy, w_down, factors, dz, dbias, tile, workspace, stream, need_bias)
 PyObject* gated_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     HANDLE_TH_ERRORS
-    if (n != 10) Py_RETURN_NONE;
+    if (n != 9) Py_RETURN_NONE;
     Args g{a};
-    const Tensor *dy = g.tensor(0), *wd = g.tensor(1), *z = g.tensor(2);
-    const uint32_t act = g.act(3);
-    const Tensor *dz = g.tensor_or_none(4), *db = g.tensor_or_none(5);
-    const int64_t tile = g.integer(6);
-    const Tensor* ws = g.tensor_or_none(7);
-    g.no_stream(8);
-    const bool need_b = g.flag(9);
+    const Tensor *dy = g.tensor(0), *wd = g.tensor(1), *f = g.tensor(2);
+    const Tensor *dz = g.tensor_or_none(3), *db = g.tensor_or_none(4);
+    const int64_t tile = g.integer(5);
+    const Tensor* ws = g.tensor_or_none(6);
+    g.no_stream(7);
+    const bool need_b = g.flag(8);
     if (!g.ready() || dy->dim() != 2 || wd->dim() != 2 || dtype_code(*dy) < 0) Py_RETURN_NONE;
     const int64_t M = dy->size(0), N = dy->size(1), F = wd->size(0);
     const at::ScalarType dt = dy->scalar_type();
     const int code = dtype_code(*dy);
-    if (!matrix(dy, M, N, dt) || !matrix(wd, F, N, dt) || !matrix(z, M, 2 * F, dt) || !matrix(dz, M, 2 * F, dt) || !vector(db, 2 * F, dt))
+    if (!matrix(dy, M, N, dt) || !matrix(wd, F, N, dt) || !matrix(f, M, 2 * F, dt) || !matrix(dz, M, 2 * F, dt) || !vector(db, 2 * F, dt))
         Py_RETURN_NONE;
     Tensor mz, mb;
     if (!dz) mz = empty({M, 2 * F}, dt, *dy), dz = &mz;
@@ -897,13 +896,13 @@ PyObject* gated_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
         if (!ws && fbl_gated_bwd_workspace(code, M, F, N, &need) != FBL_OK) Py_RETURN_NONE;
         if (!sc.set(ws, need, *dy)) Py_RETURN_NONE;
     }
-    void *s = g.stream(), *py = data(dy), *pwd = data(wd), *pz = data(z), *pdz = data(dz), *pdb = data(db);
-    const int64_t ldy = row_stride(dy), ldwd = row_stride(wd), ldz = row_stride(z), lddz = row_stride(dz);
+    void *s = g.stream(), *py = data(dy), *pwd = data(wd), *pf = data(f), *pdz = data(dz), *pdb = data(db);
+    const int64_t ldy = row_stride(dy), ldwd = row_stride(wd), ldf = row_stride(f), lddz = row_stride(dz);
     const fbl_status st = unlocked([&] {
-        return fbl_gated_bwd(code, act, M, F, N, py, ldy, pwd, ldwd, pz, ldz, pdz, lddz, pdb, (int32_t)tile, sc.p, sc.bytes, s);
+        return fbl_gated_bwd(code, M, F, N, py, ldy, pwd, ldwd, pf, ldf, pdz, lddz, pdb, (int32_t)tile, sc.p, sc.bytes, s);
     });
     if (st != FBL_OK) Py_RETURN_NONE;
-    return tuple_of<2>({object_of(a[4], mz), object_or_none(a[5], mb)});
+    return tuple_of<2>({object_of(a[3], mz), object_or_none(a[4], mb)});
     END_HANDLE_TH_ERRORS
 }
 

@@ -1,7 +1,7 @@
 // gated_finish.hip -- a gated layer's forward for a few tokens (serving), gfx950: what follows the product
 // whose contraction several workgroups shared.
-//   z = sum over the shares + bias,  h = act(gate) up
-// or, of the data gradient,  dh = sum over the shares,  d gate = dh up act'(gate),  d up = dh act(gate)
+//   (gate, up) = sum over the shares + bias,  h = act(gate) up  and the factors of h's gradient
+// or, of the data gradient,  dh = sum over the shares,  dz = dh times the factors
 //
 // As linear_finish.hip: the fp32 planes, just written and a few MB at most, are added in order, a thread a
 // column of h.
@@ -24,50 +24,64 @@ FBL_DEV float plane_sum(const float* planes, int64_t at, int64_t plane, int spli
     return z;
 }
 
-template <typename T, int ACT, bool GRAD>
+template <typename T, int ACT>
 __global__ __launch_bounds__(256) void gated_finish(GatedArgs p, const float* planes, int splits) {
     constexpr bool FAST = sizeof(T) == 2;
-    const int n = blockIdx.x * 256 + threadIdx.x, F = GRAD ? p.N : p.N / 2;
+    const int n = blockIdx.x * 256 + threadIdx.x, F = p.N / 2;
     const int64_t m = blockIdx.y, plane = (int64_t)p.M * p.N, at = m * p.N + n;
     if (n >= F) return;
-    T* const z = static_cast<T*>(p.z);
+    float gate = plane_sum(planes, at, plane, splits), up = plane_sum(planes, at + F, plane, splits);
+    if (p.bias) gate += (float)static_cast<const T*>(p.bias)[n], up += (float)static_cast<const T*>(p.bias)[F + n];
+    const float a = act<ACT, FAST>(gate);
+    if (p.factors) {
+        T* const f = static_cast<T*>(p.factors) + m * p.ldf + n;
+        f[0] = (T)(up * act_grad<ACT, FAST>(gate));
+        f[F] = (T)a;
+    }
+    static_cast<T*>(p.c)[m * p.ldc + n] = (T)(a * up);
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void gated_grad_finish(GatedArgs p, const float* planes, int splits) {
+    const int n = blockIdx.x * 256 + threadIdx.x, F = p.N;
+    const int64_t m = blockIdx.y, at = m * F + n;
+    if (n >= F) return;
+    const float v = plane_sum(planes, at, (int64_t)p.M * F, splits);
+    const T* const f = static_cast<const T*>(p.factors) + m * p.ldf + n;
+    const float dg = v * (float)f[0], du = v * (float)f[F];
     T* const c = static_cast<T*>(p.c) + m * p.ldc + n;
-    if constexpr (GRAD) {
-        const float v = plane_sum(planes, at, plane, splits), gate = (float)z[m * p.ldz + n], up = (float)z[m * p.ldz + F + n];
-        const float dg = v * up * act_grad<ACT, FAST>(gate), du = v * act<ACT, FAST>(gate);
-        c[0] = (T)dg;
-        c[F] = (T)du;
-        if (p.sums) {  // every row a block of its own
-            p.sums[m * 2 * F + n] = dg;
-            p.sums[m * 2 * F + F + n] = du;
-        }
-    } else {
-        float gate = plane_sum(planes, at, plane, splits), up = plane_sum(planes, at + F, plane, splits);
-        if (p.bias) gate += (float)static_cast<const T*>(p.bias)[n], up += (float)static_cast<const T*>(p.bias)[F + n];
-        if (z) z[m * p.ldz + n] = (T)gate, z[m * p.ldz + F + n] = (T)up;
-        c[0] = (T)(act<ACT, FAST>(gate) * up);
+    c[0] = (T)dg;
+    c[F] = (T)du;
+    if (p.sums) {  // every row a block of its own
+        p.sums[m * 2 * F + n] = dg;
+        p.sums[m * 2 * F + F + n] = du;
     }
 }
 
-template <typename T, bool GRAD>
+template <typename T>
 hipError_t finish(int act, const GatedArgs& p, const float* planes, int splits, hipStream_t s) {
-    const int F = GRAD ? p.N : p.N / 2;
-    const dim3 grid((unsigned)((F + 255) / 256), (unsigned)p.M);
+    const dim3 grid((unsigned)((p.N / 2 + 255) / 256), (unsigned)p.M);
     switch (act) {
-        case kActNone: hipLaunchKernelGGL((gated_finish<T, kActNone, GRAD>), grid, dim3(256), 0, s, p, planes, splits); break;
-        case kActRelu: hipLaunchKernelGGL((gated_finish<T, kActRelu, GRAD>), grid, dim3(256), 0, s, p, planes, splits); break;
-        case kActGelu: hipLaunchKernelGGL((gated_finish<T, kActGelu, GRAD>), grid, dim3(256), 0, s, p, planes, splits); break;
-        case kActGeluTanh: hipLaunchKernelGGL((gated_finish<T, kActGeluTanh, GRAD>), grid, dim3(256), 0, s, p, planes, splits); break;
-        default: hipLaunchKernelGGL((gated_finish<T, kActSilu, GRAD>), grid, dim3(256), 0, s, p, planes, splits); break;
+        case kActNone: hipLaunchKernelGGL((gated_finish<T, kActNone>), grid, dim3(256), 0, s, p, planes, splits); break;
+        case kActRelu: hipLaunchKernelGGL((gated_finish<T, kActRelu>), grid, dim3(256), 0, s, p, planes, splits); break;
+        case kActGelu: hipLaunchKernelGGL((gated_finish<T, kActGelu>), grid, dim3(256), 0, s, p, planes, splits); break;
+        case kActGeluTanh: hipLaunchKernelGGL((gated_finish<T, kActGeluTanh>), grid, dim3(256), 0, s, p, planes, splits); break;
+        default: hipLaunchKernelGGL((gated_finish<T, kActSilu>), grid, dim3(256), 0, s, p, planes, splits); break;
     }
     return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_gated_finish(int f32, int act, int grad, const GatedArgs& p, const float* planes, int splits, hipStream_t s) {
-    if (grad) return f32 ? finish<float, true>(act, p, planes, splits, s) : finish<bf16, true>(act, p, planes, splits, s);
-    return f32 ? finish<float, false>(act, p, planes, splits, s) : finish<bf16, false>(act, p, planes, splits, s);
+hipError_t launch_gated_finish(int f32, int act, const GatedArgs& p, const float* planes, int splits, hipStream_t s) {
+    return f32 ? finish<float>(act, p, planes, splits, s) : finish<bf16>(act, p, planes, splits, s);
+}
+
+hipError_t launch_gated_grad_finish(int f32, const GatedArgs& p, const float* planes, int splits, hipStream_t s) {
+    const dim3 grid((unsigned)((p.N + 255) / 256), (unsigned)p.M);
+    if (f32) hipLaunchKernelGGL(gated_grad_finish<float>, grid, dim3(256), 0, s, p, planes, splits);
+    else hipLaunchKernelGGL(gated_grad_finish<bf16>, grid, dim3(256), 0, s, p, planes, splits);
+    return hipGetLastError();
 }
 
 }  // namespace fbl

@@ -126,15 +126,16 @@ int64_t linear_grad_groups(int f32, int tile, const GemmArgs& p);
 // (linear_finish.hip); p.sums: M rows.
 hipError_t launch_linear_finish(int f32, int act, int grad, const LinearArgs& p, const float* planes, int splits,
                                 hipStream_t stream);
-// The gated layer's products (gated_gemm.hpp): the forward, or with `grad` the data gradient.
+// The gated layer's products: the forward (gated_gemm.hpp) and the data gradient (gated_grad.hip).
 template <int ACT>
-hipError_t launch_gated_gemm(int grad, int tile, const GatedArgs& p, hipStream_t stream);
+hipError_t launch_gated_gemm(int tile, const GatedArgs& p, hipStream_t stream);
 template <int ACT>
-hipError_t launch_gated_gemm_f32(int grad, const GatedArgs& p, hipStream_t stream);
+hipError_t launch_gated_gemm_f32(const GatedArgs& p, hipStream_t stream);
+hipError_t launch_gated_grad(int f32, int tile, const GatedArgs& p, hipStream_t stream);
 // The same from a product's planes [splits][M][2F], or of the data gradient [splits][M][F] (gated_finish.hip); p.sums: M
 // rows.
-hipError_t launch_gated_finish(int f32, int act, int grad, const GatedArgs& p, const float* planes, int splits,
-                               hipStream_t stream);
+hipError_t launch_gated_finish(int f32, int act, const GatedArgs& p, const float* planes, int splits, hipStream_t stream);
+hipError_t launch_gated_grad_finish(int f32, const GatedArgs& p, const float* planes, int splits, hipStream_t stream);
 hipError_t launch_linear_act_bwd(int f32, int act, const LinearActArgs& a, hipStream_t stream);
 
 // Sums of squares of a list's tensors, one for each workgroup; the norm from n of them; out = g min(1, limit / (norm +

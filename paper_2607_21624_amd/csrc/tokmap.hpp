@@ -145,14 +145,14 @@ struct LinearArgs : GemmArgs {
     float* sums;  // data gradient: [groups][N] sums of c down blocks of rows (linear_grad_groups), or nullptr
 };
 
-// A gated layer's product with its epilogue (gated_gemm.hpp); z [M][2F], gate columns, then up columns.
-// Forward: N is 2F, C is h = act(gate) up of z = A B + bias, z stored where given.  Data gradient: N is F, the product is
-// the gradient of h, C [M][2F] that of the given z.
+// A gated layer's products with their epilogues.  Forward (gated_gemm.hpp): N is 2F, C is h = act(gate) up of (gate, up) = A B
+// + bias, and the factors [M][2F] (up act'(gate), act(gate)) are stored where given.  Data gradient (gated_grad.hip): N is
+// F, the product is the gradient of h, C [M][2F] its products with the given factors.
 struct GatedArgs : GemmArgs {
     const void* bias;
-    void* z;
-    int64_t ldz;
-    uint32_t z_bytes;
+    void* factors;
+    int64_t ldf;
+    uint32_t f_bytes;
     float* sums;  // data gradient: [groups][2F] sums of C down blocks of rows (linear_grad_groups), or nullptr
 };
 

@@ -256,7 +256,7 @@ def _load() -> ctypes.CDLL:
     lib.fbl_gated_fwd_workspace.restype = ctypes.c_int
     lib.fbl_gated_bwd_workspace.argtypes = [i32, i64, i64, i64, sizep]
     lib.fbl_gated_bwd_workspace.restype = ctypes.c_int
-    lib.fbl_gated_bwd.argtypes = [i32, u32, i64, i64, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, i32, vp, size, vp]
+    lib.fbl_gated_bwd.argtypes = [i32, i64, i64, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, i32, vp, size, vp]
     lib.fbl_gated_bwd.restype = ctypes.c_int
     lib.fbl_grad_norm_workspace.argtypes = [i64, sizep]
     lib.fbl_grad_norm_workspace.restype = ctypes.c_int
@@ -1141,18 +1141,18 @@ def gated_fwd_workspace(x, w) -> int:
     return int(n.value)
 
 
-def gated_fwd(x, w, bias=None, act: str = "silu", out=None, z=None, tile: int = FBL_GEMM_TILE_AUTO, workspace=None,
+def gated_fwd(x, w, bias=None, act: str = "silu", out=None, factors=None, tile: int = FBL_GEMM_TILE_AUTO, workspace=None,
               stream=None):
     """h = act(gate) * up with (gate, up) = x w + bias for x [M, K], w [K, 2F] and bias [2F], gate then up columns (any row
-    strides, one storage type), act one of ACTIVATIONS.  z [M, 2F], where given, receives the pre-activations,
-    which gated_bwd needs.  workspace: gated_fwd_workspace bytes, allocated where they are needed and it is None.
-    Returns h [M, F]."""
-    done = _FAST.gated_fwd(x, w, bias, act, out, z, tile, workspace, stream)
+    strides, one storage type), act one of ACTIVATIONS.  factors [M, 2F], where given, receives h's derivatives by gate
+    and by up, which gated_bwd needs.  workspace: gated_fwd_workspace bytes, allocated where they are needed and it is
+    None.  Returns h [M, F]."""
+    done = _FAST.gated_fwd(x, w, bias, act, out, factors, tile, workspace, stream)
     if done is not None:
         return done
     import torch
     where = "gated_fwd"
-    _check_device(where, stream, x=x, w=w, bias=bias, out=out, z=z, workspace=workspace)
+    _check_device(where, stream, x=x, w=w, bias=bias, out=out, factors=factors, workspace=workspace)
     ldx = _matrix(x, where, "x")
     M, K = x.shape
     dt, code = _dtype_code(x), _act_code(act, where)
@@ -1161,7 +1161,7 @@ def gated_fwd(x, w, bias=None, act: str = "silu", out=None, z=None, tile: int = 
     if w.shape[0] != K:
         raise FblError(FBL_ERR_SHAPE, f"{where}: x {tuple(x.shape)} and w {tuple(w.shape)} do not agree")
     _vector(bias, where, "bias", 2 * F, x.dtype)
-    ldz = 0 if z is None else _matrix(z, where, "z", (M, 2 * F), x)
+    ldf = 0 if factors is None else _matrix(factors, where, "factors", (M, 2 * F), x)
     if out is None:
         out = _empty((M, F), x.dtype, x, stream)
     ldh = _matrix(out, where, "out", (M, F), x)
@@ -1169,8 +1169,8 @@ def gated_fwd(x, w, bias=None, act: str = "silu", out=None, z=None, tile: int = 
     need = gated_fwd_workspace(x, w) if workspace is None and M <= 128 and tile == FBL_GEMM_TILE_AUTO else 0
     if workspace is not None or need:
         ws, ws_bytes = _scratch(workspace, need, where, x, stream)
-    _call("fbl_gated_fwd", x, stream, dt, code, M, K, F, _ptr(x), ldx, _ptr(w), ldw, _ptr(bias), _ptr(out), ldh, _ptr(z),
-          ldz, tile, _ptr(ws), ws_bytes)
+    _call("fbl_gated_fwd", x, stream, dt, code, M, K, F, _ptr(x), ldx, _ptr(w), ldw, _ptr(bias), _ptr(out), ldh,
+          _ptr(factors), ldf, tile, _ptr(ws), ws_bytes)
     return out
 
 
@@ -1182,25 +1182,25 @@ def gated_bwd_workspace(dy, w_down) -> int:
     return int(n.value)
 
 
-def gated_bwd(dy, w_down, z, act: str = "silu", dz=None, dbias=None, tile: int = FBL_GEMM_TILE_AUTO, workspace=None,
-              stream=None, need_bias: bool = True):
+def gated_bwd(dy, w_down, factors, dz=None, dbias=None, tile: int = FBL_GEMM_TILE_AUTO, workspace=None, stream=None,
+              need_bias: bool = True):
     """Gradient of a gated layer's pre-activations from that of the block's result: dy [M, N], w_down [F, N] and the
-    forward's z [M, 2F] give dz [M, 2F] and the sums of dz over its rows, dbias [2F].  Returns (dz, dbias), dbias None
-    where not needed.  dx and dw are linear_bwd's of dz."""
-    done = _FAST.gated_bwd(dy, w_down, z, act, dz, dbias, tile, workspace, stream, need_bias)
+    forward's factors [M, 2F] give dz [M, 2F] and the sums of dz over its rows, dbias [2F].  Returns (dz, dbias), dbias
+    None where not needed.  dx and dw are linear_bwd's of dz."""
+    done = _FAST.gated_bwd(dy, w_down, factors, dz, dbias, tile, workspace, stream, need_bias)
     if done is not None:
         return done
     import torch
     where = "gated_bwd"
-    _check_device(where, stream, dy=dy, w_down=w_down, z=z, dz=dz, dbias=dbias, workspace=workspace)
+    _check_device(where, stream, dy=dy, w_down=w_down, factors=factors, dz=dz, dbias=dbias, workspace=workspace)
     lddy = _matrix(dy, where, "dy")
     M, N = dy.shape
-    dt, code = _dtype_code(dy), _act_code(act, where)
+    dt = _dtype_code(dy)
     ldwd = _matrix(w_down, where, "w_down", None, dy)
     F = w_down.shape[0]
     if w_down.shape[1] != N:
         raise FblError(FBL_ERR_SHAPE, f"{where}: dy {tuple(dy.shape)} and w_down {tuple(w_down.shape)} do not agree")
-    ldz = _matrix(z, where, "z", (M, 2 * F), dy)
+    ldf = _matrix(factors, where, "factors", (M, 2 * F), dy)
     if dz is None:
         dz = _empty((M, 2 * F), dy.dtype, dy, stream)
     lddz = _matrix(dz, where, "dz", (M, 2 * F), dy)
@@ -1211,7 +1211,7 @@ def gated_bwd(dy, w_down, z, act: str = "silu", dz=None, dbias=None, tile: int =
     if dbias is not None or workspace is not None or M <= 128:
         need = 0 if workspace is not None else gated_bwd_workspace(dy, w_down)
         ws, ws_bytes = _scratch(workspace, need, where, dy, stream)
-    _call("fbl_gated_bwd", dy, stream, dt, code, M, F, N, _ptr(dy), lddy, _ptr(w_down), ldwd, _ptr(z), ldz, _ptr(dz), lddz,
+    _call("fbl_gated_bwd", dy, stream, dt, M, F, N, _ptr(dy), lddy, _ptr(w_down), ldwd, _ptr(factors), ldf, _ptr(dz), lddz,
           _ptr(dbias), tile, _ptr(ws), ws_bytes)
     return dz, dbias
 

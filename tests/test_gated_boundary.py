@@ -25,29 +25,29 @@ def _call(f, base, kw):
 
 def fwd(**kw):
     return _call(LIB.fbl_gated_fwd, dict(dt=BF16, act=F.FBL_ACT_SILU, M=4, K=64, F=32, x=at(1), ldx=64, w=at(2), ldw=64,
-                                         b=at(3), h=at(4), ldh=32, z=at(5), ldz=64, tile=-1, ws=None, ws_bytes=0, stream=None), kw)
+                                         b=at(3), h=at(4), ldh=32, f=at(5), ldf=64, tile=-1, ws=None, ws_bytes=0, stream=None), kw)
 
 
 def bwd(**kw):
-    return _call(LIB.fbl_gated_bwd, dict(dt=BF16, act=F.FBL_ACT_SILU, M=4, F=32, N=64, dy=at(1), lddy=64, wd=at(2), ldwd=64,
-                                         z=at(3), ldz=64, dz=at(4), lddz=64, db=at(5), tile=-1, ws=at(6), ws_bytes=1 << 20,
+    return _call(LIB.fbl_gated_bwd, dict(dt=BF16, M=4, F=32, N=64, dy=at(1), lddy=64, wd=at(2), ldwd=64,
+                                         f=at(3), ldf=64, dz=at(4), lddz=64, db=at(5), tile=-1, ws=at(6), ws_bytes=1 << 20,
                                          stream=None), kw)
 
 
-COMMON = [(dict(dt=2), F.FBL_ERR_DTYPE), (dict(act=5), F.FBL_ERR_ARG), (dict(M=0), F.FBL_ERR_SHAPE), (dict(M=-1), F.FBL_ERR_SHAPE),
+COMMON = [(dict(dt=2), F.FBL_ERR_DTYPE), (dict(M=0), F.FBL_ERR_SHAPE), (dict(M=-1), F.FBL_ERR_SHAPE),
           (dict(F=0), F.FBL_ERR_SHAPE), (dict(tile=21), F.FBL_ERR_ARG), (dict(tile=-2), F.FBL_ERR_ARG)]
 
 
 @pytest.mark.parametrize("kw,status", COMMON + [
-    (dict(K=0), F.FBL_ERR_SHAPE), (dict(K=(1 << 26) + 8, ldx=(1 << 26) + 8), F.FBL_ERR_UNSUPPORTED),
-    (dict(F=(1 << 25) + 8, ldw=(1 << 26) + 16, ldh=(1 << 25) + 8, ldz=(1 << 26) + 16, M=1), F.FBL_ERR_UNSUPPORTED),
-    (dict(M=1 << 24), F.FBL_ERR_UNSUPPORTED),  # z of 2 GiB
+    (dict(act=5), F.FBL_ERR_ARG), (dict(K=0), F.FBL_ERR_SHAPE), (dict(K=(1 << 26) + 8, ldx=(1 << 26) + 8), F.FBL_ERR_UNSUPPORTED),
+    (dict(F=(1 << 25) + 8, ldw=(1 << 26) + 16, ldh=(1 << 25) + 8, ldf=(1 << 26) + 16, M=1), F.FBL_ERR_UNSUPPORTED),
+    (dict(M=1 << 24), F.FBL_ERR_UNSUPPORTED),  # factors of 2 GiB
     (dict(x=None), F.FBL_ERR_NULL), (dict(w=None), F.FBL_ERR_NULL), (dict(h=None), F.FBL_ERR_NULL),
     (dict(ldx=56), F.FBL_ERR_LAYOUT), (dict(ldw=56), F.FBL_ERR_LAYOUT), (dict(ldh=24), F.FBL_ERR_LAYOUT),
-    (dict(ldz=56), F.FBL_ERR_LAYOUT), (dict(ldw=68), F.FBL_ERR_ALIGN), (dict(x=at(1, 8)), F.FBL_ERR_ALIGN),
+    (dict(ldf=56), F.FBL_ERR_LAYOUT), (dict(ldw=68), F.FBL_ERR_ALIGN), (dict(x=at(1, 8)), F.FBL_ERR_ALIGN),
     (dict(b=at(3, 8)), F.FBL_ERR_ALIGN), (dict(K=60), F.FBL_ERR_UNSUPPORTED), (dict(F=28), F.FBL_ERR_UNSUPPORTED),
-    (dict(h=at(1)), F.FBL_ERR_ARG), (dict(h=at(2)), F.FBL_ERR_ARG), (dict(h=at(3)), F.FBL_ERR_ARG), (dict(z=at(4)), F.FBL_ERR_ARG),
-    (dict(z=at(1)), F.FBL_ERR_ARG), (dict(dt=F32, tile=0), F.FBL_ERR_ARG), (dict(dt=F32, x=at(1, 2)), F.FBL_ERR_ALIGN),
+    (dict(h=at(1)), F.FBL_ERR_ARG), (dict(h=at(2)), F.FBL_ERR_ARG), (dict(h=at(3)), F.FBL_ERR_ARG), (dict(f=at(4)), F.FBL_ERR_ARG),
+    (dict(f=at(1)), F.FBL_ERR_ARG), (dict(dt=F32, tile=0), F.FBL_ERR_ARG), (dict(dt=F32, x=at(1, 2)), F.FBL_ERR_ALIGN),
     # a contraction that is shared
     (dict(K=4096, ldx=4096, ws=at(9), ws_bytes=1023), F.FBL_ERR_WORKSPACE),
     (dict(K=4096, ldx=4096, ws=at(9, 8), ws_bytes=1 << 30), F.FBL_ERR_ALIGN),
@@ -58,9 +58,9 @@ def test_forward_refusals(kw, status):
 
 
 @pytest.mark.parametrize("kw,status", COMMON + [
-    (dict(N=0), F.FBL_ERR_SHAPE), (dict(dy=None), F.FBL_ERR_NULL), (dict(wd=None), F.FBL_ERR_NULL), (dict(z=None), F.FBL_ERR_NULL),
+    (dict(N=0), F.FBL_ERR_SHAPE), (dict(dy=None), F.FBL_ERR_NULL), (dict(wd=None), F.FBL_ERR_NULL), (dict(f=None), F.FBL_ERR_NULL),
     (dict(dz=None), F.FBL_ERR_NULL), (dict(lddy=56), F.FBL_ERR_LAYOUT), (dict(ldwd=32), F.FBL_ERR_LAYOUT),
-    (dict(ldz=32), F.FBL_ERR_LAYOUT), (dict(lddz=56), F.FBL_ERR_LAYOUT), (dict(dz=at(4, 2)), F.FBL_ERR_ALIGN),
+    (dict(ldf=32), F.FBL_ERR_LAYOUT), (dict(lddz=56), F.FBL_ERR_LAYOUT), (dict(dz=at(4, 2)), F.FBL_ERR_ALIGN),
     (dict(db=at(5, 1)), F.FBL_ERR_ALIGN), (dict(N=60), F.FBL_ERR_UNSUPPORTED), (dict(F=28), F.FBL_ERR_UNSUPPORTED),
     (dict(M=1 << 24), F.FBL_ERR_UNSUPPORTED), (dict(ws=None), F.FBL_ERR_WORKSPACE), (dict(ws_bytes=512), F.FBL_ERR_WORKSPACE),
     (dict(ws=at(6, 8)), F.FBL_ERR_ALIGN), (dict(dz=at(3)), F.FBL_ERR_ARG), (dict(dz=at(1)), F.FBL_ERR_ARG),

@@ -41,11 +41,11 @@ def test_gated(monkeypatch, dt):
     note(f"native gated {dt}")
     for M in (1, 50, 300):
         x, w, b, wd, dy = g(M, 264), g(264, 144), g(144), g(72, 136), g(M, 136)
-        z = torch.empty(M, 144, dtype=dt, device="cuda")
+        f = torch.empty(M, 144, dtype=dt, device="cuda")
         for act in pkg.ACTIVATIONS:
-            _both(monkeypatch, lambda: pkg.gated_fwd(x, w, b, act, z=z))
-            _both(monkeypatch, lambda: pkg.gated_bwd(dy, wd, z, act))
-            _both(monkeypatch, lambda: pkg.gated_bwd(dy, wd, z, act, need_bias=False))
+            _both(monkeypatch, lambda: pkg.gated_fwd(x, w, b, act, factors=f))
+            _both(monkeypatch, lambda: pkg.gated_bwd(dy, wd, f))
+            _both(monkeypatch, lambda: pkg.gated_bwd(dy, wd, f, need_bias=False, dz=torch.empty_like(f)))
         _both(monkeypatch, lambda: pkg.gated_fwd(x, w, out=torch.empty(M, 72, dtype=dt, device="cuda")))
     _both(monkeypatch, lambda: pkg.gated_fwd(g(4, 4096, scale=0) + 1, g(4096, 144, scale=0) + 1))  # shared contraction
 
@@ -88,8 +88,8 @@ def test_other_calls_go_the_general_way():
     assert fast.gated_fwd(x, w1, None, "swish", None, None, -1, None, None) is None
     assert fast.gated_fwd(x, _t(64, 31), None, "silu", None, None, -1, None, None) is None
     assert fast.gated_fwd(x, w1, None, "silu", None, None, -1, None, side) is None
-    assert fast.gated_bwd(x, _t(16, 64), _t(4, 30), "silu", None, None, -1, None, None, False) is None
-    assert fast.gated_bwd(x, _t(16, 64), _t(4, 32), "silu", None, None, -1, None, None, False) is not None
+    assert fast.gated_bwd(x, _t(16, 64), _t(4, 30), None, None, -1, None, None, False) is None
+    assert fast.gated_bwd(x, _t(16, 64), _t(4, 32), None, None, -1, None, None, False) is not None
     g = [_t(4, 6), _t(3)]
     for a in (g + [None], [], [g[0], g[0]], [g[0][:, :3]], [g[0].half()], iter(g), [g[0].cpu()]):
         assert fast.clip_grad_norm(a, 1.0, None, None, None, None) is None

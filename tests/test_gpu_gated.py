@@ -2,8 +2,9 @@
 
 Bounds, element by element, as in test_gpu_linear.py: a product's sum of K terms in fp32 is off by at most (K + 16)
 2^-24 of the sum of magnitudes, activations by 2^-20 of their argument, their derivatives by 2^-20 (1 + |argument|), and |act'|
-<= 1.2.  h = act(gate) up is made from the unrounded z and rounded once.  The backward reads a z that is given, so that
-the oracle has the same."""
+<= 1.2, |act''| <= 1 (relu's is a step: a gate within its bound of 0 may fall on either side).  h = act(gate) up and the factors
+are made from unrounded sums and rounded once each.  The backward reads factors that are given, so that the oracle has the
+same."""
 import numpy as np
 import pytest
 import torch
@@ -24,46 +25,48 @@ def _sum_bound(a, b):
 def _inputs(M, K, F, N, dt, bias, seed=0):
     rng = np.random.default_rng(seed + M * 7 + K * 3 + F)
     note(f"gated {M}x{K}x{F} -> {N} {dt} bias={bias}")
-    x, w, wd, z, dy = (rounded(rng, s, dt, k) for s, k in (((M, K), 1.0), ((K, 2 * F), K ** -0.5), ((F, N), N ** -0.5),
+    x, w, wd, f, dy = (rounded(rng, s, dt, k) for s, k in (((M, K), 1.0), ((K, 2 * F), K ** -0.5), ((F, N), N ** -0.5),
                                                            ((M, 2 * F), 1.5), ((M, N), 1.0)))
     b = rounded(rng, (2 * F,), dt, 0.5) if bias else (None, None)
-    return x, w, b, wd, z, dy
+    return x, w, b, wd, f, dy
 
 
-def _check_fwd(h, z, x, w, b, act):
+def _check_fwd(h, f, x, w, b, act):
     hr, zr = oracle.gated_fwd(x, w, b, act)
     F = hr.shape[1]
     zb = _sum_bound(x, w) + 2.0 ** -23 * (np.abs(zr) + (0 if b is None else np.abs(b)))
-    if z is not None:
-        check("z", z, zr, zb)
     gate, up = zr[:, :F], zr[:, F:]
     gb = 1.2 * zb[:, :F] + 2.0 ** -20 * np.abs(gate)  # of act(gate)
+    if f is not None:
+        slope = np.abs(act_grad(gate, act))
+        sb = zb[:, :F] + 2.0 ** -20 * (1 + np.abs(gate))
+        if act == "relu":
+            sb = np.where(np.abs(gate) <= zb[:, :F], 1.0, 0.0)
+        fr = oracle.gated_factors(zr, act)
+        check("factors", f, fr, np.concatenate([zb[:, F:] * (slope + sb) + np.abs(up) * sb, gb], axis=1) + 2.0 ** -23 * np.abs(fr))
     check("h", h, hr, gb * np.abs(up) + (np.abs(act_of(gate, act)) + gb) * zb[:, F:] + 2.0 ** -23 * np.abs(hr))
 
 
-def _check_bwd(dz, db, dy, wd, z, act):
+def _check_bwd(dz, db, dy, wd, f):
     dh = dy @ wd.T
-    ref = oracle.gated_bwd(dh, z, act)
-    F = dh.shape[1]
-    gate, up = z[:, :F], z[:, F:]
-    dhb, slope, a = _sum_bound(dy, wd.T), np.abs(act_grad(gate, act)), np.abs(act_of(gate, act))
-    bound = np.concatenate([dhb * np.abs(up) * slope + (np.abs(dh) + dhb) * np.abs(up) * 2.0 ** -20 * (1 + np.abs(gate)),
-                            dhb * a + (np.abs(dh) + dhb) * 2.0 ** -20 * np.abs(gate)], axis=1) + 2.0 ** -22 * np.abs(ref)
+    ref = oracle.gated_bwd(dh, f)
+    dhb = _sum_bound(dy, wd.T)
+    bound = np.concatenate([dhb, dhb], axis=1) * np.abs(f) + 2.0 ** -23 * np.abs(ref)
     check("dz", dz, ref, bound)
     if db is not None:
         check("dbias", db, ref.sum(0), (len(dy) + 16) * 2.0 ** -24 * (np.abs(ref) + bound).sum(0) + bound.sum(0))
 
 
 def _run(M, K, F, N, dt, act, bias=True, tile=-1):
-    (x, xr), (w, wr), (b, br), (wd, wdr), (z, zr), (dy, dyr) = _inputs(M, K, F, N, dt, bias)
-    zo = torch.full((M, 2 * F), float("nan"), dtype=dt, device="cuda")
-    h = fbl.gated_fwd(x, w, b, act, z=zo, tile=tile)
+    (x, xr), (w, wr), (b, br), (wd, wdr), (f, fr), (dy, dyr) = _inputs(M, K, F, N, dt, bias)
+    fo = torch.full((M, 2 * F), float("nan"), dtype=dt, device="cuda")
+    h = fbl.gated_fwd(x, w, b, act, factors=fo, tile=tile)
     only = fbl.gated_fwd(x, w, b, act, tile=tile)
-    dz, db = fbl.gated_bwd(dy, wd, z, act, need_bias=bias, tile=tile)
+    dz, db = fbl.gated_bwd(dy, wd, f, need_bias=bias, tile=tile)
     torch.cuda.synchronize()
-    _check_fwd(h, zo, xr, wr, br, act)
+    _check_fwd(h, fo, xr, wr, br, act)
     assert torch.equal(h, only)
-    _check_bwd(dz, db, dyr, wdr, zr, act)
+    _check_bwd(dz, db, dyr, wdr, fr)
     assert (db is None) == (not bias)
 
 
@@ -90,17 +93,17 @@ def test_without_bias(dt):
 def test_every_tile(tile):
     """Ragged against every tile: partial last steps, rows and columns; nothing written between the rows."""
     M, K, F, N = 301, 360, 280, 168
-    (x, xr), (w, wr), (b, br), (wd, wdr), (z, zr), (dy, dyr) = _inputs(M, K, F, N, torch.bfloat16, True)
-    x, w, wd, zin, dy = (padded(t, 8)[0] for t in (x, w, wd, z, dy))
+    (x, xr), (w, wr), (b, br), (wd, wdr), (f, fr), (dy, dyr) = _inputs(M, K, F, N, torch.bfloat16, True)
+    x, w, wd, fin, dy = (padded(t, 8)[0] for t in (x, w, wd, f, dy))
     h, hbuf = padded(torch.zeros(M, F, dtype=torch.bfloat16, device="cuda"), 8, 7.0)
-    zo, zbuf = padded(torch.zeros(M, 2 * F, dtype=torch.bfloat16, device="cuda"), 8, 7.0)
+    fo, fbuf = padded(torch.zeros(M, 2 * F, dtype=torch.bfloat16, device="cuda"), 8, 7.0)
     dz, dbuf = padded(torch.zeros(M, 2 * F, dtype=torch.bfloat16, device="cuda"), 8, 7.0)
-    fbl.gated_fwd(x, w, b, "gelu", out=h, z=zo, tile=tile)
-    _, db = fbl.gated_bwd(dy, wd, zin, "gelu", dz=dz, tile=tile)
+    fbl.gated_fwd(x, w, b, "gelu", out=h, factors=fo, tile=tile)
+    _, db = fbl.gated_bwd(dy, wd, fin, dz=dz, tile=tile)
     torch.cuda.synchronize()
-    _check_fwd(h, zo, xr, wr, br, "gelu")
-    _check_bwd(dz, db, dyr, wdr, zr, "gelu")
-    for buf, n in ((hbuf, F), (zbuf, 2 * F), (dbuf, 2 * F)):
+    _check_fwd(h, fo, xr, wr, br, "gelu")
+    _check_bwd(dz, db, dyr, wdr, fr)
+    for buf, n in ((hbuf, F), (fbuf, 2 * F), (dbuf, 2 * F)):
         assert torch.all(buf[:, n:] == 7.0) and torch.all(buf[-1] == 7.0)
 
 
@@ -119,50 +122,50 @@ def test_shared_contractions(dt):
     dt = DTYPES[dt]
     for M, K, F, N in ((1, 4104, 136, 4104), (13, 5000, 64, 5000), (64, 8200, 72, 8200)):
         odd = dt == torch.float32
-        (x, xr), (w, wr), (b, br), (wd, wdr), (z, zr), (dy, dyr) = _inputs(M, K + odd, F + odd, N + odd, dt, True)
+        (x, xr), (w, wr), (b, br), (wd, wdr), (f, fr), (dy, dyr) = _inputs(M, K + odd, F + odd, N + odd, dt, True)
         F = F + odd
-        x, w, wd, z, dy = (padded(t, 8)[0] for t in (x, w, wd, z, dy))
+        x, w, wd, f, dy = (padded(t, 8)[0] for t in (x, w, wd, f, dy))
         new = lambda n: padded(torch.zeros(M, n, dtype=dt, device="cuda"), 8, 7.0)
         need, back = fbl.gated_fwd_workspace(x, w), fbl.gated_bwd_workspace(dy, wd)
         assert need > 0 and need % (M * 2 * F * 4) == 0
-        (h, hbuf), (zo, zbuf), (dz, dbuf) = new(F), new(2 * F), new(2 * F)
-        fbl.gated_fwd(x, w, b, "silu", out=h, z=zo)
-        _, db = fbl.gated_bwd(dy, wd, z, "silu", dz=dz)
-        _check_fwd(h, zo, xr, wr, br, "silu")
-        _check_bwd(dz, db, dyr, wdr, zr, "silu")
-        for buf, n in ((hbuf, F), (zbuf, 2 * F), (dbuf, 2 * F)):
+        (h, hbuf), (fo, fbuf), (dz, dbuf) = new(F), new(2 * F), new(2 * F)
+        fbl.gated_fwd(x, w, b, "silu", out=h, factors=fo)
+        _, db = fbl.gated_bwd(dy, wd, f, dz=dz)
+        _check_fwd(h, fo, xr, wr, br, "silu")
+        _check_bwd(dz, db, dyr, wdr, fr)
+        for buf, n in ((hbuf, F), (fbuf, 2 * F), (dbuf, 2 * F)):
             assert torch.all(buf[:, n:] == 7.0) and torch.all(buf[-1] == 7.0)
         ws = torch.full((max(need, back) + 64,), 0xff, dtype=torch.uint8, device="cuda")
         assert torch.equal(h, fbl.gated_fwd(x, w, b, "silu", out=new(F)[0], workspace=ws[:need]))
         assert torch.all(ws[need:] == 0xff)
-        again = fbl.gated_bwd(dy, wd, z, "silu", dz=new(2 * F)[0], workspace=ws[:back])
+        again = fbl.gated_bwd(dy, wd, f, dz=new(2 * F)[0], workspace=ws[:back])
         assert torch.equal(again[0], dz) and torch.equal(again[1], db) and torch.all(ws[max(need, back):] == 0xff)
-        alone = fbl.gated_bwd(dy, wd, z, "silu", dz=new(2 * F)[0], need_bias=False)
+        alone = fbl.gated_bwd(dy, wd, f, dz=new(2 * F)[0], need_bias=False)
         assert torch.equal(alone[0], dz) and alone[1] is None
         side, got = torch.cuda.Stream(), new(F)[0]
         side.wait_stream(torch.cuda.current_stream())
         fbl.gated_fwd(x, w, b, "silu", out=got, stream=side)
         torch.cuda.synchronize()
         assert torch.equal(h, got)
-        for f in (lambda: fbl.gated_fwd(x, w, b, "silu", workspace=ws[:need - 16]),
-                  lambda: fbl.gated_bwd(dy, wd, z, "silu", workspace=ws[:back - 16])):
+        for call in (lambda: fbl.gated_fwd(x, w, b, "silu", workspace=ws[:need - 16]),
+                     lambda: fbl.gated_bwd(dy, wd, f, workspace=ws[:back - 16])):
             with pytest.raises(fbl.FblError):
-                f()
+                call()
 
 
 @pytest.mark.parametrize("dt,gap", [("bf16", 8), ("f32", 3)])
 def test_strided_operands(dt, gap):
     """Every matrix a view with gaps of NaN between its rows; bit for bit the contiguous call."""
     dt = DTYPES[dt]
-    (x, _), (w, _), (b, _), (wd, _), (z, _), (dy, _) = _inputs(75, 88, 104, 72, dt, True)
-    zo = torch.empty_like(z)
-    h = fbl.gated_fwd(x, w, b, "gelu_tanh", z=zo)
-    dz, db = fbl.gated_bwd(dy, wd, z, "gelu_tanh")
+    (x, _), (w, _), (b, _), (wd, _), (f, _), (dy, _) = _inputs(75, 88, 104, 72, dt, True)
+    fo = torch.empty_like(f)
+    h = fbl.gated_fwd(x, w, b, "gelu_tanh", factors=fo)
+    dz, db = fbl.gated_bwd(dy, wd, f)
     view = lambda t: padded(t, gap)[0]
-    zv = view(torch.zeros_like(zo))
-    assert torch.equal(h, fbl.gated_fwd(view(x), view(w), b, "gelu_tanh", z=zv, out=view(torch.zeros_like(h))))
-    got = fbl.gated_bwd(view(dy), view(wd), view(z), "gelu_tanh", dz=view(torch.zeros_like(dz)))
-    assert torch.equal(zv, zo) and torch.equal(got[0], dz) and torch.equal(got[1], db)
+    fv = view(torch.zeros_like(fo))
+    assert torch.equal(h, fbl.gated_fwd(view(x), view(w), b, "gelu_tanh", factors=fv, out=view(torch.zeros_like(h))))
+    got = fbl.gated_bwd(view(dy), view(wd), view(f), dz=view(torch.zeros_like(dz)))
+    assert torch.equal(fv, fo) and torch.equal(got[0], dz) and torch.equal(got[1], db)
 
 
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
@@ -212,10 +215,10 @@ def test_autograd(dt, lead):
     got = torch.autograd.grad(y, leaves, dy)
     with torch.no_grad():  # bit for bit the explicit calls
         x2, r2, dy2 = (t.detach().view(-1, K) for t in (x, r, dy))
-        z = torch.empty(x2.shape[0], 2 * F, dtype=dtype, device="cuda")
-        h = fbl.gated_fwd(x2, w1, b1, "silu", z=z)
+        f = torch.empty(x2.shape[0], 2 * F, dtype=dtype, device="cuda")
+        h = fbl.gated_fwd(x2, w1, b1, "silu", factors=f)
         y2 = fbl.linear_fwd(h, w2, b2, residual=r2)
-        dz, db1 = fbl.gated_bwd(dy2, w2, z, "silu")
+        dz, db1 = fbl.gated_bwd(dy2, w2, f)
         dx, dw1, _ = fbl.linear_bwd(dz, x2, w1, need_bias=False)
         _, dw2, db2 = fbl.linear_bwd(dy2, h, w2, need_dx=False)
     for a, b in zip((y, *got), (y2, dx, dw1, db1, dw2, db2, dy)):
@@ -224,7 +227,7 @@ def test_autograd(dt, lead):
     zt = p[0] @ p[1] + p[2]
     yt = (torch.nn.functional.silu(zt[..., :F]) * zt[..., F:]) @ p[3] + p[4] + p[5]
     ref = torch.autograd.grad(yt, p, torch.from_numpy(dyr))
-    # z, dz and h are rounded once each where they are kept: three half steps, and the result's own, of the largest value
+    # the factors, dz and h are rounded once each where they are kept: three half steps, and the result's own, of the largest value
     tol = 4 * 2.0 ** -8 if dt == "bf16" else 1e-5
     for a, b in zip((y, *got), (yt, *ref)):
         assert float((a.detach().double().cpu() - b.detach()).abs().max()) <= tol * float(b.detach().abs().max())
@@ -254,14 +257,14 @@ def test_graph_replays():
     b1, _ = rounded(rng, (2 * 136,), dtype, 0.1)
     w2, _ = rounded(rng, (136, 96), dtype, 0.1)
     dy, _ = rounded(rng, (130, 96), dtype)
-    z, h, dz = (torch.empty(130, n, dtype=dtype, device="cuda") for n in (272, 136, 272))
+    f, h, dz = (torch.empty(130, n, dtype=dtype, device="cuda") for n in (272, 136, 272))
     db = torch.empty(272, dtype=dtype, device="cuda")
     ws = torch.empty(fbl.gated_bwd_workspace(dy, w2), dtype=torch.uint8, device="cuda")
     note("gated graph")
 
     def step():
-        fbl.gated_fwd(x, w1, b1, z=z, out=h)
-        fbl.gated_bwd(dy, w2, z, dz=dz, dbias=db, workspace=ws)
+        fbl.gated_fwd(x, w1, b1, factors=f, out=h)
+        fbl.gated_bwd(dy, w2, f, dz=dz, dbias=db, workspace=ws)
     step()
     torch.cuda.synchronize()
     graph = torch.cuda.CUDAGraph()
@@ -271,7 +274,7 @@ def test_graph_replays():
         x.copy_(rounded(rng, (130, 96), dtype)[0])
         graph.replay()
         torch.cuda.synchronize()
-        got = [t.clone() for t in (h, z, dz, db)]
+        got = [t.clone() for t in (h, f, dz, db)]
         step()
         torch.cuda.synchronize()
-        assert all(torch.equal(a, b) for a, b in zip(got, (h, z, dz, db)))
+        assert all(torch.equal(a, b) for a, b in zip(got, (h, f, dz, db)))

@@ -57,7 +57,7 @@ def test_gated_differences(kind):
     rng = np.random.default_rng(3)
     x, w, b, dh = (rng.normal(size=s) for s in ((4, 5), (5, 12), (12,), (4, 6)))
     h, z = G.gated_fwd(x, w, b, kind)
-    dz = G.gated_bwd(dh, z, kind)
+    dz = G.gated_bwd(dh, G.gated_factors(z, kind))
     f = lambda: float((G.gated_fwd(x, w, b, kind)[0] * dh).sum())
     for a, g in ((x, dz @ w.T), (w, x.T @ dz), (b, dz.sum(0))):
         _diff(f, a, g)
