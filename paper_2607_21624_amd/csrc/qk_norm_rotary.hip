@@ -154,19 +154,29 @@ __global__ __launch_bounds__(256, (NORM && BWD ? 3 : 5)) void qk_norm_rotary(Rot
     };
     const int64_t items = p.groups * p.parts, stride = (int64_t)gridDim.x * 4;
     Two<T> nx, ng;
-    int64_t at[4];
+    // A group's angles, PAIRS of each of its tokens, are made once, 64 of them at a time, a lane each, and go to the lanes
+    // that hold the pairs through LDS: made by every lane for itself they were a sixth of the time.
+    constexpr int PAIRS = D / 2;
+    const int angles = (int)per_group * PAIRS;
+    const auto token_at = [&](uint32_t token, int& b, int& s) __attribute__((always_inline)) {
+        const bool in = token < tokens;
+        b = in ? (int)(token / (uint32_t)p.S) : 0;
+        s = in ? (int)(token - (uint32_t)b * (uint32_t)p.S) : 0;
+        return in;
+    };
+    const auto position = [&](int64_t item, int i) __attribute__((always_inline)) {  // of this lane's i-th angle
+        const int k = i * 64 + lane, j = k % PAIRS, axis = (int)(p.axes[j / 32] >> j % 32 * 2) & 3;
+        int b, s;
+        token_at((uint32_t)(item / p.parts) * per_group + (uint32_t)k / PAIRS, b, s);
+        return p.pos ? p.pos[axis * p.pos_axis + b * p.pos_batch + s * p.pos_token] : (int64_t)s;
+    };
+    int64_t at;
     const auto enter = [&](Step& k, int64_t item) __attribute__((always_inline)) {
         k.item = item;
         const uint32_t group = (uint32_t)(item / p.parts), part = (uint32_t)(item - (int64_t)group * p.parts);
-        const uint32_t token = group * per_group + tsub;
-        k.there = token < tokens;
-        k.b = k.there ? (int)(token / (uint32_t)p.S) : 0;
-        k.s = k.there ? (int)(token - (uint32_t)k.b * (uint32_t)p.S) : 0;
+        k.there = token_at(group * per_group + tsub, k.b, k.s);
         k.h0 = (int)part * p.per * p.heads;
-        if (!p.dims) return;
-#pragma unroll
-        for (int a = 0; a < 4; ++a)
-            if (a < p.num_axes) at[a] = p.pos ? p.pos[a * p.pos_axis + k.b * p.pos_batch + k.s * p.pos_token] : k.s;
+        if (p.dims) at = position(item, 0);
     };
     const auto fetch = [&](const Step& k) __attribute__((always_inline)) {
         const int h = k.h0 + hsub;
@@ -185,13 +195,14 @@ __global__ __launch_bounds__(256, (NORM && BWD ? 3 : 5)) void qk_norm_rotary(Rot
 
     // weights and frequencies in LDS: in registers, unpacked for every step, they are what keeps a third wavefront out
     __shared__ T lw[2][D] __attribute__((aligned(16)));
-    __shared__ uint64_t lfreq[D / 2] __attribute__((aligned(16)));
+    __shared__ uint64_t lfreq[PAIRS] __attribute__((aligned(16)));
     if (NORM && threadIdx.x < 2 * D) {
         const int k = threadIdx.x / D, c = threadIdx.x % D;
         const T* const wp = static_cast<const T*>(k ? p.wk : p.wq);
         lw[k][c] = wp ? wp[c] : (T)1.f;
     }
-    if (2 * (int)threadIdx.x < p.dims) lfreq[threadIdx.x] = p.turns[threadIdx.x];
+    __shared__ float langle[4][2][V * 64] __attribute__((aligned(16)));  // [wavefront][cosine, sine][token of the group][pair]
+    if (threadIdx.x < PAIRS) lfreq[threadIdx.x] = 2 * (int)threadIdx.x < p.dims ? p.turns[threadIdx.x] : 0;
     __syncthreads();
     float sum[2][2 * V];
 #pragma unroll
@@ -205,18 +216,25 @@ __global__ __launch_bounds__(256, (NORM && BWD ? 3 : 5)) void qk_norm_rotary(Rot
         const bool entered = cur.item != next.item;
         cur = next;
         Two<T> x = nx, g = ng;
-        if (entered && turns) {
-            int first = pair;
-            asm volatile("" : "+v"(first));  // read anew for every token, not kept over the loop
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                int64_t n = at[0];
-                if (p.num_axes > 1) {
-                    const int a = (int)(p.axes[D > 64 ? (pair + i) / 32 : 0] >> (pair + i) % 32 * 2) & 3;
-                    n = a == 0 ? at[0] : a == 1 ? at[1] : a == 2 ? at[2] : at[3];
-                }
-                turned<sizeof(T) == 2>((int32_t)((uint64_t)n * lfreq[first + i] >> 32), cs[i], sn[i]);
+        if (entered && p.dims) {
+            float* const lc = langle[wave][0];
+            float* const ls = langle[wave][1];
+            for (int i = 0; i * 64 < angles; ++i) {
+                const int k = i * 64 + lane;
+                float c, n;
+                // (a group of more than 128 / D tokens, of a few heads, waits for the positions behind them)
+                const int64_t where = i == 0 ? at : position(cur.item, i);
+                turned<sizeof(T) == 2>((int32_t)((uint64_t)where * lfreq[k % PAIRS] >> 32), c, n);
+                if (k < angles) lc[k] = c, ls[k] = n;
             }
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll
+            for (int i = 0; i < V; ++i) cs[i] = lc[tsub * PAIRS + pair + i], sn[i] = ls[tsub * PAIRS + pair + i];
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
         }
         next.h0 += p.heads;
         if (next.h0 >= min(H_all, (int)(cur.item % p.parts + 1) * p.per * p.heads)) {
