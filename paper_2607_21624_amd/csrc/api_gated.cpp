@@ -49,6 +49,17 @@ int gated_tile(int grad, int64_t M, int64_t cols, int64_t kc) {
     return grad ? fbl::proj_auto_tile(op, M, K, N) : fbl::forward_tile(M, K, N);
 }
 
+// Workgroups that share the contraction K of a tile of a few tokens' forward.  bf16 up to 64 tokens: as many as give every CU
+// one of its 128-column tiles, of 384 values and more each (us, cold weights, 1 token, alone / so shared / two a CU, as
+// linear layers are: 2048 -> 4096 15.1 / 11.9 / 12.9, 2048 -> 8192 19.9 / 16.2 / 17.1, 4096 -> 4096 27.1 / 17.9 / 20.2, 4096 ->
+// 8192 37.3 / 27.3 / 28.9, 4096 -> 14336 44.4 / 44.4 / 47.7; 64 tokens 2048 -> 8192 23.1 / 19.7 / 22.8; 1536 -> 4096 12.0 /
+// 10.6, but 1024 -> 4096 8.9 / 9.6).
+int forward_splits(int f32, int64_t M, int64_t K, int64_t F) {
+    if (f32 || M > 64 || 2 * M * F >= (int64_t)1 << 29) return few_splits(f32, M, K, 2 * F);
+    if (K <= 1024) return 1;
+    return (int)std::max<int64_t>(1, std::min(256 / ((2 * F + 127) / 128), K / 384));
+}
+
 // Workspace of the data gradient, a function of the shape: planes of dh, and partial sums of dz (as many rows of them as any
 // tile writes, linear_grad_groups, or one for each of a few tokens).
 struct GatedWs {
@@ -80,7 +91,7 @@ extern "C" {
 fbl_status fbl_gated_fwd_workspace(int32_t dtype, int64_t M, int64_t K, int64_t F, size_t* bytes) {
     if (!bytes) return FBL_ERR_NULL;
     const fbl_status st = gated_shape(dtype, FBL_ACT_NONE, M, K, F);
-    if (st == FBL_OK) *bytes = few_ws(few_splits(dtype == FBL_F32, M, K, 2 * F), M, 2 * F);
+    if (st == FBL_OK) *bytes = few_ws(forward_splits(dtype == FBL_F32, M, K, F), M, 2 * F);
     return st;
 }
 
@@ -103,7 +114,7 @@ fbl_status fbl_gated_fwd(int32_t dtype, uint32_t act, int64_t M, int64_t K, int6
             if (overlap(*out, *in)) return FBL_ERR_ARG;
     if (overlap(vh, vf)) return FBL_ERR_ARG;
     // with a workspace for the shares of it
-    const int splits = ws && tile == FBL_GEMM_TILE_AUTO ? few_splits(f32, M, K, 2 * F) : 1;
+    const int splits = ws && tile == FBL_GEMM_TILE_AUTO ? forward_splits(f32, M, K, F) : 1;
     if (splits > 1) {
         const size_t need = few_ws(splits, M, 2 * F);
         if (ws_bytes < need) return FBL_ERR_WORKSPACE;
