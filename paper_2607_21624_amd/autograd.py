@@ -59,48 +59,10 @@ import functools
 import math
 
 import torch
-from torch.autograd.function import once_differentiable
 
 from . import fbl as _f
-
-
-def _first_order(backward):
-    """A backward in the library's kernels, of which autograd knows no derivative: its gradients under
-    create_graph may be read, but differentiating them raises.  once_differentiable marks them so only where an
-    incoming gradient requires grad; without one (the gradient of a weighted sum) they would count as
-    constants, though they depend on what the forward saved, and a penalty on them would drop out unseen."""
-    once = once_differentiable(backward)
-
-    @functools.wraps(backward)
-    def marked(ctx, *grads):
-        if torch.is_grad_enabled():
-            grads = tuple(g if g is None or g.requires_grad else g.detach().requires_grad_() for g in grads)
-        return once(ctx, *grads)
-    return marked
-
-
-def _unit(t, what: str):
-    """The incoming gradient as it is, if its rows have unit inner stride."""
-    if t.dim() == 0 or t.stride(-1) != 1:
-        raise _f.FblError(_f.FBL_ERR_LAYOUT, f"{what}: the incoming gradient needs unit inner stride, got strides "
-                                             f"{tuple(t.stride())}; pass a contiguous gradient")
-    return t
-
-
-def _matrix_of(t, what: str):
-    """[..., N] as a matrix of rows, a view."""
-    try:
-        return t.view(-1, t.shape[-1])
-    except RuntimeError as e:
-        raise _f.FblError(_f.FBL_ERR_LAYOUT, f"{what}: the rows are not one strided matrix ({e}); pass it "
-                                             f"contiguous") from None
-
-
-def _rows_of(x, width):
-    """A new [..., width] tensor beside x [..., K], and it as a matrix of rows for the library to write.  (A function
-    that returned a view of the matrix would have an output that torch lets nobody change in place.)"""
-    out = torch.empty((*x.shape[:-1], width), dtype=x.dtype, device=x.device)
-    return out, out if out.dim() == 2 else out.view(-1, width)
+from .autograd_block import attention_packed_rotary, clip_grad_norm_, gated_mlp, qk_norm_rotary  # noqa: F401
+from .autograd_common import first_order as _first_order, matrix_of as _matrix_of, rows_of as _rows_of, unit as _unit
 
 
 class _Attention(torch.autograd.Function):
@@ -144,77 +106,14 @@ class _AttentionPacked(torch.autograd.Function):
         return dqkv, None, None, None, None
 
 
-class _AttentionPackedRotary(torch.autograd.Function):
-    @staticmethod
-    def forward(ctx, qkv, Hq, Hkv, scale, causal, turns, positions, axes, neighbours, q_weight, k_weight, eps):
-        q, k, v = _packed_views(qkv, Hq, Hkv, "attention_packed")
-        qk = torch.empty((*qkv.shape[:2], q.shape[2] + k.shape[2]), dtype=qkv.dtype, device=qkv.device)
-        qr, kr = qk[..., :q.shape[2]], qk[..., q.shape[2]:]
-        _f.qk_norm_rotary_fwd(q, k, Hq, Hkv, turns, positions, axes, neighbours, q_weight, k_weight, eps, qr, kr)
-        o, lse = _f.attn_fwd(qr, kr, v, Hq, Hkv, scale, causal)
-        ctx.save_for_backward(qkv, qk, o, lse, turns, positions, q_weight, k_weight)
-        ctx.cfg = (Hq, Hkv, scale, causal, axes, neighbours, eps)
-        return o
-
-    @staticmethod
-    @_first_order
-    def backward(ctx, do):
-        qkv, qk, o, lse, turns, positions, q_weight, k_weight = ctx.saved_tensors
-        Hq, Hkv, scale, causal, axes, neighbours, eps = ctx.cfg
-        q, k, v = _packed_views(qkv, Hq, Hkv, "attention_packed")
-        dqkv = torch.empty(qkv.shape, dtype=qkv.dtype, device=qkv.device)
-        dq, dk, dv = _packed_views(dqkv, Hq, Hkv, "attention_packed")
-        _f.attn_bwd(qk[..., :q.shape[2]], qk[..., q.shape[2]:], v, o, _unit(do, "attention_packed"), lse, Hq, Hkv, scale, causal,
-                    dq=dq, dk=dk, dv=dv)
-        # the gradients of what attention read become those of the projection where they lie
-        need = ctx.needs_input_grad[9] or ctx.needs_input_grad[10]
-        _, _, dqw, dkw = _f.qk_norm_rotary_bwd(dq, dk, q, k, Hq, Hkv, turns, positions, axes, neighbours, q_weight, k_weight,
-                                               eps, dq=dq, dk=dk, need_weights=need)
-        return (dqkv,) + (None,) * 8 + (dqw, dkw, None)
-
-
-def _packed_views(qkv, Hq: int, Hkv: int, where: str):
-    """Q, K and V in a packed [B, S, (Hq + 2 Hkv) d] tensor."""
-    if qkv.dim() != 3 or qkv.shape[2] % (Hq + 2 * Hkv):
-        raise _f.FblError(_f.FBL_ERR_SHAPE, f"{where}: qkv has shape {tuple(qkv.shape)}, needs [B, S, ({Hq} + 2 * {Hkv}) d]")
-    d = qkv.shape[2] // (Hq + 2 * Hkv)
-    return qkv[..., :Hq * d], qkv[..., Hq * d:(Hq + Hkv) * d], qkv[..., (Hq + Hkv) * d:]
-
-
 def attention_packed(qkv, Hq: int, Hkv: int, scale=None, causal: bool = False, turns=None, positions=None, axes=None,
                      neighbours: bool = False, q_weight=None, k_weight=None, eps=None):
     if scale is None:
         scale = 1.0 / math.sqrt(qkv.shape[-1] // (Hq + 2 * Hkv))
     if turns is None and eps is None and all(t is None for t in (positions, axes, q_weight, k_weight)):
         return _AttentionPacked.apply(qkv, Hq, Hkv, float(scale), bool(causal))
-    return _AttentionPackedRotary.apply(qkv, Hq, Hkv, float(scale), bool(causal), turns, positions, axes, bool(neighbours),
-                                        q_weight, k_weight, eps)
-
-
-class _QkNormRotary(torch.autograd.Function):
-    @staticmethod
-    def forward(ctx, q, k, Hq, Hkv, turns, positions, axes, neighbours, q_weight, k_weight, eps):
-        y = _f.qk_norm_rotary_fwd(q, k, Hq, Hkv, turns, positions, axes, neighbours, q_weight, k_weight, eps)
-        ctx.save_for_backward(q if eps is not None else None, k if eps is not None else None, turns, positions, q_weight,
-                              k_weight)
-        ctx.cfg = (Hq, Hkv, axes, neighbours, eps)
-        return y
-
-    @staticmethod
-    @_first_order
-    def backward(ctx, gq, gk):
-        q, k, turns, positions, q_weight, k_weight = ctx.saved_tensors
-        Hq, Hkv, axes, neighbours, eps = ctx.cfg
-        gq, gk = _unit(gq, "qk_norm_rotary"), None if gk is None else _unit(gk, "qk_norm_rotary")
-        need = ctx.needs_input_grad[8] or ctx.needs_input_grad[9]
-        dq, dk, dqw, dkw = _f.qk_norm_rotary_bwd(gq, gk, q, k, Hq, Hkv, turns, positions, axes, neighbours, q_weight,
-                                                 k_weight, eps, need_weights=need)
-        return dq, dk, None, None, None, None, None, None, dqw, dkw, None
-
-
-def qk_norm_rotary(q, k, Hq: int, Hkv: int, turns=None, positions=None, axes=None, neighbours: bool = False, q_weight=None,
-                   k_weight=None, eps=None):
-    return _QkNormRotary.apply(q, k, Hq, Hkv, turns, positions, axes, bool(neighbours), q_weight, k_weight, eps)
+    return attention_packed_rotary(qkv, Hq, Hkv, float(scale), bool(causal), turns, positions, axes, bool(neighbours),
+                                   q_weight, k_weight, eps)
 
 
 class _Linear(torch.autograd.Function):
@@ -325,59 +224,6 @@ class _Mlp(torch.autograd.Function):
 
 def mlp(x, w1, b1, w2, b2, act: str = "gelu", residual=None):
     return _Mlp.apply(x, w1, b1, w2, b2, residual, act)
-
-
-def _wide(rows: int, width: int, like):
-    """A new matrix for a kernel's intermediate.  Rows of bfloat16 that are 32 KB or more and a multiple of 1 KB begin 512
-    bytes further apart: a product that walks down them (dx takes 256 rows of dz a tile) would else meet few of the
-    memory's channels (gated step of 4096 tokens, 2048 -> 8192 1233 -> 1181 us, 4096 -> 11008 3112 -> 3085; rows of 16 KB gain
-    nothing, 8192 tokens 1024 -> 4096 705 -> 722)."""
-    row = width * like.element_size()
-    gap = 256 if like.dtype == torch.bfloat16 and row >= 1 << 15 and row % 1024 == 0 else 0
-    if rows * (row + 512) >= 1 << 31:  # the products' limit
-        gap = 0
-    return torch.empty((rows, width + gap), dtype=like.dtype, device=like.device)[:, :width]
-
-
-class _GatedMlp(torch.autograd.Function):
-    @staticmethod
-    def forward(ctx, x, w1, b1, w2, b2, residual, act):
-        x2 = _matrix_of(x, "gated_mlp")
-        res2 = None
-        if residual is not None:
-            if residual.shape != (*x.shape[:-1], w2.shape[1]):
-                raise _f.FblError(_f.FBL_ERR_SHAPE, f"gated_mlp: residual has shape {tuple(residual.shape)}, needs "
-                                                    f"{(*x.shape[:-1], w2.shape[1])}")
-            res2 = _matrix_of(residual, "gated_mlp: residual")
-        factors = None
-        if any(ctx.needs_input_grad[:3]):
-            factors = _wide(x2.shape[0], w1.shape[1], x)
-        h = _f.gated_fwd(x2, w1, b1, act, factors=factors)
-        y, y2 = _rows_of(x, w2.shape[1])
-        _f.linear_fwd(h, w2, b2, residual=res2, out=y2)
-        ctx.save_for_backward(x2, w1, w2, factors, h)
-        ctx.xshape = x.shape
-        return y
-
-    @staticmethod
-    @_first_order
-    def backward(ctx, dy):
-        x2, w1, w2, factors, h = ctx.saved_tensors
-        need = ctx.needs_input_grad
-        dx = dw1 = db1 = dw2 = db2 = None
-        if any(need[:5]):
-            dy2 = _matrix_of(_unit(dy, "gated_mlp"), "gated_mlp: the incoming gradient")
-            if any(need[:3]):
-                dz, db1 = _f.gated_bwd(dy2, w2, factors, dz=_wide(*factors.shape, factors), need_bias=need[2])
-                if need[0] or need[1]:
-                    dx, dw1, _ = _f.linear_bwd(dz, x2, w1, need_dx=need[0], need_dw=need[1], need_bias=False)
-            if need[3] or need[4]:
-                _, dw2, db2 = _f.linear_bwd(dy2, h, w2, need_dx=False, need_dw=need[3], need_bias=need[4])
-        return dx.view(ctx.xshape) if need[0] else None, dw1, db1, dw2, db2, dy if need[5] else None, None
-
-
-def gated_mlp(x, w1, b1, w2, b2, act: str = "silu", residual=None):
-    return _GatedMlp.apply(x, w1, b1, w2, b2, residual, act)
 
 
 class _LayerNorm(torch.autograd.Function):
@@ -491,10 +337,3 @@ class _LinearDistillation(torch.autograd.Function):
 
 def linear_distillation(x, w, index, logits, temperature: float = 1.0, reduction: str = "mean"):
     return _LinearDistillation.apply(x, w, index, logits, float(temperature), reduction)
-
-
-def clip_grad_norm_(parameters, limit: float):
-    grads = [p.grad for p in ([parameters] if isinstance(parameters, torch.Tensor) else parameters) if p.grad is not None]
-    norm = _f.clip_grad_norm(grads, limit)
-    torch.autograd.graph.increment_version(grads)  # changed in place
-    return norm
