@@ -13,7 +13,8 @@ namespace {
 using fbl::GradList;
 
 constexpr int kWorkgroups = 1024;  // of a launch: their sums are added by every workgroup that clips (85 M values within the limit: 2048 41, 1024 38 us)
-constexpr int64_t kMostBytes = (int64_t)1 << 45;  // of a list: its chunks count to 2^30
+constexpr int64_t kMostBytes = (int64_t)1 << 44;  // of a list: its chunks count to 2^30
+static_assert(kMostBytes / fbl::kGradChunk + fbl::kGradTensors < INT32_MAX - kWorkgroups, "a chunk's index is an int");
 
 int64_t launches(int64_t count) { return (count + fbl::kGradTensors - 1) / fbl::kGradTensors; }
 size_t norm_ws(int64_t count) { return (size_t)launches(count) * kWorkgroups * sizeof(double); }

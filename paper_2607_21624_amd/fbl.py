@@ -1673,6 +1673,8 @@ def clip_grads(grads, norm, limit: float, out=None, stream=None) -> None:
     """Every gradient times min(1, limit / (norm + 1e-6)), in place or into the tensors of `out`; norm is one float32 on
     their device (grad_norm's, or the program's own)."""
     where = "clip_grads"
+    if norm is None:
+        raise FblError(FBL_ERR_NULL, f"{where}: needs the norm; clip_grad_norm takes it by itself")
     a, like = _grad_list(grads, out, where)
     norm = _norm_out(norm, like, where, stream)
     _check_device(where, stream, grads=like, norm=norm)

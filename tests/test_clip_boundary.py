@@ -47,6 +47,7 @@ def clip(n=3, g=None, norm=at(8), limit=1.0):
     (dict(norm=None), F.FBL_ERR_NULL), (dict(norm=at(8, 2)), F.FBL_ERR_ALIGN), (dict(g=lst(("p", None))), F.FBL_ERR_NULL),
     (dict(g=lst(("dtype", 2))), F.FBL_ERR_DTYPE), (dict(g=lst(("n", -1))), F.FBL_ERR_SHAPE),
     (dict(g=lst(("n", 1 << 45))), F.FBL_ERR_UNSUPPORTED), (dict(g=lst(("n", 1 << 62))), F.FBL_ERR_UNSUPPORTED),
+    (dict(g=lst(("n", (1 << 43) + 1))), F.FBL_ERR_UNSUPPORTED),  # its chunks would not count to an int
     (dict(g=lst(("p", at(0, 1)), ("out", at(0, 1)))), F.FBL_ERR_ALIGN), (dict(g=lst(("reserved", 1))), F.FBL_ERR_ARG),
     # a tensor twice, into another, over the norm
     (dict(g=lst(("p", at(1)), ("out", at(1)))), F.FBL_ERR_ARG), (dict(g=lst(("n", MB))), F.FBL_ERR_ARG),
@@ -91,6 +92,7 @@ def test_binding_refusals():
         _refused(F.FBL_ERR_ARG, f, [t])       # not on a GPU
         _refused(F.FBL_ERR_ARG, f, [t, 3.0])  # no tensor
     _refused(F.FBL_ERR_SHAPE, fbl.clip_grad_norm, [t], 1.0, out=[t, t])
+    _refused(F.FBL_ERR_NULL, fbl.clip_grads, [t], None, 1.0)  # whose norm?
     p = torch.zeros(3, requires_grad=True)
     _refused(F.FBL_ERR_SHAPE, ag.clip_grad_norm_, [p], 1.0)  # no gradient at all
     _refused(F.FBL_ERR_SHAPE, fbl.grad_norm_workspace, [])
