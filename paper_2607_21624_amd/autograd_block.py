@@ -93,7 +93,7 @@ def _wide(rows: int, width: int, like):
 
 class _GatedMlp(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, w1, b1, w2, b2, residual, act):
+    def forward(ctx, x, w1, b1, w2, b2, residual, act, grads):
         x2 = matrix_of(x, "gated_mlp")
         res2 = None
         if residual is not None:
@@ -102,7 +102,7 @@ class _GatedMlp(torch.autograd.Function):
                                                     f"{(*x.shape[:-1], w2.shape[1])}")
             res2 = matrix_of(residual, "gated_mlp: residual")
         factors = None
-        if any(ctx.needs_input_grad[:3]):
+        if grads and any(ctx.needs_input_grad[:3]):
             factors = _wide(x2.shape[0], w1.shape[1], x)
         h = _f.gated_fwd(x2, w1, b1, act, factors=factors)
         y, y2 = rows_of(x, w2.shape[1])
@@ -125,11 +125,12 @@ class _GatedMlp(torch.autograd.Function):
                     dx, dw1, _ = _f.linear_bwd(dz, x2, w1, need_dx=need[0], need_dw=need[1], need_bias=False)
             if need[3] or need[4]:
                 _, dw2, db2 = _f.linear_bwd(dy2, h, w2, need_dx=False, need_dw=need[3], need_bias=need[4])
-        return dx.view(ctx.xshape) if need[0] else None, dw1, db1, dw2, db2, dy if need[5] else None, None
+        return dx.view(ctx.xshape) if need[0] else None, dw1, db1, dw2, db2, dy if need[5] else None, None, None
 
 
 def gated_mlp(x, w1, b1, w2, b2, act: str = "silu", residual=None):
-    return _GatedMlp.apply(x, w1, b1, w2, b2, residual, act)
+    # under no_grad needs_input_grad still tells of the parameters: nothing is kept there
+    return _GatedMlp.apply(x, w1, b1, w2, b2, residual, act, torch.is_grad_enabled())
 
 
 def clip_grad_norm_(parameters, limit: float):

@@ -144,3 +144,14 @@ def test_clipping_takes_the_parameters_that_have_gradients():
     assert torch.all(ps[0].grad == 0.5) and ps[1].grad is None
     assert all(ps[i].grad._version > v for i, v in zip((0, 2), versions))
     assert float(ag.clip_grad_norm_(ps[0], 1.0)) == 1
+
+
+@pytest.mark.parametrize("enabled", [True, False])
+def test_factors_are_kept_for_a_backward_alone(monkeypatch, enabled):
+    kept = []
+    plain = blk._f.gated_fwd
+    monkeypatch.setattr(blk._f, "gated_fwd", lambda *a, factors=None: (kept.append(factors), plain(*a, factors=factors))[1])
+    w1, w2 = torch.ones(8, 32, requires_grad=True), torch.ones(16, 8)
+    with torch.set_grad_enabled(enabled):
+        ag.gated_mlp(torch.ones(2, 3, 8), w1, None, w2, None)
+    assert len(kept) == 1 and (kept[0] is not None) == enabled
