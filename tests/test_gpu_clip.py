@@ -191,3 +191,19 @@ def test_graph_replays():
         step()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, [norm] + out))
+
+
+def test_offsets_past_32_bits():
+    # more than 2^31 values, 2^32 bytes: a few that count at either end and around both limits
+    n = (1 << 31) + 5001
+    g = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    at = torch.tensor([0, 1 << 30, (1 << 31) - 1, 1 << 31, (1 << 31) + 4097, n - 1], device="cuda")
+    g[at] = torch.arange(1, 7, device="cuda").to(torch.bfloat16)  # squares add to 91
+    note("clip past 32 bits")
+    norm = fbl.clip_grad_norm([g], math.sqrt(91) / 2)
+    assert abs(float(norm) - math.sqrt(91)) <= U * math.sqrt(91)
+    scale = oracle.clip_scale(float(norm), math.sqrt(91) / 2)
+    want = torch.arange(1, 7, dtype=torch.float64) * scale
+    assert torch.all((g[at].double().cpu() - want).abs() <= (HALF[torch.bfloat16] + 4 * U) * want)
+    g[at] = 0
+    assert not torch.any(g.view(torch.int16)[: n // 2]) and not torch.any(g.view(torch.int16)[n // 2:])

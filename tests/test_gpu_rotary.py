@@ -238,6 +238,46 @@ def test_dead_lanes_leave_the_sums():
     check("dw", dw, ref, 120 * U * (np.abs(_heads(gr, 3)) * xh).sum((0, 1, 2)))
 
 
+def test_offsets_past_32_bits():
+    # a batch is 2^32 bytes and more from the next one, a token 2^31
+    rng = np.random.default_rng(13)
+    q, _ = rounded(rng, (2, 2, 4 * 64), torch.bfloat16)
+    k, _ = rounded(rng, (2, 2, 2 * 64), torch.bfloat16)
+    w, _ = rounded(rng, (64,), torch.bfloat16, 0.2, 1.0)
+    how = dict(turns=fbl.rotary_turns(fbl.rotary_frequencies(64)), q_weight=w, k_weight=w, eps=1e-6)
+    ss, sb = 1 << 30, 1 << 31
+    buf = torch.empty(sb + ss + 1024, dtype=torch.bfloat16, device="cuda")
+    far = lambda t, col: buf.as_strided(t.shape, (sb, ss, 1), col).copy_(t)
+    fq, fk = far(q, 0), far(k, 256)
+    gq, gk = far(k.repeat(1, 1, 2), 384), far(q[..., 128:], 640)
+    note("qk_norm_rotary past 32 bits")
+    want = fbl.qk_norm_rotary_bwd(gq.contiguous(), gk.contiguous(), q, k, 4, 2, **how)
+    got = fbl.qk_norm_rotary_bwd(gq, gk, fq, fk, 4, 2, dq=gq, dk=gk, **how)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    want = fbl.qk_norm_rotary_fwd(q, k, 4, 2, **how)
+    got = fbl.qk_norm_rotary_fwd(fq, fk, 4, 2, q_out=fq, k_out=fk, **how)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_on_another_stream():
+    rng = np.random.default_rng(14)
+    q, _ = rounded(rng, (2, 65, 4 * 64), torch.bfloat16)
+    k, _ = rounded(rng, (2, 65, 64), torch.bfloat16)
+    w, _ = rounded(rng, (64,), torch.bfloat16, 0.2, 1.0)
+    how = dict(turns=fbl.rotary_turns(fbl.rotary_frequencies(64)), q_weight=w, k_weight=w, eps=1e-6)
+    run = lambda **kw: (*fbl.qk_norm_rotary_fwd(q, k, 4, 1, **how, **kw), *fbl.qk_norm_rotary_bwd(q, k, q, k, 4, 1, **how, **kw))
+    want = run()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    note("qk_norm_rotary on another stream")
+    given = run(stream=side)
+    with torch.cuda.stream(side):
+        current = run()
+    torch.cuda.synchronize()
+    for got in (given, current):
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 # ------------------------------------------------------------------------ autograd
 def _norm_rotary_torch(x, H, angle, neighbours, w, eps):
     """The same in torch, float64 on the CPU."""
