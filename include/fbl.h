@@ -800,7 +800,8 @@ fbl_status fbl_qk_norm_rotary_bwd(const fbl_layout* lgq, const void* gq, const f
  *   (gate, up) = x [M, K] . w [K, 2F] + bias [2F],   h [M, F] = act(gate) * up
  * gate is columns 0 .. F - 1, up columns F .. 2F - 1 (w and bias hold the two side by side; act as fbl_linear_fwd's).
  * bias may be NULL.  factors [M, 2F], where not NULL, receives what the backward needs, the derivatives of h by gate and by
- * up, (up * act'(gate), act(gate)), rounded to the storage type.  ws: NULL, or fbl_gated_fwd_workspace bytes (16-byte
+ * up, (up * act'(gate), act(gate)): fp32 as they are, bf16 in two bytes a value of a form for fbl_gated_bwd alone (eight
+ * consecutive ones share an exponent and keep 11 digits; one that is not finite leaves its eight so).  ws: NULL, or fbl_gated_fwd_workspace bytes (16-byte
  * aligned), with which several workgroups share the contraction of a few tokens' tiles (0 bytes where they do not).
  *
  * fbl_gated_bwd takes the gradient dy [M, N] of the block's result and w_down [F, N], its second weight, and gives

@@ -79,6 +79,26 @@ def gated_factors(z, kind="silu"):
     return np.concatenate([z[:, F:] * act_grad(z[:, :F], kind), act(z[:, :F], kind)], axis=1)
 
 
+def kept_factors(bits):
+    """The values of factors as 16-bit storage holds them [M, 2F] (uint16): eight of a row share a biased exponent, whose
+    bits are their bits 14, value 2q bit q and value 2q + 1 bit 4 + q; the rest is an fp16 below 1 or 1."""
+    b = np.asarray(bits, dtype=np.uint16).reshape(len(bits), -1, 8)
+    flags = (b >> 14 & 1).astype(np.int64)
+    e = sum(flags[..., 2 * q] << q | flags[..., 2 * q + 1] << 4 + q for q in range(4))[..., None]
+    half = (b & 0xBFFF).view(np.float16).astype(np.float64)
+    v = np.where(e == 255, np.copysign(np.inf, half), np.ldexp(half, e - 126))
+    return v.reshape(len(bits), -1)
+
+
+def keep_factors(values):
+    """uint16 [M, 2F] of finite fp32 values."""
+    v = np.asarray(values, dtype=np.float32).reshape(len(values), -1, 8)
+    e = np.abs(v).max(-1, keepdims=True).view(np.uint32).astype(np.int64) >> 23
+    b = np.ldexp(v.astype(np.float64), 126 - e).astype(np.float16).view(np.uint16)
+    at = np.arange(8)
+    return (b | (e >> (at // 2 + at % 2 * 4) & 1) << 14).astype(np.uint16).reshape(len(values), -1)
+
+
 def gated_bwd(dh, factors):
     """dz [M, 2F] from dh [M, F]."""
     dh, factors = np.asarray(dh, dtype=np.float64), np.asarray(factors, dtype=np.float64)

@@ -6,6 +6,7 @@
 // As linear_finish.hip: the fp32 planes, just written and a few MB at most, are added in order, a thread a
 // column of h.
 #include "act.hpp"
+#include "factors.hpp"
 #include "kernels.hpp"
 
 namespace fbl {
@@ -34,9 +35,16 @@ __global__ __launch_bounds__(256) void gated_finish(GatedArgs p, const float* pl
     if (p.bias) gate += (float)static_cast<const T*>(p.bias)[n], up += (float)static_cast<const T*>(p.bias)[F + n];
     const float a = act<ACT, FAST>(gate);
     if (p.factors) {
-        T* const f = static_cast<T*>(p.factors) + m * p.ldf + n;
-        f[0] = (T)(up * act_grad<ACT, FAST>(gate));
-        f[F] = (T)a;
+        const float d = up * act_grad<ACT, FAST>(gate);
+        if constexpr (FAST) {  // F is a multiple of 8: eight lanes are there or none
+            uint16_t* const f = static_cast<uint16_t*>(p.factors) + m * p.ldf + n;
+            f[0] = pack_factor(d);
+            f[F] = pack_factor(a);
+        } else {
+            T* const f = static_cast<T*>(p.factors) + m * p.ldf + n;
+            f[0] = d;
+            f[F] = a;
+        }
     }
     static_cast<T*>(p.c)[m * p.ldc + n] = (T)(a * up);
 }
@@ -47,8 +55,14 @@ __global__ __launch_bounds__(256) void gated_grad_finish(GatedArgs p, const floa
     const int64_t m = blockIdx.y, at = m * F + n;
     if (n >= F) return;
     const float v = plane_sum(planes, at, (int64_t)p.M * F, splits);
-    const T* const f = static_cast<const T*>(p.factors) + m * p.ldf + n;
-    const float dg = v * (float)f[0], du = v * (float)f[F];
+    float dg, du;
+    if constexpr (sizeof(T) == 2) {
+        const uint16_t* const f = static_cast<const uint16_t*>(p.factors) + m * p.ldf + n;
+        dg = v * unpack_factor(f[0]), du = v * unpack_factor(f[F]);
+    } else {
+        const T* const f = static_cast<const T*>(p.factors) + m * p.ldf + n;
+        dg = v * f[0], du = v * f[F];
+    }
     T* const c = static_cast<T*>(p.c) + m * p.ldc + n;
     c[0] = (T)dg;
     c[F] = (T)du;

@@ -11,14 +11,15 @@
 //
 // The factors are kept, and not gate and up: they are as many bytes, and the backward (gated_grad.hip) is then one kernel
 // for all activations that multiplies (4096 tokens 4096 -> 11008: 391 -> 381 us).  The derivative costs the forward a few
-// operations beside an exponential that it makes anyway.  bf16 dx and dw of a step are off by 0.29% of their norm, the
-// roundings of the factors, of dz, which the matrix instructions take in bf16, and of the result, 0.17% each (from rounded
-// gate and up 0.30%).  Factors in fp32 would leave 0.24%, for twice the memory that a step keeps of the layer and 5% of its
-// time.
+// operations beside an exponential that it makes anyway.  bf16 dx and dw of a step are off by 0.24% of their norm: the
+// roundings of dz, which the matrix instructions take in bf16, and of the result, 0.17% each.  Factors in bf16 added as much
+// (0.29%; rounded gate and up 0.30%), so they are kept in as many bytes of a form with 11 digits (factors.hpp).
 //
-// 4096 tokens bf16 with factors: 2048 -> 8192 254 us (1.08 PFLOP/s), 4096 -> 11008 711 us (1.04); without them 229 and 671.
+// 4096 tokens bf16 with factors: 2048 -> 8192 264 us (1.04 PFLOP/s), 4096 -> 11008 720 us (1.03); with bf16 factors 259 and
+// 716, without any 230 and 679.
 // The plain products of the same sizes, stored by the lanes as the accumulators lie, take 296 and 711.
 #include "act.hpp"
+#include "factors.hpp"
 #include "gemm_bf16.hpp"
 #include "gemm_f32.hpp"
 #include "rows.hpp"
@@ -101,8 +102,9 @@ struct GatedEp {
             if (keep) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) g[e] = u[e] * act_grad<ACT, true>(g[e]);
-                store8(rf, offset(m, n, p.ldf), g, n, F);
-                store8(rf, up_of(offset(m, n, p.ldf)), a, n, F);
+                const uint32_t off = offset(m, n, p.ldf);  // F is a multiple of 8
+                __builtin_amdgcn_raw_buffer_store_b128(pack_factors(g), rf, off, 0, 0);
+                __builtin_amdgcn_raw_buffer_store_b128(pack_factors(a), rf, up_of(off), 0, 0);
             }
             store8(rc, offset(m, n, p.ldc), h, n, F);
         });

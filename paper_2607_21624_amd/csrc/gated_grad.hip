@@ -1,10 +1,11 @@
 // gated_grad.hip -- the data gradient of a gated feed-forward part through its second projection, with what
 // follows in its epilogue, gfx950:
-//   dh = dY Wd^T;  dz = (dh f_gate, dh f_up)  by the factors that the forward kept (gated_gemm.hpp)
+//   dh = dY Wd^T;  dz = (dh f_gate, dh f_up)  by the factors that the forward kept (gated_gemm.hpp, factors.hpp)
 //   and the sums of dz over a tile's rows, the bias' gradient
 //
 // A tile reads its factors and writes both halves of dz, in whole lines by rows (by_rows); dh is never stored.  Without
 // that its memory traffic would be 7 values for each of dh's instead of 4.  The sums are of dz unrounded.
+#include "factors.hpp"
 #include "gemm_bf16.hpp"
 #include "gemm_f32.hpp"
 
@@ -28,22 +29,24 @@ struct GatedGradEp {
             return off == kNowhere ? kNowhere : off + (uint32_t)F * 2;
         };
         struct Factors {
-            bf16x8 g, u;
+            FactorWords g, u;
         };
         float sg[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, su[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         by_rows<C>(
             lds, acc, m0, n0, wm, wn,
             [&](int m, int n) __attribute__((always_inline)) {
                 const uint32_t off = offset(m, n, p.ldf);
-                return Factors{load8(rf, off), load8(rf, up_of(off))};
+                return Factors{__builtin_bit_cast(FactorWords, load8(rf, off)), __builtin_bit_cast(FactorWords, load8(rf, up_of(off)))};
             },
             [&](int m, int n, float (&v)[8], const Factors& f) __attribute__((always_inline)) {
                 float g[8], u[8];
+                unpack_factors(f.g, g);
+                unpack_factors(f.u, u);
                 const bool there = m < p.M;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    g[e] = v[e] * (float)f.g[e];
-                    u[e] = v[e] * (float)f.u[e];
+                    g[e] *= v[e];
+                    u[e] *= v[e];
                     sg[e] += there ? g[e] : 0.f;
                     su[e] += there ? u[e] : 0.f;
                 }

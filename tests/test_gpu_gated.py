@@ -3,8 +3,9 @@
 Bounds, element by element, as in test_gpu_linear.py: a product's sum of K terms in fp32 is off by at most (K + 16)
 2^-24 of the sum of magnitudes, activations by 2^-20 of their argument, their derivatives by 2^-20 (1 + |argument|), and |act'|
 <= 1.2, |act''| <= 1 (relu's is a step: a gate within its bound of 0 may fall on either side).  h = act(gate) up and the factors
-are made from unrounded sums and rounded once each.  The backward reads factors that are given, so that the oracle has the
-same."""
+are made from unrounded sums and rounded once each: factors of bf16 layers are off by 2^-11 of themselves where they are
+within 2^13 of the largest of their eight, and by 2^-24 of that otherwise.  The backward reads factors that are given, so that
+the oracle has the same."""
 import numpy as np
 import pytest
 import torch
@@ -27,6 +28,9 @@ def _inputs(M, K, F, N, dt, bias, seed=0):
     note(f"gated {M}x{K}x{F} -> {N} {dt} bias={bias}")
     x, w, wd, f, dy = (rounded(rng, s, dt, k) for s, k in (((M, K), 1.0), ((K, 2 * F), K ** -0.5), ((F, N), N ** -0.5),
                                                            ((M, 2 * F), 1.5), ((M, N), 1.0)))
+    if dt == torch.bfloat16:
+        kept = oracle.keep_factors(f[1])
+        f = torch.from_numpy(kept.view(np.int16)).cuda().view(torch.bfloat16), oracle.kept_factors(kept)
     b = rounded(rng, (2 * F,), dt, 0.5) if bias else (None, None)
     return x, w, b, wd, f, dy
 
@@ -43,7 +47,14 @@ def _check_fwd(h, f, x, w, b, act):
         if act == "relu":
             sb = np.where(np.abs(gate) <= zb[:, :F], 1.0, 0.0)
         fr = oracle.gated_factors(zr, act)
-        check("factors", f, fr, np.concatenate([zb[:, F:] * (slope + sb) + np.abs(up) * sb, gb], axis=1) + 2.0 ** -23 * np.abs(fr))
+        fb = np.concatenate([zb[:, F:] * (slope + sb) + np.abs(up) * sb, gb], axis=1) + 2.0 ** -23 * np.abs(fr)
+        if f.dtype == torch.bfloat16:
+            got = torch.from_numpy(oracle.kept_factors(f.contiguous().view(torch.int16).cpu().numpy().view(np.uint16)))
+            top = np.repeat((np.abs(fr) + fb).reshape(len(fr), -1, 8).max(-1), 8, axis=-1)
+            off = np.abs(got.numpy() - fr) - fb - np.maximum(2.0 ** -11 * (np.abs(fr) + fb), 2.0 ** -24 * top)
+            assert np.all(off <= 0), ("factors", np.unravel_index(np.argmax(off), off.shape), off.max())
+        else:
+            check("factors", f, fr, fb)
     check("h", h, hr, gb * np.abs(up) + (np.abs(act_of(gate, act)) + gb) * zb[:, F:] + 2.0 ** -23 * np.abs(hr))
 
 
@@ -180,6 +191,39 @@ def test_infinite_weights_stay_in_their_columns(dt):
         got = fbl.gated_fwd(x, bad, b)
         keep = torch.arange(72, device="cuda") != hit
         assert torch.equal(got[:, keep], clean[:, keep]) and not torch.isfinite(got[:, hit]).any()
+
+
+def test_factors_of_any_size():
+    """Every exponent keeps its digits, an element far below its neighbours what their exponent leaves it, and a factor that is
+    not finite leaves its eight so; a few tokens' as a tile's."""
+    dt = torch.bfloat16
+    eye = torch.eye(16, dtype=dt, device="cuda")
+    for M in (16, 200):
+        rows = torch.arange(M, device="cuda") % 16
+        x = eye[rows].contiguous()
+        for up in (1.0, 2.0 ** 100, 2.0 ** -120, 2.0 ** -131, 3e38):
+            w = torch.zeros(16, 48, dtype=dt, device="cuda")
+            w[:, :24] = torch.linspace(-3, 3, 16 * 24, device="cuda").view(16, 24).to(dt)
+            w[:, 24:] = (torch.linspace(0.1, 1, 16 * 24, device="cuda").view(16, 24) * up).to(dt)
+            w[3, 24 + 9] = 0
+            f = torch.empty(M, 48, dtype=dt, device="cuda")
+            h = fbl.gated_fwd(x, w, None, "none", factors=f)  # factors: up, gate, exactly within 8 digits
+            got = oracle.kept_factors(f.view(torch.int16).cpu().numpy().view(np.uint16))
+            want = torch.cat([w[:, 24:], w[:, :24]], 1)[rows].double().cpu().numpy()
+            top = np.repeat(np.abs(want).reshape(M, -1, 8).max(-1), 8, axis=-1)
+            assert np.all(np.abs(got - want) <= 2.0 ** -24 * top) and torch.isfinite(h.float()[3]).all()
+    for bad in (float("inf"), float("-inf"), float("nan")):
+        for M in (16, 200):
+            w = torch.ones(16, 48, dtype=dt, device="cuda")
+            w[5, 24 + 10] = bad  # of up, the gate's factor
+            x = eye[torch.arange(M, device="cuda") % 16].contiguous()
+            f = torch.empty(M, 48, dtype=dt, device="cuda")
+            fbl.gated_fwd(x, w, None, "none", factors=f)
+            dz, _ = fbl.gated_bwd(torch.ones(M, 16, dtype=dt, device="cuda"), torch.ones(24, 16, dtype=dt, device="cuda"), f)
+            keep = torch.ones(M, 48, dtype=torch.bool, device="cuda")
+            # (0 times an infinite weight: the other rows' products with that column are nan)
+            keep[:, 8:16] = False
+            assert torch.all(dz[keep] == 16) and not torch.isfinite(dz[:, 8:16]).any()
 
 
 def test_silu_far_out():

@@ -78,3 +78,17 @@ def test_clip():
     torch.nn.utils.clip_grad_norm_(p, 2.5)
     assert np.allclose(p[0].grad.numpy(), grads[0] * G.clip_scale(G.grad_norm(grads), 2.5), rtol=1e-12)
     assert G.clip_scale(1.0, 2.0) == 1.0
+
+
+def test_kept_factors():
+    """Within 2^13 of the largest of eight 2^-11 of the value, else 2^-24 of the largest; any exponent of fp32."""
+    rng = np.random.default_rng(5)
+    for scale in (1.0, 2.0 ** -126, 2.0 ** -140, 2.0 ** 120, 1e-30, 3e4):
+        v = np.float32(rng.standard_normal((40, 64)) * 10.0 ** rng.uniform(-6, 0, (40, 64)) * scale)
+        got = G.kept_factors(G.keep_factors(v))
+        top = np.repeat(np.abs(v).reshape(40, -1, 8).max(-1), 8, axis=-1)
+        assert np.all(np.abs(got - v) <= np.maximum(2.0 ** -11 * np.abs(v.astype(np.float64)), 2.0 ** -24 * top))
+    v = np.float32([[0] * 8 + [1, -1, 0.5, 65504, 2.0 ** -126, 0, 0, -3e38], [1, 2, 4, 8, 16, 32, 64, 128] * 2])
+    got = G.kept_factors(G.keep_factors(v))
+    assert np.all(got[0, :8] == 0) and np.all(got[1] == v[1]) and got[0, 12] == 0
+    assert np.all(np.isinf(G.kept_factors(np.full((1, 8), 0xffff, np.uint16))))
