@@ -115,10 +115,6 @@ struct Two {
     }
     FBL_DEV float operator[](int e) const { return (float)c[e / V].v[e % V]; }
     FBL_DEV void set(int e, float x) { c[e / V].v[e % V] = (T)x; }
-    FBL_DEV void clear() {
-#pragma unroll
-        for (int e = 0; e < 2 * V; ++e) set(e, 0.f);
-    }
 };
 // (a, b) by the angle, or BACK by its negative
 template <typename H, bool BACK, int V>
@@ -136,7 +132,7 @@ __global__ __launch_bounds__(256, (NORM && BWD ? 3 : 5)) void qk_norm_rotary(Rot
     using H = HeadRow<T, D, NEIGHBOURS>;
     constexpr int V = H::V, LANES = H::LANES, ROWS = H::ROWS;
     constexpr bool SUMS = NORM && BWD;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int pair = lane % LANES * V, sub = lane / LANES;
     const int c0 = H::first(pair, p.dims), c1 = H::second(pair, p.dims);
     const bool turns = 2 * pair < p.dims;  // the lane's pairs, all or none (dims are whole lanes)
@@ -147,49 +143,78 @@ __global__ __launch_bounds__(256, (NORM && BWD ? 3 : 5)) void qk_norm_rotary(Rot
     // A wavefront's items: blocks of `per` steps of heads of a group of tokens.  While one step is computed the next one's
     // rows, and its tokens' positions, are on the way.
     struct Step {
-        int64_t item;
+        uint32_t group, part;  // (the next item is found by adding: a division by parts in every step took a tenth of the time)
         int h0;
         int b, s;   // of the lane's token
         bool there;
     };
-    const int64_t items = p.groups * p.parts, stride = (int64_t)gridDim.x * 4;
+    const uint32_t groups = (uint32_t)p.groups, parts = (uint32_t)p.parts, waves = gridDim.x * 4;
+    const uint32_t group_step = waves / parts, part_step = waves % parts;
     Two<T> nx, ng;
     // A group's angles, PAIRS of each of its tokens, are made once, 64 of them at a time, a lane each, and go to the lanes
     // that hold the pairs through LDS: made by every lane for itself they were a sixth of the time.
     constexpr int PAIRS = D / 2;
     const int angles = (int)per_group * PAIRS;
     const auto token_at = [&](uint32_t token, int& b, int& s) __attribute__((always_inline)) {
-        const bool in = token < tokens;
-        b = in ? (int)(token / (uint32_t)p.S) : 0;
-        s = in ? (int)(token - (uint32_t)b * (uint32_t)p.S) : 0;
-        return in;
+        const uint32_t t = min(token, tokens - 1);
+        b = (int)(t / (uint32_t)p.S);
+        s = (int)(t - (uint32_t)b * (uint32_t)p.S);
+        return token < tokens;
     };
-    const auto position = [&](int64_t item, int i) __attribute__((always_inline)) {  // of this lane's i-th angle
-        const int k = i * 64 + lane, j = k % PAIRS, axis = (int)(p.axes[j / 32] >> j % 32 * 2) & 3;
-        int b, s;
-        token_at((uint32_t)(item / p.parts) * per_group + (uint32_t)k / PAIRS, b, s);
-        return p.pos ? p.pos[axis * p.pos_axis + b * p.pos_batch + s * p.pos_token] : (int64_t)s;
+    const int mine = lane % PAIRS, axis = (int)((mine < 32 ? p.axes[0] : p.axes[1]) >> mine % 32 * 2) & 3;
+    const int64_t* const positions = p.pos ? p.pos + axis * p.pos_axis : nullptr;
+    struct Position {
+        int64_t given;
+        int s;
+        FBL_DEV int64_t of(const int64_t* given_there) const { return given_there ? given : (int64_t)s; }
     };
-    int64_t at;
-    const auto enter = [&](Step& k, int64_t item) __attribute__((always_inline)) {
-        k.item = item;
-        const uint32_t group = (uint32_t)(item / p.parts), part = (uint32_t)(item - (int64_t)group * p.parts);
-        k.there = token_at(group * per_group + tsub, k.b, k.s);
-        k.h0 = (int)part * p.per * p.heads;
-        if (p.dims) at = position(item, 0);
+    const auto position = [&](Position& x, uint32_t group, int i) __attribute__((always_inline)) {  // of this lane's i-th angle
+        int b;
+        token_at(group * per_group + (uint32_t)(i * 64 + lane) / PAIRS, b, x.s);
+        if (p.pos) x.given = positions[b * p.pos_batch + x.s * p.pos_token];
+    };
+    Position at;
+    const auto enter = [&](Step& k) __attribute__((always_inline)) {
+        k.there = token_at(k.group * per_group + tsub, k.b, k.s);
+        k.h0 = (int)k.part * p.per * p.heads;
+        if (p.dims) position(at, k.group, 0);
+    };
+    // A tensor's address and strides in bytes, in scalar registers.  (The compiler would choose between the addresses of the
+    // arguments for queries and for keys, lane by lane, and load from there in every step, behind the rows on the way, which the
+    // stores then wait for: 4096 tokens of 32 + 32 heads of 128 53.9 us backward instead of 36.9.)
+    using Bytes = __attribute__((address_space(1))) char*;
+    struct Side {
+        Bytes p;
+        int64_t sb, ss, sh;
+    };
+    const auto side = [](const void* ptr, const TokMap& m) __attribute__((always_inline)) {
+        constexpr int64_t es = sizeof(T);
+        Side t{(Bytes)ptr, m.sb * es, m.ss * es, m.sh * es};
+        asm("" : "+s"(t.p), "+s"(t.sb), "+s"(t.ss), "+s"(t.sh));
+        return t;
+    };
+    const Side xq = side(p.q, p.mq), xk = side(p.k, p.mk), gq = side(p.gq, p.mgq), gk = side(p.gk, p.mgk), oq = side(p.oq, p.moq),
+               ok = side(p.ok, p.mok);
+    const auto row = [&](const Side& q, const Side& k, const Step& at) __attribute__((always_inline)) {
+        const auto address = [&](const Side& t, int h) __attribute__((always_inline)) {
+            return t.p + (at.b * t.sb + at.s * t.ss + h * t.sh);
+        };
+        const bool keys = at.h0 >= p.Hq;  // the same for the wavefront, as are all its heads but in one step of a token
+        const Side t{keys ? k.p : q.p, keys ? k.sb : q.sb, keys ? k.ss : q.ss, keys ? k.sh : q.sh};
+        const int h = min(at.h0 + hsub, H_all - 1);
+        Bytes a = address(t, keys ? h - p.Hq : h);
+        if (!keys && h >= p.Hq) a = address(k, h - p.Hq);
+        return (T*)a;
     };
     const auto fetch = [&](const Step& k) __attribute__((always_inline)) {
-        const int h = k.h0 + hsub;
-        if (!k.there || h >= H_all) return;
-        const bool key = h >= p.Hq;
-        const int hk = key ? h - p.Hq : h;
-        if (!BWD || NORM) nx.load(static_cast<const T*>(key ? p.k : p.q) + (key ? p.mk : p.mq).offset(k.b, hk, k.s, 0), c0, c1);
-        if (BWD) ng.load(static_cast<const T*>(key ? p.gk : p.gq) + (key ? p.mgk : p.mgq).offset(k.b, hk, k.s, 0), c0, c1);
+        if (!BWD || NORM) nx.load(row(xq, xk, k), c0, c1);
+        if (BWD) ng.load(row(gq, gk, k), c0, c1);
     };
     Step cur{}, next{};
-    next.item = (int64_t)blockIdx.x * 4 + wave;
-    if (next.item < items) {
-        enter(next, next.item);
+    const uint32_t first_item = blockIdx.x * 4 + (uint32_t)wave;
+    next.group = first_item / parts, next.part = first_item % parts;
+    if (next.group < groups) {
+        enter(next);
         fetch(next);
     }
 
@@ -210,10 +235,11 @@ __global__ __launch_bounds__(256, (NORM && BWD ? 3 : 5)) void qk_norm_rotary(Rot
 #pragma unroll
         for (int e = 0; e < 2 * V; ++e) sum[k][e] = 0.f;
     float cs[V], sn[V];
-    cur.item = -1;
+    bool entered = true;
+    // the first rows are there before the loop: else the compiler waits in every step as the first one has to, for all stores
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
 
-    while (next.item < items) {
-        const bool entered = cur.item != next.item;
+    while (next.group < groups) {
         cur = next;
         Two<T> x = nx, g = ng;
         if (entered && p.dims) {
@@ -223,8 +249,12 @@ __global__ __launch_bounds__(256, (NORM && BWD ? 3 : 5)) void qk_norm_rotary(Rot
                 const int k = i * 64 + lane;
                 float c, n;
                 // (a group of more than 128 / D tokens, of a few heads, waits for the positions behind them)
-                const int64_t where = i == 0 ? at : position(cur.item, i);
-                turned<sizeof(T) == 2>((int32_t)((uint64_t)where * lfreq[k % PAIRS] >> 32), c, n);
+                Position where = at;
+                if (i > 0) {
+                    position(where, cur.group, i);
+                    __builtin_amdgcn_s_waitcnt(0x0f70);
+                }
+                turned<sizeof(T) == 2>((int32_t)((uint64_t)where.of(p.pos) * lfreq[mine] >> 32), c, n);
                 if (k < angles) lc[k] = c, ls[k] = n;
             }
             __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
@@ -237,25 +267,24 @@ __global__ __launch_bounds__(256, (NORM && BWD ? 3 : 5)) void qk_norm_rotary(Rot
             __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
         }
         next.h0 += p.heads;
-        if (next.h0 >= min(H_all, (int)(cur.item % p.parts + 1) * p.per * p.heads)) {
-            next.item += stride;
-            if (next.item < items) enter(next, next.item);
+        entered = next.h0 >= min(H_all, ((int)cur.part + 1) * p.per * p.heads);
+        if (entered) {
+            next.group += group_step, next.part += part_step;
+            if (next.part >= parts) next.part -= parts, ++next.group;
+            if (next.group < groups) enter(next);
         }
-        if (next.item < items) fetch(next);
+        if (next.group < groups) fetch(next);
 
-        const int h = cur.h0 + hsub;
-        const bool live = cur.there && h < H_all, key = h >= p.Hq;
-        if (!live) {
-            x.clear();
-            g.clear();
-        }
+        // Lanes behind the last head or token do that one's work over again and store the same: a store that some lanes leave
+        // out is one that the next step's loads cannot be told apart from, and waits for.
+        const int h = min(cur.h0 + hsub, H_all - 1);
+        const bool live = cur.there && cur.h0 + hsub < H_all, key = h >= p.Hq;
         float r = 1.f;
         if constexpr (NORM) {
             float q = 0.f;
 #pragma unroll
             for (int e = 0; e < 2 * V; ++e) q = __builtin_fmaf(x[e], x[e], q);
             r = 1.f / sqrtf(group_sum<LANES>(q) * (1.f / D) + p.eps);
-            if (!live) r = 0.f;  // (eps may be 0)
         }
         float y[2 * V];
         if constexpr (!BWD) {
@@ -277,27 +306,32 @@ __global__ __launch_bounds__(256, (NORM && BWD ? 3 : 5)) void qk_norm_rotary(Rot
                 wh.load(lw[key], c0, c1);
                 const int first = cur.h0, last = min(H_all, cur.h0 + p.heads) - 1;
                 const bool all_q = last < p.Hq, all_k = first >= p.Hq;  // the same for the wavefront
-                float m = 0.f;
+                float m = 0.f, t[2 * V];
 #pragma unroll
                 for (int e = 0; e < 2 * V; ++e) {
-                    const float t = y[e] * (x[e] * r);
-                    if (all_q) sum[0][e] += t;
-                    else if (all_k) sum[1][e] += t;
-                    else sum[0][e] += key ? 0.f : t, sum[1][e] += key ? t : 0.f;
-                    m = __builtin_fmaf(t, wh[e], m);
+                    t[e] = y[e] * (x[e] * r);
+                    m = __builtin_fmaf(t[e], wh[e], m);
+                }
+                const float once = live ? 1.f : 0.f;  // (0 times a nan that its first lane has added too)
+                const auto add = [&](int k) __attribute__((always_inline)) {
+#pragma unroll
+                    for (int e = 0; e < 2 * V; ++e) sum[k][e] = __builtin_fmaf(t[e], once, sum[k][e]);
+                };
+                if (all_q) add(0);
+                else if (all_k) add(1);
+                else {
+#pragma unroll
+                    for (int e = 0; e < 2 * V; ++e) sum[0][e] += live && !key ? t[e] : 0.f, sum[1][e] += live && key ? t[e] : 0.f;
                 }
                 m = group_sum<LANES>(m) * (1.f / D);
 #pragma unroll
                 for (int e = 0; e < 2 * V; ++e) y[e] = r * (y[e] * wh[e] - x[e] * r * m);
             }
         }
-        if (live) {
-            Two<T> o;
+        Two<T> o;
 #pragma unroll
-            for (int e = 0; e < 2 * V; ++e) o.set(e, y[e]);
-            const int hk = key ? h - p.Hq : h;
-            o.store(static_cast<T*>(key ? p.ok : p.oq) + (key ? p.mok : p.moq).offset(cur.b, hk, cur.s, 0), c0, c1);
-        }
+        for (int e = 0; e < 2 * V; ++e) o.set(e, y[e]);
+        o.store(row(oq, ok, cur), c0, c1);
     }
 
     if constexpr (SUMS) {
