@@ -130,7 +130,7 @@ def test_workspace():
     assert f(None, None, ctypes.byref(n)) == F.FBL_ERR_NULL and f(_ref(lq), None, None) == F.FBL_ERR_NULL
     assert f(_ref(lq), _ref(lay(H=2, S=9)), ctypes.byref(n)) == F.FBL_ERR_SHAPE
     big = lay(B=1 << 10, S=1 << 15, H=32, D=128)
-    assert f(_ref(big), _ref(big), ctypes.byref(n)) == F.FBL_OK and n.value == 768 * 2 * 128 * 4
+    assert f(_ref(big), _ref(big), ctypes.byref(n)) == F.FBL_OK and n.value == 512 * 2 * 128 * 4
 
 
 def test_turns():
