@@ -2,8 +2,8 @@
 
 Multi-head (and grouped-query) attention forward and backward run directly on
 token-major [B, S, H*d] activations through hand-written HIP kernels behind a
-C ABI (include/fbl.h, libfbl.so), and so do the products, layer norms and
-losses of a linear head around it.  This package is the Python binding:
+C ABI (include/fbl.h, libfbl.so), and so do the products, layer norms, rotary
+positions, gated feed-forward parts, losses of a linear head and gradient clipping around it.  This package is the Python binding:
 argument marshalling only, torch for device memory and streams.
 """
 from .fbl import (  # noqa: F401

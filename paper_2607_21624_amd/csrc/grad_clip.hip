@@ -8,6 +8,8 @@
 // them.  Squares are summed in float64: no square overflows or vanishes, and a sum of 2^30 terms keeps fp32's digits.
 // Each workgroup leaves one sum; whoever needs the norm adds them in the same fixed order.  Clipping walks the chunks from
 // the last one back, since the end of what the norm has read is what the last-level cache still holds.
+//
+// 268 M values bf16: squares 108 us (5.0 TB/s), scaling into other tensors 185 (5.8).  85 M in place within the limit: 27 and 5.
 #include "kernels.hpp"
 #include "rows.hpp"
 

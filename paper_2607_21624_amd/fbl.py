@@ -1145,8 +1145,8 @@ def gated_fwd(x, w, bias=None, act: str = "silu", out=None, factors=None, tile: 
               stream=None):
     """h = act(gate) * up with (gate, up) = x w + bias for x [M, K], w [K, 2F] and bias [2F], gate then up columns (any row
     strides, one storage type), act one of ACTIVATIONS.  factors [M, 2F], where given, receives h's derivatives by gate
-    and by up, which gated_bwd needs (bfloat16: in a form of the library's own, two bytes a value).  workspace: gated_fwd_workspace bytes, allocated where they are needed and it is
-    None.  Returns h [M, F]."""
+    and by up, which gated_bwd needs (bfloat16: in a form of the library's own, two bytes a value).  workspace:
+    gated_fwd_workspace bytes, allocated where they are needed and it is None.  Returns h [M, F]."""
     done = _FAST.gated_fwd(x, w, bias, act, out, factors, tile, workspace, stream)
     if done is not None:
         return done
