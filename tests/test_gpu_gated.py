@@ -226,6 +226,33 @@ def test_factors_of_any_size():
             assert torch.all(dz[keep] == 16) and not torch.isfinite(dz[:, 8:16]).any()
 
 
+def test_operands_near_the_limit():
+    """Factors and dz of just below 2 GiB: the last rows are those of a call of their own, to the roundings of two tilings."""
+    M, K, F = 262143, 64, 2040
+    dt = torch.bfloat16
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    r = lambda *s, k=1.0: (torch.randn(s, generator=gen, device="cuda") * k).to(dt)
+    x, w, wd, dy = r(M, K), r(K, 2 * F, k=K ** -0.5), r(F, K, k=K ** -0.5), r(M, K)
+    note("gated near 2 GiB")
+    f = torch.empty(M, 2 * F, dtype=dt, device="cuda")
+    h = fbl.gated_fwd(x, w, None, "silu", factors=f)
+    dz, db = fbl.gated_bwd(dy, wd, f)
+    for at in (slice(M - 300, M), slice(131000, 131300)):
+        few = torch.empty(300, 2 * F, dtype=dt, device="cuda")
+        hs = fbl.gated_fwd(x[at].contiguous(), w, None, "silu", factors=few)
+        ds, _ = fbl.gated_bwd(dy[at].contiguous(), wd, few)
+        for a, b in ((h[at], hs), (dz[at], ds)):  # a rounding each way and sums of 64 terms in another order
+            a, b = a.double(), b.double()
+            assert torch.all((a - b).abs() <= 2.0 ** -7 * b.abs() + 1e-4)
+    sums = torch.zeros(2 * F, dtype=torch.float64, device="cuda")
+    most = torch.zeros(2 * F, dtype=torch.float64, device="cuda")
+    for part in dz.split(32768):
+        sums += part.double().sum(0)
+        most += part.double().abs().sum(0)
+    # dz rounded (2^-8 of each, added as they come) against sums of it unrounded in fp32 that are rounded once
+    assert torch.all((db.double() - sums).abs() <= 2.0 ** -8 * (most + sums.abs()))
+
+
 def test_silu_far_out():
     """act(gate) up where the gate saturates: no nan from the exponentials."""
     x = torch.eye(8, dtype=torch.bfloat16, device="cuda")

@@ -181,6 +181,41 @@ def test_in_place(dt, norm):
         assert torch.equal(out[2], dqw) and torch.equal(out[3], dkw)
 
 
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("S,Hq,Hkv,d", [(5, 3, 2, 64), (7, 1, 1, 32), (1, 5, 0, 128), (3, 11, 3, 32), (1, 1, 1, 64)])
+def test_in_place_where_lanes_have_no_head_or_token(dt, S, Hq, Hkv, d):
+    """Lanes behind the last head and token repeat its work: in place too, with nothing written behind it, and nothing added
+    twice."""
+    dtype = DTYPES[dt]
+    rng = np.random.default_rng(31 + S)
+    W = (Hq + Hkv) * d
+    x, xr = rounded(rng, (1, S, W), dtype)
+    g, gr = rounded(rng, (1, S, W), dtype)
+    w, wr = rounded(rng, (d,), dtype, 0.2, 1.0)
+    how = dict(turns=fbl.rotary_turns(fbl.rotary_frequencies(d)), q_weight=w, k_weight=w if Hkv else None, eps=1e-6)
+    split = lambda t: (t[..., :Hq * d], t[..., Hq * d:W] if Hkv else None)
+    note(f"in place, S={S} heads {Hq} + {Hkv} of {d} {dt}")
+    want = fbl.qk_norm_rotary_fwd(*split(x), Hq, Hkv, **how)
+    grads = fbl.qk_norm_rotary_bwd(*split(g), *split(x), Hq, Hkv, **how)
+    _, dw = oracle.qk_norm_rotary_bwd(_heads(gr[..., :Hq * d], Hq), _heads(xr[..., :Hq * d], Hq),
+                                      oracle.angles(np.arange(S)[None], fbl.rotary_frequencies(d), None), False, wr, 1e-6)
+    xh = _heads(xr[..., :Hq * d], Hq)
+    xh = np.abs(xh / np.sqrt((xh * xh).mean(-1, keepdims=True) + 1e-6))
+    check("dw", grads[2], dw, (trig(dtype) + 160 * U) * (_pair_sum(_heads(gr[..., :Hq * d], Hq), d, False) * xh).sum((0, 1, 2)))
+    for back in (False, True):
+        buf = torch.full((1, S + 2, W + 16), 7.0, dtype=dtype, device="cuda")
+        own = buf[:, :S, :W]
+        own.copy_(g if back else x)
+        q, k = split(own)
+        if back:
+            got = fbl.qk_norm_rotary_bwd(q, k, *split(x), Hq, Hkv, dq=q, dk=k, **how)
+        else:
+            got = fbl.qk_norm_rotary_fwd(q, k, Hq, Hkv, q_out=q, k_out=k, **how)
+        for a, b in zip(got, grads if back else want):
+            assert (a is None and b is None) or torch.equal(a, b)
+        assert torch.all(buf[:, S:] == 7.0) and torch.all(buf[..., W:] == 7.0)
+
+
 def test_repeatable_and_need_not():
     rng = np.random.default_rng(3)
     q, _ = rounded(rng, (2, 700, 8 * 64), torch.bfloat16)
