@@ -837,12 +837,12 @@ fbl_status fbl_gated_bwd(int32_t dtype, int64_t M, int64_t F, int64_t N, const v
  *   fbl_grad_norm       norm (float32, device memory); `out` is not looked at
  *   fbl_grad_clip       out from a norm that is given: the program's own, or of gradients that lie on several devices
  *   fbl_clip_grad_norm  both
- * In place, a norm within the limit leaves the gradients untouched (in a list of both, written unchanged).  The norm is summed in float64 in a fixed order and
- * rounded once; it does not overflow before its own value does.  An infinite norm makes the scale 0 (an infinite
+ * In place, a norm within the limit leaves the gradients untouched (in a list of both, written unchanged).  The norm is
+ * summed in float64 in a fixed order and rounded once; it does not overflow before its own value does.  An infinite norm makes the scale 0 (an infinite
  * gradient then nan), a norm of nan everything nan.  Workspace: fbl_grad_norm_workspace bytes for `count` tensors, 8-byte
  * aligned; nothing is kept in it.  A launch takes 112 tensors.
- * Checks: count >= 1, limit >= 0 (FBL_ERR_ARG; infinity: no clipping), pointers aligned to their element, no two tensors,
- * outputs, norm or workspace sharing a byte (FBL_ERR_ARG; the same tensor twice is one such case), 2^45 bytes at most.
+ * Checks: count >= 1, limit >= 0 (FBL_ERR_ARG; infinity: nothing changes, whatever the norm), pointers aligned to their element, no two tensors,
+ * outputs, norm or workspace sharing a byte (FBL_ERR_ARG; the same tensor twice is one such case), 2^44 bytes at most.
  */
 typedef struct {
     const void* p;

@@ -80,7 +80,7 @@ fbl_status gated_shape(int32_t dtype, uint32_t act, int64_t M, int64_t K, int64_
     if (act > FBL_ACT_SILU) return FBL_ERR_ARG;
     if (!fbl::extent(M) || !fbl::extent(K) || !fbl::extent(F)) return FBL_ERR_SHAPE;
     if (K > fbl::kMaxWidth || 2 * F > fbl::kMaxWidth) return FBL_ERR_UNSUPPORTED;
-    if (M * 2 * F >= ((int64_t)1 << 31) / es) return FBL_ERR_UNSUPPORTED;  // z, dz
+    if (M * 2 * F >= ((int64_t)1 << 31) / es) return FBL_ERR_UNSUPPORTED;  // factors, dz
     return FBL_OK;
 }
 

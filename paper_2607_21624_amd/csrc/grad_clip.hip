@@ -129,7 +129,8 @@ __global__ __launch_bounds__(256) void grad_scale(GradList a, const double* sums
     const float x = sums ? norm_of(sums, n, red) : norm[0];
     if (sums && norm && blockIdx.x == 0 && threadIdx.x == 0) norm[0] = x;
     const double ratio = (double)limit / ((double)x + 1e-6);
-    const float scale = ratio >= 1.0 ? 1.f : (float)ratio;  // (a norm that is nan makes everything nan)
+    // (a norm that is nan makes everything nan; without a limit nothing changes, whatever the norm)
+    const float scale = ratio >= 1.0 || limit == __builtin_inff() ? 1.f : (float)ratio;
     if (scale == 1.f && a.in_place) return;
     for (int c = a.chunks - 1 - (int)blockIdx.x; c >= 0; c -= gridDim.x) {
         const int t = tensor_of(a, c);

@@ -207,3 +207,17 @@ def test_offsets_past_32_bits():
     assert torch.all((g[at].double().cpu() - want).abs() <= (HALF[torch.bfloat16] + 4 * U) * want)
     g[at] = 0
     assert not torch.any(g.view(torch.int16)[: n // 2]) and not torch.any(g.view(torch.int16)[n // 2:])
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_without_a_limit_nothing_changes(bad):
+    g = torch.arange(300.0, device="cuda")
+    g[17] = bad
+    want = g.clone()
+    out = torch.zeros_like(g)
+    same = lambda a: torch.equal(a.view(torch.int32), want.view(torch.int32))
+    n = fbl.clip_grad_norm([g], math.inf, out=[out])
+    assert same(out) and same(g) and not math.isfinite(float(n))
+    fbl.clip_grad_norm([g], math.inf)
+    fbl.clip_grads([g], n, math.inf)
+    assert same(g)
