@@ -18,6 +18,12 @@ using FactorWords = int __attribute__((ext_vector_type(4)));
 
 constexpr uint32_t kShared = 0x40004000u;  // bit 14 of both halves of a word
 
+// Cache policy of their stores and loads (nt).  A tile's factors are read once, long after they were written; passed through the caches like
+// others they push out h, which the next product reads, and dz, which the next two do (us a step, stores alone / loads too: 8192
+// tokens 1024 -> 4096 736 -> 713 / 698 -> 678 on another card, 16384 tokens 512 -> 2048 loads 505 -> 475, 4096 tokens 2048 -> 8192
+// 1216 -> 1207 / 1183 -> 1179, 4096 -> 11008 the same, 2048 tokens 1024 -> 2816 178 -> 181).
+constexpr int kOnce = 2;
+
 FBL_DEV float with_exponent(_Float16 h, int e) { return __builtin_amdgcn_ldexpf((float)h, e - 126); }
 
 FBL_DEV FactorWords pack_factors(const float (&f)[8]) {

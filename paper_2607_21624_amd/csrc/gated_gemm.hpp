@@ -103,8 +103,8 @@ struct GatedEp {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) g[e] = u[e] * act_grad<ACT, true>(g[e]);
                 const uint32_t off = offset(m, n, p.ldf);  // F is a multiple of 8
-                __builtin_amdgcn_raw_buffer_store_b128(pack_factors(g), rf, off, 0, 0);
-                __builtin_amdgcn_raw_buffer_store_b128(pack_factors(a), rf, up_of(off), 0, 0);
+                __builtin_amdgcn_raw_buffer_store_b128(pack_factors(g), rf, off, 0, kOnce);
+                __builtin_amdgcn_raw_buffer_store_b128(pack_factors(a), rf, up_of(off), 0, kOnce);
             }
             store8(rc, offset(m, n, p.ldc), h, n, F);
         });

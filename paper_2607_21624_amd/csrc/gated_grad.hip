@@ -36,7 +36,8 @@ struct GatedGradEp {
             lds, acc, m0, n0, wm, wn,
             [&](int m, int n) __attribute__((always_inline)) {
                 const uint32_t off = offset(m, n, p.ldf);
-                return Factors{__builtin_bit_cast(FactorWords, load8(rf, off)), __builtin_bit_cast(FactorWords, load8(rf, up_of(off)))};
+                return Factors{__builtin_bit_cast(FactorWords, __builtin_amdgcn_raw_buffer_load_b128(rf, off, 0, kOnce)),
+                               __builtin_bit_cast(FactorWords, __builtin_amdgcn_raw_buffer_load_b128(rf, up_of(off), 0, kOnce))};
             },
             [&](int m, int n, float (&v)[8], const Factors& f) __attribute__((always_inline)) {
                 float g[8], u[8];
