@@ -84,11 +84,10 @@ def _wide(rows: int, width: int, like):
     bytes further apart: a product that walks down them (dx takes 256 rows of dz a tile) would else meet few of the
     memory's channels (gated step of 4096 tokens, 2048 -> 8192 1233 -> 1181 us, 4096 -> 11008 3112 -> 3085; rows of 16 KB gain
     nothing, 8192 tokens 1024 -> 4096 705 -> 722)."""
-    row = width * like.element_size()
-    gap = 256 if like.dtype == torch.bfloat16 and row >= 1 << 15 and row % 1024 == 0 else 0
-    if rows * (row + 512) >= 1 << 31:  # the products' limit
-        gap = 0
-    return torch.empty((rows, width + gap), dtype=like.dtype, device=like.device)[:, :width]
+    row = 2 * width
+    if like.dtype != torch.bfloat16 or row < 1 << 15 or row % 1024 or rows * (row + 512) >= 1 << 31:  # (the products' limit)
+        return like.new_empty((rows, width))
+    return like.new_empty((rows, width + 256))[:, :width]
 
 
 class _GatedMlp(torch.autograd.Function):
@@ -105,8 +104,11 @@ class _GatedMlp(torch.autograd.Function):
         if grads and any(ctx.needs_input_grad[:3]):
             factors = _wide(x2.shape[0], w1.shape[1], x)
         h = _f.gated_fwd(x2, w1, b1, act, factors=factors)
-        y, y2 = rows_of(x, w2.shape[1])
-        _f.linear_fwd(h, w2, b2, residual=res2, out=y2)
+        if x.dim() == 2:
+            y = _f.linear_fwd(h, w2, b2, residual=res2)
+        else:
+            y, y2 = rows_of(x, w2.shape[1])
+            _f.linear_fwd(h, w2, b2, residual=res2, out=y2)
         ctx.save_for_backward(x2, w1, w2, factors, h)
         ctx.xshape = x.shape
         return y
@@ -120,12 +122,15 @@ class _GatedMlp(torch.autograd.Function):
         if any(need[:5]):
             dy2 = matrix_of(unit(dy, "gated_mlp"), "gated_mlp: the incoming gradient")
             if any(need[:3]):
-                dz, db1 = _f.gated_bwd(dy2, w2, factors, dz=_wide(*factors.shape, factors), need_bias=need[2])
+                wide = None if factors.is_contiguous() else _wide(*factors.shape, factors)
+                dz, db1 = _f.gated_bwd(dy2, w2, factors, dz=wide, need_bias=need[2])
                 if need[0] or need[1]:
                     dx, dw1, _ = _f.linear_bwd(dz, x2, w1, need_dx=need[0], need_dw=need[1], need_bias=False)
             if need[3] or need[4]:
                 _, dw2, db2 = _f.linear_bwd(dy2, h, w2, need_dx=False, need_dw=need[3], need_bias=need[4])
-        return dx.view(ctx.xshape) if need[0] else None, dw1, db1, dw2, db2, dy if need[5] else None, None, None
+        if dx is not None and len(ctx.xshape) != 2:
+            dx = dx.view(ctx.xshape)
+        return dx, dw1, db1, dw2, db2, dy if need[5] else None, None, None
 
 
 def gated_mlp(x, w1, b1, w2, b2, act: str = "silu", residual=None):

@@ -16,9 +16,9 @@ def first_order(backward):
 
     @functools.wraps(backward)
     def marked(ctx, *grads):
-        if torch.is_grad_enabled():
-            grads = tuple(g if g is None or g.requires_grad else g.detach().requires_grad_() for g in grads)
-        return once(ctx, *grads)
+        if not torch.is_grad_enabled():
+            return backward(ctx, *grads)
+        return once(ctx, *(g if g is None or g.requires_grad else g.detach().requires_grad_() for g in grads))
     return marked
 
 
@@ -31,7 +31,9 @@ def unit(t, what: str):
 
 
 def matrix_of(t, what: str):
-    """[..., N] as a matrix of rows, a view."""
+    """[..., N] as a matrix of rows: itself, or a view."""
+    if t.dim() == 2:
+        return t
     try:
         return t.view(-1, t.shape[-1])
     except RuntimeError as e:

@@ -35,10 +35,12 @@ def _stand_ins():
 
     def gated_bwd(dy, w_down, factors, dz=None, need_bias=True):
         dh = dy @ w_down.t()
-        return dz.copy_(torch.cat([dh, dh], 1) * factors), dz.sum(0) if need_bias else None
+        got = torch.cat([dh, dh], 1) * factors
+        return got if dz is None else dz.copy_(got), got.sum(0) if need_bias else None
 
     def linear_fwd(x, w, bias=None, act="none", residual=None, out=None, z=None):
-        return out.copy_(x @ w if residual is None else x @ w + residual)
+        y = x @ w if residual is None else x @ w + residual
+        return y if out is None else out.copy_(y)
 
     def linear_bwd(dy, x, w, need_dx=True, need_dw=True, need_bias=True):
         return dy @ w.t() if need_dx else None, x.t() @ dy if need_dw else None, dy.sum(0) if need_bias else None
