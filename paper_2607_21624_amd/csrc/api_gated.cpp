@@ -60,8 +60,9 @@ int forward_splits(int f32, int64_t M, int64_t K, int64_t F) {
     return (int)std::max<int64_t>(1, std::min(256 / ((2 * F + 127) / 128), K / 384));
 }
 
-// Workspace of the data gradient, a function of the shape: planes of dh, and partial sums of dz (as many rows of them as any
-// tile writes, linear_grad_groups, or one for each of a few tokens).
+// Workspace of the data gradient, a function of the shape: planes of dh, and partial sums of dz: as many rows of them as any
+// tile writes (linear_grad_groups), or one for each of a few tokens where that is more.  A shape whose contraction would be
+// shared needs room for a tile's rows too: a caller may name a tile, which shares nothing.
 struct GatedWs {
     size_t sums, total;
     int splits;
@@ -70,7 +71,7 @@ GatedWs gated_ws(int f32, int64_t M, int64_t F, int64_t N) {
     GatedWs w;
     w.splits = few_splits(f32, M, N, F);
     w.sums = align256(few_ws(w.splits, M, F));
-    w.total = w.sums + (size_t)(w.splits > 1 ? M : M / 32 + 4) * 2 * (size_t)F * 4;
+    w.total = w.sums + (size_t)(w.splits > 1 ? std::max(M, M / 32 + 4) : M / 32 + 4) * 2 * (size_t)F * 4;
     return w;
 }
 

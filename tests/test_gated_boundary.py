@@ -89,6 +89,24 @@ def test_workspace_holds_every_tile_s_sums():
         assert all(-(-M // t["bm"]) * t["wm"] <= M // 32 + 4 for t in tiles.values()), M
 
 
+@pytest.mark.parametrize("F_", [8, 1032, 8192])
+def test_workspace_of_shared_contractions_holds_every_tile_s_sums(F_):
+    """A tile that the caller names does not share the contraction: behind the planes that AUTO would use the workspace has
+    room for that tile's rows of partial sums, and for the one row a token that the shared path writes."""
+    n = ctypes.c_size_t()
+    tiles = fbl.gemm_tiles()
+    rows = lambda M: max(max(-(-M // t["bm"]) * t["wm"] for t in tiles.values()), M)
+    for N in (64, 2048, 2056, 4096, 8192, 16384):
+        for M in range(1, 129):
+            # (the forward of a linear layer of the same extents keeps its planes alone)
+            assert LIB.fbl_linear_fwd_workspace(BF16, M, N, F_, ctypes.byref(n)) == F.FBL_OK
+            planes = (n.value + 255) // 256 * 256
+            if not planes:
+                continue
+            assert LIB.fbl_gated_bwd_workspace(BF16, M, F_, N, ctypes.byref(n)) == F.FBL_OK
+            assert n.value - planes >= rows(M) * 2 * F_ * 4, (M, F_, N)
+
+
 def _refused(status, f, *args, **kw):
     with pytest.raises(fbl.FblError) as e:
         f(*args, **kw)

@@ -164,6 +164,22 @@ def test_shared_contractions(dt):
                 call()
 
 
+@pytest.mark.parametrize("tile", range(21))
+def test_tiles_of_few_tokens(tile):
+    """A named tile shares no contraction, also where AUTO does: it writes its own rows of partial sums, and nothing behind the
+    workspace."""
+    for M, F, N in ((1, 264, 4096), (2, 136, 4104), (3, 264, 4096), (33, 136, 2056), (128, 72, 8192)):
+        _, _, _, (wd, wdr), (f, fr), (dy, dyr) = _inputs(M, 64, F, N, torch.bfloat16, False)
+        need = fbl.gated_bwd_workspace(dy, wd)
+        ws = torch.full((need + 65536,), 0xff, dtype=torch.uint8, device="cuda")
+        dz, db = fbl.gated_bwd(dy, wd, f, tile=tile, workspace=ws[:need])
+        torch.cuda.synchronize()
+        assert torch.all(ws[need:] == 0xff)
+        _check_bwd(dz, db, dyr, wdr, fr)
+        again = fbl.gated_bwd(dy, wd, f, tile=tile)
+        assert torch.equal(again[0], dz) and torch.equal(again[1], db)
+
+
 @pytest.mark.parametrize("dt,gap", [("bf16", 8), ("f32", 3)])
 def test_strided_operands(dt, gap):
     """Every matrix a view with gaps of NaN between its rows; bit for bit the contiguous call."""
