@@ -315,10 +315,10 @@ __global__ __launch_bounds__(256, (NORM && BWD ? 3 : 5)) void qk_norm_rotary(Rot
                     t[e] = y[e] * (x[e] * r);
                     m = __builtin_fmaf(t[e], wh[e], m);
                 }
-                const float once = live ? 1.f : 0.f;  // (0 times a nan that its first lane has added too)
+                // (chosen, not multiplied: 0 times an infinite value that its own lane adds would make the sum nan)
                 const auto add = [&](int k) __attribute__((always_inline)) {
 #pragma unroll
-                    for (int e = 0; e < 2 * V; ++e) sum[k][e] = __builtin_fmaf(t[e], once, sum[k][e]);
+                    for (int e = 0; e < 2 * V; ++e) sum[k][e] += live ? t[e] : 0.f;
                 };
                 if (all_q) add(0);
                 else if (all_k) add(1);

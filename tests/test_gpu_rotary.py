@@ -273,6 +273,34 @@ def test_dead_lanes_leave_the_sums():
     check("dw", dw, ref, 120 * U * (np.abs(_heads(gr, 3)) * xh).sum((0, 1, 2)))
 
 
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("S,Hq,Hkv,d", [(5, 3, 0, 128), (3, 1, 1, 32), (7, 40, 8, 64), (4, 2, 3, 64), (1, 1, 1, 128)])
+def test_an_infinite_gradient_stays_in_its_column_of_the_weights(dt, S, Hq, Hkv, d):
+    """An infinite value of dy that does not turn, times a finite r x: the weight's gradient is infinite there, of r x's sign, and
+    what it was in all other columns, also where lanes without a head or token repeat the head."""
+    dtype = DTYPES[dt]
+    rng = np.random.default_rng(41 + S)
+    W, dims = (Hq + Hkv) * d, 16
+    x, xr = rounded(rng, (1, S, W), dtype)
+    g, _ = rounded(rng, (1, S, W), dtype)
+    w, _ = rounded(rng, (d,), dtype, 0.2, 1.0)
+    how = dict(turns=fbl.rotary_turns(fbl.rotary_frequencies(dims)), q_weight=w, k_weight=w if Hkv else None, eps=1e-6)
+    split = lambda t: (t[..., :Hq * d], t[..., Hq * d:] if Hkv else None)
+    note(f"infinite gradient, S={S} heads {Hq} + {Hkv} of {d} {dt}")
+    clean = fbl.qk_norm_rotary_bwd(*split(g), *split(x), Hq, Hkv, **how)
+    col = dims + 5
+    for head, i in ((Hq - 1, 2), (Hq + Hkv - 1, 3 if Hkv else 2)):  # the last ones, which are repeated
+        for value in (float("inf"), float("-inf")):
+            bad = g.clone()
+            bad[0, S - 1, head * d + col] = value
+            got = fbl.qk_norm_rotary_bwd(*split(bad), *split(x), Hq, Hkv, **how)
+            want = clean[i].float().clone()
+            want[col] = value * np.sign(xr[0, S - 1, head * d + col])
+            assert torch.equal(got[i].float(), want)
+            other = 5 - i
+            assert clean[other] is None or torch.equal(got[other], clean[other])
+
+
 def test_offsets_past_32_bits():
     # a batch is 2^32 bytes and more from the next one, a token 2^31
     rng = np.random.default_rng(13)
