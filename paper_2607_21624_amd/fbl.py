@@ -1479,7 +1479,7 @@ def _rotary(turns, positions, axes, neighbours: bool, B: int, S: int, where: str
     if positions is not None:
         if positions.dtype != torch.int64:
             raise FblError(FBL_ERR_DTYPE, f"{where}: positions is {positions.dtype}, needs torch.int64")
-        want = {1: (S,), 2: (B, S), 3: (positions.shape[0], B, S)}.get(positions.dim())
+        want = {1: (S,), 2: (B, S), 3: (*positions.shape[:1], B, S)}.get(positions.dim())
         if want is None or tuple(positions.shape) != want or positions.shape[0] == 0:
             raise FblError(FBL_ERR_SHAPE, f"{where}: positions has shape {tuple(positions.shape)}, needs {(S,)}, {(B, S)} or "
                                           f"{('axes', B, S)}")

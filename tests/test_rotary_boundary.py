@@ -194,3 +194,11 @@ def test_binding_refuses_host_tensors():
     _refused(F.FBL_ERR_NULL, fbl.qk_norm_rotary_bwd, q, None, None, None, 2, 0, turns=t, eps=1e-6)
     _refused(F.FBL_ERR_ARG, ag.attention_packed, torch.zeros(1, 4, 6 * 32), 2, 2, turns=t)
     _refused(F.FBL_ERR_SHAPE, ag.attention_packed, torch.zeros(1, 4, 100), 2, 2, 0.1, turns=t)
+
+
+def test_a_position_alone_is_refused():
+    """positions without a dimension name no tokens."""
+    turns = fbl.rotary_turns(fbl.rotary_frequencies(64), device="cpu")
+    with pytest.raises(fbl.FblError) as e:
+        F._rotary(turns, torch.tensor(3), None, False, 1, 1, "here")
+    assert e.value.status == F.FBL_ERR_SHAPE
