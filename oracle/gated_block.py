@@ -14,13 +14,38 @@ def _pairs(D, dims, neighbours):
     return (2 * j, 2 * j + 1) if neighbours else (j, j + dims // 2)
 
 
+def _scaled_turn(bits):
+    """2 pi 2^bits to the nearest few integers: pi = 16 atan(1/5) - 4 atan(1/239), the series in integers."""
+    def atan(n):
+        term, total, k = (1 << bits + 16) // n, 0, 0
+        while term:
+            total += (-1) ** k * (term // (2 * k + 1))
+            term //= n * n
+            k += 1
+        return total
+    return 2 * (16 * atan(5) - 4 * atan(239)) >> 16
+
+
+_BITS = 256
+_TURN = _scaled_turn(_BITS)
+
+
+def _reduced(n, f):
+    """n f without its whole turns, within half a turn, rounded once: the product is an exact fraction, and so is what is
+    left of it to 2^-256 of the turns taken away."""
+    num, den = float(f).as_integer_ratio()
+    turn = den * _TURN
+    r = (int(n) * num << _BITS) % turn
+    return (r - turn if 2 * r > turn else r) / (den << _BITS)
+
+
 def angles(positions, frequencies, axes=None):
     """[B, S, dims / 2] angles from positions [B, S] or [axes, B, S]."""
     p = np.asarray(positions)
     p = p[None] if p.ndim == 2 else p
     axes = [0] * len(frequencies) if axes is None else axes
     # the whole turns go out of the product before it is rounded to float64
-    return np.stack([np.vectorize(lambda n: math.remainder(float(n) * f, 2 * math.pi), otypes=[np.float64])(p[a])
+    return np.stack([np.vectorize(lambda n: _reduced(n, f), otypes=[np.float64])(p[a])
                      for a, f in zip(axes, frequencies)], axis=-1)
 
 

@@ -126,6 +126,23 @@ def test_far_and_negative_positions(dt):
 
 
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("base", [1e4, 5e5])
+def test_ordinary_frequencies_at_far_positions(dt, base):
+    """Up to 2^31 positions from 0.  The kept frequency is off by the quotient's rounding, 2^-63 of at most 1 / 2 pi of a turn, and
+    its own to 2^-64 turns: at 2^31 positions 6e-10, a hundredth of u."""
+    rng = np.random.default_rng(15)
+    dt = DTYPES[dt]
+    far = rng.integers(-(1 << 31), 1 << 31, (3, 40))
+    far[0, :6] = [0, (1 << 31) - 1, -(1 << 31), 10 ** 9 + 7, 1 << 30, -(1 << 20) - 1]
+    freq = fbl.rotary_frequencies(64, base)
+    q, qr = rounded(rng, (3, 40, 2 * 64), dt)
+    note(f"ordinary frequencies at far positions {dt}")
+    y, _ = fbl.qk_norm_rotary_fwd(q, None, 2, 0, turns=fbl.rotary_turns(freq), positions=torch.from_numpy(far).cuda())
+    x = _heads(qr, 2)
+    check("y", y, oracle.rotate(x, oracle.angles(far, freq)).reshape(3, 40, -1), ((trig(dt) + 0.01 * U) * _pair_sum(x, 64, False)).reshape(3, 40, -1))
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
 def test_single_tokens_at_their_positions(dt):
     rng = np.random.default_rng(6)
     for B in (1, 7, 200):

@@ -1,5 +1,6 @@
 """Pins of the float64 oracle of per-head norms with rotation, the gated feed-forward part and clipping (CPU): central
 differences, torch in float64, closed forms."""
+import decimal
 import math
 
 import numpy as np
@@ -50,6 +51,22 @@ def test_angles_of_axes():
     pos = np.arange(2 * 3).reshape(3, 1, 2) * 7
     a = G.angles(pos, [1.0, 0.5, 0.25], [2, 0, 1])
     assert np.allclose(np.cos(a[0, 1]), np.cos([35 * 1.0, 7 * 0.5, 21 * 0.25]))
+
+
+def test_angles_of_far_positions():
+    """Ordinary frequencies at positions where the product has many whole turns, against 100 decimal digits: within two roundings
+    of a float64 of at most pi."""
+    turn = decimal.Decimal("6.28318530717958647692528676655900576839433879875021164194988918461563281257241799725606965")
+    far = [0, 1, -1, 4097, -(1 << 20), 10 ** 9 + 7, (1 << 31) - 1, -(1 << 31), 1 << 40, -(10 ** 15) - 3, (1 << 63) - 1, -(1 << 63)]
+    freq = [1.0, 1e4 ** -0.25, 5e5 ** -0.5, 1e4 ** (-62 / 64), 0.7]
+    a = G.angles(np.array([far]), freq)
+    with decimal.localcontext() as c:
+        c.prec = 100
+        for i, n in enumerate(far):
+            for j, f in enumerate(freq):
+                want = decimal.Decimal(n) * decimal.Decimal(f)
+                want -= turn * (want / turn).to_integral_value(decimal.ROUND_HALF_EVEN)
+                assert abs(decimal.Decimal(a[0, i, j]) - want) <= 2 * decimal.Decimal(2) ** -52, (n, f)
 
 
 @pytest.mark.parametrize("kind", ACTS)
