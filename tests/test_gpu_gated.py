@@ -242,6 +242,42 @@ def test_factors_of_any_size():
             assert torch.all(dz[keep] == 16) and not torch.isfinite(dz[:, 8:16]).any()
 
 
+@pytest.mark.parametrize("M", [40, 300])
+@pytest.mark.parametrize("size", [2.0 ** 10, 2.0 ** 16, 2.0 ** 22])
+def test_gradients_beside_outlier_columns(size, M):
+    """One up column of eight is `size` times its neighbours, and so is its gate's factor: dw of the gates against float64, column
+    by column as the factors' format has it.  A neighbour's factor keeps 2^-11 of itself, or 2^-24 of the outlier's; dz is
+    rounded once, and its products with x are summed in fp32."""
+    dt = torch.bfloat16
+    K, F, N = 72, 64, 80
+    rng = np.random.default_rng(17)
+    note(f"outlier columns of {size}, {M} tokens")
+    x, xr = rounded(rng, (M, K), dt)
+    w1 = rng.standard_normal((K, 2 * F)) * K ** -0.5
+    w1[:, F + 3::8] *= size
+    w1 = torch.from_numpy(w1.astype(np.float32)).to(dt)
+    w, wr = w1.cuda(), w1.double().numpy()
+    (wd, wdr), (dy, dyr) = rounded(rng, (F, N), dt, N ** -0.5), rounded(rng, (M, N), dt)
+    f = torch.empty(M, 2 * F, dtype=dt, device="cuda")
+    fbl.gated_fwd(x, w, None, "silu", factors=f)
+    dz, _ = fbl.gated_bwd(dy, wd, f, need_bias=False)
+    _, dw, _ = fbl.linear_bwd(dz, x, w, need_dx=False, need_bias=False)
+    _, zr = oracle.gated_fwd(xr, wr, None, "silu")
+    fr = oracle.gated_factors(zr, "silu")[:, :F]
+    zb = _sum_bound(xr, wr) + 2.0 ** -23 * np.abs(zr)
+    gate, up = zr[:, :F], zr[:, F:]
+    sb = zb[:, :F] + 2.0 ** -20 * (1 + np.abs(gate))
+    fb = zb[:, F:] * (np.abs(act_grad(gate, "silu")) + sb) + np.abs(up) * sb + 2.0 ** -23 * np.abs(fr)
+    top = np.repeat((np.abs(fr) + fb).reshape(M, -1, 8).max(-1), 8, axis=-1)
+    fb = fb + np.maximum(2.0 ** -11 * (np.abs(fr) + fb), 2.0 ** -24 * top)
+    dh = dyr @ wdr.T
+    zg = dh * fr
+    zgb = _sum_bound(dyr, wdr.T) * (np.abs(fr) + fb) + np.abs(dh) * fb
+    zgb = zgb + 2.0 ** -8 * (np.abs(zg) + zgb)
+    check("dw of the gates", dw[:, :F], xr.T @ zg,
+          np.abs(xr).T @ zgb + (M + 16) * 2.0 ** -24 * (np.abs(xr).T @ (np.abs(zg) + zgb)), halves=1 + 2.0 ** -8)
+
+
 def test_operands_near_the_limit():
     """Factors and dz of just below 2 GiB: the last rows are those of a call of their own, to the roundings of two tilings."""
     M, K, F = 262143, 64, 2040

@@ -128,8 +128,8 @@ def test_far_and_negative_positions(dt):
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
 @pytest.mark.parametrize("base", [1e4, 5e5])
 def test_ordinary_frequencies_at_far_positions(dt, base):
-    """Up to 2^31 positions from 0.  The kept frequency is off by the quotient's rounding, 2^-63 of at most 1 / 2 pi of a turn, and
-    its own to 2^-64 turns: at 2^31 positions 6e-10, a hundredth of u."""
+    """Up to 2^31 positions from 0.  The kept frequency is off by the quotient's roundings, 2^-63 of at most 1 / 2 pi of a turn,
+    and its own, 2^-65 turns: 2^31 positions make that 0.82 2^-33 turns, 6e-10 or 0.0101 u."""
     rng = np.random.default_rng(15)
     dt = DTYPES[dt]
     far = rng.integers(-(1 << 31), 1 << 31, (3, 40))
@@ -139,7 +139,7 @@ def test_ordinary_frequencies_at_far_positions(dt, base):
     note(f"ordinary frequencies at far positions {dt}")
     y, _ = fbl.qk_norm_rotary_fwd(q, None, 2, 0, turns=fbl.rotary_turns(freq), positions=torch.from_numpy(far).cuda())
     x = _heads(qr, 2)
-    check("y", y, oracle.rotate(x, oracle.angles(far, freq)).reshape(3, 40, -1), ((trig(dt) + 0.01 * U) * _pair_sum(x, 64, False)).reshape(3, 40, -1))
+    check("y", y, oracle.rotate(x, oracle.angles(far, freq)).reshape(3, 40, -1), ((trig(dt) + 0.0101 * U) * _pair_sum(x, 64, False)).reshape(3, 40, -1))
 
 
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
