@@ -751,8 +751,10 @@ fbl_status fbl_linear_kd_bwd(int32_t dtype, uint32_t order, int64_t M, int64_t K
  * Pair j is (h[j], h[j + dims / 2]), or with `neighbours` (h[2j], h[2j + 1]); values from dims on do not turn.
  *
  * fbl_rotary: turns [dims / 2] holds the frequencies as fbl_rotary_turns makes them (device memory): turns a position in
- * 64-bit fixed point, 2^64 a whole turn, so that t is exact to 2^-33 turns for any frequency up to 2^31
- * positions from 0 and a position may be any int64.  fbl_rotary_turns (host) takes radians a position.
+ * 64-bit fixed point, 2^64 a whole turn.  A frequency below one turn a position is kept to 2^-62 turns, one of 2^k turns to
+ * 2^(k - 62), and so far off is t for each position from 0 (any int64).  Of the angle the kernels drop what is below 2^-32
+ * turns and round it to fp32: 2^-26 turns at most for bf16 tensors, 2^-28 for fp32.  fbl_rotary_turns (host) takes radians a
+ * position.
  * positions: int64 device memory, token s of sequence b at axis a is positions[a * stride_axis + b * stride_batch + s *
  * stride_token] (strides in elements, 0 allowed); NULL: s itself.  With several axes (time, height, width of
  * images and video) pair j turns by its own axis' position, axes[j] (host memory, with the struct).
@@ -800,9 +802,11 @@ fbl_status fbl_qk_norm_rotary_bwd(const fbl_layout* lgq, const void* gq, const f
  *   (gate, up) = x [M, K] . w [K, 2F] + bias [2F],   h [M, F] = act(gate) * up
  * gate is columns 0 .. F - 1, up columns F .. 2F - 1 (w and bias hold the two side by side; act as fbl_linear_fwd's).
  * bias may be NULL.  factors [M, 2F], where not NULL, receives what the backward needs, the derivatives of h by gate and by
- * up, (up * act'(gate), act(gate)): fp32 as they are, bf16 in two bytes a value of a form for fbl_gated_bwd alone (eight
- * consecutive ones share an exponent and keep 11 digits; one that is not finite leaves its eight so).  ws: NULL, or fbl_gated_fwd_workspace bytes (16-byte
- * aligned), with which several workgroups share the contraction of a few tokens' tiles (0 bytes where they do not).
+ * up, (up * act'(gate), act(gate)): fp32 as they are, bf16 in two bytes a value of a form for fbl_gated_bwd alone.  Eight
+ * consecutive ones of a row share the exponent of their largest: one within 2^13 of it keeps 11 digits, a smaller one what is
+ * above 2^-24 of the largest (fewer digits than bf16 below 2^-16 of it, and nothing below 2^-25); one that is not finite leaves
+ * its eight so.  ws: NULL, or fbl_gated_fwd_workspace bytes (16-byte aligned), with which several workgroups share the contraction of
+ * a few tokens' tiles (0 bytes where they do not).
  *
  * fbl_gated_bwd takes the gradient dy [M, N] of the block's result and w_down [F, N], its second weight, and gives
  *   dz [M, 2F] = dh * factors, for gate and for up,   dh = dy . w_down^T  (never stored)

@@ -39,7 +39,8 @@ torch provides the tensors, the stream and the autograd graph.
       teacher is a constant: logits that require grad get no gradient from here.
   clip_grad_norm_(parameters, limit) -> norm
       the norm of all parameters' .grad (those that are not None), which are scaled in place where it is above
-      the limit: grad * min(1, limit / (norm + 1e-6)).  norm float32, of the gradients as they were.
+      the limit: grad * min(1, limit / (norm + 1e-6)).  norm float32, of the gradients as they were.  Where none has a
+      gradient the call is refused (FBL_ERR_SHAPE).
 
 Gradients are those of the first order: taken with create_graph they hold their
 values, and differentiating them raises an error.

@@ -15,9 +15,11 @@
 // roundings of dz, which the matrix instructions take in bf16, and of the result, 0.17% each.  Factors in bf16 added as much
 // (0.29%; rounded gate and up 0.30%), so they are kept in as many bytes of a form with 11 digits (factors.hpp).
 //
-// 4096 tokens bf16 with factors: 2048 -> 8192 264 us (1.04 PFLOP/s), 4096 -> 11008 720 us (1.03); with bf16 factors 259 and
-// 716, without any 230 and 679.
-// The plain products of the same sizes, stored by the lanes as the accumulators lie, take 296 and 711.
+// 4096 tokens bf16 with factors, one call after another: 2048 -> 8192 248 us (1.11 PFLOP/s), 4096 -> 11008 708 us (1.04), without
+// any 229 and 672; within a step, behind the backward of the one before, medians of 271 and 736.  fp32, 2048 tokens 1024 -> 4096 277 us
+// (124 TFLOP/s), without factors 269; one token of 2048 -> 8192, cold weights, 30.
+// The plain products of the same bf16 sizes, stored by the lanes as the accumulators lie, took 296 and 711 (with factors 264 and 720
+// at that time).
 #include "act.hpp"
 #include "factors.hpp"
 #include "gemm_bf16.hpp"

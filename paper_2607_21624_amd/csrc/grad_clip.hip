@@ -7,7 +7,8 @@
 // call copies nothing and can be captured.  Tensors are cut into chunks of 16 KB; a workgroup walks every gridDim-th of
 // them.  Squares are summed in float64: no square overflows or vanishes, and a sum of 2^30 terms keeps fp32's digits.
 // Each workgroup leaves one sum; whoever needs the norm adds them in the same fixed order.  Clipping walks the chunks from
-// the last one back, since the end of what the norm has read is what the last-level cache still holds.
+// the last one back: the norm has read the end of the list last (bf16, both launches, in the norm's order and back: into other
+// tensors 268 M values 311 -> 297 us, 134 M 152.8 -> 148.1; in place 268 M 319 -> 313, lists of 134 M and less the same).
 //
 // 268 M values bf16: squares 108 us (5.0 TB/s), scaling into other tensors 185 (5.8).  85 M in place within the limit: 27 and 5.
 #include "kernels.hpp"

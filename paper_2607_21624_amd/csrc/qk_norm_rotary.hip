@@ -14,15 +14,18 @@
 // room for several tokens.
 //
 // The angle is in turns of 64-bit fixed point: frequency / 2 pi times 2^64, so that the wrapped product with any 64-bit
-// position is the angle without its whole turns, off by position * 2^-65 turns.  The cosine and sine of its upper 32 bits
-// come from the hardware for bf16 (good to 2^-19 or so, against 2^-9 of the storage) and from polynomials for fp32.
+// position is the angle without its whole turns, off by the position times what the kept frequency is off (2^-62 turns at most).
+// Its upper 32 bits go to fp32, whose rounding is 2^-26 turns at most (a quarter turn at a time, for fp32, 2^-28); cosine and
+// sine come from the hardware for bf16 (good to 2^-19 or so, against 2^-9 of the storage) and from polynomials for fp32.
 //
 // The weights' gradients stay in registers over all tokens of a wavefront, are added across the lanes
 // that hold the same columns and the wavefronts, and go out as one row of partial sums a workgroup, which
 // column_sums adds in a fixed order.
 //
 // bf16 with norms and weights, forward / backward without column_sums: 4096 tokens of 32 + 32 heads of 128 23.2 us (5.8 TB/s) and
-// 35.8 (5.6), of 32 + 8 heads of 64 11.0 and 16.2 (3.8 and 3.9: a launch's start and end are a fifth).  16 tokens, the rotation alone, 3.5.
+// 35.8 (5.6), of 32 + 8 heads of 64 10.9 and 16.5 (3.9 and 3.8: a launch's start and end are a fifth, and of three steps of 16
+// heads for 40 the last one's second half repeats work).  16 tokens, the rotation alone, 3.5.  fp32, with column_sums: 4096 tokens of
+// 32 + 32 heads of 128 43 (6.2 TB/s) and 83 (4.8), of 32 + 8 heads of 64 14.8 and 25.6.
 #include "kernels.hpp"
 #include "rows.hpp"
 
